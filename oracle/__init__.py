@@ -23,6 +23,8 @@ vs. fused-GEMM scaling"):
 * ``gates``    the GDN gate transform (Eq. 1) of the fused a/b projection.
 * ``norm``     RMSNorm in front of the quantizer (for the one-pass
   normalize-and-quantize path with a calibrated activation scale).
+* ``attention`` the attention between two projections: norm and rotation of
+  heads, the paged 8-bit cache (section 7, FP8 KV), softmax over it.
 * ``stats``    block statistics of Table 2 (max/RMS, kurtosis, one-hot blocks,
   relative quantization error), used only as sanity bands for synthetic data.
 
@@ -31,4 +33,4 @@ every product that is compared, see ``quant``), so codes and scales are a
 function of the inputs alone, independent of any operation order.
 """
 
-from . import formats, gates, quant, gemm, harmonize, norm, stats  # noqa: F401
+from . import attention, formats, gates, quant, gemm, harmonize, norm, stats  # noqa: F401

@@ -10,6 +10,7 @@
 
 #include <mutex>
 
+#include "attention_launch.h"
 #include "launch.h"
 #include "nvfp4.h"
 #include "packed_layout.h"
@@ -23,6 +24,10 @@ thread_local int g_last_hip_error = 0;
 constexpr int kMaxDevices = 64;
 std::once_flag g_dev_once[kMaxDevices];
 int g_dev_ok[kMaxDevices];   // 1: gfx950, 0: other
+
+}  // namespace
+
+namespace nvfp4 {
 
 int fail_hip(hipError_t e) {
   g_last_hip_error = (int)e;
@@ -43,6 +48,13 @@ int check_device() {
   });
   return g_dev_ok[dev] ? NVFP4_OK : NVFP4_EUNSUPPORTED;
 }
+
+}  // namespace nvfp4
+
+using nvfp4::check_device;
+using nvfp4::fail_hip;
+
+namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

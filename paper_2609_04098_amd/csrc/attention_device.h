@@ -1,0 +1,92 @@
+// Device helpers of the attention kernels: bf16 and E4M3 conversions, the
+// rotation's sines and cosines, and the place of a step's rows.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "attention_launch.h"
+
+namespace nvfp4 {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float bf16_low(uint32_t d) { return __uint_as_float(d << 16); }
+__device__ __forceinline__ float bf16_high(uint32_t d) { return __uint_as_float(d & 0xFFFF0000u); }
+
+// Two values rounded to nearest even.
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, (bf16x2){(__bf16)lo, (__bf16)hi});
+}
+
+// sin and cos of the angle pos * inv_freq.  Whole turns and quarters are taken
+// off in binary64, where a position of 2^24 leaves 2^-29 turns' accuracy; the
+// rest, |x| <= pi / 4, goes through the Taylor series in T (float: to 1e-8,
+// double: to 1e-11).
+template <typename T>
+__device__ __forceinline__ void sin_cos(int pos, float inv_freq, T& sine, T& cosine) {
+  double t = (double)pos * (double)inv_freq * 0.15915494309189535;      // turns
+  t -= rint(t);
+  const double q = rint(4.0 * t);
+  const T x = (T)((t - 0.25 * q) * 6.283185307179586);
+  const T z = x * x;
+  T s, c;
+  if (sizeof(T) == 8) {
+    s = fma(z, (T)(-1.0 / 39916800.0), (T)(1.0 / 362880.0));
+    s = fma(z, s, (T)(-1.0 / 5040.0));
+    c = fma(z, (T)(1.0 / 479001600.0), (T)(-1.0 / 3628800.0));
+    c = fma(z, c, (T)(1.0 / 40320.0));
+  } else {
+    s = fma(z, (T)(1.0 / 362880.0), (T)(-1.0 / 5040.0));
+    c = fma(z, (T)(-1.0 / 3628800.0), (T)(1.0 / 40320.0));
+  }
+  s = fma(z, s, (T)(1.0 / 120.0));
+  s = fma(z, s, (T)(-1.0 / 6.0));
+  s = fma(x * z, s, x);
+  c = fma(z, c, (T)(-1.0 / 720.0));
+  c = fma(z, c, (T)(1.0 / 24.0));
+  c = fma(z, c, (T)-0.5);
+  c = fma(z, c, (T)1);
+  const int n = (int)q & 3;
+  const T a = (n & 1) ? c : s, b = (n & 1) ? s : c;
+  sine = (n & 2) ? -a : a;
+  cosine = ((n + 1) & 2) ? -b : b;
+}
+
+// The nearest E4M3 codes (ties to even) of four values of at most 448; NaN
+// gives 0x7F.
+__device__ __forceinline__ uint32_t e4m3_codes(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  r = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
+  return (uint32_t)r;
+}
+
+// Rows [row, row + rows) of sequence b and the tokens that they are: row + i is
+// token first + i (which may be below 0).  Bounded by the tensors whatever
+// cu_rows and kv_len hold.
+struct SeqRows {
+  int row, rows, first, len;
+};
+
+__device__ __forceinline__ SeqRows seq_rows(const KvBatchArgs& a, int b) {
+  SeqRows s;
+  if (a.cu_rows == nullptr) {
+    s.row = b;
+    s.rows = 1;
+  } else {
+    s.row = min(max(a.cu_rows[b], 0), a.rows);
+    s.rows = min(max(a.cu_rows[b + 1], s.row), a.rows) - s.row;
+  }
+  const int len = a.kv_len[b];
+  s.first = (len < 0 ? 0 : len) - s.rows;      // a length above the table's keeps its tokens' numbers
+  s.len = min(max(len, 0), a.max_tokens);
+  return s;
+}
+
+}  // namespace nvfp4

@@ -1,0 +1,98 @@
+"""ctypes binding of the attention entry points of libnvfp4.so
+(include/nvfp4_attention.h): argument marshalling only.
+"""
+
+import ctypes
+
+from . import nvfp4 as _c
+
+_i64, _vp, _sz, _int, _f = ctypes.c_int64, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_float
+
+
+class KvCacheStruct(ctypes.Structure):
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("num_pages", _i64), ("page_size", _i64),
+                ("kv_heads", _i64), ("head_dim", _i64), ("k_page_stride", _i64), ("v_page_stride", _i64),
+                ("scale_page_stride", _i64)]
+
+
+class KvBatchStruct(ctypes.Structure):
+    _fields_ = [("page_table", _vp), ("kv_len", _vp), ("cu_rows", _vp), ("page_table_stride", _i64),
+                ("max_pages", _i64), ("n_seqs", _i64), ("rows", _i64), ("max_kv_len", _i64)]
+
+
+_cache, _batch = ctypes.POINTER(KvCacheStruct), ctypes.POINTER(KvBatchStruct)
+
+# name -> (restype, argtypes), in the order of include/nvfp4_attention.h
+SIGNATURES = {
+    "nvfp4_qk_norm_rope": (_int, [_vp, _i64, _i64, _vp, _vp, _i64, _vp, _i64, _i64, _vp, _vp, _i64, _i64, _i64, _f,
+                                  _vp, _vp, _i64, _int, _vp]),
+    "nvfp4_kv_append": (_int, [_cache, _batch, _vp, _i64, _vp, _i64, _vp, _f, _vp, _vp, _i64, _int, _int, _vp]),
+    "nvfp4_kv_attention_workspace": (_sz, [_cache, _batch, _i64]),
+    "nvfp4_kv_attention": (_int, [_cache, _batch, _vp, _i64, _i64, _vp, _i64, _vp, _f, _int, _i64, _vp, _sz, _vp]),
+}
+
+_lib = None
+
+
+def lib():
+    """The loaded library with the attention entry points declared."""
+    global _lib
+    if _lib is None:
+        l = _c.lib()
+        for name, (res, args) in SIGNATURES.items():
+            fn = getattr(l, name)
+            fn.restype, fn.argtypes = res, args
+        _lib = l
+    return _lib
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def cache_struct(k, v, k_scale, v_scale, page_size):
+    """k, v uint8 [num_pages, kv_heads, page_size * head_dim]; k_scale, v_scale
+    float32 [num_pages, kv_heads]."""
+    return KvCacheStruct(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), k.shape[0], page_size,
+                         k.shape[1], k.shape[2] // page_size, k.stride(0), v.stride(0), k_scale.stride(0))
+
+
+def batch_struct(page_table, kv_len, cu_rows, rows, max_kv_len):
+    """page_table int32 [n_seqs, max_pages]; kv_len int32 [n_seqs]; cu_rows
+    int32 [n_seqs + 1] or None."""
+    return KvBatchStruct(page_table.data_ptr(), kv_len.data_ptr(), _at(cu_rows), page_table.stride(0),
+                         page_table.shape[1], kv_len.shape[0], rows, max_kv_len)
+
+
+def nvfp4_qk_norm_rope(q, q_gamma, q_out, k, k_gamma, k_out, eps, positions, inv_freq, interleaved, stream=None):
+    """q, q_out, k, k_out bf16 [rows, heads, head_dim] or None (q or k, with its output)."""
+    one = q if q is not None else k
+    rows, dim = one.shape[0], one.shape[2]
+    st = lib().nvfp4_qk_norm_rope(
+        _at(q), 0 if q is None else q.stride(0), 0 if q is None else q.shape[1], _at(q_gamma), _at(q_out),
+        0 if q is None else q_out.stride(0), _at(k), 0 if k is None else k.stride(0), 0 if k is None else k.shape[1],
+        _at(k_gamma), _at(k_out), 0 if k is None else k_out.stride(0), rows, dim, eps, _at(positions), _at(inv_freq),
+        0 if inv_freq is None else 2 * inv_freq.shape[0], interleaved, _c._stream(stream))
+    _c._check(st, "nvfp4_qk_norm_rope")
+
+
+def nvfp4_kv_append(cache, batch, k, v, k_gamma, eps, positions, inv_freq, interleaved, mode=_c.NVFP4_DYNAMIC,
+                    stream=None):
+    """cache, batch: the structures above; k, v bf16 [rows, kv_heads, head_dim]."""
+    st = lib().nvfp4_kv_append(cache, batch, k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), _at(k_gamma), eps,
+                               _at(positions), _at(inv_freq), 0 if inv_freq is None else 2 * inv_freq.shape[0],
+                               interleaved, mode, _c._stream(stream))
+    _c._check(st, "nvfp4_kv_append")
+
+
+def nvfp4_kv_attention_workspace(cache, batch, q_heads):
+    return lib().nvfp4_kv_attention_workspace(cache, batch, q_heads)
+
+
+def nvfp4_kv_attention(cache, batch, q, y, lse, scale, causal, window, workspace=None, stream=None):
+    """q, y bf16 [rows, q_heads, head_dim]; lse float32 [rows, q_heads] or None."""
+    st = lib().nvfp4_kv_attention(cache, batch, q.data_ptr(), q.stride(0), q.shape[1], y.data_ptr(), y.stride(0),
+                                  _at(lse), scale, causal, window, _at(workspace),
+                                  0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                  _c._stream(stream))
+    _c._check(st, "nvfp4_kv_attention")
