@@ -178,7 +178,7 @@ size_t nvfp4_kv_attention_workspace(const nvfp4_kv_cache* cache, const nvfp4_kv_
  *                do not matter; calls sharing one must be ordered.
  * Requirements: those of the structures; strides multiples of 8, at least
  * q_heads * head_dim and below 2^31; q, y 16-byte aligned, lse 4-byte;
- * softmax_scale finite; 0 <= window < 2^31.
+ * softmax_scale finite; 0 <= window < 2^31; rows * q_heads < 2^31.
  * Errors: NVFP4_EINVAL, NVFP4_EWORKSPACE, NVFP4_EUNSUPPORTED, NVFP4_EHIP.
  */
 int nvfp4_kv_attention(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const void* q, int64_t ldq,

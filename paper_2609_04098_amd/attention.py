@@ -18,7 +18,6 @@ import math
 import torch
 
 from . import linear as _l
-from . import nvfp4 as _c
 from . import nvfp4_attention as _a
 
 
@@ -27,33 +26,40 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _rows_ok(x, heads, dim, name):
-    """bf16 [rows, heads, dim], heads side by side."""
-    _need(x.dtype == torch.bfloat16 and x.dim() == 3, "%s must be a bf16 [rows, heads, head_dim] tensor" % name)
-    _need(x.shape[2] == dim and (heads is None or x.shape[1] == heads), "%s has the wrong heads or head_dim" % name)
-    _need(x.numel() == 0 or (x.stride(2) == 1 and (x.shape[1] == 1 or x.stride(1) == dim)),
-          "%s must have its heads side by side" % name)
+# These checks run once a call and layer, in front of kernels of a few
+# microseconds: no formatted text, no tensor property read twice.
+
+_BF16 = torch.bfloat16
+
+
+def _rows(x, name):
+    """(rows, heads, head_dim, row stride) of a bf16 [rows, heads, head_dim]
+    tensor whose heads lie side by side."""
+    if x.dtype is not _BF16 or x.dim() != 3:
+        raise ValueError(name + " must be a bf16 [rows, heads, head_dim] tensor")
+    rows, heads, dim = x.shape
+    ld, head, one = x.stride()
+    if (one != 1 or (head != dim and heads > 1)) and rows * heads * dim > 0:
+        raise ValueError(name + " must have its heads side by side")
+    return rows, heads, dim, ld
 
 
 def _like_rows(x, stream):
     """A contiguous [rows, heads, head_dim] tensor from the stream that uses it."""
+    if stream is None:
+        return torch.empty_like(x, memory_format=torch.contiguous_format)
     with _l._on(stream, x.device):
-        return torch.empty(x.shape, dtype=x.dtype, device=x.device)
-
-
-def _on_device(t):
-    """Context in which t's device is the current one (kernels are launched on
-    the current device, on its current stream)."""
-    if t.device.type != "cuda":
-        raise ValueError("tensors must be on the GPU")
-    return torch.cuda.device(t.device)
+        return torch.empty_like(x, memory_format=torch.contiguous_format)
 
 
 def _run(t, call, *args):
-    """``call(*args)`` with t's device current; no context where it is."""
-    if t.is_cuda and t.get_device() == torch.cuda.current_device():
+    """``call(*args)`` with t's device current (kernels are launched on the
+    current device, on its current stream); no context where it is already."""
+    if not t.is_cuda:
+        raise ValueError("tensors must be on the GPU")
+    if t.get_device() == torch.cuda.current_device():
         return call(*args)
-    with _on_device(t):
+    with torch.cuda.device(t.device):
         return call(*args)
 
 
@@ -66,8 +72,9 @@ class Rope:
         _need(inv_freq.dtype == torch.float32 and inv_freq.dim() == 1 and inv_freq.shape[0] % 8 == 0,
               "inv_freq must be a float32 vector of a multiple of 8 elements")
         _need(not inv_freq.requires_grad, "inv_freq takes no gradient here")
-        self.inv_freq = inv_freq.contiguous() if inv_freq.shape[0] else None
-        self.interleaved = 1 if interleaved else 0
+        self.inv_freq = inv_freq.contiguous()
+        half = inv_freq.shape[0]
+        self.pointer = (self.inv_freq.data_ptr() if half else None, half, 1 if interleaved else 0)
 
 
 class KVCache:
@@ -89,6 +96,7 @@ class KVCache:
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.page_size, self.kv_heads, self.head_dim = page_size, k.shape[1], k.shape[2] // page_size
         self.device = k.device
+        self.softmax_scale = 1.0 / math.sqrt(self.head_dim)
         self.struct = _a.cache_struct(k, v, k_scale, v_scale, page_size)
         self.ref = ctypes.byref(self.struct)
 
@@ -148,19 +156,25 @@ class Batch:
     def workspace_bytes(self, cache, q_heads):
         key = (q_heads, cache.kv_heads, cache.head_dim, cache.page_size)
         if key not in self._workspace:
-            self._workspace[key] = _a.nvfp4_kv_attention_workspace(cache.ref, self.ref, q_heads)
+            self._workspace[key] = _a.kv_attention_workspace(cache.ref, self.ref, q_heads)
         return self._workspace[key]
 
 
-def _gamma_ok(gamma, dim, name):
-    if gamma is not None:
-        _need(gamma.dtype == torch.bfloat16 and gamma.shape == (dim,) and gamma.is_contiguous(),
-              "%s must be bf16 [head_dim]" % name)
+def _gamma(gamma, dim, name):
+    """Address of a bf16 [head_dim] vector, or None."""
+    if gamma is None:
+        return None
+    if gamma.dtype is not _BF16 or gamma.shape != (dim,) or gamma.stride(0) != 1:
+        raise ValueError(name + " must be bf16 [head_dim]")
+    return gamma.data_ptr()
 
 
-def _positions_ok(positions, rows):
-    _need(positions.dtype == torch.int32 and positions.shape == (rows,) and positions.is_contiguous(),
-          "positions must be int32 [rows]")
+def _positions(positions, rows):
+    if positions is None:
+        return None
+    if positions.dtype is not torch.int32 or positions.shape != (rows,) or not positions.is_contiguous():
+        raise ValueError("positions must be int32 [rows]")
+    return positions.data_ptr()
 
 
 def qk_norm_rope(q, k, positions=None, rope: Rope = None, q_gamma=None, k_gamma=None, eps=1e-6, q_out=None, k_out=None,
@@ -169,28 +183,36 @@ def qk_norm_rope(q, k, positions=None, rope: Rope = None, q_gamma=None, k_gamma=
     its gamma) and the rotation of its first elements by ``positions`` (int32
     [rows]), in one pass.  Returns (q, k); q_out and k_out may be q and k."""
     one = q if q is not None else k
-    _need(one is not None, "q or k must be given")
-    dim, rows = one.shape[-1], one.shape[0]
-    inv_freq = rope.inv_freq if rope is not None else None
-    for name, x, gamma in (("q", q, q_gamma), ("k", k, k_gamma)):
-        if x is not None:
-            _rows_ok(x, None, dim, name)
-            _need(x.shape[0] == rows and x.device == one.device, "q and k differ in rows or device")
-            _gamma_ok(gamma, dim, name + "_gamma")
-    if inv_freq is not None:
-        _need(positions is not None, "a rotation needs positions")
-        _positions_ok(positions, rows)
-    if q is not None:
-        q_out = _like_rows(q, stream) if q_out is None else q_out
-        _rows_ok(q_out, q.shape[1], dim, "q_out")
-        _need(q_out.shape[0] == rows, "q_out has the wrong rows")
-    if k is not None:
-        k_out = _like_rows(k, stream) if k_out is None else k_out
-        _rows_ok(k_out, k.shape[1], dim, "k_out")
-        _need(k_out.shape[0] == rows, "k_out has the wrong rows")
-    _run(one, _a.nvfp4_qk_norm_rope, q, q_gamma, q_out, k, k_gamma, k_out, eps, positions if inv_freq is not None else None,
-         inv_freq, 0 if rope is None else rope.interleaved, stream)
-    return (q_out if q is not None else None), (k_out if k is not None else None)
+    if one is None:
+        raise ValueError("q or k must be given")
+    rows = one.shape[0]
+    args, out, dim = [], [], None
+    for x, gamma, y, names in ((q, q_gamma, q_out, ("q", "q_gamma", "q_out")), (k, k_gamma, k_out, ("k", "k_gamma", "k_out"))):
+        if x is None:
+            args += (None, 0, 0, None, None, 0)
+            out.append(None)
+            continue
+        n, heads, d, ld = _rows(x, names[0])
+        dim = d if dim is None else dim
+        if n != rows or d != dim:
+            raise ValueError("q and k differ in rows or head_dim")
+        if y is None:
+            y = _like_rows(x, stream)
+            ldy = heads * d
+        else:
+            ny, hy, dy, ldy = _rows(y, names[2])
+            if (ny, hy, dy) != (n, heads, d) or y.device != x.device:
+                raise ValueError(names[2] + " must have the shape and device of its input")
+        args += (x.data_ptr(), ld, heads, _gamma(gamma, d, names[1]), y.data_ptr(), ldy)
+        out.append(y)
+    if q is not None and k is not None and q.device != k.device:
+        raise ValueError("q and k are on several devices")
+    inv_freq, half, interleaved = rope.pointer if rope is not None else (None, 0, 0)
+    if half and positions is None:
+        raise ValueError("a rotation needs positions")
+    _run(one, _a.qk_norm_rope, *args, rows, dim, eps, _positions(positions, rows) if half else None, inv_freq, 2 * half,
+         interleaved, stream)
+    return tuple(out)
 
 
 def kv_append(cache: KVCache, batch: Batch, k, v, k_gamma=None, eps=1e-6, rope: Rope = None, positions=None,
@@ -198,16 +220,17 @@ def kv_append(cache: KVCache, batch: Batch, k, v, k_gamma=None, eps=1e-6, rope: 
     """Append a step's keys (normed and rotated on the way, each token by its
     number in its sequence unless ``positions`` are given) and values to the
     cache, with scales taken from the values, or the cache's own if ``static``."""
-    _rows_ok(k, cache.kv_heads, cache.head_dim, "k")
-    _rows_ok(v, cache.kv_heads, cache.head_dim, "v")
-    _need(k.shape[0] == v.shape[0] == batch.rows, "k and v must have the batch's rows")
-    _need(k.device == v.device == cache.device == batch.device, "tensors are on several devices")
-    _gamma_ok(k_gamma, cache.head_dim, "k_gamma")
-    if positions is not None:
-        _positions_ok(positions, batch.rows)
-    inv_freq = rope.inv_freq if rope is not None else None
-    _run(k, _a.nvfp4_kv_append, cache.ref, batch.ref, k, v, k_gamma, eps, positions, inv_freq,
-         0 if rope is None else rope.interleaved, _c.NVFP4_STATIC if static else _c.NVFP4_DYNAMIC, stream)
+    rows, heads, dim, ldk = _rows(k, "k")
+    rows_v, heads_v, dim_v, ldv = _rows(v, "v")
+    if rows != batch.rows or rows_v != rows:
+        raise ValueError("k and v must have the batch's rows")
+    if heads != cache.kv_heads or heads_v != heads or dim != cache.head_dim or dim_v != dim:
+        raise ValueError("k and v must have the cache's heads and head_dim")
+    if not k.device == v.device == cache.device == batch.device:
+        raise ValueError("tensors are on several devices")
+    inv_freq, half, interleaved = rope.pointer if rope is not None else (None, 0, 0)
+    _run(k, _a.kv_append, cache.ref, batch.ref, k.data_ptr(), ldk, v.data_ptr(), ldv, _gamma(k_gamma, dim, "k_gamma"),
+         eps, _positions(positions, rows), inv_freq, 2 * half, interleaved, 1 if static else 0, stream)
 
 
 def attention(q, cache: KVCache, batch: Batch, scale=None, causal=True, window=0, out=None, return_lse=False,
@@ -216,20 +239,28 @@ def attention(q, cache: KVCache, batch: Batch, scale=None, causal=True, window=0
     tokens already.  ``scale``: 1 / sqrt(head_dim) unless given.  Returns y
     (bf16, q's shape), with the rows' log-sum-exp (float32 [rows, q_heads]) if
     ``return_lse``.  Rows behind the batch's last sequence are left as they are."""
-    _rows_ok(q, None, cache.head_dim, "q")
-    _need(q.shape[0] == batch.rows and q.shape[1] % cache.kv_heads == 0, "q has the wrong rows or heads")
-    _need(q.device == cache.device == batch.device, "tensors are on several devices")
-    y = _like_rows(q, stream) if out is None else out
-    if out is not None:
-        _rows_ok(y, q.shape[1], cache.head_dim, "out")
-        _need(y.shape[0] == q.shape[0] and y.device == q.device, "out has the wrong rows or device")
+    rows, heads, dim, ldq = _rows(q, "q")
+    if rows != batch.rows or dim != cache.head_dim or heads == 0 or heads % cache.kv_heads:
+        raise ValueError("q has the wrong rows, heads or head_dim")
+    if not q.device == cache.device == batch.device:
+        raise ValueError("tensors are on several devices")
+    if out is None:
+        y, ldy = _like_rows(q, stream), heads * dim
+    else:
+        y = out
+        rows_y, heads_y, dim_y, ldy = _rows(y, "out")
+        if (rows_y, heads_y, dim_y) != (rows, heads, dim) or y.device != q.device:
+            raise ValueError("out must have q's shape and device")
     lse = None
     if return_lse:
         with _l._on(stream, q.device):
-            lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+            lse = torch.empty((rows, heads), dtype=torch.float32, device=q.device)
     if workspace is None:
-        nbytes = batch.workspace_bytes(cache, q.shape[1])
+        nbytes = batch.workspace_bytes(cache, heads)
         workspace = _l._scratch(nbytes, q.device, stream) if nbytes else None
-    scale = 1.0 / math.sqrt(cache.head_dim) if scale is None else scale
-    _run(q, _a.nvfp4_kv_attention, cache.ref, batch.ref, q, y, lse, scale, 1 if causal else 0, window, workspace, stream)
+    else:
+        nbytes = workspace.numel() * workspace.element_size()
+    _run(q, _a.kv_attention, cache.ref, batch.ref, q.data_ptr(), ldq, heads, y.data_ptr(), ldy,
+         None if lse is None else lse.data_ptr(), cache.softmax_scale if scale is None else scale, 1 if causal else 0,
+         window, None if workspace is None else workspace.data_ptr(), nbytes, stream)
     return (y, lse) if return_lse else y

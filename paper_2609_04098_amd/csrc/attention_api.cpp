@@ -169,6 +169,7 @@ int nvfp4_kv_attention(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
       !valid_rows(y, ldy, q_heads, cache->head_dim, batch->rows) || !aligned(lse, 4))
     return NVFP4_EINVAL;
   const double scale = (double)softmax_scale * 1.4426950408889634;      // (powers of two)
+  if (batch->rows * q_heads >= kI32Lim) return NVFP4_EINVAL;
   if (!isfinite((float)scale) || (causal != 0 && causal != 1) || window < 0 || window >= kI32Lim) return NVFP4_EINVAL;
   const size_t need = nvfp4_kv_attention_workspace(cache, batch, q_heads);
   if (need > 0) {

@@ -89,4 +89,28 @@ __device__ __forceinline__ SeqRows seq_rows(const KvBatchArgs& a, int b) {
   return s;
 }
 
+__device__ __forceinline__ int row_bound(const KvBatchArgs& a, int b) { return min(max(a.cu_rows[b], 0), a.rows); }
+
+// The last of n entries (n >= 1) whose key is at most `value` (the first if
+// none is), and its key.  Keys do not decrease.  A wave looks at 64 entries at
+// a time, so that up to 64 entries cost one load's latency and up to 4096 two;
+// all 64 lanes call it with the same arguments.
+template <typename Key>
+__device__ __forceinline__ int last_at_most(int n, int value, int& entry, Key key) {
+  const int lane = threadIdx.x & 63;
+  int stride = 1, lo = 0;
+  while (stride * 64 < n) stride *= 64;
+  int found = 0;
+  for (; stride > 0; stride /= 64) {
+    const int at = lo + lane * stride;
+    const int k = key(min(at, n - 1));
+    const unsigned long long hit = __ballot(at < n && k <= value);
+    const int i = hit == 0 ? 0 : 63 - __builtin_clzll(hit);
+    found = __builtin_amdgcn_readlane(k, i);
+    lo += i * stride;
+  }
+  entry = __builtin_amdgcn_readfirstlane(min(lo, n - 1));
+  return found;
+}
+
 }  // namespace nvfp4

@@ -72,6 +72,9 @@ struct AttentionArgs {
 hipError_t launch_qk_norm_rope(const NormRopeArgs& a, int dim, hipStream_t stream);
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream);
 size_t kv_attention_workspace_bytes(const KvCacheArgs& cache, const KvBatchArgs& batch, int q_heads);
+// The attention of many rows in tiles of 128 packed rows (kv_attention_tile.hip;
+// called by launch_kv_attention, which joins the pieces).
+hipError_t launch_kv_attention_tile(const AttentionArgs& a, int64_t tiles, hipStream_t stream);
 hipError_t launch_kv_attention(const AttentionArgs& a, void* workspace, hipStream_t stream);
 
 // attention_api.cpp and api.cpp share the device check and the record of the

@@ -1,25 +1,32 @@
 // Append of keys and values to the paged E4M3 cache, keys normed and rotated on
 // the way, for gfx950 (layout: nvfp4_attention.h).
 //
-// One workgroup per touched page, head, and keys or values: it holds all its
-// new tokens (at most 16384 elements, 64 a lane) in registers between the
-// maximum and the rounding, so the input is read once, no workgroup waits for
-// another and the result does not depend on any order.  Codes go through LDS
-// into the cache's order and leave it in 16-byte pieces.
+// Many rows: one workgroup for each touched page, head, and keys or values.  It
+// holds its new tokens (at most 16384 elements, 64 a lane) in registers between
+// the maximum and the rounding, so the input is read once, no workgroup waits
+// for another and the result does not depend on any order.  Codes go through
+// LDS into the cache's order and leave it in 16-byte pieces.
+// Few rows (under 8 for a sequence): one wave for each touched page, keys or
+// values, and as many heads as it has lanes for (512 / D); the codes are stored
+// from registers.
 //
 // Keys are computed in binary64: an 8-bit rounding turns the last bit of a
-// binary32 value that is next to a border into a step of 6 to 12 %.  The value
-// reaches the rounding as the binary32 number with the sticky last bit (cut
-// towards zero, last bit set where anything was cut), whose rounding to E4M3 is
-// that of the value itself; a power-of-two scale does not change that.
+// binary32 value that is next to a border into a step of 6 to 12 %, and binary64
+// products issue at the rate of binary32 ones here.  A value reaches the rounding
+// as the binary32 number with the sticky last bit (cut towards zero, last bit
+// set where anything was cut), whose rounding to E4M3 is that of the value
+// itself; a power-of-two scale does not change that.  (In binary32, with the
+// codes of the value less and plus its error compared and waves computed again
+// where they differ, the same took 123 us for 16000 tokens of 8 heads of 128.)
 #include "attention_device.h"
 
 namespace nvfp4 {
 
 constexpr int kAppendThreads = 256;
+constexpr float kLargest = 3.40282347e38f;
 
 // The binary32 number next to d towards zero, with its last bit set unless it
-// is d itself.
+// is d itself: rounds to E4M3 as d does, also after a division by a power of two.
 __device__ __forceinline__ float sticky(double d) {
   const float f = (float)d;
   const double back = (double)f;
@@ -35,11 +42,6 @@ __device__ __forceinline__ float page_scale(float a) {
   return __uint_as_float((uint32_t)(max(k, -100) + 127) << 23);
 }
 
-__device__ __forceinline__ double shfl_xor_f64(double v, int m) {
-  const int lo = __shfl_xor(__double2loint(v), m), hi = __shfl_xor(__double2hiint(v), m);
-  return __hiloint2double(hi, lo);
-}
-
 __device__ __forceinline__ double shfl_f64(double v, int l) {
   const int lo = __shfl(__double2loint(v), l), hi = __shfl(__double2hiint(v), l);
   return __hiloint2double(hi, lo);
@@ -51,155 +53,231 @@ __device__ __forceinline__ uint32_t rescaled(uint32_t codes, float ratio) {
   return e4m3_codes(lo.x * ratio, lo.y * ratio, hi.x * ratio, hi.y * ratio);
 }
 
-// kPasses * 2048 / D tokens at most.
+// What a lane does to its 8 elements e0 .. e0 + 7 of a head held by D / 8 lanes.
+struct Treatment {
+  bool norm, rotate;             // keys only
+  bool turned;                   // these elements are among the rotated ones
+  bool interleaved;
+  int half, e0, partner;         // the lane that holds the other elements of the pairs
+  uint4 gamma;
+  float eps;
+};
+
+template <int D>
+__device__ __forceinline__ Treatment treatment(const AppendArgs& a, int kind) {
+  Treatment t;
+  const int lane = threadIdx.x & 63;
+  t.half = a.rope.rot / 2;
+  t.e0 = (lane % (D / 8)) * 8;
+  t.norm = kind == 0 && a.gamma != nullptr;
+  t.rotate = kind == 0 && t.half > 0;
+  t.turned = t.rotate && t.e0 < a.rope.rot;
+  t.interleaved = a.rope.interleaved;
+  t.partner = lane;
+  if (t.turned && !t.interleaved) t.partner = lane + (t.e0 < t.half ? t.half / 8 : -(t.half / 8));
+  t.gamma = make_uint4(0, 0, 0, 0);
+  if (t.norm) t.gamma = *reinterpret_cast<const uint4*>(a.gamma + t.e0);
+  t.eps = a.eps;
+  return t;
+}
+
+__device__ __forceinline__ void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// 1 / sqrt(x) to 2^-42, from the binary32 one (2^-21).
+__device__ __forceinline__ double reciprocal_root(double x) {
+  const double r = (double)(1.0f / sqrtf((float)x));
+  return r * fma(-0.5 * x * r, r, 1.5);
+}
+
+// The lane's 8 values, ready for rounding.  turn: cosines and sines of the
+// token's angles.  All lanes of the wave call it.
+template <int D>
+__device__ __forceinline__ void values(const Treatment& t, uint4 in, const double2* turn, float (&v)[8]) {
+  const uint32_t d[4] = {in.x, in.y, in.z, in.w}, g[4] = {t.gamma.x, t.gamma.y, t.gamma.z, t.gamma.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) v[2 * j] = bf16_low(d[j]), v[2 * j + 1] = bf16_high(d[j]);
+  if (!t.norm && !t.rotate) return;
+  double w[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) w[j] = (double)v[j];
+  if (t.norm) {
+    double sum = 0.0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum = fma(w[j], w[j], sum);
+#pragma unroll
+    for (int m = 1; m < D / 8; m *= 2) sum += shfl_f64(sum, (threadIdx.x & 63) ^ m);
+    const double r = reciprocal_root(sum * (1.0 / D) + (double)t.eps);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      w[2 * j] *= r * (double)bf16_low(g[j]);
+      w[2 * j + 1] *= r * (double)bf16_high(g[j]);
+    }
+  }
+  if (t.rotate) {
+    double p[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) p[j] = t.interleaved ? w[j ^ 1] : shfl_f64(w[j], t.partner);
+    if (t.turned) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int e = t.e0 + j;
+        const bool second = t.interleaved ? (j & 1) : e >= t.half;
+        const double2 cs = turn[t.interleaved ? e / 2 : (second ? e - t.half : e)];
+        w[j] = fma(w[j], cs.x, second ? p[j] * cs.y : -(p[j] * cs.y));
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = sticky(w[j]);
+}
+
+// v / scale with the sticky last bit.
+__device__ __forceinline__ float quotient(float v, float scale) { return sticky((double)v / (double)scale); }
+
+// Codes of 8 values over the scale (inverse: 1 / scale, used where it is exact).
+// Values that are not finite give NaN.
+__device__ __forceinline__ uint2 eight_codes(const float (&v)[8], bool dynamic, float scale, float inverse) {
+  float q[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float x = dynamic ? v[j] * inverse : quotient(v[j], scale);
+    q[j] = fabsf(v[j]) <= kLargest ? __builtin_amdgcn_fmed3f(x, -448.0f, 448.0f) : __uint_as_float(0x7FC00000u);
+  }
+  return make_uint2(e4m3_codes(q[0], q[1], q[2], q[3]), e4m3_codes(q[4], q[5], q[6], q[7]));
+}
+
+// The page that a workgroup or wave writes to, and which of the step's tokens.
+struct Touch {
+  int page;
+  int n, slot0, row0, token0;      // tokens, first slot, first row, first token's number
+};
+
+// Item of the step: sequence b's pages have the numbers from
+// cu_rows[b] / page_size + 2 b on (n rows reach (n - 1) / page_size + 2 pages).
+__device__ __forceinline__ bool find_touch(const AppendArgs& a, int item, Touch& t) {
+  const int shift = a.cache.page_shift;
+  int b = item, ordinal = 0;
+  if (a.batch.cu_rows != nullptr)
+    ordinal = item - last_at_most(a.batch.seqs, item, b, [&](int x) { return (row_bound(a.batch, x) >> shift) + 2 * x; });
+  const SeqRows s = seq_rows(a.batch, b);
+  const int begin = max(s.first, 0), entry = (begin >> shift) + ordinal;
+  if (ordinal < 0 || entry >= (a.batch.max_tokens >> shift)) return false;
+  const int t0 = max(begin, entry << shift), t1 = min(s.len, (entry + 1) << shift);
+  if (t0 >= t1) return false;
+  t.page = a.batch.table[(int64_t)b * a.batch.table_stride + entry];
+  t.n = t1 - t0;
+  t.slot0 = t0 - (entry << shift);
+  t.row0 = s.row + (t0 - s.first);
+  t.token0 = t0;
+  return t.page >= 0 && t.page < a.cache.num_pages;
+}
+
+__device__ __forceinline__ int position(const AppendArgs& a, const Touch& t, int i) {
+  return a.rope.positions != nullptr ? a.rope.positions[t.row0 + i] : t.token0 + i;
+}
+
+// Held tokens (slots below slot0) of one page and head, brought to a grown
+// scale: pieces start, start + step, ...
+template <int D>
+__device__ __forceinline__ void bring_along(uint8_t* out, int kind, int slot0, float ratio, int start, int step) {
+  const int pieces = ((slot0 + 15) / 16) * D;
+  for (int x = start; x < pieces; x += step) {
+    const int group = x / D, in_group = x % D;
+    uint4* at = reinterpret_cast<uint4*>(out) + x;
+    // Of a piece of keys, one token; of values, four, held ones first.
+    const int held = slot0 - (kind == 0 ? group * 16 + (in_group & 15) : group * 16 + ((in_group >> 4) & 3) * 4);
+    if (held <= 0) continue;
+    const uint32_t keep = kind == 0 || held >= 4 ? 0u : 0xFFFFFFFFu << (8 * held);
+    const uint4 c = *at;
+    *at = make_uint4((c.x & keep) | (rescaled(c.x, ratio) & ~keep), (c.y & keep) | (rescaled(c.y, ratio) & ~keep),
+                     (c.z & keep) | (rescaled(c.z, ratio) & ~keep), (c.w & keep) | (rescaled(c.w, ratio) & ~keep));
+  }
+}
+
+// A lane's 8 codes of the token in slot t into a page and head's bytes.
+template <int D>
+__device__ __forceinline__ void put_codes(uint8_t* out, int kind, int t, int e0, uint2 c) {
+  const int base = (t / 16) * 16 * D, u = t % 16;
+  if (kind == 0) {
+    *reinterpret_cast<uint2*>(out + base + (e0 / 16) * 256 + u * 16 + (e0 & 8)) = c;
+  } else {
+    uint8_t* to = out + base + (e0 / 64) * 1024 + ((u / 4) * 16 + (e0 & 8)) * 16 + (e0 / 16 % 4) * 4 + u % 4;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) to[j * 16] = (uint8_t)((j < 4 ? c.x : c.y) >> (8 * (j & 3)));
+  }
+}
+
+// Many rows.  kPasses * 2048 / D tokens at most.
 template <int D, int kPasses>
-__global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs a) {
-  constexpr int kLanes = D / 8, kTokens = kAppendThreads / kLanes;        // of one pass
+__global__ __launch_bounds__(kAppendThreads, 2) void kv_append_pages_kernel(AppendArgs a) {
+  constexpr int kLanes = D / 8, kTokens = kAppendThreads / kLanes, kWaveTokens = 64 / kLanes;        // of one pass
   __shared__ union {
-    double2 turn[kTokens * D / 2];
+    double2 turn[kAppendThreads / 64][kWaveTokens][D / 2];
     uint8_t codes[kPasses * kTokens * D];
   } lds;
   __shared__ float wave_max[kAppendThreads / 64];
 
   const int kind = blockIdx.x & 1;                        // 0: keys, 1: values
-  const int h = (int)(blockIdx.x >> 1) % a.cache.heads, item = (int)(blockIdx.x >> 1) / a.cache.heads;
-  const int shift = a.cache.page_shift, page_size = a.cache.page_size;
+  const int h = (int)(blockIdx.x >> 1) % a.cache.heads;
+  Touch t;
+  if (!find_touch(a, (int)(blockIdx.x >> 1) / a.cache.heads, t)) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine = threadIdx.x / kLanes;
+  const Treatment how = treatment<D>(a, kind);
+  const int e0 = how.e0;
+  const uint16_t* x = (kind ? a.x[1] : a.x[0]) + (int64_t)t.row0 * (kind ? a.ld[1] : a.ld[0]) + (int64_t)h * D + e0;
+  const int64_t ld = kind ? a.ld[1] : a.ld[0];
+  const auto load = [&](int i) { return i < t.n ? *reinterpret_cast<const uint4*>(x + i * ld) : make_uint4(0, 0, 0, 0); };
 
-  // Sequence and page: sequence b's pages have the numbers from
-  // cu_rows[b] / page_size + 2 b on (n rows reach (n - 1) / page_size + 2 pages).
-  int b = item, ordinal = 0;
-  if (a.batch.cu_rows != nullptr) {
-    int lo = 0, hi = a.batch.seqs - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if ((min(max(a.batch.cu_rows[mid], 0), a.batch.rows) >> shift) + 2 * mid <= item)
-        lo = mid;
-      else
-        hi = mid - 1;
-    }
-    b = lo;
-    ordinal = item - ((min(max(a.batch.cu_rows[b], 0), a.batch.rows) >> shift) + 2 * b);
-  }
-  const SeqRows s = seq_rows(a.batch, b);
-  const int begin = max(s.first, 0);
-  const int entry = (begin >> shift) + ordinal;
-  const int t0 = max(begin, entry << shift), t1 = min(s.len, (entry + 1) << shift);      // tokens
-  if (ordinal < 0 || t0 >= t1 || entry >= (a.batch.max_tokens >> shift)) return;
-  const int page = a.batch.table[(int64_t)b * a.batch.table_stride + entry];
-  if (page < 0 || page >= a.cache.num_pages) return;
-  const int n = t1 - t0, slot0 = t0 - (entry << shift);
-  const int row0 = s.row + (t0 - s.first);
-
-  const int lane = threadIdx.x & 63, e0 = (threadIdx.x % kLanes) * 8;
-  const int rot = a.rope.rot, half = rot / 2;
-  const bool norm = kind == 0 && a.gamma != nullptr, rotate = kind == 0 && rot > 0;
-  int partner = lane;
-  if (rotate && e0 < rot && !a.rope.interleaved) partner = lane + (e0 < half ? half / 8 : -(half / 8));
-
+  uint4 in[kPasses];
+#pragma unroll
+  for (int p = 0; p < kPasses; ++p) in[p] = load(p * kTokens + mine);
   float v[kPasses][8];
   float top = 0.0f;
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) {
-    if (p * kTokens >= n) break;
-    const int i = p * kTokens + threadIdx.x / kLanes;
-    uint4 in = make_uint4(0, 0, 0, 0);
-    if (i < n)
-      in = *reinterpret_cast<const uint4*>(a.x[kind] + (int64_t)(row0 + i) * a.ld[kind] + (int64_t)h * D + e0);
-    const uint32_t d[4] = {in.x, in.y, in.z, in.w};
-    if (!norm && !rotate) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) v[p][2 * j] = bf16_low(d[j]), v[p][2 * j + 1] = bf16_high(d[j]);
-    } else {
-      double w[8];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) w[2 * j] = (double)bf16_low(d[j]), w[2 * j + 1] = (double)bf16_high(d[j]);
-      if (norm) {
-        double sum = 0.0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum = fma(w[j], w[j], sum);
-#pragma unroll
-        for (int m = 1; m < kLanes; m *= 2) sum += shfl_xor_f64(sum, m);
-        const double r = 1.0 / sqrt(sum * (1.0 / D) + (double)a.eps);
-        const uint4 g4 = *reinterpret_cast<const uint4*>(a.gamma + e0);
-        const uint32_t g[4] = {g4.x, g4.y, g4.z, g4.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          w[2 * j] *= r * (double)bf16_low(g[j]);
-          w[2 * j + 1] *= r * (double)bf16_high(g[j]);
-        }
+    if (p * kTokens >= t.n) break;
+    const int i = p * kTokens + mine;
+    double2* turn = lds.turn[wave][lane / kLanes];
+    if (how.rotate) {
+      // The token's angles, by the D / 8 lanes that hold it (at most 4 each).
+      const int pos = position(a, t, min(i, t.n - 1));
+      wave_lds_fence();
+      for (int f = e0 / 8; f < how.half; f += kLanes) {
+        double s, c;
+        sin_cos<double>(pos, a.rope.inv_freq[f], s, c);
+        turn[f] = make_double2(c, s);
       }
-      if (rotate) {
-        const int tokens = min(kTokens, n - p * kTokens);
-        __syncthreads();
-        for (int x = threadIdx.x; x < tokens * half; x += kAppendThreads) {
-          const int t = x / half, f = x % half, at = p * kTokens + t;
-          const int pos = a.rope.positions != nullptr ? a.rope.positions[row0 + at] : t0 + at;
-          double si, co;
-          sin_cos<double>(pos, a.rope.inv_freq[f], si, co);
-          lds.turn[x] = make_double2(co, si);
-        }
-        __syncthreads();
-        double q[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = a.rope.interleaved ? w[j ^ 1] : shfl_f64(w[j], partner);
-        if (e0 < rot && i < n) {
-          const double2* t = lds.turn + (threadIdx.x / kLanes) * half;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int e = e0 + j;
-            const bool second = a.rope.interleaved ? (j & 1) : e >= half;
-            const double2 cs = t[a.rope.interleaved ? e / 2 : (second ? e - half : e)];
-            w[j] = fma(w[j], cs.x, second ? q[j] * cs.y : -(q[j] * cs.y));
-          }
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[p][j] = sticky(w[j]);
+      wave_lds_fence();
     }
-    if (i < n) {
+    values<D>(how, in[p], turn, v[p]);
+    if (i < t.n) {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const float m = fabsf(v[p][j]);
-        if (m <= 3.40282347e38f) top = fmaxf(top, m);      // (a value that is not finite has no part in the scale)
+        if (m <= kLargest) top = fmaxf(top, m);      // (a value that is not finite has no part in the scale)
       }
     }
   }
 
-  float* scale_at = a.cache.scale[kind] + (int64_t)page * a.cache.scale_stride + h;
-  uint8_t* out = a.cache.kv[kind] + (int64_t)page * a.cache.page_stride[kind] + (int64_t)h * page_size * D;
+  float* scale_at = (kind ? a.cache.scale[1] : a.cache.scale[0]) + (int64_t)t.page * a.cache.scale_stride + h;
+  uint8_t* out = (kind ? a.cache.kv[1] : a.cache.kv[0]) +
+                 (int64_t)t.page * (kind ? a.cache.page_stride[1] : a.cache.page_stride[0]) +
+                 (int64_t)h * a.cache.page_size * D;
   float scale;
   if (a.dynamic) {
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
-    if (lane == 0) wave_max[threadIdx.x >> 6] = top;
-    const float held = slot0 > 0 ? *scale_at : 0.0f;
+    if (lane == 0) wave_max[wave] = top;
+    const float held = t.slot0 > 0 ? *scale_at : 0.0f;
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < kAppendThreads / 64; ++w) top = fmaxf(top, wave_max[w]);
     scale = fmaxf(held, page_scale(top));
-    if (scale > held && slot0 > 0) {
-      // The tokens that the page holds, brought to the grown scale.
-      const float ratio = held / scale;
-      const int pieces = ((slot0 + 15) / 16) * D;
-      for (int x = threadIdx.x; x < pieces; x += kAppendThreads) {
-        const int group = x / D, in_group = x % D;
-        uint4* at = reinterpret_cast<uint4*>(out) + x;
-        if (kind == 0) {
-          if (group * 16 + (in_group & 15) < slot0) {
-            const uint4 c = *at;
-            *at = make_uint4(rescaled(c.x, ratio), rescaled(c.y, ratio), rescaled(c.z, ratio), rescaled(c.w, ratio));
-          }
-        } else {
-          const int held_here = slot0 - (group * 16 + ((in_group >> 4) & 3) * 4);        // of the piece's four tokens
-          if (held_here > 0) {
-            const uint32_t keep = held_here >= 4 ? 0u : 0xFFFFFFFFu << (8 * held_here);
-            const uint4 c = *at;
-            *at = make_uint4((c.x & keep) | (rescaled(c.x, ratio) & ~keep), (c.y & keep) | (rescaled(c.y, ratio) & ~keep),
-                             (c.z & keep) | (rescaled(c.z, ratio) & ~keep), (c.w & keep) | (rescaled(c.w, ratio) & ~keep));
-          }
-        }
-      }
-    }
+    if (scale > held && t.slot0 > 0) bring_along<D>(out, kind, t.slot0, held / scale, threadIdx.x, kAppendThreads);
   } else {
     scale = *scale_at;
   }
@@ -208,46 +286,29 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs a)
   __syncthreads();      // the rotation's table has been read, the held codes are written
 #pragma unroll
   for (int p = 0; p < kPasses; ++p) {
-    if (p * kTokens >= n) break;
-    const int i = p * kTokens + threadIdx.x / kLanes;
-    if (i < n) {
-      const int t = slot0 + i;
-      float q[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float x = a.dynamic ? v[p][j] * inverse : v[p][j] / scale;
-        q[j] = fabsf(v[p][j]) <= 3.40282347e38f ? __builtin_amdgcn_fmed3f(x, -448.0f, 448.0f) : __uint_as_float(0x7FC00000u);
-      }
-      const uint32_t c0 = e4m3_codes(q[0], q[1], q[2], q[3]), c1 = e4m3_codes(q[4], q[5], q[6], q[7]);
-      const int base = (t / 16) * 16 * D, u = t % 16;
-      if (kind == 0) {
-        *reinterpret_cast<uint2*>(lds.codes + base + (e0 / 16) * 256 + u * 16 + (e0 & 8)) = make_uint2(c0, c1);
-      } else {
-        uint8_t* to = lds.codes + base + (e0 / 64) * 1024 + ((u / 4) * 16 + (e0 & 8)) * 16 + (e0 / 16 % 4) * 4 + u % 4;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) to[j * 16] = (uint8_t)((j < 4 ? c0 : c1) >> (8 * (j & 3)));
-      }
-    }
+    if (p * kTokens >= t.n) break;
+    const int i = p * kTokens + mine;
+    if (i < t.n) put_codes<D>(lds.codes, kind, t.slot0 + i, e0, eight_codes(v[p], a.dynamic, scale, inverse));
   }
   __syncthreads();
-  const int last = slot0 + n;
-  for (int x = (slot0 / 16) * D + threadIdx.x; x < ((last + 15) / 16) * D; x += kAppendThreads) {
-    const int group = x / D, in_group = x % D;
-    const uint4 c = reinterpret_cast<const uint4*>(lds.codes)[x];
-    uint4* at = reinterpret_cast<uint4*>(out) + x;
+  const int last = t.slot0 + t.n;
+  for (int y = (t.slot0 / 16) * D + threadIdx.x; y < ((last + 15) / 16) * D; y += kAppendThreads) {
+    const int group = y / D, in_group = y % D;
+    const uint4 c = reinterpret_cast<const uint4*>(lds.codes)[y];
+    uint4* at = reinterpret_cast<uint4*>(out) + y;
     if (kind == 0) {
-      const int t = group * 16 + (in_group & 15);
-      if (t >= slot0 && t < last) *at = c;
+      const int s = group * 16 + (in_group & 15);
+      if (s >= t.slot0 && s < last) *at = c;
     } else {
-      const int t = group * 16 + ((in_group >> 4) & 3) * 4;
-      if (t >= slot0 && t + 4 <= last) {
+      const int s = group * 16 + ((in_group >> 4) & 3) * 4;
+      if (s >= t.slot0 && s + 4 <= last) {
         *at = c;
       } else {
         const uint32_t word[4] = {c.x, c.y, c.z, c.w};
         uint8_t* bytes = reinterpret_cast<uint8_t*>(at);
 #pragma unroll
         for (int u = 0; u < 4; ++u)
-          if (t + u >= slot0 && t + u < last)
+          if (s + u >= t.slot0 && s + u < last)
 #pragma unroll
             for (int j = 0; j < 4; ++j) bytes[j * 4 + u] = (uint8_t)(word[j] >> (8 * u));
       }
@@ -256,29 +317,95 @@ __global__ __launch_bounds__(kAppendThreads) void kv_append_kernel(AppendArgs a)
   if (a.dynamic && threadIdx.x == 0) *scale_at = scale;
 }
 
+// Few rows: one wave for a page, keys or values, and 512 / D heads; its lanes
+// hold one token of each head at a time.
 template <int D>
-hipError_t launch_append(const AppendArgs& a, int64_t blocks, hipStream_t stream) {
+__global__ __launch_bounds__(64) void kv_append_tokens_kernel(AppendArgs a) {
+  constexpr int kLanes = D / 8, kHeads = 64 / kLanes;
+  __shared__ double2 turn[D / 2];
+  const int groups = (a.cache.heads + kHeads - 1) / kHeads;
+  const int kind = blockIdx.x & 1, lane = threadIdx.x;
+  const int h0 = (int)(blockIdx.x >> 1) % groups * kHeads;
+  Touch t;
+  if (!find_touch(a, (int)(blockIdx.x >> 1) / groups, t)) return;
+  const Treatment how = treatment<D>(a, kind);
+  const bool live = h0 + lane / kLanes < a.cache.heads;
+  const int h = min(h0 + lane / kLanes, a.cache.heads - 1);
+  const int64_t ld = kind ? a.ld[1] : a.ld[0];
+  const uint16_t* x = (kind ? a.x[1] : a.x[0]) + (int64_t)t.row0 * ld + (int64_t)h * D + how.e0;
+  const auto load = [&](int i) { return *reinterpret_cast<const uint4*>(x + i * ld); };
+  const auto treated = [&](int i, float(&v)[8]) __attribute__((always_inline)) {
+    const uint4 in = load(i);
+    if (how.rotate) {
+      wave_lds_fence();
+      const int pos = position(a, t, i);
+      for (int f = lane; f < how.half; f += 64) {
+        double s, c;
+        sin_cos<double>(pos, a.rope.inv_freq[f], s, c);
+        turn[f] = make_double2(c, s);
+      }
+      wave_lds_fence();
+    }
+    values<D>(how, in, turn, v);
+  };
+
+  float* scale_at = (kind ? a.cache.scale[1] : a.cache.scale[0]) + (int64_t)t.page * a.cache.scale_stride + h;
+  const float held = a.dynamic && t.slot0 == 0 ? 0.0f : *scale_at;
+  float v[8], scale = held;
+  if (a.dynamic) {
+    float top = 0.0f;
+    for (int i = 0; i < t.n; ++i) {
+      treated(i, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float m = fabsf(v[j]);
+        if (m <= kLargest) top = fmaxf(top, m);
+      }
+    }
+#pragma unroll
+    for (int m = 1; m < kLanes; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+    scale = fmaxf(held, page_scale(top));
+  }
+  uint8_t* out = (kind ? a.cache.kv[1] : a.cache.kv[0]) +
+                 (int64_t)t.page * (kind ? a.cache.page_stride[1] : a.cache.page_stride[0]) +
+                 (int64_t)h * a.cache.page_size * D;
+  if (live && scale > held && t.slot0 > 0) bring_along<D>(out, kind, t.slot0, held / scale, lane % kLanes, kLanes);
+  __syncthreads();      // (the held codes of pieces that new values share are written)
+  const float inverse = 1.0f / scale;
+  for (int i = t.n - 1; i >= 0; --i) {      // (the last one's values are at hand)
+    if (!a.dynamic || i != t.n - 1) treated(i, v);
+    const uint2 c = eight_codes(v, a.dynamic, scale, inverse);
+    if (live) put_codes<D>(out, kind, t.slot0 + i, how.e0, c);
+  }
+  if (a.dynamic && live && lane % kLanes == 0) *scale_at = scale;
+}
+
+template <int D>
+static hipError_t launch(const AppendArgs& a, int64_t items, hipStream_t stream) {
+  const bool few = a.batch.cu_rows == nullptr || a.batch.rows < 8 * (int64_t)a.batch.seqs;
+  const int64_t blocks = 2 * items * (few ? (a.cache.heads * D + 511) / 512 : a.cache.heads);
+  if (blocks >= (int64_t)1 << 31) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks);
   const int elements = a.cache.page_size * D;
-  if (elements <= 2048)
-    kv_append_kernel<D, 1><<<grid, kAppendThreads, 0, stream>>>(a);
+  if (few)
+    kv_append_tokens_kernel<D><<<grid, 64, 0, stream>>>(a);
+  else if (elements <= 2048)
+    kv_append_pages_kernel<D, 1><<<grid, kAppendThreads, 0, stream>>>(a);
   else if (elements <= 4096)
-    kv_append_kernel<D, 2><<<grid, kAppendThreads, 0, stream>>>(a);
+    kv_append_pages_kernel<D, 2><<<grid, kAppendThreads, 0, stream>>>(a);
   else if (elements <= 8192)
-    kv_append_kernel<D, 4><<<grid, kAppendThreads, 0, stream>>>(a);
+    kv_append_pages_kernel<D, 4><<<grid, kAppendThreads, 0, stream>>>(a);
   else
-    kv_append_kernel<D, 8><<<grid, kAppendThreads, 0, stream>>>(a);
+    kv_append_pages_kernel<D, 8><<<grid, kAppendThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream) {
   const int64_t items = a.batch.cu_rows == nullptr ? a.batch.seqs
                                                    : (a.batch.rows >> a.cache.page_shift) + 2 * (int64_t)a.batch.seqs;
-  const int64_t blocks = items * a.cache.heads * 2;
-  if (blocks >= (int64_t)1 << 31) return hipErrorInvalidValue;
-  return a.cache.dim == 64    ? launch_append<64>(a, blocks, stream)
-         : a.cache.dim == 128 ? launch_append<128>(a, blocks, stream)
-                              : launch_append<256>(a, blocks, stream);
+  return a.cache.dim == 64 ? launch<64>(a, items, stream)
+         : a.cache.dim == 128 ? launch<128>(a, items, stream)
+                              : launch<256>(a, items, stream);
 }
 
 }  // namespace nvfp4

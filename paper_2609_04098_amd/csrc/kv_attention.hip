@@ -1,131 +1,17 @@
-// Attention over the paged E4M3 cache for gfx950 (layout and definition:
-// nvfp4_attention.h).
+// Attention of few rows over the paged E4M3 cache for gfx950 (layout and
+// definition: nvfp4_attention.h; the products: kv_attention_device.h).
 //
-// Rows.  The `group` query heads of one key head read the same keys, so a
-// sequence's rows are packed: packed row r is new token r / group with query
-// head h * group + r % group.  A workgroup takes 16 packed rows of one sequence
-// and key head; its four waves take turns with tiles of 32 tokens.
+// A workgroup takes 16 or 32 packed rows of one sequence and key head; its
+// waves take turns with tiles of 32 tokens, and join their results in LDS at
+// the end.  Keys and values go from memory to registers, one tile ahead.  Long
+// sequences are divided further, into pieces for several workgroups, which a
+// second launch joins.
 //
-// One pass with a running maximum m and sum l (in powers of two; the scale
-// holds log2 e):  S^T = K Q^T by v_mfma_f32_16x16x32_bf16 (E4M3 keys are exact
-// in bf16), P = 2^(S - m), Y^T += V^T P^T by v_mfma_f32_16x16x32_f16 (E4M3
-// values are exact in f16).  With the products transposed, a lane holds the
-// scores of ONE row, for the tokens 4 g .. 4 g + 3 of two groups of 16 (g =
-// lane / 16), and these are the elements that the second product wants of it:
-// its contraction index is taken in that order, 8 g + e being token 4 g + e of
-// the first group and 8 g + 4 + e of the second.  So P never leaves its lane.
-// The cache's order makes both operands whole 16-byte loads of a contiguous
-// kilobyte for each wave, without LDS.
-//
-// The page's key scale goes into the scores.  Its value scale goes into P,
-// divided by the largest one met so far (s_ref, by which Y is multiplied at the
-// end), so that P stays at most 1 in binary16: what falls below 2^-25 of the
-// largest value met is dropped.
-//
-// Bound by HBM for few rows: the waves' loads of one tile ahead are what covers
-// its latency.
-#include "attention_device.h"
+// Bound by HBM: the waves' loads of one tile ahead (8 KB a wave for heads of
+// 128) are what covers its latency.
+#include "kv_attention_device.h"
 
 namespace nvfp4 {
-
-constexpr int kRowsThreads = 256;
-constexpr int kRowsWaves = kRowsThreads / 64;
-constexpr int kTileTokens = 32;
-
-// Packed rows of one tile and the tokens that they see.
-struct Tile {
-  int b, row0, rows, r0, n;      // sequence, its first row and rows, first packed row, packed rows of this tile
-  int first;                     // token of the sequence's first new row
-  int begin, end;                // tokens that some row of the tile sees
-};
-
-__device__ __forceinline__ int row_bound(const KvBatchArgs& a, int b) { return min(max(a.cu_rows[b], 0), a.rows); }
-
-// Sequence b's tiles have the numbers from cu_rows[b] * group / kRows + b on
-// (it has ceil(n_b * group / kRows) of them).
-template <int kRows>
-__device__ __forceinline__ bool find_tile(const AttentionArgs& a, int number, Tile& t) {
-  int ordinal;
-  if (a.batch.cu_rows == nullptr) {
-    const int each = (a.group + kRows - 1) / kRows;
-    t.b = number / each;
-    ordinal = number % each;
-  } else {
-    int lo = 0, hi = a.batch.seqs - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) / 2;
-      if ((int)((int64_t)row_bound(a.batch, mid) * a.group / kRows) + mid <= number)
-        lo = mid;
-      else
-        hi = mid - 1;
-    }
-    t.b = lo;
-    ordinal = number - ((int)((int64_t)row_bound(a.batch, lo) * a.group / kRows) + lo);
-  }
-  const SeqRows s = seq_rows(a.batch, t.b);
-  t.row0 = s.row;
-  t.rows = s.rows;
-  t.first = s.first;
-  t.r0 = ordinal * kRows;
-  t.n = min(kRows, s.rows * a.group - t.r0);
-  if (ordinal < 0 || t.n <= 0) return false;
-  const int lowest = t.first + t.r0 / a.group, highest = t.first + (t.r0 + t.n - 1) / a.group;
-  t.end = a.causal ? min(s.len, highest + 1) : s.len;
-  t.begin = a.window > 0 ? max(0, lowest - a.window + 1) : 0;
-  return true;
-}
-
-__device__ __forceinline__ int64_t tiles_of(const KvBatchArgs& a, int group, int rows) {
-  return a.cu_rows == nullptr ? (int64_t)a.seqs * ((group + rows - 1) / rows)
-                              : (int64_t)a.rows * group / rows + a.seqs;
-}
-
-// 8 E4M3 values in bf16 or f16 (exact).
-__device__ __forceinline__ bf16x8 bf16_of(uint32_t a, uint32_t b) {
-  union {
-    bf16x2 p[4];
-    bf16x8 v;
-  } u;
-  u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false);
-  u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true);
-  u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false);
-  u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true);
-  return u.v;
-}
-
-__device__ __forceinline__ f16x8 f16_of(uint32_t a, uint32_t b) {
-  union {
-    f16x2 p[4];
-    f16x8 v;
-  } u;
-  u.p[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false);
-  u.p[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true);
-  u.p[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false);
-  u.p[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true);
-  return u.v;
-}
-
-// E4M3 NaN codes (0x7F, 0xFF) to zero: a masked token's probability is zero,
-// and zero times whatever its slot holds has to be.
-__device__ __forceinline__ uint32_t without_nan(uint32_t x) {
-  const uint32_t hit = ((x & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;      // a byte's top bit where it is NaN
-  return x & ~((hit >> 7) * 255u);
-}
-
-// Maximum and sum over the four lanes lane % 16 + 16 i.
-__device__ __forceinline__ float over_quarters_max(float x) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-
-__device__ __forceinline__ float over_quarters_sum(float x) {
-  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  const float y = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-  const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
-  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
-}
 
 // Keys and values of one tile of 32 tokens, as loaded: [group of 16][64
 // elements of the head].
@@ -133,31 +19,6 @@ template <int D>
 struct TileCodes {
   u32x4 k[2][D / 64], v[2][D / 64];
 };
-
-// Page and scales of the groups of 16 tokens that this wave meets: lane 2 i
-// and 2 i + 1 hold those of its i-th tile from `from` on, page -1 where the
-// group is past the end or its page is not in the cache.
-struct GroupPages {
-  int page;
-  float k_scale, v_scale;
-};
-
-__device__ __forceinline__ GroupPages group_pages(const AttentionArgs& a, int b, int h, int from, int step, int end,
-                                                  int lane) {
-  GroupPages g;
-  g.page = -1;
-  g.k_scale = g.v_scale = 0.0f;
-  const int64_t token = (int64_t)from + (int64_t)(lane >> 1) * step + (lane & 1) * 16;
-  if (token < end) {
-    const int p = a.batch.table[(int64_t)b * a.batch.table_stride + (token >> a.cache.page_shift)];
-    if (p >= 0 && p < a.cache.num_pages) {
-      g.page = p;
-      g.k_scale = a.cache.scale[0][(int64_t)p * a.cache.scale_stride + h];
-      g.v_scale = a.cache.scale[1][(int64_t)p * a.cache.scale_stride + h];
-    }
-  }
-  return g;
-}
 
 template <int D>
 __device__ __forceinline__ void load_tile(const AttentionArgs& a, int h, int token, int page0, int page1, int lane,
@@ -177,16 +38,22 @@ __device__ __forceinline__ void load_tile(const AttentionArgs& a, int h, int tok
   }
 }
 
-constexpr float kNone = -__builtin_inff();
+// Heads of 256: two tiles of codes would take 128 registers a lane, so they go
+// through a ring of two in LDS, of each wave's own.
+template <int D, int kTiles, int kWaves, bool kSplit>
+__global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : kTiles == 1 ? 3 : 2) void
+kv_attention_rows_kernel(AttentionArgs a) {
+  constexpr int kRows = 16 * kTiles, kThreads = kWaves * 64;
+  constexpr int kPart = kWaves > 4 ? 32 : (D > 128 ? 128 : D);            // elements of a row that are joined at a time
+  constexpr bool kRing = D == 256;
+  constexpr int kLoads = 4 * (D / 64);                                    // of a tile into the ring
+  __shared__ union {
+    float joined[kWaves][16][kPart + 4];
+    uint8_t ring[kRing ? kWaves : 1][2][2][2][kRing ? 16 * D : 16];       // [wave][stage][keys, values][group]
+  } lds;
+  __shared__ float2 stats[kWaves][kRows];
 
-template <int D, bool kSplit>
-__global__ __launch_bounds__(kRowsThreads, 2) void kv_attention_rows_kernel(AttentionArgs a) {
-  constexpr int kSteps = D / 32, kOut = D / 16;
-  constexpr int kHalf = D > 128 ? 128 : D;             // elements of a row that are joined at a time
-  __shared__ float joined[kRowsWaves][16][kHalf + 4];
-  __shared__ float2 stats[kRowsWaves][16];
-
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quarter = lane >> 4;
   int id = blockIdx.x;
   const int h = id % a.cache.heads;
@@ -194,7 +61,7 @@ __global__ __launch_bounds__(kRowsThreads, 2) void kv_attention_rows_kernel(Atte
   const int piece = kSplit ? id % a.splits : 0;
   const int number = kSplit ? id / a.splits : id;
   Tile t;
-  if (!find_tile<16>(a, number, t)) return;
+  if (!find_tile<kRows>(a, number, t)) return;
   int begin = t.begin, end = t.end;
   if (kSplit) {
     begin = max(begin, piece * a.chunk);
@@ -202,219 +69,222 @@ __global__ __launch_bounds__(kRowsThreads, 2) void kv_attention_rows_kernel(Atte
     if (begin >= end && !(piece == 0 && t.begin >= t.end)) return;      // (rows that see nothing: piece 0 says so)
   }
 
-  // This lane's row; Q in the order of the keys' loads.
-  const int r = t.r0 + min(col, t.n - 1);
-  const int token_row = t.row0 + r / a.group, head = h * a.group + r % a.group;
-  const int at = t.first + r / a.group;
-  bf16x8 q[kSteps];
-  {
-    const uint16_t* src = a.q + (int64_t)token_row * a.ldq + (int64_t)head * D + quarter * 16;
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-      q[s] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(src + (s / 2) * 64 + (s & 1) * 8));
-  }
-  // Tokens [see0, see1) are seen by this lane's row; [all0, all1) by every row.
-  const int see1 = a.causal ? min(end, at + 1) : end;
-  const int see0 = a.window > 0 ? max(begin, at - a.window + 1) : begin;
-  const int low = t.first + t.r0 / a.group, high = t.first + (t.r0 + t.n - 1) / a.group;
-  const int all1 = a.causal ? min(end, low + 1) : end;
-  const int all0 = a.window > 0 ? max(begin, high - a.window + 1) : begin;
+  RowTiles<D, kTiles> rows;
+  rows.start(a, t, h, t.r0, t.n, lane, begin, end);
+  const float scale = fabsf(a.scale);
 
-  f32x4 o[kOut];
-#pragma unroll
-  for (int i = 0; i < kOut; ++i) o[i] = (f32x4){0, 0, 0, 0};
-  float m = kNone, l = 0.0f, s_ref = 1.17549435e-38f, s_inv = 1.0f / 1.17549435e-38f;
-
-  const int step = kRowsWaves * kTileTokens;
+  const int step = kWaves * kTileTokens;
   int token = (begin & ~(kTileTokens - 1)) + wave * kTileTokens;
-  GroupPages pages = group_pages(a, t.b, h, token, step, end, lane);
+  GroupPages pages = group_pages(a, t.b, h, (int64_t)token + (lane >> 1) * step + (lane & 1) * 16, end);
   int in_batch = 0;
-  TileCodes<D> now, next;
-  if (token < end)
-    load_tile<D>(a, h, token, __builtin_amdgcn_readlane(pages.page, 0), __builtin_amdgcn_readlane(pages.page, 1), lane,
-                 now);
-  while (token < end) {
-    const int page0 = __builtin_amdgcn_readlane(pages.page, 2 * in_batch);
-    const int page1 = __builtin_amdgcn_readlane(pages.page, 2 * in_batch + 1);
-    float ks[2], vs[2];
+  // The tile's scales; then the next batch of pages, if the next tile needs it.
+  const auto scales = [&](bool (&there)[2], float (&ks)[2], float (&vs)[2]) __attribute__((always_inline)) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      ks[g] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(pages.k_scale), 2 * in_batch + g)) * a.scale;
-      vs[g] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(pages.v_scale), 2 * in_batch + g));
+      there[g] = __builtin_amdgcn_readlane(pages.page, 2 * in_batch + g) >= 0;
+      ks[g] = fmaxf(lane_of(pages.k_scale, 2 * in_batch + g) * scale, 1e-37f);      // (not 0: -infinity stays)
+      vs[g] = lane_of(pages.v_scale, 2 * in_batch + g);
     }
-    const int ahead = token + step;
     if (++in_batch == 32) {
-      pages = group_pages(a, t.b, h, ahead, step, end, lane);
+      pages = group_pages(a, t.b, h, (int64_t)token + step + (lane >> 1) * step + (lane & 1) * 16, end);
       in_batch = 0;
     }
-    if (ahead < end)
-      load_tile<D>(a, h, ahead, __builtin_amdgcn_readlane(pages.page, 2 * in_batch),
-                   __builtin_amdgcn_readlane(pages.page, 2 * in_batch + 1), lane, next);
-
-    f32x4 s[2];
+  };
+  bool there[2];
+  float ks[2], vs[2];
+  if constexpr (kRing) {
+    const int mask = a.cache.page_size - 1;
+    const auto issue = [&](int at, int to) __attribute__((always_inline)) {
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      s[g] = (f32x4){0, 0, 0, 0};
+      for (int g = 0; g < 2; ++g) {
+        const int page = __builtin_amdgcn_readlane(pages.page, 2 * in_batch + g);
 #pragma unroll
-      for (int c = 0; c < D / 64; ++c) {
-        s[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of(now.k[g][c][0], now.k[g][c][1]), q[2 * c], s[g], 0, 0, 0);
-        s[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bf16_of(now.k[g][c][2], now.k[g][c][3]), q[2 * c + 1], s[g], 0, 0, 0);
+        for (int kind = 0; kind < 2; ++kind)
+          stage_group<D>(a.cache, kind, page, (at + 16 * g) & mask, h, lane, lds.ring[wave][to][kind][g]);
       }
-    }
-    const bool whole = token >= all0 && token + kTileTokens <= all1 && page0 >= 0 && page1 >= 0;
-    float x[8];
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * g + e] = s[g][e] * ks[g];
-    if (!whole) {
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int j = token + 16 * g + 4 * quarter + e;
-          if (j < see0 || j >= see1 || (g ? page1 : page0) < 0) x[4 * g + e] = kNone;
-        }
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) now.v[g][c][i] = without_nan(now.v[g][c][i]);
-    }
-    float top = fmaxf(fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])), fmaxf(fmaxf(x[4], x[5]), fmaxf(x[6], x[7])));
-    top = over_quarters_max(top);
-    if (__any(top > m)) {
-      const float m_new = fmaxf(m, top);
-      const float f = m == m_new ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);      // (0 from nothing)
-      l *= f;
-#pragma unroll
-      for (int i = 0; i < kOut; ++i) o[i] *= f;
-      m = m_new;
-    }
-    const float v_top = fmaxf(vs[0], vs[1]);
-    if (v_top > s_ref) {
-      const float f = s_ref / v_top;
-#pragma unroll
-      for (int i = 0; i < kOut; ++i) o[i] *= f;
-      s_ref = v_top;
-      s_inv = 1.0f / v_top;
-    }
-    const float base = m == kNone ? 0.0f : m;
-    f16x8 p;
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const float ratio = vs[g] * s_inv;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float w = __builtin_amdgcn_exp2f(x[4 * g + e] - base);
-        l += w;
-        p[4 * g + e] = (_Float16)(w * ratio);
-      }
-    }
-#pragma unroll
-    for (int c = 0; c < D / 64; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        o[4 * c + i] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f16_of(now.v[0][c][i], now.v[1][c][i]), p, o[4 * c + i],
-                                                             0, 0, 0);
-    now = next;
-    token = ahead;
-  }
-
-  // The four waves' results, joined: Y = sum_w 2^(m_w - m) Y_w.
-  l = over_quarters_sum(l);
-  if (quarter == 0) stats[wave][col] = make_float2(m, l);
-  __syncthreads();
-  float m_all = kNone, l_all = 0.0f;
-#pragma unroll
-  for (int w = 0; w < kRowsWaves; ++w) m_all = fmaxf(m_all, stats[w][col].x);
-  const float zero_m = m_all == kNone ? 0.0f : m_all;
-#pragma unroll
-  for (int w = 0; w < kRowsWaves; ++w) l_all += stats[w][col].y * __builtin_amdgcn_exp2f(stats[w][col].x - zero_m);
-  float mine = __builtin_amdgcn_exp2f(m - zero_m) * s_ref;
-  if (!kSplit) mine *= l_all == 0.0f ? 0.0f : 1.0f / l_all;
-  if (threadIdx.x < 16 && threadIdx.x < t.n) {
-    if (kSplit) {
-      float2* to = reinterpret_cast<float2*>(a.part) + (((int64_t)number * a.cache.heads + h) * a.splits + piece) * 16;
-      to[threadIdx.x] = make_float2(m_all, l_all);
-    } else if (a.lse != nullptr) {
-      a.lse[(int64_t)token_row * a.q_heads + head] =
-          l_all == 0.0f ? kNone : (m_all + __builtin_amdgcn_logf(l_all)) * 0.69314718055994531f;
-    }
-  }
-#pragma unroll
-  for (int d0 = 0; d0 < D; d0 += kHalf) {
-    if (d0 > 0) __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kHalf / 16; ++i)
-      *reinterpret_cast<f32x4*>(&joined[wave][col][16 * i + 4 * quarter]) = o[d0 / 16 + i] * mine;
-    __syncthreads();
-    // A thread takes four elements of one row.
-    for (int x = threadIdx.x; x < 16 * kHalf / 4; x += kRowsThreads) {
-      const int row = x / (kHalf / 4), e = (x % (kHalf / 4)) * 4;
-      if (row >= t.n) continue;
-      f32x4 y = (f32x4){0, 0, 0, 0};
-#pragma unroll
-      for (int w = 0; w < kRowsWaves; ++w) y += *reinterpret_cast<const f32x4*>(&joined[w][row][e]);
-      if (kSplit) {
-        const int64_t pieces = (tiles_of(a.batch, a.group, 16) * a.cache.heads) * a.splits * 32;      // floats of stats
-        float* to = a.part + pieces +
-                    ((((int64_t)number * a.cache.heads + h) * a.splits + piece) * 16 + row) * D + d0 + e;
-        *reinterpret_cast<f32x4*>(to) = y;
+    };
+    int stage = 0;
+    if (token < end) issue(token, 0);
+    while (token < end) {
+      scales(there, ks, vs);
+      __builtin_amdgcn_s_waitcnt(kWaitLds);      // the other stage has been read
+      if (token + step < end) {
+        issue(token + step, stage ^ 1);
+        __builtin_amdgcn_s_waitcnt(wait_loads(kLoads));
       } else {
-        const int rr = t.r0 + row;
-        uint16_t* to = a.y + (int64_t)(t.row0 + rr / a.group) * a.ldy + (int64_t)(h * a.group + rr % a.group) * D + d0 + e;
-        *reinterpret_cast<uint2*>(to) = make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
+        __builtin_amdgcn_s_waitcnt(wait_loads(0));
+      }
+      const uint8_t *k = lds.ring[wave][stage][0][0] + lane * 16, *v = lds.ring[wave][stage][1][0] + lane * 16;
+      rows.pass(
+          a, token, there[0], there[1], ks, vs, lane,
+          [&](int g, int c) { return *reinterpret_cast<const u32x4*>(k + g * 16 * D + c * 1024); },
+          [&](int g, int c) { return *reinterpret_cast<const u32x4*>(v + g * 16 * D + c * 1024); });
+      stage ^= 1;
+      token += step;
+    }
+    __syncthreads();      // (the ring's memory joins the results)
+  } else {
+    TileCodes<D> even, odd;
+    const auto load = [&](int at, TileCodes<D>& to) __attribute__((always_inline)) {
+      load_tile<D>(a, h, at, __builtin_amdgcn_readlane(pages.page, 2 * in_batch),
+                   __builtin_amdgcn_readlane(pages.page, 2 * in_batch + 1), lane, to);
+    };
+    const auto pass = [&](TileCodes<D>& now, TileCodes<D>& next) __attribute__((always_inline)) {
+      scales(there, ks, vs);
+      if (token + step < end) load(token + step, next);
+      rows.pass(a, token, there[0], there[1], ks, vs, lane, [&](int g, int c) { return now.k[g][c]; },
+                [&](int g, int c) { return now.v[g][c]; });
+      token += step;
+    };
+    if (token < end) load(token, even);
+    while (token < end) {
+      pass(even, odd);
+      if (token >= end) break;
+      pass(odd, even);
+    }
+  }
+
+  // The waves' results, joined: Y = sum_w 2^(m_w - m) Y_w.
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    rows.l[i] = over_quarters_sum(rows.l[i]);
+    if (quarter == 0) stats[wave][16 * i + col] = make_float2(rows.m[i], rows.l[i]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    float m_all = kNone, l_all = 0.0f;
+    for (int w = 0; w < kWaves; ++w) m_all = fmaxf(m_all, stats[w][16 * i + col].x);
+    const float zero_m = m_all == kNone ? 0.0f : m_all;
+    for (int w = 0; w < kWaves; ++w)
+      l_all += stats[w][16 * i + col].y * __builtin_amdgcn_exp2f(stats[w][16 * i + col].x - zero_m);
+    float mine = __builtin_amdgcn_exp2f(rows.m[i] - zero_m) * rows.s_ref;
+    if (!kSplit) mine *= l_all == 0.0f ? 0.0f : 1.0f / l_all;
+    const int r = t.r0 + 16 * i + col;
+    if (threadIdx.x < 16 && 16 * i + col < t.n) {
+      if (kSplit) {
+        float2* to = reinterpret_cast<float2*>(a.part) + (((int64_t)number * a.cache.heads + h) * a.splits + piece) * kRows;
+        to[16 * i + col] = make_float2(m_all, l_all);
+      } else if (a.lse != nullptr) {
+        a.lse[(int64_t)(t.row0 + r / a.group) * a.q_heads + h * a.group + r % a.group] =
+            l_all == 0.0f ? kNone : (m_all + __builtin_amdgcn_logf(l_all)) * 0.69314718055994531f;
+      }
+    }
+#pragma unroll
+    for (int d0 = 0; d0 < D; d0 += kPart) {
+      if (i > 0 || d0 > 0) __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kPart / 16; ++j)
+        *reinterpret_cast<f32x4*>(&lds.joined[wave][col][16 * j + 4 * quarter]) = rows.o[i][d0 / 16 + j] * mine;
+      __syncthreads();
+      // A thread takes four elements of one row.
+      for (int x = threadIdx.x; x < 16 * kPart / 4; x += kThreads) {
+        const int row = 16 * i + x / (kPart / 4), e = (x % (kPart / 4)) * 4;
+        if (row >= t.n) continue;
+        f32x4 y = (f32x4){0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) y += *reinterpret_cast<const f32x4*>(&lds.joined[w][x / (kPart / 4)][e]);
+        if (kSplit) {
+          const int64_t stats_floats = tiles_of(a.batch, a.group, kRows) * a.cache.heads * a.splits * (2 * kRows);
+          float* to = a.part + stats_floats +
+                      ((((int64_t)number * a.cache.heads + h) * a.splits + piece) * kRows + row) * D + d0 + e;
+          *reinterpret_cast<f32x4*>(to) = y;
+        } else {
+          const int rr = t.r0 + row;
+          uint16_t* to = a.y + (int64_t)(t.row0 + rr / a.group) * a.ldy + (int64_t)(h * a.group + rr % a.group) * D + d0 + e;
+          *reinterpret_cast<uint2*>(to) = make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
+        }
       }
     }
   }
 }
 
-// Joins the pieces of a sequence: one wave for each packed row.
-template <int D>
+// Joins the pieces of a sequence.  kShare waves take a packed row, each its
+// share of the pieces, four pieces' loads in flight.
+template <int D, int kTiles, int kShare>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t task = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int row = (int)(task % 16);
-  const int h = (int)(task / 16 % a.cache.heads);
-  const int64_t number = task / 16 / a.cache.heads;
-  const int64_t tiles = tiles_of(a.batch, a.group, 16);
-  if (number >= tiles) return;
+  constexpr int kRows = 16 * kTiles, kEach = D / 64, kAhead = 4, kBlockRows = 4 / kShare;
+  __shared__ float sums[kShare > 1 ? 4 : 1][kShare > 1 ? D : 1];
+  __shared__ float totals[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, share = wave % kShare;
+  const int row = (int)(blockIdx.x % (kRows / kBlockRows)) * kBlockRows + wave / kShare;
+  const int h = (int)(blockIdx.x / (kRows / kBlockRows)) % a.cache.heads;
+  const int number = (int)(blockIdx.x / (kRows / kBlockRows)) / a.cache.heads;
   Tile t;
-  if (!find_tile<16>(a, (int)number, t) || row >= t.n) return;
-  const int64_t first = (number * a.cache.heads + h) * a.splits;
-  const float2* stats = reinterpret_cast<const float2*>(a.part) + first * 16 + row;
-  const float* part = a.part + tiles * a.cache.heads * a.splits * 32 + (first * 16 + row) * D;
+  if (!find_tile<kRows>(a, number, t) || row >= t.n) return;      // (with kShare 4, the whole workgroup)
+  const int64_t first = ((int64_t)number * a.cache.heads + h) * a.splits;
+  const float2* stats = reinterpret_cast<const float2*>(a.part) + first * kRows + row;
+  const float* part = a.part + tiles_of(a.batch, a.group, kRows) * a.cache.heads * a.splits * (2 * kRows) +
+                      (first * kRows + row) * D + lane * kEach;
   int p0 = 0, p1 = 1;
   if (t.begin < t.end) {
     p0 = min(t.begin / a.chunk, a.splits - 1);
     p1 = min((t.end - 1) / a.chunk, a.splits - 1) + 1;
   }
-  float m = kNone;
-  for (int p = p0 + lane; p < p1; p += 64) m = fmaxf(m, stats[p * 16].x);
+  float m = kNone, l = 0.0f, y[kEach];
 #pragma unroll
-  for (int x = 1; x < 64; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
-  const float base = m == kNone ? 0.0f : m;
-  float l = 0.0f, y[D / 64];
+  for (int i = 0; i < kEach; ++i) y[i] = 0.0f;
+  for (int p = p0 + share; p < p1; p += kShare * kAhead) {
+    float2 st[kAhead];
+    float v[kAhead][kEach];
 #pragma unroll
-  for (int i = 0; i < D / 64; ++i) y[i] = 0.0f;
-  for (int p = p0; p < p1; ++p) {
-    const float2 st = stats[p * 16];
-    const float f = __builtin_amdgcn_exp2f(st.x - base);
-    l += st.y * f;
+    for (int u = 0; u < kAhead; ++u) {
+      const int at = p + u * kShare;
+      st[u] = make_float2(kNone, 0.0f);
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) y[i] = fmaf(part[(int64_t)p * 16 * D + lane * (D / 64) + i], f, y[i]);
+      for (int i = 0; i < kEach; ++i) v[u][i] = 0.0f;
+      if (at < p1) {
+        st[u] = stats[at * kRows];
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) v[u][i] = part[(int64_t)at * kRows * D + i];
+      }
+    }
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) top = fmaxf(top, st[u].x);
+    const float base = top == kNone ? 0.0f : top;
+    const float f = __builtin_amdgcn_exp2f(m - base);
+    m = top;
+    l *= f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) y[i] *= f;
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const float g = __builtin_amdgcn_exp2f(st[u].x - base);
+      l = fmaf(st[u].y, g, l);
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) y[i] = fmaf(v[u][i], g, y[i]);
+    }
   }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   const int r = t.r0 + row, head = h * a.group + r % a.group;
   const int64_t token_row = t.row0 + r / a.group;
-  uint16_t* to = a.y + token_row * a.ldy + (int64_t)head * D + lane * (D / 64);
+  uint16_t* to = a.y + token_row * a.ldy + (int64_t)head * D;
+  if (kShare > 1) {
+    if (lane == 0) totals[wave] = m;
+    __syncthreads();
+    const float top = fmaxf(fmaxf(totals[0], totals[1]), fmaxf(totals[2], totals[3]));
+    const float g = __builtin_amdgcn_exp2f(m - (top == kNone ? 0.0f : top));
+    __syncthreads();
+    if (lane == 0) totals[wave] = l * g;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) sums[kShare > 1 ? wave : 0][kShare > 1 ? lane * kEach + i : 0] = y[i] * g;
+    __syncthreads();
+    m = top;
+    l = (totals[0] + totals[1]) + (totals[2] + totals[3]);
+    if (wave != 0) return;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int e = kShare > 1 ? lane * kEach + i : 0;
+      y[i] = (sums[0][e] + sums[kShare > 1 ? 1 : 0][e]) + (sums[kShare > 1 ? 2 : 0][e] + sums[kShare > 1 ? 3 : 0][e]);
+    }
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   if (D == 64)
-    *to = __builtin_bit_cast(uint16_t, (__bf16)(y[0] * inv));
+    to[lane] = __builtin_bit_cast(uint16_t, (__bf16)(y[0] * inv));
   else
 #pragma unroll
-    for (int i = 0; i + 1 < D / 64; i += 2) *reinterpret_cast<uint32_t*>(to + i) = bf16_pair(y[i] * inv, y[i + 1] * inv);
+    for (int i = 0; i + 1 < kEach; i += 2)
+      *reinterpret_cast<uint32_t*>(to + lane * kEach + i) = bf16_pair(y[i] * inv, y[i + 1] * inv);
   if (a.lse != nullptr && lane == 0)
     a.lse[token_row * a.q_heads + head] = l == 0.0f ? kNone : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
@@ -425,52 +295,86 @@ int64_t host_tiles(const KvBatchArgs& b, int group, int rows) {
   return b.cu_rows == nullptr ? (int64_t)b.seqs * ((group + rows - 1) / rows) : (int64_t)b.rows * group / rows + b.seqs;
 }
 
-// Pieces of a sequence: enough workgroups for four on each of 256 compute
-// units, of 256 tokens at least.
-void plan(const KvCacheArgs& c, const KvBatchArgs& b, int group, int& chunk, int& splits) {
-  const int64_t work = host_tiles(b, group, 16) * c.heads;
-  int64_t want = work > 0 ? (1024 + work - 1) / work : 1;
-  int64_t each = want > 0 ? (b.max_kv_len + want - 1) / want : b.max_kv_len;
+struct Plan {
+  int tiles;               // of 16 rows, for a workgroup
+  int waves;
+  int chunk, splits;
+};
+
+// Row tiles: a workgroup takes as many as an average sequence has.  Pieces:
+// enough workgroups for all 256 compute units, of 256 tokens a piece at least.
+Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group) {
+  Plan p;
+  const int64_t rows = (int64_t)b.rows * group / (b.seqs > 0 ? b.seqs : 1);
+  p.tiles = rows <= 16 ? 1 : rows <= 64 ? 2 : 8;
+  const int64_t work = host_tiles(b, group, 16 * p.tiles) * c.heads;
+  p.waves = p.tiles == 1 && work < 256 && c.dim < 256 ? 8 : 4;
+  const int64_t groups = p.waves == 8 ? 512 : 1024;
+  const int64_t least = p.waves == 8 ? 512 : 256;
+  const int64_t want = work > 0 ? (groups + work - 1) / work : 1;
+  int64_t each = (b.max_kv_len + want - 1) / want;
   each = (each + 127) / 128 * 128;
-  if (each < 256) each = 256;
-  splits = (int)((b.max_kv_len + each - 1) / each);
-  if (splits < 1) splits = 1;
-  chunk = (int)each;
+  if (each < least) each = least;
+  p.splits = (int)((b.max_kv_len + each - 1) / each);
+  if (p.splits < 1) p.splits = 1;
+  p.chunk = (int)each;
+  return p;
+}
+
+template <int D, int kTiles>
+hipError_t launch_join(const AttentionArgs& a, int64_t work, hipStream_t stream) {
+  if (a.splits == 1) return hipSuccess;
+  if (a.splits > 8)
+    kv_attention_join_kernel<D, kTiles, 4><<<dim3((unsigned)(work * 16 * kTiles)), 256, 0, stream>>>(a);
+  else
+    kv_attention_join_kernel<D, kTiles, 1><<<dim3((unsigned)(work * 4 * kTiles)), 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <int D, int kTiles, int kWaves>
+hipError_t launch_rows(const AttentionArgs& a, int64_t work, hipStream_t stream) {
+  if (a.splits == 1)
+    kv_attention_rows_kernel<D, kTiles, kWaves, false><<<dim3((unsigned)work), kWaves * 64, 0, stream>>>(a);
+  else
+    kv_attention_rows_kernel<D, kTiles, kWaves, true><<<dim3((unsigned)(work * a.splits)), kWaves * 64, 0, stream>>>(a);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : launch_join<D, kTiles>(a, work, stream);
+}
+
+template <int D>
+hipError_t launch_attention(const AttentionArgs& a, const Plan& p, hipStream_t stream) {
+  const int64_t work = host_tiles(a.batch, a.group, 16 * p.tiles) * a.cache.heads;
+  if (work * (a.splits > 16 * p.tiles ? a.splits : 16 * p.tiles) >= (int64_t)1 << 31) return hipErrorInvalidValue;
+  if (p.tiles == 8) {
+    const hipError_t e = launch_kv_attention_tile(a, work / a.cache.heads, stream);
+    return e != hipSuccess ? e : launch_join<D, 8>(a, work, stream);
+  }
+  if (p.tiles == 2) return launch_rows<D, 2, 4>(a, work, stream);
+  if constexpr (D < 256) {
+    if (p.waves == 8) return launch_rows<D, 1, 8>(a, work, stream);
+  }
+  return launch_rows<D, 1, 4>(a, work, stream);
 }
 
 }  // namespace
 
 size_t kv_attention_workspace_bytes(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads) {
   if (b.seqs == 0 || b.rows == 0) return 0;
-  int chunk, splits;
   const int group = q_heads / c.heads;
-  plan(c, b, group, chunk, splits);
-  if (splits == 1) return 0;
-  return (size_t)(host_tiles(b, group, 16) * c.heads * splits * 16) * (c.dim + 2) * sizeof(float);
-}
-
-template <int D>
-hipError_t launch_attention(const AttentionArgs& a, hipStream_t stream) {
-  const int64_t work = host_tiles(a.batch, a.group, 16) * a.cache.heads;
-  if (work * a.splits >= (int64_t)1 << 31) return hipErrorInvalidValue;
-  if (a.splits == 1) {
-    kv_attention_rows_kernel<D, false><<<dim3((unsigned)work), kRowsThreads, 0, stream>>>(a);
-    return hipGetLastError();
-  }
-  kv_attention_rows_kernel<D, true><<<dim3((unsigned)(work * a.splits)), kRowsThreads, 0, stream>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  kv_attention_join_kernel<D><<<dim3((unsigned)(work * 4)), 256, 0, stream>>>(a);
-  return hipGetLastError();
+  const Plan p = plan(c, b, group);
+  if (p.splits == 1) return 0;
+  return (size_t)(host_tiles(b, group, 16 * p.tiles) * c.heads * p.splits * 16 * p.tiles) * (c.dim + 2) * sizeof(float);
 }
 
 hipError_t launch_kv_attention(const AttentionArgs& args, void* workspace, hipStream_t stream) {
   AttentionArgs a = args;
-  plan(a.cache, a.batch, a.group, a.chunk, a.splits);
+  const Plan p = plan(a.cache, a.batch, a.group);
+  a.chunk = p.chunk;
+  a.splits = p.splits;
   a.part = static_cast<float*>(workspace);
-  return a.cache.dim == 64    ? launch_attention<64>(a, stream)
-         : a.cache.dim == 128 ? launch_attention<128>(a, stream)
-                              : launch_attention<256>(a, stream);
+  return a.cache.dim == 64    ? launch_attention<64>(a, p, stream)
+         : a.cache.dim == 128 ? launch_attention<128>(a, p, stream)
+                              : launch_attention<256>(a, p, stream);
 }
 
 }  // namespace nvfp4

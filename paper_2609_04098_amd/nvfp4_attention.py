@@ -64,35 +64,27 @@ def batch_struct(page_table, kv_len, cu_rows, rows, max_kv_len):
                          page_table.shape[1], kv_len.shape[0], rows, max_kv_len)
 
 
-def nvfp4_qk_norm_rope(q, q_gamma, q_out, k, k_gamma, k_out, eps, positions, inv_freq, interleaved, stream=None):
-    """q, q_out, k, k_out bf16 [rows, heads, head_dim] or None (q or k, with its output)."""
-    one = q if q is not None else k
-    rows, dim = one.shape[0], one.shape[2]
-    st = lib().nvfp4_qk_norm_rope(
-        _at(q), 0 if q is None else q.stride(0), 0 if q is None else q.shape[1], _at(q_gamma), _at(q_out),
-        0 if q is None else q_out.stride(0), _at(k), 0 if k is None else k.stride(0), 0 if k is None else k.shape[1],
-        _at(k_gamma), _at(k_out), 0 if k is None else k_out.stride(0), rows, dim, eps, _at(positions), _at(inv_freq),
-        0 if inv_freq is None else 2 * inv_freq.shape[0], interleaved, _c._stream(stream))
-    _c._check(st, "nvfp4_qk_norm_rope")
+def qk_norm_rope(*args):
+    """nvfp4_qk_norm_rope: its arguments in order, addresses as integers (or
+    None), the stream a torch stream, a handle or None (the current one)."""
+    status = (_lib or lib()).nvfp4_qk_norm_rope(*args[:-1], _c._stream(args[-1]))
+    if status:
+        _c._check(status, "nvfp4_qk_norm_rope")
 
 
-def nvfp4_kv_append(cache, batch, k, v, k_gamma, eps, positions, inv_freq, interleaved, mode=_c.NVFP4_DYNAMIC,
-                    stream=None):
-    """cache, batch: the structures above; k, v bf16 [rows, kv_heads, head_dim]."""
-    st = lib().nvfp4_kv_append(cache, batch, k.data_ptr(), k.stride(0), v.data_ptr(), v.stride(0), _at(k_gamma), eps,
-                               _at(positions), _at(inv_freq), 0 if inv_freq is None else 2 * inv_freq.shape[0],
-                               interleaved, mode, _c._stream(stream))
-    _c._check(st, "nvfp4_kv_append")
+def kv_append(*args):
+    """nvfp4_kv_append, its arguments as above, the structures by reference."""
+    status = (_lib or lib()).nvfp4_kv_append(*args[:-1], _c._stream(args[-1]))
+    if status:
+        _c._check(status, "nvfp4_kv_append")
 
 
-def nvfp4_kv_attention_workspace(cache, batch, q_heads):
+def kv_attention_workspace(cache, batch, q_heads):
     return lib().nvfp4_kv_attention_workspace(cache, batch, q_heads)
 
 
-def nvfp4_kv_attention(cache, batch, q, y, lse, scale, causal, window, workspace=None, stream=None):
-    """q, y bf16 [rows, q_heads, head_dim]; lse float32 [rows, q_heads] or None."""
-    st = lib().nvfp4_kv_attention(cache, batch, q.data_ptr(), q.stride(0), q.shape[1], y.data_ptr(), y.stride(0),
-                                  _at(lse), scale, causal, window, _at(workspace),
-                                  0 if workspace is None else workspace.numel() * workspace.element_size(),
-                                  _c._stream(stream))
-    _c._check(st, "nvfp4_kv_attention")
+def kv_attention(*args):
+    """nvfp4_kv_attention, its arguments as above."""
+    status = (_lib or lib()).nvfp4_kv_attention(*args[:-1], _c._stream(args[-1]))
+    if status:
+        _c._check(status, "nvfp4_kv_attention")

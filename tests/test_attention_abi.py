@@ -128,6 +128,12 @@ def test_attention_refuses(bad):
     assert _attend(**bad) == C.NVFP4_EINVAL
 
 
+def test_attention_refuses_more_rows_than_it_counts():
+    c = _cache()
+    b = _batch(rows=(1 << 24) - 1)
+    assert _attend(cache=c, batch=b, hq=130, ldq=1 << 15, ldy=1 << 15) == C.NVFP4_EINVAL
+
+
 def test_attention_wants_its_workspace():
     c, b = _cache(num_pages=4096), _batch(cu_rows=None, n_seqs=1, rows=1, max_pages=4096, page_table_stride=4096,
                                           max_kv_len=131072)
