@@ -1,11 +1,13 @@
 // Append of keys and values to the paged E4M3 cache, keys normed and rotated on
 // the way, for gfx950 (layout: nvfp4_attention.h).
 //
-// Many rows: one workgroup for each touched page, head, and keys or values.  It
-// holds its new tokens (at most 16384 elements, 64 a lane) in registers between
-// the maximum and the rounding, so the input is read once, no workgroup waits
-// for another and the result does not depend on any order.  Codes go through
-// LDS into the cache's order and leave it in 16-byte pieces.
+// Many rows: one workgroup for each touched page and some of the heads, one head's
+// keys or values after the other.  It holds their new tokens (at most 16384
+// elements, 64 a lane) in registers between the maximum and the rounding, with
+// the next ones' loads in flight, so the input is read once, no workgroup waits
+// for another and the result does not depend on any order.  The tokens' sines
+// and cosines are computed once for all heads.  Codes go through LDS into the
+// cache's order and leave it in 16-byte pieces.
 // Few rows (under 8 for a sequence): one wave for each touched page, keys or
 // values, and as many heads as it has lanes for (512 / D); the codes are stored
 // from registers.
@@ -59,6 +61,7 @@ struct Treatment {
   bool turned;                   // these elements are among the rotated ones
   bool interleaved;
   int half, e0, partner;         // the lane that holds the other elements of the pairs
+  uint32_t flip[2];              // sign bit where an even, an odd element's partner counts negative
   uint4 gamma;
   float eps;
 };
@@ -75,11 +78,17 @@ __device__ __forceinline__ Treatment treatment(const AppendArgs& a, int kind) {
   t.interleaved = a.rope.interleaved;
   t.partner = lane;
   if (t.turned && !t.interleaved) t.partner = lane + (t.e0 < t.half ? t.half / 8 : -(t.half / 8));
+  t.flip[0] = t.interleaved || t.e0 < t.half ? 0x80000000u : 0u;
+  t.flip[1] = !t.interleaved && t.e0 < t.half ? 0x80000000u : 0u;
   t.gamma = make_uint4(0, 0, 0, 0);
   if (t.norm) t.gamma = *reinterpret_cast<const uint4*>(a.gamma + t.e0);
   t.eps = a.eps;
   return t;
 }
+
+// Place of angle f in a token's table: neighbouring lanes, which want f and f + 8,
+// read neighbouring places.
+__device__ __forceinline__ int turn_at(int half, int f) { return (f & 7) * (half >> 3) + (f >> 3); }
 
 __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -87,10 +96,13 @@ __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// 1 / sqrt(x) to 2^-42, from the binary32 one (2^-21).
+// 1 / sqrt(x), to a few last bits: v_rsq_f64 and two Newton steps.
 __device__ __forceinline__ double reciprocal_root(double x) {
-  const double r = (double)(1.0f / sqrtf((float)x));
-  return r * fma(-0.5 * x * r, r, 1.5);
+  double r = __builtin_amdgcn_rsq(x);
+  const double h = -0.5 * x;
+  r *= fma(h * r, r, 1.5);
+  r *= fma(h * r, r, 1.5);
+  return r;
 }
 
 // The lane's 8 values, ready for rounding.  turn: cosines and sines of the
@@ -126,8 +138,9 @@ __device__ __forceinline__ void values(const Treatment& t, uint4 in, const doubl
       for (int j = 0; j < 8; ++j) {
         const int e = t.e0 + j;
         const bool second = t.interleaved ? (j & 1) : e >= t.half;
-        const double2 cs = turn[t.interleaved ? e / 2 : (second ? e - t.half : e)];
-        w[j] = fma(w[j], cs.x, second ? p[j] * cs.y : -(p[j] * cs.y));
+        const double2 cs = turn[turn_at(t.half, t.interleaved ? e / 2 : (second ? e - t.half : e))];
+        const double other = __hiloint2double(__double2hiint(p[j]) ^ (int)t.flip[j & 1], __double2loint(p[j]));
+        w[j] = fma(w[j], cs.x, other * cs.y);
       }
     }
   }
@@ -135,19 +148,33 @@ __device__ __forceinline__ void values(const Treatment& t, uint4 in, const doubl
   for (int j = 0; j < 8; ++j) v[j] = sticky(w[j]);
 }
 
-// v / scale with the sticky last bit.
-__device__ __forceinline__ float quotient(float v, float scale) { return sticky((double)v / (double)scale); }
-
-// Codes of 8 values over the scale (inverse: 1 / scale, used where it is exact).
-// Values that are not finite give NaN.
-__device__ __forceinline__ uint2 eight_codes(const float (&v)[8], bool dynamic, float scale, float inverse) {
+// Codes of 8 values over the scale.  In dynamic mode none is over 448 scales and
+// 1 / scale is exact; in static mode a quotient over 448 is cut, and rounded
+// once.  Values that are not finite give NaN.
+template <bool kDynamic>
+__device__ __forceinline__ uint2 eight_codes(const float (&v)[8], float scale, float inverse) {
   float q[8];
+  if (kDynamic) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float x = dynamic ? v[j] * inverse : quotient(v[j], scale);
-    q[j] = fabsf(v[j]) <= kLargest ? __builtin_amdgcn_fmed3f(x, -448.0f, 448.0f) : __uint_as_float(0x7FC00000u);
+    for (int j = 0; j < 8; ++j) q[j] = v[j] * inverse;
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float x = sticky((double)v[j] / (double)scale);
+      q[j] = fabsf(v[j]) <= kLargest ? __builtin_amdgcn_fmed3f(x, -448.0f, 448.0f) : __uint_as_float(0x7FC00000u);
+    }
   }
   return make_uint2(e4m3_codes(q[0], q[1], q[2], q[3]), e4m3_codes(q[4], q[5], q[6], q[7]));
+}
+
+// The largest |v| of 8 values (all: without those that are not finite).
+__device__ __forceinline__ float largest(const float (&v)[8], float top, bool all) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float m = fabsf(v[j]);
+    top = fmaxf(top, all || m <= kLargest ? m : 0.0f);
+  }
+  return top;
 }
 
 // The page that a workgroup or wave writes to, and which of the step's tokens.
@@ -211,115 +238,127 @@ __device__ __forceinline__ void put_codes(uint8_t* out, int kind, int t, int e0,
   }
 }
 
-// Many rows.  kPasses * 2048 / D tokens at most.
-template <int D, int kPasses>
-__global__ __launch_bounds__(kAppendThreads, 2) void kv_append_pages_kernel(AppendArgs a) {
-  constexpr int kLanes = D / 8, kTokens = kAppendThreads / kLanes, kWaveTokens = 64 / kLanes;        // of one pass
-  __shared__ union {
-    double2 turn[kAppendThreads / 64][kWaveTokens][D / 2];
-    uint8_t codes[kPasses * kTokens * D];
-  } lds;
+// Many rows.  kPasses * 2048 / D tokens at most; heads_each heads a workgroup.
+template <int D, int kPasses, bool kDynamic>
+__global__ __launch_bounds__(kAppendThreads, kPasses <= 2 ? 4 : kPasses == 4 ? 2 : 1) void kv_append_pages_kernel(AppendArgs a, int heads_each) {
+  constexpr int kLanes = D / 8, kTokens = kAppendThreads / kLanes;        // of one pass
+  __shared__ double2 turn[kPasses * kTokens][D / 2];
+  __shared__ uint8_t __attribute__((aligned(16))) codes[kPasses * kTokens * D];
   __shared__ float wave_max[kAppendThreads / 64];
 
-  const int kind = blockIdx.x & 1;                        // 0: keys, 1: values
-  const int h = (int)(blockIdx.x >> 1) % a.cache.heads;
+  const int parts = (a.cache.heads + heads_each - 1) / heads_each;
   Touch t;
-  if (!find_touch(a, (int)(blockIdx.x >> 1) / a.cache.heads, t)) return;
+  if (!find_touch(a, (int)blockIdx.x / parts, t)) return;
+  const int h0 = (int)blockIdx.x % parts * heads_each, h1 = min(h0 + heads_each, a.cache.heads);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine = threadIdx.x / kLanes;
-  const Treatment how = treatment<D>(a, kind);
-  const int e0 = how.e0;
-  const uint16_t* x = (kind ? a.x[1] : a.x[0]) + (int64_t)t.row0 * (kind ? a.ld[1] : a.ld[0]) + (int64_t)h * D + e0;
-  const int64_t ld = kind ? a.ld[1] : a.ld[0];
-  const auto load = [&](int i) { return i < t.n ? *reinterpret_cast<const uint4*>(x + i * ld) : make_uint4(0, 0, 0, 0); };
+  const Treatment for_keys = treatment<D>(a, 0);
+  Treatment for_values = for_keys;
+  for_values.norm = for_values.rotate = for_values.turned = false;
+  const int e0 = for_keys.e0;
 
   uint4 in[kPasses];
+  const auto load = [&](int h, int kind) __attribute__((always_inline)) {
+    const int64_t ld = kind ? a.ld[1] : a.ld[0];
+    const uint16_t* x = (kind ? a.x[1] : a.x[0]) + (int64_t)t.row0 * ld + (int64_t)h * D + e0;
 #pragma unroll
-  for (int p = 0; p < kPasses; ++p) in[p] = load(p * kTokens + mine);
-  float v[kPasses][8];
-  float top = 0.0f;
-#pragma unroll
-  for (int p = 0; p < kPasses; ++p) {
-    if (p * kTokens >= t.n) break;
-    const int i = p * kTokens + mine;
-    double2* turn = lds.turn[wave][lane / kLanes];
-    if (how.rotate) {
-      // The token's angles, by the D / 8 lanes that hold it (at most 4 each).
-      const int pos = position(a, t, min(i, t.n - 1));
-      wave_lds_fence();
-      for (int f = e0 / 8; f < how.half; f += kLanes) {
+    for (int p = 0; p < kPasses; ++p) {
+      const int i = p * kTokens + mine;
+      in[p] = make_uint4(0, 0, 0, 0);
+      if (i < t.n) in[p] = *reinterpret_cast<const uint4*>(x + i * ld);
+    }
+  };
+  load(h0, 0);
+  if (for_keys.rotate) {
+    // A token's angles, by the D / 8 lanes that hold it (at most 4 each): the
+    // lanes of one wave, like those that use them.
+    for (int i = mine; i < t.n; i += kTokens) {
+      const int pos = position(a, t, i);
+      for (int f = e0 / 8; f < for_keys.half; f += kLanes) {
         double s, c;
         sin_cos<double>(pos, a.rope.inv_freq[f], s, c);
-        turn[f] = make_double2(c, s);
-      }
-      wave_lds_fence();
-    }
-    values<D>(how, in[p], turn, v[p]);
-    if (i < t.n) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float m = fabsf(v[p][j]);
-        if (m <= kLargest) top = fmaxf(top, m);      // (a value that is not finite has no part in the scale)
+        turn[i][turn_at(for_keys.half, f)] = make_double2(c, s);
       }
     }
+    wave_lds_fence();
   }
 
-  float* scale_at = (kind ? a.cache.scale[1] : a.cache.scale[0]) + (int64_t)t.page * a.cache.scale_stride + h;
-  uint8_t* out = (kind ? a.cache.kv[1] : a.cache.kv[0]) +
-                 (int64_t)t.page * (kind ? a.cache.page_stride[1] : a.cache.page_stride[0]) +
-                 (int64_t)h * a.cache.page_size * D;
-  float scale;
-  if (a.dynamic) {
+  const auto one = [&](const Treatment& how, int h, int kind, bool more, int next_h, int next_kind)
+      __attribute__((always_inline)) {
+    float v[kPasses][8], top = 0.0f;
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+      if (p * kTokens >= t.n) break;
+      values<D>(how, in[p], turn[min(p * kTokens + mine, t.n - 1)], v[p]);
+      top = largest(v[p], top, true);      // (0 behind the last token)
+      __builtin_amdgcn_sched_barrier(0);   // (one pass's binary64 values at a time: registers)
+    }
+    if (more) load(next_h, next_kind);
+    float* scale_at = (kind ? a.cache.scale[1] : a.cache.scale[0]) + (int64_t)t.page * a.cache.scale_stride + h;
+    uint8_t* out = (kind ? a.cache.kv[1] : a.cache.kv[0]) +
+                   (int64_t)t.page * (kind ? a.cache.page_stride[1] : a.cache.page_stride[0]) +
+                   (int64_t)h * a.cache.page_size * D;
+    const float held = kDynamic && t.slot0 == 0 ? 0.0f : *scale_at;
+    if (kDynamic && __any(!(top <= kLargest))) {      // without what is not finite
+      top = 0.0f;
+#pragma unroll
+      for (int p = 0; p < kPasses; ++p) {
+        if (p * kTokens >= t.n) break;
+        top = largest(v[p], top, false);
+      }
+    }
 #pragma unroll
     for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
     if (lane == 0) wave_max[wave] = top;
-    const float held = t.slot0 > 0 ? *scale_at : 0.0f;
-    __syncthreads();
+    __syncthreads();      // (the last head's codes have left LDS, too)
+    float scale = held;
+    if (kDynamic) {
 #pragma unroll
-    for (int w = 0; w < kAppendThreads / 64; ++w) top = fmaxf(top, wave_max[w]);
-    scale = fmaxf(held, page_scale(top));
-    if (scale > held && t.slot0 > 0) bring_along<D>(out, kind, t.slot0, held / scale, threadIdx.x, kAppendThreads);
-  } else {
-    scale = *scale_at;
-  }
-  const float inverse = 1.0f / scale;      // exact for the powers of two of the dynamic mode
-
-  __syncthreads();      // the rotation's table has been read, the held codes are written
+      for (int w = 0; w < kAppendThreads / 64; ++w) top = fmaxf(top, wave_max[w]);
+      scale = fmaxf(held, page_scale(top));
+      if (scale > held && t.slot0 > 0) bring_along<D>(out, kind, t.slot0, held / scale, threadIdx.x, kAppendThreads);
+    }
+    const float inverse = 1.0f / scale;
 #pragma unroll
-  for (int p = 0; p < kPasses; ++p) {
-    if (p * kTokens >= t.n) break;
-    const int i = p * kTokens + mine;
-    if (i < t.n) put_codes<D>(lds.codes, kind, t.slot0 + i, e0, eight_codes(v[p], a.dynamic, scale, inverse));
-  }
-  __syncthreads();
-  const int last = t.slot0 + t.n;
-  for (int y = (t.slot0 / 16) * D + threadIdx.x; y < ((last + 15) / 16) * D; y += kAppendThreads) {
-    const int group = y / D, in_group = y % D;
-    const uint4 c = reinterpret_cast<const uint4*>(lds.codes)[y];
-    uint4* at = reinterpret_cast<uint4*>(out) + y;
-    if (kind == 0) {
-      const int s = group * 16 + (in_group & 15);
-      if (s >= t.slot0 && s < last) *at = c;
-    } else {
-      const int s = group * 16 + ((in_group >> 4) & 3) * 4;
-      if (s >= t.slot0 && s + 4 <= last) {
-        *at = c;
+    for (int p = 0; p < kPasses; ++p) {
+      if (p * kTokens >= t.n) break;
+      const int i = p * kTokens + mine;
+      if (i < t.n) put_codes<D>(codes, kind, t.slot0 + i, e0, eight_codes<kDynamic>(v[p], scale, inverse));
+    }
+    __syncthreads();      // (the held codes are written, too)
+    const int last = t.slot0 + t.n;
+    for (int y = (t.slot0 / 16) * D + threadIdx.x; y < ((last + 15) / 16) * D; y += kAppendThreads) {
+      const int group = y / D, in_group = y % D;
+      const uint4 c = reinterpret_cast<const uint4*>(codes)[y];
+      uint4* at = reinterpret_cast<uint4*>(out) + y;
+      if (kind == 0) {
+        const int s = group * 16 + (in_group & 15);
+        if (s >= t.slot0 && s < last) *at = c;
       } else {
-        const uint32_t word[4] = {c.x, c.y, c.z, c.w};
-        uint8_t* bytes = reinterpret_cast<uint8_t*>(at);
+        const int s = group * 16 + ((in_group >> 4) & 3) * 4;
+        if (s >= t.slot0 && s + 4 <= last) {
+          *at = c;
+        } else {
+          const uint32_t word[4] = {c.x, c.y, c.z, c.w};
+          uint8_t* bytes = reinterpret_cast<uint8_t*>(at);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-          if (s + u >= t.slot0 && s + u < last)
+          for (int u = 0; u < 4; ++u)
+            if (s + u >= t.slot0 && s + u < last)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) bytes[j * 4 + u] = (uint8_t)(word[j] >> (8 * u));
+              for (int j = 0; j < 4; ++j) bytes[j * 4 + u] = (uint8_t)(word[j] >> (8 * u));
+        }
       }
     }
+    if (kDynamic && threadIdx.x == 0) *scale_at = scale;
+  };
+  for (int h = h0; h < h1; ++h) {
+    one(for_keys, h, 0, true, h, 1);
+    one(for_values, h, 1, h + 1 < h1, h + 1, 0);
   }
-  if (a.dynamic && threadIdx.x == 0) *scale_at = scale;
 }
 
 // Few rows: one wave for a page, keys or values, and 512 / D heads; its lanes
 // hold one token of each head at a time.
-template <int D>
+template <int D, bool kDynamic>
 __global__ __launch_bounds__(64) void kv_append_tokens_kernel(AppendArgs a) {
   constexpr int kLanes = D / 8, kHeads = 64 / kLanes;
   __shared__ double2 turn[D / 2];
@@ -342,7 +381,7 @@ __global__ __launch_bounds__(64) void kv_append_tokens_kernel(AppendArgs a) {
       for (int f = lane; f < how.half; f += 64) {
         double s, c;
         sin_cos<double>(pos, a.rope.inv_freq[f], s, c);
-        turn[f] = make_double2(c, s);
+        turn[turn_at(how.half, f)] = make_double2(c, s);
       }
       wave_lds_fence();
     }
@@ -350,17 +389,13 @@ __global__ __launch_bounds__(64) void kv_append_tokens_kernel(AppendArgs a) {
   };
 
   float* scale_at = (kind ? a.cache.scale[1] : a.cache.scale[0]) + (int64_t)t.page * a.cache.scale_stride + h;
-  const float held = a.dynamic && t.slot0 == 0 ? 0.0f : *scale_at;
+  const float held = kDynamic && t.slot0 == 0 ? 0.0f : *scale_at;
   float v[8], scale = held;
-  if (a.dynamic) {
+  if (kDynamic) {
     float top = 0.0f;
     for (int i = 0; i < t.n; ++i) {
       treated(i, v);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float m = fabsf(v[j]);
-        if (m <= kLargest) top = fmaxf(top, m);
-      }
+      top = largest(v, top, false);
     }
 #pragma unroll
     for (int m = 1; m < kLanes; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
@@ -373,39 +408,54 @@ __global__ __launch_bounds__(64) void kv_append_tokens_kernel(AppendArgs a) {
   __syncthreads();      // (the held codes of pieces that new values share are written)
   const float inverse = 1.0f / scale;
   for (int i = t.n - 1; i >= 0; --i) {      // (the last one's values are at hand)
-    if (!a.dynamic || i != t.n - 1) treated(i, v);
-    const uint2 c = eight_codes(v, a.dynamic, scale, inverse);
+    if (!kDynamic || i != t.n - 1) treated(i, v);
+    const uint2 c = eight_codes<kDynamic>(v, scale, inverse);
     if (live) put_codes<D>(out, kind, t.slot0 + i, how.e0, c);
   }
-  if (a.dynamic && live && lane % kLanes == 0) *scale_at = scale;
+  if (kDynamic && live && lane % kLanes == 0) *scale_at = scale;
 }
 
-template <int D>
+template <int D, bool kDynamic>
 static hipError_t launch(const AppendArgs& a, int64_t items, hipStream_t stream) {
-  const bool few = a.batch.cu_rows == nullptr || a.batch.rows < 8 * (int64_t)a.batch.seqs;
-  const int64_t blocks = 2 * items * (few ? (a.cache.heads * D + 511) / 512 : a.cache.heads);
+  if (a.batch.cu_rows == nullptr || a.batch.rows < 8 * (int64_t)a.batch.seqs) {
+    const int64_t blocks = 2 * items * ((a.cache.heads * D + 511) / 512);
+    if (blocks >= (int64_t)1 << 31) return hipErrorInvalidValue;
+    kv_append_tokens_kernel<D, kDynamic><<<dim3((unsigned)blocks), 64, 0, stream>>>(a);
+    return hipGetLastError();
+  }
+  // Heads of a workgroup: as many as leave four workgroups for each of 256
+  // compute units (pages that are written, about rows / page_size).
+  const int64_t pages = (a.batch.rows >> a.cache.page_shift) + a.batch.seqs;
+  int64_t each = (pages * a.cache.heads + 1023) / 1024;
+  if (each > a.cache.heads) each = a.cache.heads;
+  const int64_t parts = (a.cache.heads + each - 1) / each;
+  each = (a.cache.heads + parts - 1) / parts;
+  const int64_t blocks = items * ((a.cache.heads + each - 1) / each);
   if (blocks >= (int64_t)1 << 31) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks);
   const int elements = a.cache.page_size * D;
-  if (few)
-    kv_append_tokens_kernel<D><<<grid, 64, 0, stream>>>(a);
-  else if (elements <= 2048)
-    kv_append_pages_kernel<D, 1><<<grid, kAppendThreads, 0, stream>>>(a);
+  if (elements <= 2048)
+    kv_append_pages_kernel<D, 1, kDynamic><<<grid, kAppendThreads, 0, stream>>>(a, (int)each);
   else if (elements <= 4096)
-    kv_append_pages_kernel<D, 2><<<grid, kAppendThreads, 0, stream>>>(a);
+    kv_append_pages_kernel<D, 2, kDynamic><<<grid, kAppendThreads, 0, stream>>>(a, (int)each);
   else if (elements <= 8192)
-    kv_append_pages_kernel<D, 4><<<grid, kAppendThreads, 0, stream>>>(a);
+    kv_append_pages_kernel<D, 4, kDynamic><<<grid, kAppendThreads, 0, stream>>>(a, (int)each);
   else
-    kv_append_pages_kernel<D, 8><<<grid, kAppendThreads, 0, stream>>>(a);
+    kv_append_pages_kernel<D, 8, kDynamic><<<grid, kAppendThreads, 0, stream>>>(a, (int)each);
   return hipGetLastError();
+}
+
+template <bool kDynamic>
+static hipError_t launch_mode(const AppendArgs& a, int64_t items, hipStream_t stream) {
+  return a.cache.dim == 64    ? launch<64, kDynamic>(a, items, stream)
+         : a.cache.dim == 128 ? launch<128, kDynamic>(a, items, stream)
+                              : launch<256, kDynamic>(a, items, stream);
 }
 
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream) {
   const int64_t items = a.batch.cu_rows == nullptr ? a.batch.seqs
                                                    : (a.batch.rows >> a.cache.page_shift) + 2 * (int64_t)a.batch.seqs;
-  return a.cache.dim == 64 ? launch<64>(a, items, stream)
-         : a.cache.dim == 128 ? launch<128>(a, items, stream)
-                              : launch<256>(a, items, stream);
+  return a.dynamic ? launch_mode<true>(a, items, stream) : launch_mode<false>(a, items, stream);
 }
 
 }  // namespace nvfp4
