@@ -58,15 +58,22 @@ kv_attention_rows_kernel(AttentionArgs a) {
   int id = blockIdx.x;
   const int h = id % a.cache.heads;
   id /= a.cache.heads;
-  const int piece = kSplit ? id % a.splits : 0;
+  // Pieces in another order for each tile: workgroups go to the shader engines in
+  // turn, and the last pieces, which short sequences do not have, would otherwise
+  // be the same engine's.
   const int number = kSplit ? id / a.splits : id;
+  const int piece = kSplit ? (id + number) % a.splits : 0;
   Tile t;
   if (!find_tile<kRows>(a, number, t)) return;
   int begin = t.begin, end = t.end;
+  bool whole = true;             // this piece is all that the rows see
   if (kSplit) {
+    int p0, p1;
+    pieces_of(a, t, p0, p1);
+    if (piece < p0 || piece >= p1) return;
+    whole = p1 - p0 == 1;
     begin = max(begin, piece * a.chunk);
     if (piece + 1 < a.splits) end = min(end, (piece + 1) * a.chunk);
-    if (begin >= end && !(piece == 0 && t.begin >= t.end)) return;      // (rows that see nothing: piece 0 says so)
   }
 
   RowTiles<D, kTiles> rows;
@@ -159,10 +166,10 @@ kv_attention_rows_kernel(AttentionArgs a) {
     for (int w = 0; w < kWaves; ++w)
       l_all += stats[w][16 * i + col].y * __builtin_amdgcn_exp2f(stats[w][16 * i + col].x - zero_m);
     float mine = __builtin_amdgcn_exp2f(rows.m[i] - zero_m) * rows.s_ref;
-    if (!kSplit) mine *= l_all == 0.0f ? 0.0f : 1.0f / l_all;
+    if (whole) mine *= l_all == 0.0f ? 0.0f : 1.0f / l_all;
     const int r = t.r0 + 16 * i + col;
     if (threadIdx.x < 16 && 16 * i + col < t.n) {
-      if (kSplit) {
+      if (!whole) {
         float2* to = reinterpret_cast<float2*>(a.part) + (((int64_t)number * a.cache.heads + h) * a.splits + piece) * kRows;
         to[16 * i + col] = make_float2(m_all, l_all);
       } else if (a.lse != nullptr) {
@@ -184,7 +191,7 @@ kv_attention_rows_kernel(AttentionArgs a) {
         f32x4 y = (f32x4){0, 0, 0, 0};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) y += *reinterpret_cast<const f32x4*>(&lds.joined[w][x / (kPart / 4)][e]);
-        if (kSplit) {
+        if (!whole) {
           const int64_t stats_floats = tiles_of(a.batch, a.group, kRows) * a.cache.heads * a.splits * (2 * kRows);
           float* to = a.part + stats_floats +
                       ((((int64_t)number * a.cache.heads + h) * a.splits + piece) * kRows + row) * D + d0 + e;
@@ -212,15 +219,13 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a)
   const int number = (int)(blockIdx.x / (kRows / kBlockRows)) / a.cache.heads;
   Tile t;
   if (!find_tile<kRows>(a, number, t) || row >= t.n) return;      // (with kShare 4, the whole workgroup)
+  int p0, p1;
+  pieces_of(a, t, p0, p1);
+  if (p1 - p0 == 1) return;      // its rows are written already
   const int64_t first = ((int64_t)number * a.cache.heads + h) * a.splits;
   const float2* stats = reinterpret_cast<const float2*>(a.part) + first * kRows + row;
   const float* part = a.part + tiles_of(a.batch, a.group, kRows) * a.cache.heads * a.splits * (2 * kRows) +
                       (first * kRows + row) * D + lane * kEach;
-  int p0 = 0, p1 = 1;
-  if (t.begin < t.end) {
-    p0 = min(t.begin / a.chunk, a.splits - 1);
-    p1 = min((t.end - 1) / a.chunk, a.splits - 1) + 1;
-  }
   float m = kNone, l = 0.0f, y[kEach];
 #pragma unroll
   for (int i = 0; i < kEach; ++i) y[i] = 0.0f;
@@ -301,23 +306,50 @@ struct Plan {
   int chunk, splits;
 };
 
-// Row tiles: a workgroup takes as many as an average sequence has.  Pieces:
-// enough workgroups for all 256 compute units, of 256 tokens a piece at least.
+// Row tiles: a workgroup takes 16 rows where an average sequence has no more, 32
+// up to 64 (the keys are read from memory once and from L2 again), else 128.
+// Pieces: the number of them for which an estimate of the time is least, of a
+// step whose sequences all have the largest length and of one that has 0.55 times
+// as many workgroups (lengths of all sizes).
 Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group) {
   Plan p;
   const int64_t rows = (int64_t)b.rows * group / (b.seqs > 0 ? b.seqs : 1);
   p.tiles = rows <= 16 ? 1 : rows <= 64 ? 2 : 8;
   const int64_t work = host_tiles(b, group, 16 * p.tiles) * c.heads;
   p.waves = p.tiles == 1 && work < 256 && c.dim < 256 ? 8 : 4;
-  const int64_t groups = p.waves == 8 ? 512 : 1024;
-  const int64_t least = p.waves == 8 ? 512 : 256;
-  const int64_t want = work > 0 ? (groups + work - 1) / work : 1;
-  int64_t each = (b.max_kv_len + want - 1) / want;
-  each = (each + 127) / 128 * 128;
-  if (each < least) each = least;
-  p.splits = (int)((b.max_kv_len + each - 1) / each);
-  if (p.splits < 1) p.splits = 1;
-  p.chunk = (int)each;
+  // Workgroups that fit 256 compute units (registers, LDS).
+  const int fit = p.tiles == 8 ? (c.dim == 256 ? 2 : c.dim == 128 ? 3 : 4)
+                  : c.dim == 256 || p.waves == 8 ? 1
+                  : p.tiles == 2 ? (c.dim == 128 ? 2 : 3)
+                                 : (c.dim == 128 ? 3 : 4);
+  const double slots = 256.0 * fit;
+  // Tokens that a workgroup takes in a microsecond alone, and that all of them
+  // take together (5.5 TB/s of memory; 0.9 PFLOP/s of products).
+  const double alone = p.tiles == 8 ? 35.0 * 128 / c.dim : 40.0 * p.waves * 128 / c.dim;
+  const double together = p.tiles == 8 ? 0.9e9 / (512.0 * c.dim) : 5.5e6 / (2.0 * c.dim);
+  const double part = (double)(rows < 16 * p.tiles ? rows : 16 * p.tiles) * c.dim * 8.0 / 4e6;      // write and read
+  static const int candidates[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128};
+  double best = 0.0;
+  p.splits = 1;
+  p.chunk = b.max_kv_len > 0 ? b.max_kv_len : 1;
+  for (const int s : candidates) {
+    const int64_t each = ((int64_t)b.max_kv_len + 128 * s - 1) / (128 * s) * 128;
+    if (s > 1 && each < 256) break;
+    double time = 0.0;
+    for (const double share : {1.0, 0.55}) {
+      const double n = share * (double)(work * s), longest = (double)each / alone;
+      const double all = n * (double)each / together;
+      time += all > longest ? all : longest;
+      if (n > slots) time += 0.5 * longest + 2.0 * n / slots;  // the last ones; beginnings and ends
+      if (s > 1) time += 0.05 * all + 6.0 + n * part;          // the join
+    }
+    if (s == 1 || time < best) {
+      best = time;
+      p.splits = s;
+      p.chunk = each > 0 ? (int)each : 1;
+    }
+  }
+  if (p.splits > 1) p.splits = (b.max_kv_len + p.chunk - 1) / p.chunk;
   return p;
 }
 

@@ -64,6 +64,17 @@ __device__ __forceinline__ bool find_tile(const AttentionArgs& a, int number, Ti
   return true;
 }
 
+// Pieces [p0, p1) of a tile hold tokens that its rows see; a tile that sees
+// nothing has piece 0.
+__device__ __forceinline__ void pieces_of(const AttentionArgs& a, const Tile& t, int& p0, int& p1) {
+  p0 = 0;
+  p1 = 1;
+  if (t.begin < t.end) {
+    p0 = min(t.begin / a.chunk, a.splits - 1);
+    p1 = min((t.end - 1) / a.chunk, a.splits - 1) + 1;
+  }
+}
+
 __device__ __forceinline__ int64_t tiles_of(const KvBatchArgs& a, int group, int rows) {
   return a.cu_rows == nullptr ? (int64_t)a.seqs * ((group + rows - 1) / rows)
                               : (int64_t)a.rows * group / rows + a.seqs;

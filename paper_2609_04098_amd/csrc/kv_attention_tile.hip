@@ -147,7 +147,7 @@ struct WideRows {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const float power = g ? power1 : power0;
-      constexpr int kBatch = D == 256 ? 2 : D / 64;      // (registers)
+      constexpr int kBatch = D == 256 ? 1 : D / 64;      // (registers)
 #pragma unroll
       for (int c0 = 0; c0 < D / 64; c0 += kBatch) {
         u32x2 v[kBatch][2];
@@ -181,15 +181,19 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_tile_kerne
   int id = blockIdx.x;
   const int h = id % a.cache.heads;
   id /= a.cache.heads;
-  const int piece = kSplit ? id % a.splits : 0;
   const int number = tiles - 1 - (kSplit ? id / a.splits : id);      // the longest rows first
+  const int piece = kSplit ? (id + number) % a.splits : 0;           // (in another order for each tile)
   Tile t;
   if (!find_tile<kTileRows>(a, number, t)) return;
   int begin = t.begin, end = t.end;
+  bool whole = true;             // this piece is all that the rows see
   if (kSplit) {
+    int p0, p1;
+    pieces_of(a, t, p0, p1);
+    if (piece < p0 || piece >= p1) return;
+    whole = p1 - p0 == 1;
     begin = max(begin, piece * a.chunk);
     if (piece + 1 < a.splits) end = min(end, (piece + 1) * a.chunk);
-    if (begin >= end && !(piece == 0 && t.begin >= t.end)) return;      // (rows that see nothing: piece 0 says so)
   }
 
   const int first = 32 * wave, n = min(32, t.n - first);      // this wave's rows (none: it only loads)
@@ -245,7 +249,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_tile_kerne
   const float l = over_halves_sum(rows.l);
   if ((lane & 31) >= n) return;
   const int in_tile = first + (lane & 31), e0 = 4 * (lane >> 5);
-  if (kSplit) {
+  if (!whole) {
     const int64_t at = (((int64_t)number * a.cache.heads + h) * a.splits + piece) * kTileRows + in_tile;
     if (lane < 32) reinterpret_cast<float2*>(a.part)[at] = make_float2(rows.m, l);
     float* to = a.part + (int64_t)tiles * a.cache.heads * a.splits * (2 * kTileRows) + at * D + e0;

@@ -478,9 +478,9 @@ def test_a_captured_step_replays_with_new_lengths():
     lengths, the tokens and the eager work between the replays go on."""
     hq, hkv, dim, hidden, page = 8, 2, 128, 256, 16
     gen, w_qkv, w_out, gammas, rope = _layer_inputs(12, hq, hkv, dim, hidden)
-    caches = [A.alloc_kv_cache(200, hkv, dim, page, "cuda") for _ in range(2)]
-    table = torch.randperm(200, generator=gen)[:198].view(3, 66).int().cuda()
-    start = [900, 40, 15]
+    caches = [A.alloc_kv_cache(1262, hkv, dim, page, "cuda") for _ in range(2)]
+    table = torch.randperm(1262, generator=gen)[:1260].view(3, 420).int().cuda()
+    start = [4900, 40, 15]
     prompt = _bf16(gen, sum(start), hidden).cuda()
     lens, pos = _i32(start), _i32(start)
     ppos = _i32(np.concatenate([np.arange(n) for n in start]).tolist())
@@ -488,7 +488,7 @@ def test_a_captured_step_replays_with_new_lengths():
     for c in caches:
         _layer(prompt, w_qkv, w_out, gammas, rope, c,
                A.Batch(table, lens.clone(), _i32(_cu(start)), rows=sum(start)), ppos, hq, hkv, dim)
-    step = A.Batch(table, lens, max_len=66 * page)
+    step = A.Batch(table, lens, max_len=420 * page)
     assert step.workspace_bytes(caches[0], hq) > 0
     lens += 1
     side = torch.cuda.Stream()
@@ -502,7 +502,7 @@ def test_a_captured_step_replays_with_new_lengths():
     for i in range(6):
         x.copy_(_bf16(gen, 3, hidden))
         graph.replay()
-        want = _layer(x, w_qkv, w_out, gammas, rope, caches[0], A.Batch(table, lens.clone(), max_len=66 * page),
+        want = _layer(x, w_qkv, w_out, gammas, rope, caches[0], A.Batch(table, lens.clone(), max_len=420 * page),
                       pos.clone(), hq, hkv, dim)
         for a, b in zip(got, want):
             assert torch.equal(a, b), "replay %d" % i
