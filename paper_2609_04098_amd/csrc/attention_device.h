@@ -67,24 +67,18 @@ __device__ __forceinline__ uint32_t e4m3_codes(float a, float b, float c, float 
   return (uint32_t)r;
 }
 
-// Rows [row, row + rows) of sequence b and the tokens that they are: row + i is
+// Rows [row, row + rows) of a sequence and the tokens that they are: row + i is
 // token first + i (which may be below 0).  Bounded by the tensors whatever
 // cu_rows and kv_len hold.
 struct SeqRows {
   int row, rows, first, len;
 };
 
-__device__ __forceinline__ SeqRows seq_rows(const KvBatchArgs& a, int b) {
+__device__ __forceinline__ SeqRows seq_rows(const KvBatchArgs& a, int row0, int row1, int len) {
   SeqRows s;
-  if (a.cu_rows == nullptr) {
-    s.row = b;
-    s.rows = 1;
-  } else {
-    s.row = min(max(a.cu_rows[b], 0), a.rows);
-    s.rows = min(max(a.cu_rows[b + 1], s.row), a.rows) - s.row;
-  }
-  const int len = a.kv_len[b];
-  s.first = (len < 0 ? 0 : len) - s.rows;      // a length above the table's keeps its tokens' numbers
+  s.row = min(max(row0, 0), a.rows);
+  s.rows = min(max(row1, s.row), a.rows) - s.row;
+  s.first = max(len, 0) - s.rows;              // a length above the table's keeps its tokens' numbers
   s.len = min(max(len, 0), a.max_tokens);
   return s;
 }
@@ -111,6 +105,32 @@ __device__ __forceinline__ int last_at_most(int n, int value, int& entry, Key ke
   }
   entry = __builtin_amdgcn_readfirstlane(min(lo, n - 1));
   return found;
+}
+
+// The sequence b of work item `item` and its rows: the last one whose first item,
+// first_item(first row, b), is at most `item`; ordinal: which of its items this
+// is.  (Without cu_rows, sequence item / each.)  For up to 64 sequences all that
+// there is to know of them comes in one load's latency.
+template <typename First>
+__device__ __forceinline__ SeqRows find_rows(const KvBatchArgs& a, int item, int each, int& b, int& ordinal,
+                                             First first_item) {
+  if (a.cu_rows == nullptr) {
+    b = item / each;
+    ordinal = item - b * each;
+    return seq_rows(a, b, b + 1, a.kv_len[b]);
+  }
+  if (a.seqs <= 64) {
+    const int lane = threadIdx.x & 63, at = min(lane, a.seqs - 1);
+    const int row0 = a.cu_rows[at], row1 = a.cu_rows[at + 1], len = a.kv_len[at];
+    const int k = first_item(min(max(row0, 0), a.rows), at);
+    const unsigned long long hit = __ballot(lane < a.seqs && k <= item);
+    b = hit == 0 ? 0 : 63 - __builtin_clzll(hit);
+    ordinal = item - __builtin_amdgcn_readlane(k, b);
+    return seq_rows(a, __builtin_amdgcn_readlane(row0, b), __builtin_amdgcn_readlane(row1, b),
+                    __builtin_amdgcn_readlane(len, b));
+  }
+  ordinal = item - last_at_most(a.seqs, item, b, [&](int x) { return first_item(row_bound(a, x), x); });
+  return seq_rows(a, a.cu_rows[b], a.cu_rows[b + 1], a.kv_len[b]);
 }
 
 }  // namespace nvfp4

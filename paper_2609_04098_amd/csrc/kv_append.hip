@@ -187,10 +187,9 @@ struct Touch {
 // cu_rows[b] / page_size + 2 b on (n rows reach (n - 1) / page_size + 2 pages).
 __device__ __forceinline__ bool find_touch(const AppendArgs& a, int item, Touch& t) {
   const int shift = a.cache.page_shift;
-  int b = item, ordinal = 0;
-  if (a.batch.cu_rows != nullptr)
-    ordinal = item - last_at_most(a.batch.seqs, item, b, [&](int x) { return (row_bound(a.batch, x) >> shift) + 2 * x; });
-  const SeqRows s = seq_rows(a.batch, b);
+  int b, ordinal;
+  const SeqRows s =
+      find_rows(a.batch, item, 1, b, ordinal, [&](int row, int x) { return (row >> shift) + 2 * x; });
   const int begin = max(s.first, 0), entry = (begin >> shift) + ordinal;
   if (ordinal < 0 || entry >= (a.batch.max_tokens >> shift)) return false;
   const int t0 = max(begin, entry << shift), t1 = min(s.len, (entry + 1) << shift);

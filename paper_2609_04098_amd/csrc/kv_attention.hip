@@ -41,7 +41,7 @@ __device__ __forceinline__ void load_tile(const AttentionArgs& a, int h, int tok
 // Heads of 256: two tiles of codes would take 128 registers a lane, so they go
 // through a ring of two in LDS, of each wave's own.
 template <int D, int kTiles, int kWaves, bool kSplit>
-__global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : kTiles == 1 ? 3 : 2) void
+__global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : kWaves == 16 ? 4 : kTiles == 1 ? 3 : 2) void
 kv_attention_rows_kernel(AttentionArgs a) {
   constexpr int kRows = 16 * kTiles, kThreads = kWaves * 64;
   constexpr int kPart = kWaves > 4 ? 32 : (D > 128 ? 128 : D);            // elements of a row that are joined at a time
@@ -306,47 +306,62 @@ struct Plan {
   int chunk, splits;
 };
 
-// Row tiles: a workgroup takes 16 rows where an average sequence has no more, 32
-// up to 64 (the keys are read from memory once and from L2 again), else 128.
+// Row tiles: a workgroup takes 16 rows where an average sequence has no more.  It
+// takes 128 where sequences have over 64 and that gives every compute unit two
+// workgroups (heads of 256, whose smaller tiles go through a ring in LDS, one
+// workgroup a compute unit: every other one), else 32.  With 4 key heads of 128
+// and 8 query heads each, 2000 to 4000 tokens: 8 sequences of 128 new ones 96 us
+// in tiles of 32 and 125 us in tiles of 128, 2 of 256 31 and 40 us; 6 of 512 among
+// 512 63 and 37 us.  Heads of 256: 8 of 128 261 and 172 us.
 // Pieces: the number of them for which an estimate of the time is least, of a
 // step whose sequences all have the largest length and of one that has 0.55 times
-// as many workgroups (lengths of all sizes).
+// as many workgroups (lengths of all sizes), together.
 Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group) {
   Plan p;
-  const int64_t rows = (int64_t)b.rows * group / (b.seqs > 0 ? b.seqs : 1);
-  p.tiles = rows <= 16 ? 1 : rows <= 64 ? 2 : 8;
-  const int64_t work = host_tiles(b, group, 16 * p.tiles) * c.heads;
-  p.waves = p.tiles == 1 && work < 256 && c.dim < 256 ? 8 : 4;
-  // Workgroups that fit 256 compute units (registers, LDS).
-  const int fit = p.tiles == 8 ? (c.dim == 256 ? 2 : c.dim == 128 ? 3 : 4)
-                  : c.dim == 256 || p.waves == 8 ? 1
+  const int64_t seqs = b.seqs > 0 ? b.seqs : 1, rows = ((int64_t)b.rows * group + seqs - 1) / seqs;
+  const auto of_rows = [&](int tile) { return (rows + tile - 1) / tile; };
+  p.tiles = rows <= 16 ? 1 : rows > 64 && of_rows(128) * seqs * c.heads >= (c.dim == 256 ? 128 : 512) ? 8 : 2;
+  const int64_t each_seq = of_rows(16 * p.tiles), work = each_seq * seqs * c.heads;
+  // Workgroups of four waves that fit 256 compute units (registers, LDS).
+  const int fit = p.tiles == 8   ? (c.dim == 256 ? 2 : c.dim == 128 ? 3 : 4)
+                  : c.dim == 256 ? 1
                   : p.tiles == 2 ? (c.dim == 128 ? 2 : 3)
                                  : (c.dim == 128 ? 3 : 4);
-  const double slots = 256.0 * fit;
   // Tokens that a workgroup takes in a microsecond alone, and that all of them
   // take together (5.5 TB/s of memory; 0.9 PFLOP/s of products).
-  const double alone = p.tiles == 8 ? 35.0 * 128 / c.dim : 40.0 * p.waves * 128 / c.dim;
-  const double together = p.tiles == 8 ? 0.9e9 / (512.0 * c.dim) : 5.5e6 / (2.0 * c.dim);
+  const double alone = p.tiles == 8 ? 35.0 * 128 / c.dim : 160.0 * 128 / c.dim;
+  // (The tiles of one sequence share its keys and values.)
+  const double together = p.tiles == 8 ? 0.9e9 / (512.0 * c.dim)
+                                       : 5.5e6 / (2.0 * c.dim) * (each_seq < 2.4 ? (double)each_seq : 2.4);
   const double part = (double)(rows < 16 * p.tiles ? rows : 16 * p.tiles) * c.dim * 8.0 / 4e6;      // write and read
   static const int candidates[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128};
   double best = 0.0;
+  p.waves = 4;
   p.splits = 1;
   p.chunk = b.max_kv_len > 0 ? b.max_kv_len : 1;
   for (const int s : candidates) {
     const int64_t each = ((int64_t)b.max_kv_len + 128 * s - 1) / (128 * s) * 128;
     if (s > 1 && each < 256) break;
-    double time = 0.0;
-    for (const double share : {1.0, 0.55}) {
-      const double n = share * (double)(work * s), longest = (double)each / alone;
-      const double all = n * (double)each / together;
-      time += all > longest ? all : longest;
-      if (n > slots) time += 0.5 * longest + 2.0 * n / slots;  // the last ones; beginnings and ends
-      if (s > 1) time += 0.05 * all + 6.0 + n * part;          // the join
-    }
-    if (s == 1 || time < best) {
-      best = time;
-      p.splits = s;
-      p.chunk = each > 0 ? (int)each : 1;
+    // (One piece: also with eight waves, or sixteen for heads of 64, of which a
+    // compute unit holds one workgroup.  24 sequences of up to 6 rows of 4 key heads
+    // of 64, a window of 4096: 23.5 us with four, 18.2 us with eight.)
+    for (const int waves : {4, 8, 16}) {
+      if (waves > 4 && (s > 1 || p.tiles != 1 || waves * c.dim > 1024)) continue;
+      const double slots = 256.0 * (waves > 4 ? 1 : fit);
+      double time = 0.0;
+      for (const double share : {1.0, 0.55}) {
+        const double n = share * (double)(work * s), longest = (double)each / (alone * waves / 4);
+        const double all = n * (double)each / together;
+        time += all > longest ? all : longest;
+        if (n > slots) time += 0.5 * longest + 6.0 * 256.0 * n / (slots * slots);      // the last ones; beginnings and ends
+        if (s > 1) time += 0.05 * all + 6.0 + n * part;                           // the join
+      }
+      if ((s == 1 && waves == 4) || time < best) {
+        best = time;
+        p.waves = waves;
+        p.splits = s;
+        p.chunk = each > 0 ? (int)each : 1;
+      }
     }
   }
   if (p.splits > 1) p.splits = (b.max_kv_len + p.chunk - 1) / p.chunk;
@@ -382,6 +397,9 @@ hipError_t launch_attention(const AttentionArgs& a, const Plan& p, hipStream_t s
     return e != hipSuccess ? e : launch_join<D, 8>(a, work, stream);
   }
   if (p.tiles == 2) return launch_rows<D, 2, 4>(a, work, stream);
+  if constexpr (D == 64) {
+    if (p.waves == 16) return launch_rows<D, 1, 16>(a, work, stream);
+  }
   if constexpr (D < 256) {
     if (p.waves == 8) return launch_rows<D, 1, 8>(a, work, stream);
   }

@@ -42,16 +42,9 @@ struct Tile {
 template <int kRows>
 __device__ __forceinline__ bool find_tile(const AttentionArgs& a, int number, Tile& t) {
   int ordinal;
-  if (a.batch.cu_rows == nullptr) {
-    const int each = (a.group + kRows - 1) / kRows;
-    t.b = number / each;
-    ordinal = number % each;
-  } else {
-    ordinal = number - last_at_most(a.batch.seqs, number, t.b, [&](int b) {
-                return (int)((int64_t)row_bound(a.batch, b) * a.group / kRows) + b;
-              });
-  }
-  const SeqRows s = seq_rows(a.batch, t.b);
+  const SeqRows s = find_rows(a.batch, number, (a.group + kRows - 1) / kRows, t.b, ordinal, [&](int row, int b) {
+    return (int)((int64_t)row * a.group / kRows) + b;
+  });
   t.row0 = s.row;
   t.rows = s.rows;
   t.first = s.first;

@@ -47,14 +47,16 @@ struct WideRows {
   bf16x8 q[kSteps];
   f32x16 o[D / 32];
   float m, l;
-  int at;
+  int first, r0, rows;           // token of the first new row; first packed row, packed rows
   int begin, end, all0, all1;
   float s_ref;
 
-  __device__ __forceinline__ void start(const AttentionArgs& a, const Tile& t, int h, int r0, int n, int lane,
+  __device__ __forceinline__ void start(const AttentionArgs& a, const Tile& t, int h, int row, int n, int lane,
                                         int from, int to) {
+    first = t.first;
+    r0 = row;
+    rows = n;
     const int r = r0 + min(lane & 31, n - 1);
-    at = t.first + r / a.group;
     const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;      // the scale's sign goes into Q
     // Steps 2 x and 2 x + 1: the halves of piece 2 x + lane / 32 of 16 elements.
     const uint16_t* src = a.q + (int64_t)(t.row0 + r / a.group) * a.ldq + (int64_t)(h * a.group + r % a.group) * D +
@@ -112,6 +114,7 @@ struct WideRows {
     const bool plain = whole && max(v0, v1) <= ref && ((v0 | v1 | ref) & 0x7FFFFFu) == 0;
     if (!plain || __any(!(sum <= 4096.0f))) {
       if (!whole) {
+        const int at = first + (r0 + min(lane & 31, rows - 1)) / a.group;
         const int see1 = a.causal ? min(end, at + 1) : end;
         const int see0 = a.window > 0 ? max(begin, at - a.window + 1) : begin;
 #pragma unroll
@@ -246,12 +249,14 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_tile_kerne
   }
 
   // This lane's elements of its row: 64 c + 32 x + 16 n + 8 y + 4 half + 0 .. 3 in o[2 c + n][8 x + 4 y + 0 .. 3].
+  // (The lane's number again, so that nothing made of it is kept through the loop.)
+  const int own_lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
   const float l = over_halves_sum(rows.l);
-  if ((lane & 31) >= n) return;
-  const int in_tile = first + (lane & 31), e0 = 4 * (lane >> 5);
+  if ((own_lane & 31) >= n) return;
+  const int in_tile = first + (own_lane & 31), e0 = 4 * (own_lane >> 5);
   if (!whole) {
     const int64_t at = (((int64_t)number * a.cache.heads + h) * a.splits + piece) * kTileRows + in_tile;
-    if (lane < 32) reinterpret_cast<float2*>(a.part)[at] = make_float2(rows.m, l);
+    if (own_lane < 32) reinterpret_cast<float2*>(a.part)[at] = make_float2(rows.m, l);
     float* to = a.part + (int64_t)tiles * a.cache.heads * a.splits * (2 * kTileRows) + at * D + e0;
 #pragma unroll
     for (int j = 0; j < D / 32; ++j)
@@ -265,7 +270,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_tile_kerne
   } else {
     const int r = t.r0 + in_tile, head = h * a.group + r % a.group;
     const int64_t row = t.row0 + r / a.group;
-    if (a.lse != nullptr && lane < 32)
+    if (a.lse != nullptr && own_lane < 32)
       a.lse[row * a.q_heads + head] = l == 0.0f ? kNone : (rows.m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
     const float f = l == 0.0f ? 0.0f : rows.s_ref / l;
     uint16_t* to = a.y + row * a.ldy + (int64_t)head * D + e0;
