@@ -41,10 +41,10 @@ __device__ __forceinline__ void load_tile(const AttentionArgs& a, int h, int tok
 // Heads of 256: two tiles of codes would take 128 registers a lane, so they go
 // through a ring of two in LDS, of each wave's own.
 template <int D, int kTiles, int kWaves, bool kSplit>
-__global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : kWaves == 16 ? 4 : kTiles == 1 ? 3 : 2) void
+__global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : kTiles == 1 ? 3 : 2) void
 kv_attention_rows_kernel(AttentionArgs a) {
   constexpr int kRows = 16 * kTiles, kThreads = kWaves * 64;
-  constexpr int kPart = kWaves > 4 ? 32 : (D > 128 ? 128 : D);            // elements of a row that are joined at a time
+  constexpr int kPart = kWaves > 4 ? 64 : (D > 128 ? 128 : D);            // elements of a row that are joined at a time
   constexpr bool kRing = D == 256;
   constexpr int kLoads = 4 * (D / 64);                                    // of a tile into the ring
   __shared__ union {
@@ -342,11 +342,12 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group) {
   for (const int s : candidates) {
     const int64_t each = ((int64_t)b.max_kv_len + 128 * s - 1) / (128 * s) * 128;
     if (s > 1 && each < 256) break;
-    // (One piece: also with eight waves, or sixteen for heads of 64, of which a
-    // compute unit holds one workgroup.  24 sequences of up to 6 rows of 4 key heads
-    // of 64, a window of 4096: 23.5 us with four, 18.2 us with eight.)
-    for (const int waves : {4, 8, 16}) {
-      if (waves > 4 && (s > 1 || p.tiles != 1 || waves * c.dim > 1024)) continue;
+    // (One piece: also with eight waves, of which a compute unit holds one workgroup.
+    // 24 sequences of up to 6 rows of 4 key heads of 64, a window of 4096: 23.5 us
+    // with four, 18.2 us with eight, 18.3 us with sixteen.  A ring of three tiles
+    // ahead in LDS for four waves: 20.5 us.)
+    for (const int waves : {4, 8}) {
+      if (waves > 4 && (s > 1 || p.tiles != 1 || c.dim == 256)) continue;
       const double slots = 256.0 * (waves > 4 ? 1 : fit);
       double time = 0.0;
       for (const double share : {1.0, 0.55}) {
@@ -380,12 +381,15 @@ hipError_t launch_join(const AttentionArgs& a, int64_t work, hipStream_t stream)
 
 template <int D, int kTiles, int kWaves>
 hipError_t launch_rows(const AttentionArgs& a, int64_t work, hipStream_t stream) {
-  if (a.splits == 1)
-    kv_attention_rows_kernel<D, kTiles, kWaves, false><<<dim3((unsigned)work), kWaves * 64, 0, stream>>>(a);
-  else
-    kv_attention_rows_kernel<D, kTiles, kWaves, true><<<dim3((unsigned)(work * a.splits)), kWaves * 64, 0, stream>>>(a);
-  const hipError_t e = hipGetLastError();
-  return e != hipSuccess ? e : launch_join<D, kTiles>(a, work, stream);
+  if constexpr (kWaves == 4) {      // (eight waves take one piece)
+    if (a.splits > 1) {
+      kv_attention_rows_kernel<D, kTiles, 4, true><<<dim3((unsigned)(work * a.splits)), 256, 0, stream>>>(a);
+      const hipError_t e = hipGetLastError();
+      return e != hipSuccess ? e : launch_join<D, kTiles>(a, work, stream);
+    }
+  }
+  kv_attention_rows_kernel<D, kTiles, kWaves, false><<<dim3((unsigned)work), kWaves * 64, 0, stream>>>(a);
+  return hipGetLastError();
 }
 
 template <int D>
@@ -397,9 +401,6 @@ hipError_t launch_attention(const AttentionArgs& a, const Plan& p, hipStream_t s
     return e != hipSuccess ? e : launch_join<D, 8>(a, work, stream);
   }
   if (p.tiles == 2) return launch_rows<D, 2, 4>(a, work, stream);
-  if constexpr (D == 64) {
-    if (p.waves == 16) return launch_rows<D, 1, 16>(a, work, stream);
-  }
   if constexpr (D < 256) {
     if (p.waves == 8) return launch_rows<D, 1, 8>(a, work, stream);
   }
