@@ -58,11 +58,8 @@ kv_attention_rows_kernel(AttentionArgs a) {
   int id = blockIdx.x;
   const int h = id % a.cache.heads;
   id /= a.cache.heads;
-  // Pieces in another order for each tile: workgroups go to the shader engines in
-  // turn, and the last pieces, which short sequences do not have, would otherwise
-  // be the same engine's.
   const int number = kSplit ? id / a.splits : id;
-  const int piece = kSplit ? (id + number) % a.splits : 0;
+  const int piece = kSplit ? piece_of(id % a.splits, number, a.splits) : 0;
   Tile t;
   if (!find_tile<kRows>(a, number, t)) return;
   int begin = t.begin, end = t.end;
@@ -333,7 +330,9 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group) {
   // (The tiles of one sequence share its keys and values.)
   const double together = p.tiles == 8 ? 0.9e9 / (512.0 * c.dim)
                                        : 5.5e6 / (2.0 * c.dim) * (each_seq < 2.4 ? (double)each_seq : 2.4);
-  const double part = (double)(rows < 16 * p.tiles ? rows : 16 * p.tiles) * c.dim * 8.0 / 4e6;      // write and read
+  // A piece's results, written and read (tiles of 128 rows: two thirds of it behind
+  // the products).
+  const double part = (double)(rows < 16 * p.tiles ? rows : 16 * p.tiles) * c.dim * 8.0 / (p.tiles == 8 ? 12e6 : 4e6);
   static const int candidates[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64, 96, 128};
   double best = 0.0;
   p.waves = 4;
@@ -354,7 +353,8 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group) {
         const double n = share * (double)(work * s), longest = (double)each / (alone * waves / 4);
         const double all = n * (double)each / together;
         time += all > longest ? all : longest;
-        if (n > slots) time += 0.5 * longest + 6.0 * 256.0 * n / (slots * slots);      // the last ones; beginnings and ends
+        if (n > slots)                                             // the last ones; beginnings and ends
+          time += (p.tiles == 8 ? 0.25 : 0.5) * longest + 6.0 * 256.0 * n / (slots * slots);
         if (s > 1) time += 0.05 * all + 6.0 + n * part;                           // the join
       }
       if ((s == 1 && waves == 4) || time < best) {

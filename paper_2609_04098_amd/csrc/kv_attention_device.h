@@ -57,6 +57,13 @@ __device__ __forceinline__ bool find_tile(const AttentionArgs& a, int number, Ti
   return true;
 }
 
+// The piece of a tile that its x-th workgroup takes: another order for each tile.
+// Workgroups go to the dies and to their shader engines in turn, and the last
+// pieces, which short sequences do not have, would otherwise be the same one's.
+__device__ __forceinline__ int piece_of(int x, int number, int splits) {
+  return (x + number + (number >> 2) + (number >> 5)) % splits;
+}
+
 // Pieces [p0, p1) of a tile hold tokens that its rows see; a tile that sees
 // nothing has piece 0.
 __device__ __forceinline__ void pieces_of(const AttentionArgs& a, const Tile& t, int& p0, int& p1) {

@@ -185,7 +185,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_tile_kerne
   const int h = id % a.cache.heads;
   id /= a.cache.heads;
   const int number = tiles - 1 - (kSplit ? id / a.splits : id);      // the longest rows first
-  const int piece = kSplit ? (id + number) % a.splits : 0;           // (in another order for each tile)
+  const int piece = kSplit ? piece_of(id % a.splits, number, a.splits) : 0;
   Tile t;
   if (!find_tile<kTileRows>(a, number, t)) return;
   int begin = t.begin, end = t.end;
