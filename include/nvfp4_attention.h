@@ -102,8 +102,8 @@ typedef struct nvfp4_kv_batch {
  *   angle_i = position * inv_freq[i],  0 <= i < rot_dim / 2
  *   (y_a, y_b) <- (y_a cos_i - y_b sin_i, y_b cos_i + y_a sin_i)
  *   with (a, b) = (i, i + rot_dim / 2), or (2 i, 2 i + 1) if interleaved;
- * evaluated in binary32 (the angle's whole turns are taken off in binary64)
- * and rounded to bf16 once.
+ * evaluated in binary32 (the angle's whole turns are taken off in binary64;
+ * sum_e x^2 has to stay below 2^128) and rounded to bf16 once.
  *
  *   q, q_out     bf16 [rows x q_heads x head_dim], row strides ldq, ldq_out
  *                (elements).  q_out may be q itself with the same stride.
@@ -126,13 +126,14 @@ int nvfp4_qk_norm_rope(const void* q, int64_t ldq, int64_t q_heads, const void* 
  * Appends a step's keys and values to the cache; keys are normed (k_gamma not
  * NULL) and rotated (rot_dim > 0) on the way, as by nvfp4_qk_norm_rope but
  * without the rounding to bf16: each code is one rounding (to nearest, ties to
- * even) of the value over the scale, computed in binary64 in dynamic mode.
+ * even) of the value over the scale, computed in binary64.
  *   NVFP4_DYNAMIC: a page and head's scale is the smallest power of two s >=
  *     2^-100 with |value| <= 448 s for all its tokens.  A call that writes slot
  *     0 starts the page anew; one that writes behind tokens that the page
  *     holds keeps the larger of its scale and theirs, and where the scale
  *     grows the held codes are brought to it (one more rounding, which changes
- *     only values below 2^-6 of the new scale).
+ *     only values below 2^-6 of the new scale).  Held scales are powers of two,
+ *     as this mode leaves them: a page is written in one mode.
  *   NVFP4_STATIC: the scales (> 0, finite) are read and kept; values over
  *     448 s are cut to it.
  * Slots that the step does not write to keep their codes (those held ones

@@ -34,14 +34,14 @@ _BF16 = torch.bfloat16
 
 def _rows(x, name):
     """(rows, heads, head_dim, row stride) of a bf16 [rows, heads, head_dim]
-    tensor whose heads lie side by side."""
+    tensor whose heads lie side by side (the stride of a single row says nothing)."""
     if x.dtype is not _BF16 or x.dim() != 3:
         raise ValueError(name + " must be a bf16 [rows, heads, head_dim] tensor")
     rows, heads, dim = x.shape
     ld, head, one = x.stride()
     if (one != 1 or (head != dim and heads > 1)) and rows * heads * dim > 0:
         raise ValueError(name + " must have its heads side by side")
-    return rows, heads, dim, ld
+    return rows, heads, dim, ld if rows > 1 else heads * dim
 
 
 def _like_rows(x, stream):
@@ -73,6 +73,7 @@ class Rope:
               "inv_freq must be a float32 vector of a multiple of 8 elements")
         _need(not inv_freq.requires_grad, "inv_freq takes no gradient here")
         self.inv_freq = inv_freq.contiguous()
+        self.device = inv_freq.device
         half = inv_freq.shape[0]
         self.pointer = (self.inv_freq.data_ptr() if half else None, half, 1 if interleaved else 0)
 
@@ -160,21 +161,34 @@ class Batch:
         return self._workspace[key]
 
 
-def _gamma(gamma, dim, name):
+def _gamma(gamma, dim, device, name):
     """Address of a bf16 [head_dim] vector, or None."""
     if gamma is None:
         return None
     if gamma.dtype is not _BF16 or gamma.shape != (dim,) or gamma.stride(0) != 1:
         raise ValueError(name + " must be bf16 [head_dim]")
+    if gamma.device != device:
+        raise ValueError(name + " is on another device")
     return gamma.data_ptr()
 
 
-def _positions(positions, rows):
+def _positions(positions, rows, device):
     if positions is None:
         return None
     if positions.dtype is not torch.int32 or positions.shape != (rows,) or not positions.is_contiguous():
         raise ValueError("positions must be int32 [rows]")
+    if positions.device != device:
+        raise ValueError("positions are on another device")
     return positions.data_ptr()
+
+
+def _rotation(rope, device):
+    """(inv_freq's address, its elements, interleaved)."""
+    if rope is None:
+        return None, 0, 0
+    if rope.device != device:
+        raise ValueError("the rotation's inv_freq is on another device")
+    return rope.pointer
 
 
 def qk_norm_rope(q, k, positions=None, rope: Rope = None, q_gamma=None, k_gamma=None, eps=1e-6, q_out=None, k_out=None,
@@ -185,7 +199,7 @@ def qk_norm_rope(q, k, positions=None, rope: Rope = None, q_gamma=None, k_gamma=
     one = q if q is not None else k
     if one is None:
         raise ValueError("q or k must be given")
-    rows = one.shape[0]
+    rows, device = one.shape[0], one.device
     args, out, dim = [], [], None
     for x, gamma, y, names in ((q, q_gamma, q_out, ("q", "q_gamma", "q_out")), (k, k_gamma, k_out, ("k", "k_gamma", "k_out"))):
         if x is None:
@@ -194,23 +208,21 @@ def qk_norm_rope(q, k, positions=None, rope: Rope = None, q_gamma=None, k_gamma=
             continue
         n, heads, d, ld = _rows(x, names[0])
         dim = d if dim is None else dim
-        if n != rows or d != dim:
-            raise ValueError("q and k differ in rows or head_dim")
+        if n != rows or d != dim or x.device != device:
+            raise ValueError("q and k differ in rows, head_dim or device")
         if y is None:
             y = _like_rows(x, stream)
             ldy = heads * d
         else:
             ny, hy, dy, ldy = _rows(y, names[2])
-            if (ny, hy, dy) != (n, heads, d) or y.device != x.device:
+            if (ny, hy, dy) != (n, heads, d) or y.device != device:
                 raise ValueError(names[2] + " must have the shape and device of its input")
-        args += (x.data_ptr(), ld, heads, _gamma(gamma, d, names[1]), y.data_ptr(), ldy)
+        args += (x.data_ptr(), ld, heads, _gamma(gamma, d, device, names[1]), y.data_ptr(), ldy)
         out.append(y)
-    if q is not None and k is not None and q.device != k.device:
-        raise ValueError("q and k are on several devices")
-    inv_freq, half, interleaved = rope.pointer if rope is not None else (None, 0, 0)
+    inv_freq, half, interleaved = _rotation(rope, device)
     if half and positions is None:
         raise ValueError("a rotation needs positions")
-    _run(one, _a.qk_norm_rope, *args, rows, dim, eps, _positions(positions, rows) if half else None, inv_freq, 2 * half,
+    _run(one, _a.qk_norm_rope, *args, rows, dim, eps, _positions(positions, rows, device) if half else None, inv_freq, 2 * half,
          interleaved, stream)
     return tuple(out)
 
@@ -226,11 +238,12 @@ def kv_append(cache: KVCache, batch: Batch, k, v, k_gamma=None, eps=1e-6, rope: 
         raise ValueError("k and v must have the batch's rows")
     if heads != cache.kv_heads or heads_v != heads or dim != cache.head_dim or dim_v != dim:
         raise ValueError("k and v must have the cache's heads and head_dim")
-    if not k.device == v.device == cache.device == batch.device:
+    device = k.device
+    if not device == v.device == cache.device == batch.device:
         raise ValueError("tensors are on several devices")
-    inv_freq, half, interleaved = rope.pointer if rope is not None else (None, 0, 0)
-    _run(k, _a.kv_append, cache.ref, batch.ref, k.data_ptr(), ldk, v.data_ptr(), ldv, _gamma(k_gamma, dim, "k_gamma"),
-         eps, _positions(positions, rows), inv_freq, 2 * half, interleaved, 1 if static else 0, stream)
+    inv_freq, half, interleaved = _rotation(rope, device)
+    _run(k, _a.kv_append, cache.ref, batch.ref, k.data_ptr(), ldk, v.data_ptr(), ldv,
+         _gamma(k_gamma, dim, device, "k_gamma"), eps, _positions(positions, rows, device), inv_freq, 2 * half, interleaved, 1 if static else 0, stream)
 
 
 def attention(q, cache: KVCache, batch: Batch, scale=None, causal=True, window=0, out=None, return_lse=False,
@@ -259,6 +272,8 @@ def attention(q, cache: KVCache, batch: Batch, scale=None, causal=True, window=0
         nbytes = batch.workspace_bytes(cache, heads)
         workspace = _l._scratch(nbytes, q.device, stream) if nbytes else None
     else:
+        if workspace.device != q.device or not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous, on q's device")
         nbytes = workspace.numel() * workspace.element_size()
     _run(q, _a.kv_attention, cache.ref, batch.ref, q.data_ptr(), ldq, heads, y.data_ptr(), ldy,
          None if lse is None else lse.data_ptr(), cache.softmax_scale if scale is None else scale, 1 if causal else 0,

@@ -292,13 +292,15 @@ struct RowTiles {
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
       const float base = m[i] == kNone ? 0.0f : m[i];
+      float sum = 0.0f;      // (the tile's own first: fewer roundings at the size of the whole)
 #pragma unroll
       for (int g = 0; g < 2; ++g)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           w[i][4 * g + e] = __builtin_amdgcn_exp2f(fmaf(s[i][g][e], ks[g], -base));
-          l[i] += w[i][4 * g + e];
+          sum += w[i][4 * g + e];
         }
+      l[i] += sum;
     }
     float power[2];
     bool rest = false;

@@ -192,3 +192,28 @@ def test_struct_of_strided_buffers():
     assert (c.struct.k_page_stride, c.struct.v_page_stride, c.struct.scale_page_stride) == (4096, 4096, 4)
     assert (c.struct.num_pages, c.struct.page_size, c.struct.kv_heads, c.struct.head_dim) == (6, 16, 2, 64)
     assert c.struct.v - c.struct.k == 2048
+
+
+def test_python_layer_refuses_several_devices():
+    c, b, x = _tensors()
+    rope, pos, gamma = A.Rope(torch.zeros(32)), torch.zeros(3, dtype=torch.int32), torch.ones(64, dtype=torch.bfloat16)
+    far = [t.to("meta") for t in (x, pos, gamma)]
+    far_rope = A.Rope(torch.zeros(32, device="meta"))
+    for call in (lambda: A.qk_norm_rope(x, far[0]), lambda: A.qk_norm_rope(x, None, far[1], rope),
+                 lambda: A.qk_norm_rope(x, None, pos, far_rope), lambda: A.qk_norm_rope(x, x, q_gamma=gamma, k_gamma=far[2]),
+                 lambda: A.qk_norm_rope(x, None, q_out=far[0]), lambda: A.kv_append(c, b, x, far[0]),
+                 lambda: A.kv_append(c, b, x, x, far[2]), lambda: A.kv_append(c, b, x, x, gamma, rope=far_rope),
+                 lambda: A.kv_append(c, b, x, x, gamma, rope=rope, positions=far[1]), lambda: A.attention(far[0], c, b),
+                 lambda: A.attention(x, c, b, out=far[0]), lambda: A.attention(x, c, b, workspace=far[0]),
+                 lambda: A.Batch(b.page_table, far[1]), lambda: A.Batch(b.page_table.to("meta"), b.kv_len),
+                 lambda: A.Batch(b.page_table, b.kv_len, torch.zeros(4, dtype=torch.int32, device="meta"), rows=3),
+                 lambda: A.KVCache(c.k, c.v, c.k_scale, c.v_scale.to("meta"), 16)):
+        with pytest.raises(ValueError, match="device"):
+            call()
+
+
+def test_a_single_row_has_any_stride():
+    x = torch.zeros(640, dtype=torch.bfloat16)
+    for t in (x[:128].view(2, 64)[None], torch.as_strided(x, (1, 2, 64), (3, 64, 1)), x[:128].view(1, 2, 64)):
+        assert A._rows(t, "q") == (1, 2, 64, 128)
+    assert A._rows(torch.as_strided(x, (2, 2, 64), (256, 64, 1)), "q") == (2, 2, 64, 256)
