@@ -28,7 +28,7 @@ __device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
 // sin and cos of the angle pos * inv_freq.  Whole turns and quarters are taken
 // off in binary64, where a position of 2^24 leaves 2^-29 turns' accuracy; the
 // rest, |x| <= pi / 4, goes through the Taylor series in T (float: to 1e-8,
-// double: to 1e-11).
+// double: to 5e-13).
 template <typename T>
 __device__ __forceinline__ void sin_cos(int pos, float inv_freq, T& sine, T& cosine) {
   double t = (double)pos * (double)inv_freq * 0.15915494309189535;      // turns
@@ -38,7 +38,8 @@ __device__ __forceinline__ void sin_cos(int pos, float inv_freq, T& sine, T& cos
   const T z = x * x;
   T s, c;
   if (sizeof(T) == 8) {
-    s = fma(z, (T)(-1.0 / 39916800.0), (T)(1.0 / 362880.0));
+    s = fma(z, (T)(1.0 / 6227020800.0), (T)(-1.0 / 39916800.0));
+    s = fma(z, s, (T)(1.0 / 362880.0));
     s = fma(z, s, (T)(-1.0 / 5040.0));
     c = fma(z, (T)(1.0 / 479001600.0), (T)(-1.0 / 3628800.0));
     c = fma(z, c, (T)(1.0 / 40320.0));

@@ -49,6 +49,47 @@ __device__ __forceinline__ double shfl_f64(double v, int l) {
   return __hiloint2double(hi, lo);
 }
 
+// Another lane's value within the row of 16 (all lanes active): from lane ^ 1,
+// ^ 2, ^ 7, ^ 15 for step 1, 2, 4, 8.  After the steps before, whose sums or
+// maxima groups of that many lanes share, ^ 7 and ^ 15 are as good as ^ 4 and ^ 8.
+template <int kStep>
+__device__ __forceinline__ int of_other(int v) {
+  constexpr int kHow = kStep == 1 ? 0xB1 : kStep == 2 ? 0x4E : kStep == 4 ? 0x141 : 0x140;
+  return __builtin_amdgcn_update_dpp(0, v, kHow, 0xF, 0xF, true);
+}
+
+template <int kStep>
+__device__ __forceinline__ double of_other(double v) {
+  return __hiloint2double(of_other<kStep>(__double2hiint(v)), of_other<kStep>(__double2loint(v)));
+}
+
+// The sum over the kLanes (8, 16 or 32) lanes that hold a token.
+template <int kLanes>
+__device__ __forceinline__ double sum_over(double v) {
+  v += of_other<1>(v);
+  v += of_other<2>(v);
+  v += of_other<4>(v);
+  if (kLanes >= 16) v += of_other<8>(v);
+  if (kLanes >= 32) {
+    const auto lo = __builtin_amdgcn_permlane16_swap(__double2loint(v), __double2loint(v), false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(__double2hiint(v), __double2hiint(v), false, false);
+    v = __hiloint2double((int)hi[0], (int)lo[0]) + __hiloint2double((int)hi[1], (int)lo[1]);
+  }
+  return v;
+}
+
+// The maximum over the wave.
+__device__ __forceinline__ float wave_max_of(float v) {
+  v = fmaxf(v, __int_as_float(of_other<1>(__float_as_int(v))));
+  v = fmaxf(v, __int_as_float(of_other<2>(__float_as_int(v))));
+  v = fmaxf(v, __int_as_float(of_other<4>(__float_as_int(v))));
+  v = fmaxf(v, __int_as_float(of_other<8>(__float_as_int(v))));
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // Four codes times the ratio of the old scale to the new one.
 __device__ __forceinline__ uint32_t rescaled(uint32_t codes, float ratio) {
   const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(codes, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(codes, true);
@@ -61,8 +102,8 @@ struct Treatment {
   bool turned;                   // these elements are among the rotated ones
   bool interleaved;
   int half, e0, partner;         // the lane that holds the other elements of the pairs
-  uint32_t flip[2];              // sign bit where an even, an odd element's partner counts negative
-  uint4 gamma;
+  uint32_t flip;                 // split halves: sign bit where the partner counts negative
+  double gamma[8];
   float eps;
 };
 
@@ -78,10 +119,12 @@ __device__ __forceinline__ Treatment treatment(const AppendArgs& a, int kind) {
   t.interleaved = a.rope.interleaved;
   t.partner = lane;
   if (t.turned && !t.interleaved) t.partner = lane + (t.e0 < t.half ? t.half / 8 : -(t.half / 8));
-  t.flip[0] = t.interleaved || t.e0 < t.half ? 0x80000000u : 0u;
-  t.flip[1] = !t.interleaved && t.e0 < t.half ? 0x80000000u : 0u;
-  t.gamma = make_uint4(0, 0, 0, 0);
-  if (t.norm) t.gamma = *reinterpret_cast<const uint4*>(a.gamma + t.e0);
+  t.flip = t.e0 < t.half ? 0x80000000u : 0u;
+  uint4 gamma = make_uint4(0, 0, 0, 0);
+  if (t.norm) gamma = *reinterpret_cast<const uint4*>(a.gamma + t.e0);
+  const uint32_t g[4] = {gamma.x, gamma.y, gamma.z, gamma.w};
+#pragma unroll
+  for (int j = 0; j < 4; ++j) t.gamma[2 * j] = (double)bf16_low(g[j]), t.gamma[2 * j + 1] = (double)bf16_high(g[j]);
   t.eps = a.eps;
   return t;
 }
@@ -107,9 +150,13 @@ __device__ __forceinline__ double reciprocal_root(double x) {
 
 // The lane's 8 values, ready for rounding.  turn: cosines and sines of the
 // token's angles.  All lanes of the wave call it.
-template <int D>
+// The binary32 number next to a value rounds to E4M3 as the value itself does,
+// and is over 448 scales where it is, unless it is a border itself, halfway
+// between two codes or 448 scales: then its last 19 bits are zero (5 significant
+// bits; scales are powers of two), and the wave takes the sticky ones.
+template <int D, bool kDynamic>
 __device__ __forceinline__ void values(const Treatment& t, uint4 in, const double2* turn, float (&v)[8]) {
-  const uint32_t d[4] = {in.x, in.y, in.z, in.w}, g[4] = {t.gamma.x, t.gamma.y, t.gamma.z, t.gamma.w};
+  const uint32_t d[4] = {in.x, in.y, in.z, in.w};
 #pragma unroll
   for (int j = 0; j < 4; ++j) v[2 * j] = bf16_low(d[j]), v[2 * j + 1] = bf16_high(d[j]);
   if (!t.norm && !t.rotate) return;
@@ -120,32 +167,45 @@ __device__ __forceinline__ void values(const Treatment& t, uint4 in, const doubl
     double sum = 0.0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) sum = fma(w[j], w[j], sum);
+    const double r = reciprocal_root(sum_over<D / 8>(sum) * (1.0 / D) + (double)t.eps);
 #pragma unroll
-    for (int m = 1; m < D / 8; m *= 2) sum += shfl_f64(sum, (threadIdx.x & 63) ^ m);
-    const double r = reciprocal_root(sum * (1.0 / D) + (double)t.eps);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      w[2 * j] *= r * (double)bf16_low(g[j]);
-      w[2 * j + 1] *= r * (double)bf16_high(g[j]);
-    }
+    for (int j = 0; j < 8; ++j) w[j] *= r * t.gamma[j];
   }
-  if (t.rotate) {
+  if (t.rotate && t.interleaved) {
+    if (t.turned) {
+      const double2* at = turn + turn_at(t.half, t.e0 / 2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const double2 cs = at[j * (t.half >> 3)];
+        const double x = w[2 * j], y = w[2 * j + 1];
+        w[2 * j] = fma(x, cs.x, -(y * cs.y));
+        w[2 * j + 1] = fma(y, cs.x, x * cs.y);
+      }
+    }
+  } else if (t.rotate) {
     double p[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) p[j] = t.interleaved ? w[j ^ 1] : shfl_f64(w[j], t.partner);
+    for (int j = 0; j < 8; ++j) p[j] = shfl_f64(w[j], t.partner);
     if (t.turned) {
+      const double2* at = turn + turn_at(t.half, t.e0 < t.half ? t.e0 : t.e0 - t.half);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int e = t.e0 + j;
-        const bool second = t.interleaved ? (j & 1) : e >= t.half;
-        const double2 cs = turn[turn_at(t.half, t.interleaved ? e / 2 : (second ? e - t.half : e))];
-        const double other = __hiloint2double(__double2hiint(p[j]) ^ (int)t.flip[j & 1], __double2loint(p[j]));
+        const double2 cs = at[j * (t.half >> 3)];
+        const double other = __hiloint2double(__double2hiint(p[j]) ^ (int)t.flip, __double2loint(p[j]));
         w[j] = fma(w[j], cs.x, other * cs.y);
       }
     }
   }
+  uint32_t border = ~0u;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = sticky(w[j]);
+  for (int j = 0; j < 8; ++j) {
+    v[j] = (float)w[j];
+    border = min(border, __float_as_uint(v[j]) & 0x7FFFFu);
+  }
+  if (!kDynamic || __any(border == 0)) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = sticky(w[j]);
+  }
 }
 
 // Codes of 8 values over the scale.  In dynamic mode none is over 448 scales and
@@ -237,7 +297,33 @@ __device__ __forceinline__ void put_codes(uint8_t* out, int kind, int t, int e0,
   }
 }
 
-// Many rows.  kPasses * 2048 / D tokens at most; heads_each heads a workgroup.
+// Codes of values, four tokens to a 32-bit word as the cache has them, from lanes
+// that hold 8 elements of one token each.
+//   D <= 128: bits 4 and 5 of the lane are the token's place in the four.  The lane
+//   gets elements first, first + 1 of its 8, first = 4 (lane / 32) + 2 (lane / 16 % 2).
+__device__ __forceinline__ uint2 fours(uint2 c) {
+  const auto a = __builtin_amdgcn_permlane32_swap(c.x, c.y, false, false);      // tokens 0, 1 and 2, 3
+  const uint32_t lo = __builtin_amdgcn_perm(a[1], a[0], 0x05010400u), hi = __builtin_amdgcn_perm(a[1], a[0], 0x07030602u);
+  const auto b = __builtin_amdgcn_permlane16_swap(lo, hi, false, false);        // 0 2 0 2 and 1 3 1 3
+  return make_uint2(__builtin_amdgcn_perm(b[1], b[0], 0x05010400u), __builtin_amdgcn_perm(b[1], b[0], 0x07030602u));
+}
+
+//   D = 256: bit 5 is the place's low bit, and c0, c1 are two tokens.  The lane
+//   gets elements first .. first + 3, first = 4 (lane / 32).
+__device__ __forceinline__ uint4 fours(uint2 c0, uint2 c1) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__builtin_amdgcn_perm(c1.x, c0.x, 0x05010400u),
+                                                  __builtin_amdgcn_perm(c1.y, c0.y, 0x05010400u), false, false);
+  const auto b = __builtin_amdgcn_permlane32_swap(__builtin_amdgcn_perm(c1.x, c0.x, 0x07030602u),
+                                                  __builtin_amdgcn_perm(c1.y, c0.y, 0x07030602u), false, false);
+  return make_uint4(__builtin_amdgcn_perm(a[1], a[0], 0x05010400u), __builtin_amdgcn_perm(a[1], a[0], 0x07030602u),
+                    __builtin_amdgcn_perm(b[1], b[0], 0x05010400u), __builtin_amdgcn_perm(b[1], b[0], 0x07030602u));
+}
+
+// Place of a 16-byte piece of keys in LDS: the pieces of a token, 256 bytes apart
+// in the cache's order, in different banks.
+__device__ __forceinline__ int key_piece(int x) { return x ^ ((x >> 4) & 15); }
+
+// Many rows.  kPasses * 2048 / D slots at most; heads_each heads a workgroup.
 template <int D, int kPasses, bool kDynamic>
 __global__ __launch_bounds__(kAppendThreads, kPasses <= 2 ? 4 : kPasses == 4 ? 2 : 1) void kv_append_pages_kernel(AppendArgs a, int heads_each) {
   constexpr int kLanes = D / 8, kTokens = kAppendThreads / kLanes;        // of one pass
@@ -249,11 +335,21 @@ __global__ __launch_bounds__(kAppendThreads, kPasses <= 2 ? 4 : kPasses == 4 ? 2
   Touch t;
   if (!find_touch(a, (int)blockIdx.x / parts, t)) return;
   const int h0 = (int)blockIdx.x % parts * heads_each, h1 = min(h0 + heads_each, a.cache.heads);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mine = threadIdx.x / kLanes;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Treatment for_keys = treatment<D>(a, 0);
-  Treatment for_values = for_keys;
-  for_values.norm = for_values.rotate = for_values.turned = false;
-  const int e0 = for_keys.e0;
+  const int e0 = for_keys.e0, last = t.slot0 + t.n;
+  // The slot of this lane's token in pass p, so that the four tokens of a word of
+  // values are in lanes (or passes) that fours() joins; and the passes that hold some.
+  const auto slot = [&](int p) __attribute__((always_inline)) {
+    const int g = lane / kLanes;
+    return D == 256 ? p / 2 * 16 + wave * 4 + p % 2 * 2 + g
+                    : p * kTokens + wave * (64 / kLanes) + (D == 64 ? (g & 1) * 4 + (g >> 1) : g);
+  };
+  const auto holds = [&](int p) __attribute__((always_inline)) {
+    constexpr int kSpan = D == 256 ? 16 : kTokens;
+    const int s0 = (D == 256 ? p / 2 : p) * kSpan;
+    return s0 < last && s0 + kSpan > t.slot0;
+  };
 
   uint4 in[kPasses];
   const auto load = [&](int h, int kind) __attribute__((always_inline)) {
@@ -261,34 +357,51 @@ __global__ __launch_bounds__(kAppendThreads, kPasses <= 2 ? 4 : kPasses == 4 ? 2
     const uint16_t* x = (kind ? a.x[1] : a.x[0]) + (int64_t)t.row0 * ld + (int64_t)h * D + e0;
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
-      const int i = p * kTokens + mine;
+      const int i = slot(p) - t.slot0;
       in[p] = make_uint4(0, 0, 0, 0);
-      if (i < t.n) in[p] = *reinterpret_cast<const uint4*>(x + i * ld);
+      if (i >= 0 && i < t.n) in[p] = *reinterpret_cast<const uint4*>(x + i * ld);
     }
   };
   load(h0, 0);
   if (for_keys.rotate) {
-    // A token's angles, by the D / 8 lanes that hold it (at most 4 each): the
-    // lanes of one wave, like those that use them.
-    for (int i = mine; i < t.n; i += kTokens) {
-      const int pos = position(a, t, i);
-      for (int f = e0 / 8; f < for_keys.half; f += kLanes) {
-        double s, c;
-        sin_cos<double>(pos, a.rope.inv_freq[f], s, c);
+    // A thread takes one angle of 8 tokens; where a token's position is the last
+    // one's and 1, from that one's sine and cosine (4 operations instead of 50).
+    const int runs = (t.n + 7) / 8;
+    for (int x = threadIdx.x; x < runs * for_keys.half; x += kAppendThreads) {
+      const int run = x / for_keys.half, f = x - run * for_keys.half;
+      const float freq = a.rope.inv_freq[f];
+      double s, c, s1, c1;
+      sin_cos<double>(1, freq, s1, c1);
+      uint32_t before = 0;
+      for (int i = 8 * run; i < min(8 * run + 8, t.n); ++i) {
+        const int pos = position(a, t, i);
+        if (i % 8 != 0 && (uint32_t)pos == before + 1) {
+          const double c0 = c;
+          c = fma(c0, c1, -(s * s1));
+          s = fma(s, c1, c0 * s1);
+        } else {
+          sin_cos<double>(pos, freq, s, c);
+        }
+        before = (uint32_t)pos;
         turn[i][turn_at(for_keys.half, f)] = make_double2(c, s);
       }
     }
-    wave_lds_fence();
+    __syncthreads();
   }
 
-  const auto one = [&](const Treatment& how, int h, int kind, bool more, int next_h, int next_kind)
-      __attribute__((always_inline)) {
+  const auto one = [&](int h, int kind, bool more, int next_h, int next_kind) __attribute__((always_inline)) {
     float v[kPasses][8], top = 0.0f;
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
-      if (p * kTokens >= t.n) break;
-      values<D>(how, in[p], turn[min(p * kTokens + mine, t.n - 1)], v[p]);
-      top = largest(v[p], top, true);      // (0 behind the last token)
+      if (!holds(p)) continue;
+      if (kind == 0) {
+        values<D, kDynamic>(for_keys, in[p], turn[min(max(slot(p) - t.slot0, 0), t.n - 1)], v[p]);
+      } else {
+        const uint32_t d[4] = {in[p].x, in[p].y, in[p].z, in[p].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[p][2 * j] = bf16_low(d[j]), v[p][2 * j + 1] = bf16_high(d[j]);
+      }
+      top = largest(v[p], top, true);      // (0 where there is no token)
       __builtin_amdgcn_sched_barrier(0);   // (one pass's binary64 values at a time: registers)
     }
     if (more) load(next_h, next_kind);
@@ -301,12 +414,10 @@ __global__ __launch_bounds__(kAppendThreads, kPasses <= 2 ? 4 : kPasses == 4 ? 2
       top = 0.0f;
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
-        if (p * kTokens >= t.n) break;
-        top = largest(v[p], top, false);
+        if (holds(p)) top = largest(v[p], top, false);
       }
     }
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+    top = wave_max_of(top);
     if (lane == 0) wave_max[wave] = top;
     __syncthreads();      // (the last head's codes have left LDS, too)
     float scale = held;
@@ -319,15 +430,32 @@ __global__ __launch_bounds__(kAppendThreads, kPasses <= 2 ? 4 : kPasses == 4 ? 2
     const float inverse = 1.0f / scale;
 #pragma unroll
     for (int p = 0; p < kPasses; ++p) {
-      if (p * kTokens >= t.n) break;
-      const int i = p * kTokens + mine;
-      if (i < t.n) put_codes<D>(codes, kind, t.slot0 + i, e0, eight_codes<kDynamic>(v[p], scale, inverse));
+      if (!holds(p) || (D == 256 && kind == 1 && p % 2 == 1)) continue;
+      const int s = slot(p);
+      if (kind == 0) {
+        uint8_t* to = codes + 16 * key_piece(s / 16 * D + e0 / 16 * 16 + s % 16) + (e0 & 8);
+        *reinterpret_cast<uint2*>(to) = eight_codes<kDynamic>(v[p], scale, inverse);
+      } else {
+        uint8_t* to = codes + s / 16 * 16 * D + e0 / 64 * 1024 + (s % 16 / 4 * 16 + (e0 & 8)) * 16 + e0 / 16 % 4 * 4;
+        if constexpr (D == 256) {
+          const uint4 c = fours(eight_codes<kDynamic>(v[p], scale, inverse), eight_codes<kDynamic>(v[p + 1], scale, inverse));
+          uint8_t* at = to + lane / 32 * 64;
+          *reinterpret_cast<uint32_t*>(at) = c.x;
+          *reinterpret_cast<uint32_t*>(at + 16) = c.y;
+          *reinterpret_cast<uint32_t*>(at + 32) = c.z;
+          *reinterpret_cast<uint32_t*>(at + 48) = c.w;
+        } else {
+          const uint2 c = fours(eight_codes<kDynamic>(v[p], scale, inverse));
+          uint8_t* at = to + lane / 32 * 64 + lane / 16 % 2 * 32;
+          *reinterpret_cast<uint32_t*>(at) = c.x;
+          *reinterpret_cast<uint32_t*>(at + 16) = c.y;
+        }
+      }
     }
     __syncthreads();      // (the held codes are written, too)
-    const int last = t.slot0 + t.n;
     for (int y = (t.slot0 / 16) * D + threadIdx.x; y < ((last + 15) / 16) * D; y += kAppendThreads) {
       const int group = y / D, in_group = y % D;
-      const uint4 c = reinterpret_cast<const uint4*>(codes)[y];
+      const uint4 c = reinterpret_cast<const uint4*>(codes)[kind == 0 ? key_piece(y) : y];
       uint4* at = reinterpret_cast<uint4*>(out) + y;
       if (kind == 0) {
         const int s = group * 16 + (in_group & 15);
@@ -350,8 +478,8 @@ __global__ __launch_bounds__(kAppendThreads, kPasses <= 2 ? 4 : kPasses == 4 ? 2
     if (kDynamic && threadIdx.x == 0) *scale_at = scale;
   };
   for (int h = h0; h < h1; ++h) {
-    one(for_keys, h, 0, true, h, 1);
-    one(for_values, h, 1, h + 1 < h1, h + 1, 0);
+    one(h, 0, true, h, 1);
+    one(h, 1, h + 1 < h1, h + 1, 0);
   }
 }
 
@@ -384,7 +512,7 @@ __global__ __launch_bounds__(64) void kv_append_tokens_kernel(AppendArgs a) {
       }
       wave_lds_fence();
     }
-    values<D>(how, in, turn, v);
+    values<D, kDynamic>(how, in, turn, v);
   };
 
   float* scale_at = (kind ? a.cache.scale[1] : a.cache.scale[0]) + (int64_t)t.page * a.cache.scale_stride + h;
@@ -433,14 +561,16 @@ static hipError_t launch(const AppendArgs& a, int64_t items, hipStream_t stream)
   if (blocks >= (int64_t)1 << 31) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks);
   const int elements = a.cache.page_size * D;
-  if (elements <= 2048)
-    kv_append_pages_kernel<D, 1, kDynamic><<<grid, kAppendThreads, 0, stream>>>(a, (int)each);
-  else if (elements <= 4096)
-    kv_append_pages_kernel<D, 2, kDynamic><<<grid, kAppendThreads, 0, stream>>>(a, (int)each);
-  else if (elements <= 8192)
-    kv_append_pages_kernel<D, 4, kDynamic><<<grid, kAppendThreads, 0, stream>>>(a, (int)each);
-  else
-    kv_append_pages_kernel<D, 8, kDynamic><<<grid, kAppendThreads, 0, stream>>>(a, (int)each);
+  const auto run = [&](auto* kernel) { kernel<<<grid, kAppendThreads, 0, stream>>>(a, (int)each); };
+  if (elements <= 2048) {
+    if constexpr (D <= 128) run(kv_append_pages_kernel<D, 1, kDynamic>);
+  } else if (elements <= 4096) {
+    run(kv_append_pages_kernel<D, 2, kDynamic>);
+  } else if (elements <= 8192) {
+    run(kv_append_pages_kernel<D, 4, kDynamic>);
+  } else {
+    if constexpr (D >= 128) run(kv_append_pages_kernel<D, 8, kDynamic>);
+  }
   return hipGetLastError();
 }
 
