@@ -24,7 +24,6 @@
 
 namespace nvfp4 {
 
-constexpr int kAppendThreads = 256;
 constexpr float kLargest = 3.40282347e38f;
 
 // The binary32 number next to d towards zero, with its last bit set unless it
@@ -323,13 +322,13 @@ __device__ __forceinline__ uint4 fours(uint2 c0, uint2 c1) {
 // in the cache's order, in different banks.
 __device__ __forceinline__ int key_piece(int x) { return x ^ ((x >> 4) & 15); }
 
-// Many rows.  kPasses * 2048 / D slots at most; heads_each heads a workgroup.
-template <int D, int kPasses, bool kDynamic>
-__global__ __launch_bounds__(kAppendThreads, kPasses <= 2 ? 4 : kPasses == 4 ? 2 : 1) void kv_append_pages_kernel(AppendArgs a, int heads_each) {
-  constexpr int kLanes = D / 8, kTokens = kAppendThreads / kLanes;        // of one pass
+// Many rows.  kPasses * kThreads * 8 / D slots at most; heads_each heads a workgroup.
+template <int D, int kThreads, int kPasses, bool kDynamic>
+__global__ __launch_bounds__(kThreads, 4) void kv_append_pages_kernel(AppendArgs a, int heads_each) {
+  constexpr int kLanes = D / 8, kTokens = kThreads / kLanes;        // of one pass
   __shared__ double2 turn[kPasses * kTokens][D / 2];
   __shared__ uint8_t __attribute__((aligned(16))) codes[kPasses * kTokens * D];
-  __shared__ float wave_max[kAppendThreads / 64];
+  __shared__ float wave_max[kThreads / 64];
 
   const int parts = (a.cache.heads + heads_each - 1) / heads_each;
   Touch t;
@@ -342,11 +341,11 @@ __global__ __launch_bounds__(kAppendThreads, kPasses <= 2 ? 4 : kPasses == 4 ? 2
   // values are in lanes (or passes) that fours() joins; and the passes that hold some.
   const auto slot = [&](int p) __attribute__((always_inline)) {
     const int g = lane / kLanes;
-    return D == 256 ? p / 2 * 16 + wave * 4 + p % 2 * 2 + g
+    return D == 256 ? p / 2 * 2 * kTokens + wave * 4 + p % 2 * 2 + g
                     : p * kTokens + wave * (64 / kLanes) + (D == 64 ? (g & 1) * 4 + (g >> 1) : g);
   };
   const auto holds = [&](int p) __attribute__((always_inline)) {
-    constexpr int kSpan = D == 256 ? 16 : kTokens;
+    constexpr int kSpan = D == 256 ? 2 * kTokens : kTokens;
     const int s0 = (D == 256 ? p / 2 : p) * kSpan;
     return s0 < last && s0 + kSpan > t.slot0;
   };
@@ -367,7 +366,7 @@ __global__ __launch_bounds__(kAppendThreads, kPasses <= 2 ? 4 : kPasses == 4 ? 2
     // A thread takes one angle of 8 tokens; where a token's position is the last
     // one's and 1, from that one's sine and cosine (4 operations instead of 50).
     const int runs = (t.n + 7) / 8;
-    for (int x = threadIdx.x; x < runs * for_keys.half; x += kAppendThreads) {
+    for (int x = threadIdx.x; x < runs * for_keys.half; x += kThreads) {
       const int run = x / for_keys.half, f = x - run * for_keys.half;
       const float freq = a.rope.inv_freq[f];
       double s, c, s1, c1;
@@ -423,9 +422,9 @@ __global__ __launch_bounds__(kAppendThreads, kPasses <= 2 ? 4 : kPasses == 4 ? 2
     float scale = held;
     if (kDynamic) {
 #pragma unroll
-      for (int w = 0; w < kAppendThreads / 64; ++w) top = fmaxf(top, wave_max[w]);
+      for (int w = 0; w < kThreads / 64; ++w) top = fmaxf(top, wave_max[w]);
       scale = fmaxf(held, page_scale(top));
-      if (scale > held && t.slot0 > 0) bring_along<D>(out, kind, t.slot0, held / scale, threadIdx.x, kAppendThreads);
+      if (scale > held && t.slot0 > 0) bring_along<D>(out, kind, t.slot0, held / scale, threadIdx.x, kThreads);
     }
     const float inverse = 1.0f / scale;
 #pragma unroll
@@ -453,7 +452,7 @@ __global__ __launch_bounds__(kAppendThreads, kPasses <= 2 ? 4 : kPasses == 4 ? 2
       }
     }
     __syncthreads();      // (the held codes are written, too)
-    for (int y = (t.slot0 / 16) * D + threadIdx.x; y < ((last + 15) / 16) * D; y += kAppendThreads) {
+    for (int y = (t.slot0 / 16) * D + threadIdx.x; y < ((last + 15) / 16) * D; y += kThreads) {
       const int group = y / D, in_group = y % D;
       const uint4 c = reinterpret_cast<const uint4*>(codes)[kind == 0 ? key_piece(y) : y];
       uint4* at = reinterpret_cast<uint4*>(out) + y;
@@ -550,26 +549,26 @@ static hipError_t launch(const AppendArgs& a, int64_t items, hipStream_t stream)
     kv_append_tokens_kernel<D, kDynamic><<<dim3((unsigned)blocks), 64, 0, stream>>>(a);
     return hipGetLastError();
   }
-  // Heads of a workgroup: as many as leave four workgroups for each of 256
-  // compute units (pages that are written, about rows / page_size).
+  // Heads of a workgroup: as many as leave one round of workgroups on 256 compute
+  // units, four of 4096 elements each (pages that are written, about rows / page_size).
+  const int elements = a.cache.page_size * D;
   const int64_t pages = (a.batch.rows >> a.cache.page_shift) + a.batch.seqs;
-  int64_t each = (pages * a.cache.heads + 1023) / 1024;
+  const int64_t fit = elements <= 4096 ? 1024 : 1024 * 4096 / elements;
+  int64_t each = (pages * a.cache.heads + fit - 1) / fit;
   if (each > a.cache.heads) each = a.cache.heads;
   const int64_t parts = (a.cache.heads + each - 1) / each;
   each = (a.cache.heads + parts - 1) / parts;
-  const int64_t blocks = items * ((a.cache.heads + each - 1) / each);
+  const int64_t blocks = items * parts;
   if (blocks >= (int64_t)1 << 31) return hipErrorInvalidValue;
   const dim3 grid((unsigned)blocks);
-  const int elements = a.cache.page_size * D;
-  const auto run = [&](auto* kernel) { kernel<<<grid, kAppendThreads, 0, stream>>>(a, (int)each); };
   if (elements <= 2048) {
-    if constexpr (D <= 128) run(kv_append_pages_kernel<D, 1, kDynamic>);
+    if constexpr (D <= 128) kv_append_pages_kernel<D, 256, 1, kDynamic><<<grid, 256, 0, stream>>>(a, (int)each);
   } else if (elements <= 4096) {
-    run(kv_append_pages_kernel<D, 2, kDynamic>);
+    kv_append_pages_kernel<D, 256, 2, kDynamic><<<grid, 256, 0, stream>>>(a, (int)each);
   } else if (elements <= 8192) {
-    run(kv_append_pages_kernel<D, 4, kDynamic>);
+    kv_append_pages_kernel<D, 512, 2, kDynamic><<<grid, 512, 0, stream>>>(a, (int)each);
   } else {
-    if constexpr (D >= 128) run(kv_append_pages_kernel<D, 8, kDynamic>);
+    if constexpr (D >= 128) kv_append_pages_kernel<D, 1024, 2, kDynamic><<<grid, 1024, 0, stream>>>(a, (int)each);
   }
   return hipGetLastError();
 }
