@@ -45,11 +45,12 @@ def _rows(x, name):
 
 
 def _like_rows(x, stream):
-    """A contiguous [rows, heads, head_dim] tensor from the stream that uses it."""
+    """A contiguous [rows, heads, head_dim] tensor from the stream that uses it.
+    (empty_like closes the gaps between x's rows.)"""
     if stream is None:
-        return torch.empty_like(x, memory_format=torch.contiguous_format)
+        return torch.empty_like(x)
     with _l._on(stream, x.device):
-        return torch.empty_like(x, memory_format=torch.contiguous_format)
+        return torch.empty_like(x)
 
 
 def _run(t, call, *args):
@@ -191,6 +192,22 @@ def _rotation(rope, device):
     return rope.pointer
 
 
+def _head_args(x, gamma, y, rows, dim, device, name, stream):
+    """((x, stride, heads, gamma, y, stride), y) of the queries or the keys."""
+    if x is None:
+        return (None, 0, 0, None, None, 0), None
+    n, heads, d, ld = _rows(x, name)
+    if n != rows or d != dim or x.device != device:
+        raise ValueError("q and k differ in rows, head_dim or device")
+    if y is None:
+        y, ldy = _like_rows(x, stream), heads * d
+    else:
+        ny, hy, dy, ldy = _rows(y, name + "_out")
+        if (ny, hy, dy) != (n, heads, d) or y.device != device:
+            raise ValueError(name + "_out must have the shape and device of its input")
+    return (x.data_ptr(), ld, heads, None if gamma is None else _gamma(gamma, d, device, name + "_gamma"), y.data_ptr(), ldy), y
+
+
 def qk_norm_rope(q, k, positions=None, rope: Rope = None, q_gamma=None, k_gamma=None, eps=1e-6, q_out=None, k_out=None,
                  stream=None):
     """RMSNorm of each head of q and of k (either may be None; no norm without
@@ -199,32 +216,15 @@ def qk_norm_rope(q, k, positions=None, rope: Rope = None, q_gamma=None, k_gamma=
     one = q if q is not None else k
     if one is None:
         raise ValueError("q or k must be given")
-    rows, device = one.shape[0], one.device
-    args, out, dim = [], [], None
-    for x, gamma, y, names in ((q, q_gamma, q_out, ("q", "q_gamma", "q_out")), (k, k_gamma, k_out, ("k", "k_gamma", "k_out"))):
-        if x is None:
-            args += (None, 0, 0, None, None, 0)
-            out.append(None)
-            continue
-        n, heads, d, ld = _rows(x, names[0])
-        dim = d if dim is None else dim
-        if n != rows or d != dim or x.device != device:
-            raise ValueError("q and k differ in rows, head_dim or device")
-        if y is None:
-            y = _like_rows(x, stream)
-            ldy = heads * d
-        else:
-            ny, hy, dy, ldy = _rows(y, names[2])
-            if (ny, hy, dy) != (n, heads, d) or y.device != device:
-                raise ValueError(names[2] + " must have the shape and device of its input")
-        args += (x.data_ptr(), ld, heads, _gamma(gamma, d, device, names[1]), y.data_ptr(), ldy)
-        out.append(y)
+    rows, dim, device = one.shape[0], one.shape[-1], one.device
+    q_args, q_out = _head_args(q, q_gamma, q_out, rows, dim, device, "q", stream)
+    k_args, k_out = _head_args(k, k_gamma, k_out, rows, dim, device, "k", stream)
     inv_freq, half, interleaved = _rotation(rope, device)
     if half and positions is None:
         raise ValueError("a rotation needs positions")
-    _run(one, _a.qk_norm_rope, *args, rows, dim, eps, _positions(positions, rows, device) if half else None, inv_freq, 2 * half,
-         interleaved, stream)
-    return tuple(out)
+    _run(one, _a.qk_norm_rope, stream, *q_args, *k_args, rows, dim, eps,
+         _positions(positions, rows, device) if half else None, inv_freq, 2 * half, interleaved)
+    return q_out, k_out
 
 
 def kv_append(cache: KVCache, batch: Batch, k, v, k_gamma=None, eps=1e-6, rope: Rope = None, positions=None,
@@ -242,8 +242,8 @@ def kv_append(cache: KVCache, batch: Batch, k, v, k_gamma=None, eps=1e-6, rope: 
     if not device == v.device == cache.device == batch.device:
         raise ValueError("tensors are on several devices")
     inv_freq, half, interleaved = _rotation(rope, device)
-    _run(k, _a.kv_append, cache.ref, batch.ref, k.data_ptr(), ldk, v.data_ptr(), ldv,
-         _gamma(k_gamma, dim, device, "k_gamma"), eps, _positions(positions, rows, device), inv_freq, 2 * half, interleaved, 1 if static else 0, stream)
+    _run(k, _a.kv_append, stream, cache.ref, batch.ref, k.data_ptr(), ldk, v.data_ptr(), ldv,
+         _gamma(k_gamma, dim, device, "k_gamma"), eps, _positions(positions, rows, device), inv_freq, 2 * half, interleaved, 1 if static else 0)
 
 
 def attention(q, cache: KVCache, batch: Batch, scale=None, causal=True, window=0, out=None, return_lse=False,
@@ -275,7 +275,7 @@ def attention(q, cache: KVCache, batch: Batch, scale=None, causal=True, window=0
         if workspace.device != q.device or not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous, on q's device")
         nbytes = workspace.numel() * workspace.element_size()
-    _run(q, _a.kv_attention, cache.ref, batch.ref, q.data_ptr(), ldq, heads, y.data_ptr(), ldy,
+    _run(q, _a.kv_attention, stream, cache.ref, batch.ref, q.data_ptr(), ldq, heads, y.data_ptr(), ldy,
          None if lse is None else lse.data_ptr(), cache.softmax_scale if scale is None else scale, 1 if causal else 0,
-         window, None if workspace is None else workspace.data_ptr(), nbytes, stream)
+         window, None if workspace is None else workspace.data_ptr(), nbytes)
     return (y, lse) if return_lse else y

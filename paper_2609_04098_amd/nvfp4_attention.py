@@ -64,17 +64,22 @@ def batch_struct(page_table, kv_len, cu_rows, rows, max_kv_len):
                          page_table.shape[1], kv_len.shape[0], rows, max_kv_len)
 
 
-def qk_norm_rope(*args):
+def _handle(stream):
+    """Handle of a torch stream, a handle itself, or of the current stream (None)."""
+    return _c._current_stream() if stream is None else getattr(stream, "cuda_stream", stream)
+
+
+def qk_norm_rope(stream, *args):
     """nvfp4_qk_norm_rope: its arguments in order, addresses as integers (or
-    None), the stream a torch stream, a handle or None (the current one)."""
-    status = (_lib or lib()).nvfp4_qk_norm_rope(*args[:-1], _c._stream(args[-1]))
+    None), after the stream: a torch stream, a handle or None (the current one)."""
+    status = (_lib or lib()).nvfp4_qk_norm_rope(*args, _handle(stream))
     if status:
         _c._check(status, "nvfp4_qk_norm_rope")
 
 
-def kv_append(*args):
+def kv_append(stream, *args):
     """nvfp4_kv_append, its arguments as above, the structures by reference."""
-    status = (_lib or lib()).nvfp4_kv_append(*args[:-1], _c._stream(args[-1]))
+    status = (_lib or lib()).nvfp4_kv_append(*args, _handle(stream))
     if status:
         _c._check(status, "nvfp4_kv_append")
 
@@ -83,8 +88,8 @@ def kv_attention_workspace(cache, batch, q_heads):
     return lib().nvfp4_kv_attention_workspace(cache, batch, q_heads)
 
 
-def kv_attention(*args):
+def kv_attention(stream, *args):
     """nvfp4_kv_attention, its arguments as above."""
-    status = (_lib or lib()).nvfp4_kv_attention(*args[:-1], _c._stream(args[-1]))
+    status = (_lib or lib()).nvfp4_kv_attention(*args, _handle(stream))
     if status:
         _c._check(status, "nvfp4_kv_attention")
