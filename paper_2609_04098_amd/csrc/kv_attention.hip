@@ -344,7 +344,9 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group) {
     // (One piece: also with eight waves, of which a compute unit holds one workgroup.
     // 24 sequences of up to 6 rows of 4 key heads of 64, a window of 4096: 23.5 us
     // with four, 18.2 us with eight, 18.3 us with sixteen.  A ring of three tiles
-    // ahead in LDS for four waves: 20.5 us.)
+    // ahead in LDS for four waves: 20.5 us.  They start later where there are many:
+    // 30 sequences of 8 key heads of 128, 400 tokens: 8.0 us with four, 11.1 us with
+    // eight; and have twice the loads in flight: 32 of 3000, 45.2 and 38.1 us.)
     for (const int waves : {4, 8}) {
       if (waves > 4 && (s > 1 || p.tiles != 1 || c.dim == 256)) continue;
       const double slots = 256.0 * (waves > 4 ? 1 : fit);
@@ -352,7 +354,8 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group) {
       for (const double share : {1.0, 0.55}) {
         const double n = share * (double)(work * s), longest = (double)each / (alone * waves / 4);
         const double all = n * (double)each / together;
-        time += all > longest ? all : longest;
+        const double work_time = all > longest ? all : longest;
+        time += waves > 4 ? 0.85 * work_time + 1.5 * n / slots : work_time;
         if (n > slots)                                             // the last ones; beginnings and ends
           time += (p.tiles == 8 ? 0.25 : 0.5) * longest + 6.0 * 256.0 * n / (slots * slots);
         if (s > 1) time += 0.05 * all + 6.0 + n * part;                           // the join
