@@ -66,12 +66,10 @@ kv_attention_rows_kernel(AttentionArgs a) {
   int begin = t.begin, end = t.end;
   bool whole = true;             // this piece is all that the rows see
   if (kSplit) {
-    int p0, p1;
-    pieces_of(a, t, p0, p1);
-    if (piece < p0 || piece >= p1) return;
-    whole = p1 - p0 == 1;
-    begin = max(begin, piece * a.chunk);
-    if (piece + 1 < a.splits) end = min(end, (piece + 1) * a.chunk);
+    const int pieces = pieces_of(a, t);
+    if (piece >= pieces) return;
+    whole = pieces == 1;
+    piece_tokens(a, t, piece, begin, end);
   }
 
   RowTiles<D, kTiles> rows;
@@ -217,9 +215,8 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a)
   const int number = (int)(blockIdx.x / (kRows / kBlockRows)) / a.cache.heads;
   Tile t;
   if (!find_tile<kRows>(a, number, t) || row >= t.n) return;      // (with kShare 4, the whole workgroup)
-  int p0, p1;
-  pieces_of(a, t, p0, p1);
-  if (p1 - p0 == 1) return;      // its rows are written already
+  const int pieces = pieces_of(a, t);
+  if (pieces == 1) return;      // its rows are written already
   const int64_t first = ((int64_t)number * a.cache.heads + h) * a.splits;
   const float2* stats = reinterpret_cast<const float2*>(a.part) + first * kRows + row;
   const float* part = a.part + tiles_of(a.batch, a.group, kRows) * a.cache.heads * a.splits * (2 * kRows) +
@@ -227,7 +224,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a)
   float m = kNone, l = 0.0f, y[kEach];
 #pragma unroll
   for (int i = 0; i < kEach; ++i) y[i] = 0.0f;
-  for (int p = p0 + share; p < p1; p += kShare * kAhead) {
+  for (int p = share; p < pieces; p += kShare * kAhead) {
     float2 st[kAhead];
     float v[kAhead][kEach];
 #pragma unroll
@@ -236,7 +233,7 @@ __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a)
       st[u] = make_float2(kNone, 0.0f);
 #pragma unroll
       for (int i = 0; i < kEach; ++i) v[u][i] = 0.0f;
-      if (at < p1) {
+      if (at < pieces) {
         st[u] = stats[at * kRows];
 #pragma unroll
         for (int i = 0; i < kEach; ++i) v[u][i] = part[(int64_t)at * kRows * D + i];
@@ -298,6 +295,8 @@ int64_t host_tiles(const KvBatchArgs& b, int group, int rows) {
   return b.cu_rows == nullptr ? (int64_t)b.seqs * ((group + rows - 1) / rows) : (int64_t)b.rows * group / rows + b.seqs;
 }
 
+constexpr int64_t kAnyRoom = (int64_t)1 << 62;
+
 struct Plan {
   int tiles;               // of 16 rows, for a workgroup
   int waves;
@@ -314,7 +313,9 @@ struct Plan {
 // Pieces: the number of them for which an estimate of the time is least, of a
 // step whose sequences all have the largest length and of one that has 0.55 times
 // as many workgroups (lengths of all sizes), together.
-Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group) {
+// A window bounds what a tile sees, and a step's workspace is sized without it:
+// with one, only numbers of pieces that fit `room` partial results are looked at.
+Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group, int window, int64_t room) {
   Plan p;
   const int64_t seqs = b.seqs > 0 ? b.seqs : 1, rows = ((int64_t)b.rows * group + seqs - 1) / seqs;
   const auto of_rows = [&](int tile) { return (rows + tile - 1) / tile; };
@@ -338,10 +339,12 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group) {
   double best = 0.0;
   p.waves = 4;
   p.splits = 1;
-  p.chunk = b.max_kv_len > 0 ? b.max_kv_len : 1;
+  const int64_t reach = (int64_t)window + 16 * p.tiles + 64;
+  const int length = window > 0 && reach < b.max_kv_len ? (int)reach : b.max_kv_len;
+  p.chunk = length > 0 ? length : 1;
   for (const int s : candidates) {
-    const int64_t each = ((int64_t)b.max_kv_len + 128 * s - 1) / (128 * s) * 128;
-    if (s > 1 && each < 256) break;
+    const int64_t each = ((int64_t)length + 128 * s - 1) / (128 * s) * 128;
+    if (s > 1 && (each < 256 || s > room)) break;
     // (One piece: also with eight waves, of which a compute unit holds one workgroup.
     // 24 sequences of up to 6 rows of 4 key heads of 64, a window of 4096: 23.5 us
     // with four, 18.2 us with eight, 18.3 us with sixteen.  A ring of three tiles
@@ -369,7 +372,7 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group) {
       }
     }
   }
-  if (p.splits > 1) p.splits = (b.max_kv_len + p.chunk - 1) / p.chunk;
+  if (p.splits > 1) p.splits = (length + p.chunk - 1) / p.chunk;
   return p;
 }
 
@@ -416,14 +419,15 @@ hipError_t launch_attention(const AttentionArgs& a, const Plan& p, hipStream_t s
 size_t kv_attention_workspace_bytes(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads) {
   if (b.seqs == 0 || b.rows == 0) return 0;
   const int group = q_heads / c.heads;
-  const Plan p = plan(c, b, group);
+  const Plan p = plan(c, b, group, 0, kAnyRoom);
   if (p.splits == 1) return 0;
   return (size_t)(host_tiles(b, group, 16 * p.tiles) * c.heads * p.splits * 16 * p.tiles) * (c.dim + 2) * sizeof(float);
 }
 
 hipError_t launch_kv_attention(const AttentionArgs& args, void* workspace, hipStream_t stream) {
   AttentionArgs a = args;
-  const Plan p = plan(a.cache, a.batch, a.group);
+  Plan p = plan(a.cache, a.batch, a.group, 0, kAnyRoom);
+  if (a.window > 0) p = plan(a.cache, a.batch, a.group, a.window, p.splits);
   a.chunk = p.chunk;
   a.splits = p.splits;
   a.part = static_cast<float*>(workspace);

@@ -64,15 +64,18 @@ __device__ __forceinline__ int piece_of(int x, int number, int splits) {
   return (x + number + (number >> 2) + (number >> 5)) % splits;
 }
 
-// Pieces [p0, p1) of a tile hold tokens that its rows see; a tile that sees
-// nothing has piece 0.
-__device__ __forceinline__ void pieces_of(const AttentionArgs& a, const Tile& t, int& p0, int& p1) {
-  p0 = 0;
-  p1 = 1;
-  if (t.begin < t.end) {
-    p0 = min(t.begin / a.chunk, a.splits - 1);
-    p1 = min((t.end - 1) / a.chunk, a.splits - 1) + 1;
-  }
+// A tile's pieces of a.chunk tokens each, from the first token that one of its rows
+// sees (its step of 64) on; the last one takes what is left.  A tile that sees
+// nothing has one.
+__device__ __forceinline__ int pieces_of(const AttentionArgs& a, const Tile& t) {
+  return t.begin < t.end ? min((t.end - 1 - (t.begin & ~63)) / a.chunk, a.splits - 1) + 1 : 1;
+}
+
+// Tokens [begin, end) of a tile's piece.
+__device__ __forceinline__ void piece_tokens(const AttentionArgs& a, const Tile& t, int piece, int& begin, int& end) {
+  const int from = (t.begin & ~63) + piece * a.chunk;
+  begin = max(t.begin, from);
+  end = piece + 1 < a.splits ? min(t.end, from + a.chunk) : t.end;
 }
 
 __device__ __forceinline__ int64_t tiles_of(const KvBatchArgs& a, int group, int rows) {

@@ -195,12 +195,10 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_tile_kerne
   int begin = t.begin, end = t.end;
   bool whole = true;             // this piece is all that the rows see
   if (kSplit) {
-    int p0, p1;
-    pieces_of(a, t, p0, p1);
-    if (piece < p0 || piece >= p1) return;
-    whole = p1 - p0 == 1;
-    begin = max(begin, piece * a.chunk);
-    if (piece + 1 < a.splits) end = min(end, (piece + 1) * a.chunk);
+    const int pieces = pieces_of(a, t);
+    if (piece >= pieces) return;
+    whole = pieces == 1;
+    piece_tokens(a, t, piece, begin, end);
   }
 
   const int first = 32 * wave, n = min(32, t.n - first);      // this wave's rows (none: it only loads)

@@ -156,6 +156,14 @@ def test_tiles_of_128_rows_in_pieces(dim, hkv, group, lens, counts):
     _run(dim, 64, hkv, group, lens, counts, seed=7, heads=[hkv // 2], causal=False, powers=False)
 
 
+@pytest.mark.parametrize("dim,group,window", [(128, 8, 3000), (64, 2, 1025), (256, 3, 4096), (128, 40, 700), (128, 5, 1)])
+@pytest.mark.parametrize("new", [1, 7])
+def test_windows_of_long_sequences_in_pieces(dim, group, window, new):
+    """Pieces begin where a tile's window does; its tokens next to the borders."""
+    assert _run(dim, 32, 2, group, [40000, 5001, window, window + 65], [new, new, 1, new], window=window, seed=8, every=range) > 0
+    _run(dim, 32, 2, group, [20011, 9000], [new, new], causal=False, window=window, seed=9, every=range, max_len=20000)
+
+
 def test_tiles_of_128_rows_with_pages_outside_the_cache():
     _run(128, 16, 32, 8, [300, 70, 700, 257], [64, 70, 65, 57], cut=[(0, 3), (1, 0), (1, 1), (1, 2), (1, 3), (1, 4), (2, 43)])
     _run(256, 32, 32, 2, [300, 240], [75, 60], cut=[(0, 9), (1, 0)], causal=False)
