@@ -312,7 +312,9 @@ struct Plan {
 // 512 63 and 37 us.  Heads of 256: 8 of 128 261 and 172 us.
 // Pieces: the number of them for which an estimate of the time is least, of a
 // step whose sequences all have the largest length and of one that has 0.55 times
-// as many workgroups (lengths of all sizes), together.
+// as many workgroups (lengths of all sizes), together.  (Its figures are those that
+// fit measured times best; 8 sequences of 30000 tokens, a window of 3000, 4 key
+// heads of 128: 18.0 us in one piece with eight waves, 12.4 us in six.)
 // A window bounds what a tile sees, and a step's workspace is sized without it:
 // with one, only numbers of pieces that fit `room` partial results are looked at.
 Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group, int window, int64_t room) {
@@ -328,7 +330,12 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group, int window, int
                                  : (c.dim == 128 ? 3 : 4);
   // Tokens that a workgroup takes in a microsecond alone, and that all of them
   // take together (5.5 TB/s of memory; 0.9 PFLOP/s of products).
-  const double alone = p.tiles == 8 ? 35.0 * 128 / c.dim : 160.0 * 128 / c.dim;
+  const double alone = p.tiles == 8   ? 35.0 * 128 / c.dim
+                       : p.tiles == 2 ? 160.0 * 128 / c.dim
+                       : c.dim == 64  ? 180.0
+                       : c.dim == 128 ? 150.0
+                                      : 100.0;
+  const double join = p.tiles == 1 ? 5.0 : 6.0;
   // (The tiles of one sequence share its keys and values.)
   const double together = p.tiles == 8 ? 0.9e9 / (512.0 * c.dim)
                                        : 5.5e6 / (2.0 * c.dim) * (each_seq < 2.4 ? (double)each_seq : 2.4);
@@ -356,13 +363,13 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group, int window, int
       const double slots = 256.0 * (waves > 4 ? 1 : fit);
       double time = 0.0;
       for (const double share : {1.0, 0.55}) {
-        const double n = share * (double)(work * s), longest = (double)each / (alone * waves / 4);
+        const double n = share * (double)(work * s), longest = (double)each / (waves > 4 ? 1.3 * alone : alone);
         const double all = n * (double)each / together;
         const double work_time = all > longest ? all : longest;
-        time += waves > 4 ? 0.85 * work_time + 1.5 * n / slots : work_time;
+        time += waves > 4 ? 0.75 * work_time + 2.5 * n / slots : work_time;
         if (n > slots)                                             // the last ones; beginnings and ends
           time += (p.tiles == 8 ? 0.25 : 0.5) * longest + 6.0 * 256.0 * n / (slots * slots);
-        if (s > 1) time += 0.05 * all + 6.0 + n * part;                           // the join
+        if (s > 1) time += 0.05 * all + join + n * part;                           // the join
       }
       if ((s == 1 && waves == 4) || time < best) {
         best = time;
