@@ -192,7 +192,7 @@ int nvfp4_kv_attention(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
   a.scale = (float)scale;
   a.causal = causal;
   a.window = (int)(window < kMaxTokens ? window : kMaxTokens);
-  const hipError_t e = nvfp4::launch_kv_attention(a, workspace, static_cast<hipStream_t>(stream));
+  const hipError_t e = nvfp4::launch_kv_attention(a, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? NVFP4_OK : nvfp4::fail_hip(e);
 }
 

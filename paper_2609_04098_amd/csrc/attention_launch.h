@@ -75,7 +75,7 @@ size_t kv_attention_workspace_bytes(const KvCacheArgs& cache, const KvBatchArgs&
 // The attention of many rows in tiles of 128 packed rows (kv_attention_tile.hip;
 // called by launch_kv_attention, which joins the pieces).
 hipError_t launch_kv_attention_tile(const AttentionArgs& a, int64_t tiles, hipStream_t stream);
-hipError_t launch_kv_attention(const AttentionArgs& a, void* workspace, hipStream_t stream);
+hipError_t launch_kv_attention(const AttentionArgs& a, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 // attention_api.cpp and api.cpp share the device check and the record of the
 // last HIP error (api.cpp).

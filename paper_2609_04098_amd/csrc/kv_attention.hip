@@ -423,18 +423,22 @@ hipError_t launch_attention(const AttentionArgs& a, const Plan& p, hipStream_t s
 
 }  // namespace
 
-size_t kv_attention_workspace_bytes(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads) {
-  if (b.seqs == 0 || b.rows == 0) return 0;
-  const int group = q_heads / c.heads;
-  const Plan p = plan(c, b, group, 0, kAnyRoom);
+static size_t part_bytes(const KvCacheArgs& c, const KvBatchArgs& b, int group, const Plan& p) {
   if (p.splits == 1) return 0;
   return (size_t)(host_tiles(b, group, 16 * p.tiles) * c.heads * p.splits * 16 * p.tiles) * (c.dim + 2) * sizeof(float);
 }
 
-hipError_t launch_kv_attention(const AttentionArgs& args, void* workspace, hipStream_t stream) {
+size_t kv_attention_workspace_bytes(const KvCacheArgs& c, const KvBatchArgs& b, int q_heads) {
+  if (b.seqs == 0 || b.rows == 0) return 0;
+  const int group = q_heads / c.heads;
+  return part_bytes(c, b, group, plan(c, b, group, 0, kAnyRoom));
+}
+
+hipError_t launch_kv_attention(const AttentionArgs& args, void* workspace, size_t workspace_bytes, hipStream_t stream) {
   AttentionArgs a = args;
   Plan p = plan(a.cache, a.batch, a.group, 0, kAnyRoom);
   if (a.window > 0) p = plan(a.cache, a.batch, a.group, a.window, p.splits);
+  if (part_bytes(a.cache, a.batch, a.group, p) > workspace_bytes) return hipErrorInvalidValue;      // (by the plan, never)
   a.chunk = p.chunk;
   a.splits = p.splits;
   a.part = static_cast<float*>(workspace);

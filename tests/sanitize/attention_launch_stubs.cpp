@@ -11,6 +11,6 @@ hipError_t launch_kv_append(const AppendArgs&, hipStream_t) { return hipErrorNoD
 size_t kv_attention_workspace_bytes(const KvCacheArgs&, const KvBatchArgs& b, int) {
   return b.max_kv_len > 1024 ? 4096 : 0;
 }
-hipError_t launch_kv_attention(const AttentionArgs&, void*, hipStream_t) { return hipErrorNoDevice; }
+hipError_t launch_kv_attention(const AttentionArgs&, void*, size_t, hipStream_t) { return hipErrorNoDevice; }
 
 }  // namespace nvfp4
