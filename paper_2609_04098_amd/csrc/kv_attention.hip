@@ -304,12 +304,13 @@ struct Plan {
 };
 
 // Row tiles: a workgroup takes 16 rows where an average sequence has no more.  It
-// takes 128 where sequences have over 64 and that gives every compute unit two
-// workgroups (heads of 256, whose smaller tiles go through a ring in LDS, one
-// workgroup a compute unit: every other one), else 32.  With 4 key heads of 128
-// and 8 query heads each, 2000 to 4000 tokens: 8 sequences of 128 new ones 96 us
-// in tiles of 32 and 125 us in tiles of 128, 2 of 256 31 and 40 us; 6 of 512 among
-// 512 63 and 37 us.  Heads of 256: 8 of 128 261 and 172 us.
+// takes 128 where sequences have over 64 and there are enough rows to fill the
+// compute units with such workgroups (heads of 256, whose smaller tiles go through a
+// ring in LDS, one workgroup a compute unit: few), more of them for long sequences,
+// where a workgroup that is alone takes long; else 32.  Full tiles times key heads, and
+// the times in tiles of 32 and of 128 rows: heads of 128, 400 of 1500 tokens 74 and 62
+// us, 503 of 447 39 and 22 us, 375 of 3000 104 and 107 us, 192 of 967 29 and 31 us;
+// heads of 256, 81 of 856 40 and 36 us, 31 of 8000 98 and 59 us, 62 of 1000 27 and 31.
 // Pieces: the number of them for which an estimate of the time is least, of a
 // step whose sequences all have the largest length and of one that has 0.55 times
 // as many workgroups (lengths of all sizes), together.  (Its figures are those that
@@ -321,7 +322,9 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group, int window, int
   Plan p;
   const int64_t seqs = b.seqs > 0 ? b.seqs : 1, rows = ((int64_t)b.rows * group + seqs - 1) / seqs;
   const auto of_rows = [&](int tile) { return (rows + tile - 1) / tile; };
-  p.tiles = rows <= 16 ? 1 : rows > 64 && of_rows(128) * seqs * c.heads >= (c.dim == 256 ? 128 : 512) ? 8 : 2;
+  const double full = (double)b.rows * group * c.heads / 128.0;
+  const double enough = c.dim == 256 ? (b.max_kv_len < 2000 ? 64.0 : 24.0) : (b.max_kv_len < 1600 ? 330.0 : 480.0);
+  p.tiles = rows <= 16 ? 1 : rows > 64 && full >= enough ? 8 : 2;
   const int64_t each_seq = of_rows(16 * p.tiles), work = each_seq * seqs * c.heads;
   // Workgroups of four waves that fit 256 compute units (registers, LDS).
   const int fit = p.tiles == 8   ? (c.dim == 256 ? 2 : c.dim == 128 ? 3 : 4)
