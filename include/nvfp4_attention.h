@@ -126,7 +126,8 @@ int nvfp4_qk_norm_rope(const void* q, int64_t ldq, int64_t q_heads, const void* 
  * Appends a step's keys and values to the cache; keys are normed (k_gamma not
  * NULL) and rotated (rot_dim > 0) on the way, as by nvfp4_qk_norm_rope but
  * without the rounding to bf16: each code is one rounding (to nearest, ties to
- * even) of the value over the scale, computed in binary64.
+ * even) of the value over the scale, computed in binary64 (with a scale that is
+ * no power of two, of the value cut to binary32, over the scale in binary64).
  *   NVFP4_DYNAMIC: a page and head's scale is the smallest power of two s >=
  *     2^-100 with |value| <= 448 s for all its tokens.  A call that writes slot
  *     0 starts the page anew; one that writes behind tokens that the page

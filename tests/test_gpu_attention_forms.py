@@ -252,3 +252,77 @@ def test_two_captured_steps_share_a_workspace():
             want = torch.full_like(y, 7.0)
             A.attention(x, cache, A.Batch(table, _i32(l), _i32(c), rows=8, max_len=width * page), out=want)
             assert torch.equal(y, want), step
+
+
+@pytest.mark.parametrize("dim,page,heads,rot,interleaved", [
+    (128, 32, 3, 48, False), (128, 16, 5, 80, True), (64, 128, 2, 16, False), (256, 16, 2, 240, False),
+    (256, 64, 3, 112, True), (128, 128, 2, 96, False), (64, 16, 9, 64, True)])
+@pytest.mark.parametrize("static", [None, 0.25])
+def test_append_of_many_rows_at_given_positions(dim, page, heads, rot, interleaved, static):
+    """Positions that jump, run on, repeat and fall within a page; odd rotations;
+    codes of normed keys are those of one rounding also with a static scale of a power of two."""
+    log("append at positions %s" % ((dim, page, heads, rot, interleaved, static),))
+    rng = np.random.RandomState(dim + page + rot)
+    gen = torch.Generator("cuda").manual_seed(dim + page + rot)
+    lens, counts = [3 * page + 5, 2 * page, page + 1], [2 * page + 9, 2 * page, page - 3]
+    rows, width = sum(counts), 4
+    table = torch.randperm(3 * width, generator=gen, device="cuda").view(3, width)
+    cache = _cache(gen, 3 * width, heads, page, dim)
+    if static:
+        cache.k_scale.fill_(static), cache.v_scale.fill_(static)
+    pos = np.arange(rows) + 1000
+    jump = rng.rand(rows) < 0.2
+    pos[jump] = rng.randint(0, 2 ** 24, jump.sum())
+    pos[5] = pos[4]
+    pos[8:11] = [2 ** 24, 2 ** 24 + 1, 0]
+    freq = (1e5 ** (-torch.arange(rot // 2).double() / (rot // 2))).float()
+    gamma = (1 + 0.2 * torch.randn(dim, generator=gen, device="cuda")).to(torch.bfloat16)
+    k, v = (torch.randn(rows, heads, dim, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    want = OA.Cache.from_bytes(cache.k.cpu().numpy(), cache.v.cpu().numpy(), cache.k_scale.cpu().double().numpy(),
+                               cache.v_scale.cpu().double().numpy(), page)
+    want.append(table.cpu().numpy(), [l - c for l, c in zip(lens, counts)], counts,
+                OA.norm_rope(k.double().cpu().numpy(), gamma.double().cpu().numpy(), 1e-6, pos, freq.numpy(), interleaved),
+                v.double().cpu().numpy(), static=static is not None)
+    A.kv_append(cache, A.Batch(table.int(), _i32(lens), _i32(_cu(counts)), rows=rows), k, v, gamma, 1e-6,
+                A.Rope(freq.cuda(), interleaved), _i32(pos.tolist()), static=static is not None)
+    _same_cache(cache, want)
+
+
+@pytest.mark.parametrize("rows_each", [2, 30])
+def test_append_static_scales_that_are_no_powers_of_two(rows_each):
+    gen = torch.Generator("cuda").manual_seed(rows_each)
+    cache = _cache(gen, 8, 2, 32, 128, powers=False)
+    cache.k_scale.mul_(20), cache.v_scale.mul_(20)
+    want = OA.Cache.from_bytes(cache.k.cpu().numpy(), cache.v.cpu().numpy(), cache.k_scale.cpu().double().numpy(),
+                               cache.v_scale.cpu().double().numpy(), 32)
+    table = torch.arange(8, device="cuda").view(2, 4)
+    k, v = ((20 * torch.randn(2 * rows_each, 2, 128, generator=gen, device="cuda")).to(torch.bfloat16) for _ in range(2))
+    want.append(table.cpu().numpy(), [20, 40], [rows_each] * 2, k.double().cpu().numpy(), v.double().cpu().numpy(), static=True)
+    A.kv_append(cache, A.Batch(table.int(), _i32([20 + rows_each, 40 + rows_each]), _i32([0, rows_each, 2 * rows_each]),
+                               rows=2 * rows_each), k, v, static=True)
+    _same_cache(cache, want)
+
+
+def test_calls_on_another_stream_than_the_tensors_own():
+    """The three calls handed a side stream, on tensors made on the current one."""
+    gen = torch.Generator("cuda").manual_seed(1)
+    cache = _cache(gen, 40, 2, 16, 64)
+    twin = A.KVCache(cache.k.clone(), cache.v.clone(), cache.k_scale.clone(), cache.v_scale.clone(), 16)
+    table, lens = torch.arange(40, device="cuda").view(2, 20).int(), _i32([300, 17])
+    x = [torch.randn(2, h, 64, generator=gen, device="cuda").to(torch.bfloat16) for h in (8, 2, 2)]
+    rope, pos = A.Rope(torch.full((32,), 0.1, device="cuda")), _i32([299, 16])
+    side = torch.cuda.Stream()
+
+    def run(c, stream):
+        b = A.Batch(table, lens)
+        q, k = A.qk_norm_rope(x[0], x[1], pos, rope, stream=stream)
+        A.kv_append(c, b, k, x[2], stream=stream)
+        return (q, k) + A.attention(q, c, b, return_lse=True, stream=stream)
+
+    want = run(cache, None)
+    torch.cuda.synchronize()
+    for stream in (side, side.cuda_stream):
+        got = run(twin, stream)
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert torch.equal(twin.k, cache.k) and torch.equal(twin.v, cache.v)
