@@ -115,10 +115,6 @@ __device__ __forceinline__ uint32_t without_nan(uint32_t x) {
   return x & ~((hit >> 7) * 255u);
 }
 
-// The larger of two (without the quieting of NaN in front that fmaxf costs; of a
-// NaN and a number, the number).
-__device__ __forceinline__ float greater(float a, float b) { return __builtin_amdgcn_fmed3f(a, b, __builtin_inff()); }
-
 // Maximum and sum over the four lanes lane % 16 + 16 i.
 __device__ __forceinline__ float over_quarters_max(float x) {
   const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -133,7 +129,6 @@ __device__ __forceinline__ float over_quarters_sum(float x) {
   const auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(y), __float_as_uint(y), false, false);
   return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
-
 
 // Page and scales of the groups of 16 tokens that a wave meets next: its lane
 // holds those of the group at `token`, page -1 where that is past the end or
