@@ -13,9 +13,11 @@
 // lane: 16000 tokens of 8 heads of 128 take 28 us, 18 of them issue, where the bytes
 // would take 19.  (Pages of 16384 elements with 64 elements a lane, four waves to a
 // compute unit: 74 us; with 16 a lane 31.)
-// Few rows (under 8 for a sequence): one wave for each touched page, keys or
-// values, and as many heads as it has lanes for (512 / D); the codes are stored
-// from registers.
+// Few rows (under 5 for a sequence): four waves for each touched page, keys or
+// values, and as many heads as a wave has lanes for (512 / D), a token at a time
+// each; the codes are stored from registers.  96 sequences, 8 heads of 128, of 1, 4
+// and 16 tokens: 6.8, 7.0 and (30 sequences) 9.1 us, in the other form 9.2, 9.5 and
+// 8.2; 100 of one and one of 500: 18.4 and 12.5 (with one wave for a page 54).
 //
 // Keys are computed in binary64: an 8-bit rounding turns the last bit of a
 // binary32 value that is next to a border into a step of 6 to 12 %, and binary64
@@ -487,17 +489,22 @@ __global__ __launch_bounds__(kThreads, 4) void kv_append_pages_kernel(AppendArgs
   }
 }
 
-// Few rows: one wave for a page, keys or values, and 512 / D heads; its lanes
-// hold one token of each head at a time.
+// Few rows: a workgroup for a page, keys or values, and 512 / D heads; a wave's lanes
+// hold one token of each head at a time, and its four waves take turns with the
+// tokens (a page may have all that a sequence among many short ones has).
 template <int D, bool kDynamic>
-__global__ __launch_bounds__(64) void kv_append_tokens_kernel(AppendArgs a) {
-  constexpr int kLanes = D / 8, kHeads = 64 / kLanes;
-  __shared__ double2 turn[D / 2];
+__global__ __launch_bounds__(256) void kv_append_tokens_kernel(AppendArgs a) {
+  constexpr int kLanes = D / 8, kHeads = 64 / kLanes, kWaves = 4;
+  __shared__ double2 turns[kWaves][D / 2];
+  __shared__ float tops[kWaves][64];
   const int groups = (a.cache.heads + kHeads - 1) / kHeads;
-  const int kind = blockIdx.x & 1, lane = threadIdx.x;
+  const int kind = blockIdx.x & 1, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h0 = (int)(blockIdx.x >> 1) % groups * kHeads;
   Touch t;
   if (!find_touch(a, (int)(blockIdx.x >> 1) / groups, t)) return;
+  const int waves = min(t.n, kWaves);
+  if (wave >= waves) return;
+  double2* turn = turns[wave];
   const Treatment how = treatment<D>(a, kind);
   const bool live = h0 + lane / kLanes < a.cache.heads;
   const int h = min(h0 + lane / kLanes, a.cache.heads - 1);
@@ -521,37 +528,44 @@ __global__ __launch_bounds__(64) void kv_append_tokens_kernel(AppendArgs a) {
 
   float* scale_at = (kind ? a.cache.scale[1] : a.cache.scale[0]) + (int64_t)t.page * a.cache.scale_stride + h;
   const float held = kDynamic && t.slot0 == 0 ? 0.0f : *scale_at;
+  const int last = wave + (t.n - 1 - wave) / waves * waves;      // of this wave's tokens
   float v[8], scale = held;
   if (kDynamic) {
     float top = 0.0f;
-    for (int i = 0; i < t.n; ++i) {
+    for (int i = wave; i < t.n; i += waves) {
       treated(i, v);
       top = largest(v, top, false);
     }
 #pragma unroll
     for (int m = 1; m < kLanes; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+    if (waves > 1) {
+      tops[wave][lane] = top;
+      __syncthreads();
+      for (int w = 0; w < waves; ++w) top = fmaxf(top, tops[w][lane]);
+    }
     scale = fmaxf(held, page_scale(top));
   }
   uint8_t* out = (kind ? a.cache.kv[1] : a.cache.kv[0]) +
                  (int64_t)t.page * (kind ? a.cache.page_stride[1] : a.cache.page_stride[0]) +
                  (int64_t)h * a.cache.page_size * D;
-  if (live && scale > held && t.slot0 > 0) bring_along<D>(out, kind, t.slot0, held / scale, lane % kLanes, kLanes);
+  if (live && scale > held && t.slot0 > 0)
+    bring_along<D>(out, kind, t.slot0, held / scale, wave * kLanes + lane % kLanes, waves * kLanes);
   __syncthreads();      // (the held codes of pieces that new values share are written)
   const float inverse = 1.0f / scale;
-  for (int i = t.n - 1; i >= 0; --i) {      // (the last one's values are at hand)
-    if (!kDynamic || i != t.n - 1) treated(i, v);
+  for (int i = last; i >= 0; i -= waves) {      // (the last one's values are at hand)
+    if (!kDynamic || i != last) treated(i, v);
     const uint2 c = eight_codes<kDynamic>(v, scale, inverse);
     if (live) put_codes<D>(out, kind, t.slot0 + i, how.e0, c);
   }
-  if (kDynamic && live && lane % kLanes == 0) *scale_at = scale;
+  if (kDynamic && live && wave == 0 && lane % kLanes == 0) *scale_at = scale;
 }
 
 template <int D, bool kDynamic>
 static hipError_t launch(const AppendArgs& a, int64_t items, hipStream_t stream) {
-  if (a.batch.cu_rows == nullptr || a.batch.rows < 8 * (int64_t)a.batch.seqs) {
+  if (a.batch.cu_rows == nullptr || a.batch.rows < 5 * (int64_t)a.batch.seqs) {
     const int64_t blocks = 2 * items * ((a.cache.heads * D + 511) / 512);
     if (blocks >= (int64_t)1 << 31) return hipErrorInvalidValue;
-    kv_append_tokens_kernel<D, kDynamic><<<dim3((unsigned)blocks), 64, 0, stream>>>(a);
+    kv_append_tokens_kernel<D, kDynamic><<<dim3((unsigned)blocks), 256, 0, stream>>>(a);
     return hipGetLastError();
   }
   // Heads of a workgroup: as many as leave one round of workgroups on 256 compute

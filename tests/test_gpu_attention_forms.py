@@ -326,3 +326,27 @@ def test_calls_on_another_stream_than_the_tensors_own():
         side.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
         assert torch.equal(twin.k, cache.k) and torch.equal(twin.v, cache.v)
+
+
+@pytest.mark.parametrize("dim,page,singles,long", [(128, 32, 30, 70), (64, 128, 30, 90), (256, 16, 9, 30), (128, 16, 3, 100)])
+def test_append_of_a_prompt_among_single_tokens(dim, page, singles, long):
+    """Both sides of the rule that picks a form by the average; the prompt begins within a page."""
+    gen = torch.Generator("cuda").manual_seed(dim + page)
+    counts = [1] * singles + [long]
+    lens = [1 + 7 * i % 50 for i in range(singles)] + [long + 5]
+    width = -(-max(lens) // page)
+    n = singles + 1
+    cache = _cache(gen, n * width, 3, page, dim)
+    table = torch.randperm(n * width, generator=gen, device="cuda").view(n, width)
+    rows = sum(counts)
+    k, v = (torch.randn(rows, 3, dim, generator=gen, device="cuda").to(torch.bfloat16) for _ in range(2))
+    v[-long // 2:] *= 64                                            # the held codes are brought along
+    gamma, freq = torch.ones(dim, device="cuda").to(torch.bfloat16), (1e4 ** (-torch.arange(32).double() / 32)).float()
+    starts = [l - c for l, c in zip(lens, counts)]
+    pos = np.concatenate([np.arange(s, s + c) for s, c in zip(starts, counts)])
+    want = OA.Cache.from_bytes(cache.k.cpu().numpy(), cache.v.cpu().numpy(), cache.k_scale.cpu().double().numpy(),
+                               cache.v_scale.cpu().double().numpy(), page)
+    want.append(table.cpu().numpy(), starts, counts,
+                OA.norm_rope(k.double().cpu().numpy(), np.ones(dim), 1e-6, pos, freq.numpy(), False), v.double().cpu().numpy())
+    A.kv_append(cache, A.Batch(table.int(), _i32(lens), _i32(_cu(counts)), rows=rows), k, v, gamma, 1e-6, A.Rope(freq.cuda()))
+    _same_cache(cache, want)
