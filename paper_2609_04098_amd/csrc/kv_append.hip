@@ -341,19 +341,19 @@ __global__ __launch_bounds__(kThreads, 4) void kv_append_pages_kernel(AppendArgs
   Touch t;
   if (!find_touch(a, (int)blockIdx.x / parts, t)) return;
   const int h0 = (int)blockIdx.x % parts * heads_each, h1 = min(h0 + heads_each, a.cache.heads);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Treatment for_keys = treatment<D>(a, 0);
   const int e0 = for_keys.e0, last = t.slot0 + t.n;
   // The slot of this lane's token in pass p, so that the four tokens of a word of
-  // values are in lanes (or passes) that fours() joins; and the passes that hold some.
+  // values are in lanes (or passes) that fours() joins; and whether the wave has some.
   const auto slot = [&](int p) __attribute__((always_inline)) {
     const int g = lane / kLanes;
     return D == 256 ? p / 2 * 2 * kTokens + wave * 4 + p % 2 * 2 + g
                     : p * kTokens + wave * (64 / kLanes) + (D == 64 ? (g & 1) * 4 + (g >> 1) : g);
   };
   const auto holds = [&](int p) __attribute__((always_inline)) {
-    constexpr int kSpan = D == 256 ? 2 * kTokens : kTokens;
-    const int s0 = (D == 256 ? p / 2 : p) * kSpan;
+    constexpr int kSpan = D == 256 ? 4 : 64 / kLanes;
+    const int s0 = (D == 256 ? p / 2 * 2 : p) * kTokens + wave * kSpan;
     return s0 < last && s0 + kSpan > t.slot0;
   };
 
