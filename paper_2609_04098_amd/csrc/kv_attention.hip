@@ -22,35 +22,35 @@ struct TileCodes {
 };
 
 template <int D>
-__device__ __forceinline__ void load_tile(const AttentionArgs& a, int h, int token, int page0, int page1, int lane,
-                                          TileCodes<D>& t) {
+__device__ __forceinline__ void load_codes(const AttentionArgs& a, int kind, int h, int token, int page0, int page1,
+                                           int lane, u32x4 (&to)[2][D / 64]) {
   const int mask = a.cache.page_size - 1;
   const int64_t head = (int64_t)h * a.cache.page_size * D;
 #pragma unroll
   for (int g = 0; g < 2; ++g) {
     const int page = g ? page1 : page0, slot = (token + 16 * g) & mask;
-    const uint8_t* k = a.cache.kv[0] + (int64_t)max(page, 0) * a.cache.page_stride[0] + head + slot * D;
-    const uint8_t* v = a.cache.kv[1] + (int64_t)max(page, 0) * a.cache.page_stride[1] + head + slot * D;
+    const uint8_t* from = a.cache.kv[kind] + (int64_t)max(page, 0) * a.cache.page_stride[kind] + head + slot * D;
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) {
-      t.k[g][c] = *reinterpret_cast<const u32x4*>(k + c * 1024 + lane * 16);
-      t.v[g][c] = *reinterpret_cast<const u32x4*>(v + c * 1024 + lane * 16);
-    }
+    for (int c = 0; c < D / 64; ++c) to[g][c] = *reinterpret_cast<const u32x4*>(from + c * 1024 + lane * 16);
   }
 }
 
-// Heads of 256: two tiles of codes would take 128 registers a lane, so they go
-// through a ring of two in LDS, of each wave's own.
+// Heads of 256 (kOne): two tiles of codes would take 128 registers a lane; the next
+// tile's keys are loaded where this one's have been read, and so the values.  (Through
+// a ring of two tiles in LDS, one workgroup a compute unit: 40 sequences of up to 2500
+// tokens, 3 key heads, 32 us; so 25.)  A piece's workgroup has a compute unit to
+// itself all the same: those that short sequences leave empty make room for others
+// then, and two long ones do not share a unit (16 of up to 32768, 4 key heads, in
+// four pieces: 105 us; two to a unit 173).
 template <int D, int kTiles, int kWaves, bool kSplit>
-__global__ __launch_bounds__(kWaves * 64, D == 256 ? 1 : kTiles == 1 ? 3 : 2) void
+__global__ __launch_bounds__(kWaves * 64, D == 256 ? (kTiles == 1 && !kSplit ? 2 : 1) : (kTiles == 1 ? 3 : 2)) void
 kv_attention_rows_kernel(AttentionArgs a) {
   constexpr int kRows = 16 * kTiles, kThreads = kWaves * 64;
   constexpr int kPart = kWaves > 4 ? 64 : (D > 128 ? 128 : D);            // elements of a row that are joined at a time
-  constexpr bool kRing = D == 256;
-  constexpr int kLoads = 4 * (D / 64);                                    // of a tile into the ring
-  __shared__ union {
+  constexpr bool kOne = D == 256;
+  __shared__ struct {
     float joined[kWaves][16][kPart + 4];
-    uint8_t ring[kRing ? kWaves : 1][2][2][2][kRing ? 16 * D : 16];       // [wave][stage][keys, values][group]
+    char alone[kOne && kTiles == 1 && kSplit ? 65536 : 1];      // (so that it is)
   } lds;
   __shared__ float2 stats[kWaves][kRows];
 
@@ -91,55 +91,49 @@ kv_attention_rows_kernel(AttentionArgs a) {
     if (++in_batch == 32) {
       pages = group_pages(a, t.b, h, (int64_t)token + step + (lane >> 1) * step + (lane & 1) * 16, end);
       in_batch = 0;
+      // (Waited for here, or the compiler would, and with them for the tile's values,
+      // in front of every tile.)
+      if (kOne) __builtin_amdgcn_s_waitcnt(wait_loads(0));
     }
   };
   bool there[2];
   float ks[2], vs[2];
-  if constexpr (kRing) {
-    const int mask = a.cache.page_size - 1;
-    const auto issue = [&](int at, int to) __attribute__((always_inline)) {
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const int page = __builtin_amdgcn_readlane(pages.page, 2 * in_batch + g);
-#pragma unroll
-        for (int kind = 0; kind < 2; ++kind)
-          stage_group<D>(a.cache, kind, page, (at + 16 * g) & mask, h, lane, lds.ring[wave][to][kind][g]);
-      }
-    };
-    int stage = 0;
-    if (token < end) issue(token, 0);
+  const auto load = [&](int kind, int at, u32x4(&to)[2][D / 64]) __attribute__((always_inline)) {
+    load_codes<D>(a, kind, h, at, __builtin_amdgcn_readlane(pages.page, 2 * in_batch),
+                  __builtin_amdgcn_readlane(pages.page, 2 * in_batch + 1), lane, to);
+  };
+  if constexpr (kOne) {
+    TileCodes<D> now;
+    // (No branch around the loads: behind the end they read a page that is there.)
+    load(0, token, now.k);
+    load(1, token, now.v);
     while (token < end) {
       scales(there, ks, vs);
-      __builtin_amdgcn_s_waitcnt(kWaitLds);      // the other stage has been read
-      if (token + step < end) {
-        issue(token + step, stage ^ 1);
-        __builtin_amdgcn_s_waitcnt(wait_loads(kLoads));
-      } else {
-        __builtin_amdgcn_s_waitcnt(wait_loads(0));
-      }
-      const uint8_t *k = lds.ring[wave][stage][0][0] + lane * 16, *v = lds.ring[wave][stage][1][0] + lane * 16;
       rows.pass(
-          a, token, there[0], there[1], ks, vs, lane,
-          [&](int g, int c) { return *reinterpret_cast<const u32x4*>(k + g * 16 * D + c * 1024); },
-          [&](int g, int c) { return *reinterpret_cast<const u32x4*>(v + g * 16 * D + c * 1024); });
-      stage ^= 1;
+          a, token, there[0], there[1], ks, vs, lane, [&](int g, int c) { return now.k[g][c]; },
+          [&](int g, int c) { return now.v[g][c]; },
+          [&]() __attribute__((always_inline)) {
+            load(0, token + step, now.k);
+          },
+          [&]() __attribute__((always_inline)) {
+            load(1, token + step, now.v);
+          });
       token += step;
     }
-    __syncthreads();      // (the ring's memory joins the results)
   } else {
     TileCodes<D> even, odd;
-    const auto load = [&](int at, TileCodes<D>& to) __attribute__((always_inline)) {
-      load_tile<D>(a, h, at, __builtin_amdgcn_readlane(pages.page, 2 * in_batch),
-                   __builtin_amdgcn_readlane(pages.page, 2 * in_batch + 1), lane, to);
+    const auto load_tile = [&](int at, TileCodes<D>& to) __attribute__((always_inline)) {
+      load(0, at, to.k);
+      load(1, at, to.v);
     };
     const auto pass = [&](TileCodes<D>& now, TileCodes<D>& next) __attribute__((always_inline)) {
       scales(there, ks, vs);
-      if (token + step < end) load(token + step, next);
+      if (token + step < end) load_tile(token + step, next);
       rows.pass(a, token, there[0], there[1], ks, vs, lane, [&](int g, int c) { return now.k[g][c]; },
-                [&](int g, int c) { return now.v[g][c]; });
+                [&](int g, int c) { return now.v[g][c]; }, []() {}, []() {});
       token += step;
     };
-    if (token < end) load(token, even);
+    if (token < end) load_tile(token, even);
     while (token < end) {
       pass(even, odd);
       if (token >= end) break;
@@ -305,8 +299,8 @@ struct Plan {
 
 // Row tiles: a workgroup takes 16 rows where an average sequence has no more.  It
 // takes 128 where sequences have over 64 and there are enough rows to fill the
-// compute units with such workgroups (heads of 256, whose smaller tiles go through a
-// ring in LDS, one workgroup a compute unit: few), more of them for long sequences,
+// compute units with such workgroups (heads of 256, whose smaller tiles have a compute
+// unit's registers to themselves: few), more of them for long sequences,
 // where a workgroup that is alone takes long; else 32.  Full tiles times key heads, and
 // the times in tiles of 32 and of 128 rows: heads of 128, 400 of 1500 tokens 74 and 62
 // us, 503 of 447 39 and 22 us, 375 of 3000 104 and 107 us, 192 of 967 29 and 31 us;
@@ -327,18 +321,21 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group, int window, int
   p.tiles = rows <= 16 ? 1 : rows > 64 && full >= enough ? 8 : 2;
   const int64_t each_seq = of_rows(16 * p.tiles), work = each_seq * seqs * c.heads;
   // Workgroups of four waves that fit 256 compute units (registers, LDS).
-  const int fit = p.tiles == 8   ? (c.dim == 256 ? 2 : c.dim == 128 ? 3 : 4)
-                  : c.dim == 256 ? 1
-                  : p.tiles == 2 ? (c.dim == 128 ? 2 : 3)
-                                 : (c.dim == 128 ? 3 : 4);
+  const auto fit = [&](int s) {
+    return p.tiles == 8   ? (c.dim == 256 ? 2 : c.dim == 128 ? 3 : 4)
+                  : p.tiles == 2 ? (c.dim == 256 ? 1 : c.dim == 128 ? 2 : 3)
+                                 : (c.dim == 256 ? (s == 1 ? 2 : 1) : c.dim == 128 ? 3 : 4);
+  };
   // Tokens that a workgroup takes in a microsecond alone, and that all of them
   // take together (5.5 TB/s of memory; 0.9 PFLOP/s of products).
   const double alone = p.tiles == 8   ? 35.0 * 128 / c.dim
                        : p.tiles == 2 ? 160.0 * 128 / c.dim
                        : c.dim == 64  ? 180.0
                        : c.dim == 128 ? 150.0
-                                      : 100.0;
-  const double join = p.tiles == 1 ? 5.0 : 6.0;
+                                      : 80.0;
+  const double join = p.tiles != 1 ? 6.0 : c.dim == 256 ? 2.0 : 5.0;
+  // Eight waves: their rate, and their later start where there are many.
+  const double eight = c.dim == 256 ? 1.1 : 1.3, start = c.dim == 256 ? 8.0 : 2.5;
   // (The tiles of one sequence share its keys and values.)
   const double together = p.tiles == 8 ? 0.9e9 / (512.0 * c.dim)
                                        : 5.5e6 / (2.0 * c.dim) * (each_seq < 2.4 ? (double)each_seq : 2.4);
@@ -362,14 +359,14 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group, int window, int
     // 30 sequences of 8 key heads of 128, 400 tokens: 8.0 us with four, 11.1 us with
     // eight; and have twice the loads in flight: 32 of 3000, 45.2 and 38.1 us.)
     for (const int waves : {4, 8}) {
-      if (waves > 4 && (s > 1 || p.tiles != 1 || c.dim == 256)) continue;
-      const double slots = 256.0 * (waves > 4 ? 1 : fit);
+      if (waves > 4 && (s > 1 || p.tiles != 1)) continue;
+      const double slots = 256.0 * (waves > 4 ? 1 : fit(s));
       double time = 0.0;
       for (const double share : {1.0, 0.55}) {
-        const double n = share * (double)(work * s), longest = (double)each / (waves > 4 ? 1.3 * alone : alone);
+        const double n = share * (double)(work * s), longest = (double)each / (waves > 4 ? eight * alone : alone);
         const double all = n * (double)each / together;
         const double work_time = all > longest ? all : longest;
-        time += waves > 4 ? 0.75 * work_time + 2.5 * n / slots : work_time;
+        time += waves > 4 ? 0.75 * work_time + start * n / slots : work_time;
         if (n > slots)                                             // the last ones; beginnings and ends
           time += (p.tiles == 8 ? 0.25 : 0.5) * longest + 6.0 * 256.0 * n / (slots * slots);
         if (s > 1) time += 0.05 * all + join + n * part;                           // the join
@@ -400,7 +397,7 @@ template <int D, int kTiles, int kWaves>
 hipError_t launch_rows(const AttentionArgs& a, int64_t work, hipStream_t stream) {
   if constexpr (kWaves == 4) {      // (eight waves take one piece)
     if (a.splits > 1) {
-      kv_attention_rows_kernel<D, kTiles, 4, true><<<dim3((unsigned)(work * a.splits)), 256, 0, stream>>>(a);
+      kv_attention_rows_kernel<D, kTiles, kWaves, true><<<dim3((unsigned)(work * a.splits)), kWaves * 64, 0, stream>>>(a);
       const hipError_t e = hipGetLastError();
       return e != hipSuccess ? e : launch_join<D, kTiles>(a, work, stream);
     }
@@ -418,9 +415,7 @@ hipError_t launch_attention(const AttentionArgs& a, const Plan& p, hipStream_t s
     return e != hipSuccess ? e : launch_join<D, 8>(a, work, stream);
   }
   if (p.tiles == 2) return launch_rows<D, 2, 4>(a, work, stream);
-  if constexpr (D < 256) {
-    if (p.waves == 8) return launch_rows<D, 1, 8>(a, work, stream);
-  }
+  if (p.waves == 8) return launch_rows<D, 1, 8>(a, work, stream);
   return launch_rows<D, 1, 4>(a, work, stream);
 }
 

@@ -221,9 +221,11 @@ struct RowTiles {
   // Tokens token .. token + 31: the codes of keys(g, c) and values(g, c) are
   // those of group g and elements 64 c .. 64 c + 63; ks holds the key scales
   // times |scale|, vs the value scales; there: both pages are in the cache.
-  template <typename Keys, typename Values>
+  // keys_done, values_done: called where the codes have been read.
+  template <typename Keys, typename Values, typename KeysDone, typename ValuesDone>
   __device__ __forceinline__ void pass(const AttentionArgs& a, int token, bool there0, bool there1, const float (&ks)[2],
-                                       const float (&vs)[2], int lane, Keys keys, Values values) {
+                                       const float (&vs)[2], int lane, Keys keys, Values values, KeysDone keys_done,
+                                       ValuesDone values_done) {
     f32x4 s[kTiles][2];
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
@@ -240,6 +242,7 @@ struct RowTiles {
           s[i][g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, q[i][2 * c + 1], s[i][g], 0, 0, 0);
       }
     }
+    keys_done();
     const bool whole = token >= all0 && token + kTileTokens <= all1 && there0 && there1;
     if (!whole) {
 #pragma unroll
@@ -338,6 +341,7 @@ struct RowTiles {
           o[i][4 * c + j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, p[i], o[i][4 * c + j], 0, 0, 0);
       }
     }
+    values_done();
   }
 };
 
