@@ -3,13 +3,12 @@
 //
 // A workgroup takes 16 or 32 packed rows of one sequence and key head; its
 // waves take turns with tiles of 32 tokens, and join their results in LDS at
-// the end.  Keys and values go from memory to registers, one tile ahead.  Long
-// sequences are divided further, into pieces for several workgroups, which a
-// second launch joins.
+// the end.  Keys and values go from memory to registers.  Long sequences are
+// divided further, into pieces for several workgroups, which a second launch joins.
 //
-// Bound by HBM: the waves' loads of one tile ahead (8 KB a wave for heads of
-// 128) are what covers its latency.  128 sequences of up to 8000 tokens, 8 key
-// heads of 128: 192 us, 5.3 TB/s; one of 131072: 53 us with its join, 5.05 TB/s.
+// Bound by HBM where there are enough workgroups: 128 sequences of up to 8000
+// tokens, 8 key heads of 128: 192 us, 5.3 TB/s; one of 131072: 53 us with its join,
+// 5.05 TB/s.  Else by a wave's 250 instructions for a tile and its loads' latency.
 #include "kv_attention_device.h"
 
 namespace nvfp4 {
@@ -35,22 +34,27 @@ __device__ __forceinline__ void load_codes(const AttentionArgs& a, int kind, int
   }
 }
 
-// Heads of 256 (kOne): two tiles of codes would take 128 registers a lane; the next
-// tile's keys are loaded where this one's have been read, and so the values.  (Through
-// a ring of two tiles in LDS, one workgroup a compute unit: 40 sequences of up to 2500
-// tokens, 3 key heads, 32 us; so 25.)  A piece's workgroup has a compute unit to
-// itself all the same: those that short sequences leave empty make room for others
-// then, and two long ones do not share a unit (16 of up to 32768, 4 key heads, in
-// four pieces: 105 us; two to a unit 173).
+// The next tile's keys are loaded where this one's have been read, and so the values:
+// one tile's registers, and a load's latency to cover either.  (Two tiles' registers,
+// loaded a whole tile ahead: 60 sequences of 2000 tokens, 4 key heads of 64, 17.0 us;
+// so 13.7.  Heads of 256 through a ring of two tiles in LDS: 40 of up to 2500, 3 key
+// heads, 32 us; so 25.)
+// Workgroups of eight waves, and those that take pieces of heads of 256, have a
+// compute unit to themselves, though registers would let in two: those that short
+// sequences leave empty make room for others then, and two long ones do not share a
+// unit (16 sequences of up to 32768, 4 key heads of 256, in four pieces: 105 us, two
+// to a unit 173; 32 of 3000, 8 key heads of 128, eight waves: 38 and 48 us).
 template <int D, int kTiles, int kWaves, bool kSplit>
-__global__ __launch_bounds__(kWaves * 64, D == 256 ? (kTiles == 1 && !kSplit ? 2 : 1) : (kTiles == 1 ? 3 : 2)) void
+__global__ __launch_bounds__(kWaves * 64, kWaves > 4                ? 2
+                                                  : D == 256 && kSplit ? 1
+                                                  : D == 256           ? 3 - kTiles
+                                                                       : 4 - kTiles) void
 kv_attention_rows_kernel(AttentionArgs a) {
   constexpr int kRows = 16 * kTiles, kThreads = kWaves * 64;
   constexpr int kPart = kWaves > 4 ? 64 : (D > 128 ? 128 : D);            // elements of a row that are joined at a time
-  constexpr bool kOne = D == 256;
   __shared__ struct {
     float joined[kWaves][16][kPart + 4];
-    char alone[kOne && kTiles == 1 && kSplit ? 65536 : 1];      // (so that it is)
+    char alone[kWaves > 4 || (D == 256 && kTiles == 1 && kSplit) ? 65536 : 1];      // (so that they have)
   } lds;
   __shared__ float2 stats[kWaves][kRows];
 
@@ -93,7 +97,7 @@ kv_attention_rows_kernel(AttentionArgs a) {
       in_batch = 0;
       // (Waited for here, or the compiler would, and with them for the tile's values,
       // in front of every tile.)
-      if (kOne) __builtin_amdgcn_s_waitcnt(wait_loads(0));
+      __builtin_amdgcn_s_waitcnt(wait_loads(0));
     }
   };
   bool there[2];
@@ -102,43 +106,18 @@ kv_attention_rows_kernel(AttentionArgs a) {
     load_codes<D>(a, kind, h, at, __builtin_amdgcn_readlane(pages.page, 2 * in_batch),
                   __builtin_amdgcn_readlane(pages.page, 2 * in_batch + 1), lane, to);
   };
-  if constexpr (kOne) {
-    TileCodes<D> now;
-    // (No branch around the loads: behind the end they read a page that is there.)
-    load(0, token, now.k);
-    load(1, token, now.v);
-    while (token < end) {
-      scales(there, ks, vs);
-      rows.pass(
-          a, token, there[0], there[1], ks, vs, lane, [&](int g, int c) { return now.k[g][c]; },
-          [&](int g, int c) { return now.v[g][c]; },
-          [&]() __attribute__((always_inline)) {
-            load(0, token + step, now.k);
-          },
-          [&]() __attribute__((always_inline)) {
-            load(1, token + step, now.v);
-          });
-      token += step;
-    }
-  } else {
-    TileCodes<D> even, odd;
-    const auto load_tile = [&](int at, TileCodes<D>& to) __attribute__((always_inline)) {
-      load(0, at, to.k);
-      load(1, at, to.v);
-    };
-    const auto pass = [&](TileCodes<D>& now, TileCodes<D>& next) __attribute__((always_inline)) {
-      scales(there, ks, vs);
-      if (token + step < end) load_tile(token + step, next);
-      rows.pass(a, token, there[0], there[1], ks, vs, lane, [&](int g, int c) { return now.k[g][c]; },
-                [&](int g, int c) { return now.v[g][c]; }, []() {}, []() {});
-      token += step;
-    };
-    if (token < end) load_tile(token, even);
-    while (token < end) {
-      pass(even, odd);
-      if (token >= end) break;
-      pass(odd, even);
-    }
+  // (No branch around the loads, where the compiler would wait for whatever may be
+  // outstanding on one of its paths: behind the end they read a page that is there.)
+  TileCodes<D> now;
+  load(0, token, now.k);
+  load(1, token, now.v);
+  while (token < end) {
+    scales(there, ks, vs);
+    rows.pass(
+        a, token, there[0], there[1], ks, vs, lane, [&](int g, int c) { return now.k[g][c]; },
+        [&](int g, int c) { return now.v[g][c]; }, [&]() __attribute__((always_inline)) { load(0, token + step, now.k); },
+        [&]() __attribute__((always_inline)) { load(1, token + step, now.v); });
+    token += step;
   }
 
   // The waves' results, joined: Y = sum_w 2^(m_w - m) Y_w.
@@ -320,7 +299,7 @@ Plan plan(const KvCacheArgs& c, const KvBatchArgs& b, int group, int window, int
   const double enough = c.dim == 256 ? (b.max_kv_len < 2000 ? 64.0 : 24.0) : (b.max_kv_len < 1600 ? 330.0 : 480.0);
   p.tiles = rows <= 16 ? 1 : rows > 64 && full >= enough ? 8 : 2;
   const int64_t each_seq = of_rows(16 * p.tiles), work = each_seq * seqs * c.heads;
-  // Workgroups of four waves that fit 256 compute units (registers, LDS).
+  // Workgroups of four waves that the estimate counts on a compute unit at a time.
   const auto fit = [&](int s) {
     return p.tiles == 8   ? (c.dim == 256 ? 2 : c.dim == 128 ? 3 : 4)
                   : p.tiles == 2 ? (c.dim == 256 ? 1 : c.dim == 128 ? 2 : 3)
