@@ -53,7 +53,8 @@ __device__ __forceinline__ bool find_tile(const AttentionArgs& a, int number, Ti
   t.n = min(kRows, s.rows * a.group - t.r0);
   const int lowest = t.first + t.r0 / a.group, highest = t.first + (t.r0 + t.n - 1) / a.group;
   t.end = a.causal ? min(s.len, highest + 1) : s.len;
-  t.begin = a.window > 0 ? max(0, lowest - a.window + 1) : 0;
+  // (Not behind the end: a length that makes no sense would put it near 2^31.)
+  t.begin = a.window > 0 ? min(max(0, lowest - a.window + 1), max(0, t.end)) : 0;
   return true;
 }
 

@@ -350,3 +350,19 @@ def test_append_of_a_prompt_among_single_tokens(dim, page, singles, long):
                 OA.norm_rope(k.double().cpu().numpy(), np.ones(dim), 1e-6, pos, freq.numpy(), False), v.double().cpu().numpy())
     A.kv_append(cache, A.Batch(table.int(), _i32(lens), _i32(_cu(counts)), rows=rows), k, v, gamma, 1e-6, A.Rope(freq.cuda()))
     _same_cache(cache, want)
+
+
+@pytest.mark.parametrize("dim,hkv,group,n,new", [(128, 2, 4, 2, 1), (64, 1, 40, 3, 2), (256, 2, 3, 2, 1), (128, 32, 8, 2, 128),
+                                                 (256, 16, 4, 2, 70)])
+@pytest.mark.parametrize("window", [1, 5, 100])
+def test_lengths_far_behind_the_table_with_a_window(dim, hkv, group, n, new, window):
+    """A length of 2^31 - 1 is cut to what the table holds, its rows keep their
+    numbers and see nothing of it."""
+    gen = torch.Generator("cuda").manual_seed(dim)
+    cache = _cache(gen, 8, hkv, 16, dim)
+    q = torch.randn(n * new, hkv * group, dim, generator=gen, device="cuda").to(torch.bfloat16)
+    for lens in ([2 ** 31 - 1] * n, [2 ** 31 - 2 - 32 * i for i in range(n)], [2 ** 31 - 200] * n):
+        batch = A.Batch(torch.arange(8, device="cuda").int().expand(n, 8).contiguous(), _i32(lens), _i32(_cu([new] * n)),
+                        rows=n * new)
+        y, lse = A.attention(q, cache, batch, window=window, out=torch.full_like(q, 7.0), return_lse=True)
+        assert not y.any() and torch.isneginf(lse).all()
