@@ -165,10 +165,14 @@ size_t nvfp4_kv_attention_workspace(const nvfp4_kv_cache* cache, const nvfp4_kv_
  *   lse = log sum_j exp(s_j)
  * over the tokens j < kv_len[b] with j <= t if causal and j > t - window if
  * window > 0.  A row that sees no token gets y = 0 and lse = -infinity.
- * Scores, exponentials and sums are binary32; the probabilities of one token
- * enter the product with v in binary16 (2^-11 relative, which keeps the error
- * of y below that of its rounding to bf16; sums of 2^-25 of a tile's largest
- * value are dropped), and v, like k, exactly.
+ * Scores (which have to stay below 2^23 in magnitude), exponentials and sums are
+ * binary32, and k is taken exactly.  The product with v is one of binary16
+ * factors, summed in binary32: a token's probability is rounded by at most 2^-11
+ * of itself or 2^-34 of the largest one that the row has met, whichever is more
+ * (exp(-16) of the largest keeps all its 11 bits, exp(-20) is off by 2% at most);
+ * v is exact, but in pages whose scale is under 2^-22 of the largest value scale
+ * among the pages that the row's workgroup looks at, where it is off by 2^-31 of
+ * that scale at most.
  *
  *   q            bf16 [rows x q_heads x head_dim], row stride ldq.
  *   q_heads      a multiple of kv_heads, at most 1024.

@@ -121,9 +121,9 @@ kv_attention_rows_kernel(AttentionArgs a) {
   }
 
   // The waves' results, joined: Y = sum_w 2^(m_w - m) Y_w.
+  rows.finish();
 #pragma unroll
   for (int i = 0; i < kTiles; ++i) {
-    rows.l[i] = over_quarters_sum(rows.l[i]);
     if (quarter == 0) stats[wave][16 * i + col] = make_float2(rows.m[i], rows.l[i]);
   }
   __syncthreads();

@@ -16,11 +16,17 @@
 // The cache's order makes both operands whole 16-byte loads of a contiguous
 // kilobyte for each wave.
 //
-// The page's key scale goes into the scores.  Its value scale, divided by the
-// largest one met so far (s_ref, by which Y is multiplied at the end), goes
-// into the values' conversion to binary16 (its power of two) and into P (what
-// is left of it, nothing for the powers of two that the append takes): what
-// falls below 2^-25 of the largest value met is dropped.
+// m is kept kAbove below the largest score met, whose P is then about 2^kAbove: so
+// P uses binary16's range up to its end, and a token keeps its 11 bits down to 2^-23
+// of the largest P and is off by 2^-34 of that below.  With a largest P of 1, tokens
+// behind an attention sink were lost from Y but not from l (8192 tokens 17 nats
+// below one whose values are zero: Y 41% off; now 0.1%).
+//
+// The page's key scale goes into the scores.  Its value scale, over s_ref (the
+// largest one met so far, less the 2^7 that 448 leaves of binary16's range; Y is
+// multiplied by it at the end), goes into the values' conversion to binary16 (its
+// power of two) and into P (what is left of it, nothing for the powers of two that
+// the append takes).  Values are exact down to a scale of 2^-22 of the largest.
 #pragma once
 
 #include "attention_device.h"
@@ -29,6 +35,17 @@ namespace nvfp4 {
 
 constexpr int kTileTokens = 32;
 constexpr float kNone = -__builtin_inff();
+
+// The largest P is 2^kAbove, within half a power of two.  The tile kernel takes
+// 16 of them before it looks for a maximum, so no more than 2^11 would do; with 10,
+// a score may pass the largest by 2^4 (kSlack) or 2^5.5 until it does.
+constexpr float kAbove = 10.0f, kSlack = 4.0f;
+constexpr float kValueRoom = 0.0078125f;      // 2^-7: 448 * 2^7 < 65504
+constexpr float kSmallest = 1.17549435e-38f;
+
+// The running m for a largest score: a whole number, so that what it is changed by
+// is exact.  (Scores that have no fraction left, and -infinity, stay.)
+__device__ __forceinline__ float reference(float top) { return fabsf(top) < 16777216.0f ? rintf(top) - kAbove : top; }
 
 // Packed rows of one tile and the tokens that they see.
 struct Tile {
@@ -82,6 +99,14 @@ __device__ __forceinline__ void piece_tokens(const AttentionArgs& a, const Tile&
 __device__ __forceinline__ int64_t tiles_of(const KvBatchArgs& a, int group, int rows) {
   return a.cu_rows == nullptr ? (int64_t)a.seqs * ((group + rows - 1) / rows)
                               : (int64_t)a.rows * group / rows + a.seqs;
+}
+
+// s_ref for a largest P of 1, and what Y is multiplied by before: 1, but where s_ref
+// over l might otherwise be no normal number (value scales below 2^-89).
+__device__ __forceinline__ float last_factor(float& s_ref) {
+  const bool tiny = s_ref < 0x1p-96f;
+  s_ref *= tiny ? 0x1p+30f : 0x1p-10f;
+  return tiny ? 0x1p-40f : 1.0f;
 }
 
 // 8 E4M3 values in bf16 (exact), and in f16 times a power of two.
@@ -215,8 +240,22 @@ struct RowTiles {
     const int low = t.first + r0 / a.group, high = t.first + (r0 + n - 1) / a.group;
     all1 = a.causal ? min(end, low + 1) : end;
     all0 = a.window > 0 ? max(begin, high - a.window + 1) : begin;
-    s_ref = 1.17549435e-38f;
-    s_inv = 1.0f / 1.17549435e-38f;
+    s_ref = kSmallest;
+    s_inv = 1.0f / kSmallest;
+  }
+
+  // At the end: m, l and what Y is multiplied by, for a largest P of 1.
+  __device__ __forceinline__ void finish() {
+    const float down = last_factor(s_ref);
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+      l[i] = over_quarters_sum(l[i]) * (1.0f / 1024.0f);
+      m[i] += kAbove;
+      if (down != 1.0f) {
+#pragma unroll
+        for (int j = 0; j < kOut; ++j) o[i][j] *= down;
+      }
+    }
   }
 
   // Tokens token .. token + 31: the codes of keys(g, c) and values(g, c) are
@@ -259,20 +298,20 @@ struct RowTiles {
           }
       }
     }
-    // The maximum follows only where a score is over it by more than 8: P is
-    // then at most 2^8, which binary16 holds as well as 1.
+    // m follows only where P would pass 2^(kAbove + kSlack): with what is left of a
+    // value scale below 2^15, which binary16 holds.
     float top[kTiles];
     bool over = false;
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
       top[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])) * ks[0],
                      fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3])) * ks[1]);
-      over |= top[i] > m[i] + 8.0f;
+      over |= top[i] - m[i] > kAbove + kSlack;
     }
     if (__any(over)) {
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
-        const float m_new = fmaxf(m[i], over_quarters_max(top[i]));
+        const float m_new = fmaxf(m[i], reference(over_quarters_max(top[i])));
         const float f = m[i] == m_new ? 1.0f : __builtin_amdgcn_exp2f(m[i] - m_new);      // (0 from nothing)
         l[i] *= f;
 #pragma unroll
@@ -280,7 +319,7 @@ struct RowTiles {
         m[i] = m_new;
       }
     }
-    const float v_top = fmaxf(vs[0], vs[1]);
+    const float v_top = fmaxf(vs[0], vs[1]) * kValueRoom;
     if (v_top > s_ref) {
       const float f = s_ref / v_top;
 #pragma unroll

@@ -79,7 +79,7 @@ struct WideRows {
     const int low = t.first + r0 / a.group, high = t.first + (r0 + n - 1) / a.group;
     all1 = a.causal ? min(end, low + 1) : end;
     all0 = a.window > 0 ? max(begin, high - a.window + 1) : begin;
-    s_ref = 1.17549435e-38f;
+    s_ref = kSmallest;
   }
 
   // Tokens token .. token + 31, whose keys and values are the two groups at
@@ -113,10 +113,10 @@ struct WideRows {
     float power1 = __uint_as_float(max((int)(v1 - ref) + 0x3F800000, 0));
     // Where all rows see all tokens and the value scales are powers of two, at
     // most the largest met, the scores need no maximum: as long as their
-    // exponentials' sum stays below 2^12, each fits binary16 as well as 1 does.
-    // (Before a row's first token m is -infinity, and the sum is not below.)
-    const bool plain = whole && max(v0, v1) <= ref && ((v0 | v1 | ref) & 0x7FFFFFu) == 0;
-    if (!plain || __any(!(sum <= 4096.0f))) {
+    // exponentials' sum fits binary16, so does each.
+    // (Before a row's first token m is -infinity, and the sum does not.)
+    const bool plain = whole && max(v0, v1) <= ref + (7u << 23) && ((v0 | v1 | ref) & 0x7FFFFFu) == 0;
+    if (!plain || __any(!(sum <= 65504.0f))) {
       if (!whole) {
         const int at = first + (r0 + min(lane & 31, rows - 1)) / a.group;
         const int see1 = a.causal ? min(end, at + 1) : end;
@@ -130,11 +130,11 @@ struct WideRows {
       float t0 = s[0], t1 = s[8];
 #pragma unroll
       for (int r = 1; r < 8; ++r) t0 = fmaxf(t0, s[r]), t1 = fmaxf(t1, s[8 + r]);
-      const float m_new = fmaxf(m, over_halves_max(fmaxf(t0 * f0, t1 * f1)));
+      const float m_new = fmaxf(m, reference(over_halves_max(fmaxf(t0 * f0, t1 * f1))));
       const float f = m == m_new ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);      // (0 from nothing)
       l *= f;
       m = m_new;
-      const float s_new = fmaxf(fmaxf(vs0, vs1), s_ref), less = f * (s_ref / s_new);
+      const float s_new = fmaxf(fmaxf(vs0, vs1) * kValueRoom, s_ref), less = f * (s_ref / s_new);
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) o[j] *= less;
       s_ref = s_new;
@@ -253,12 +253,19 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_tile_kerne
   // This lane's elements of its row: 64 c + 32 x + 16 n + 8 y + 4 half + 0 .. 3 in o[2 c + n][8 x + 4 y + 0 .. 3].
   // (The lane's number again, so that nothing made of it is kept through the loop.)
   const int own_lane = __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, 0u));
-  const float l = over_halves_sum(rows.l);
+  // (For a largest P of 1.)
+  const float l = over_halves_sum(rows.l) * (1.0f / 1024.0f), m = rows.m + kAbove;
+  float s_ref = rows.s_ref;
+  const float down = last_factor(s_ref);
+  if (down != 1.0f) {
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) rows.o[j] *= down;
+  }
   if ((own_lane & 31) >= n) return;
   const int in_tile = first + (own_lane & 31), e0 = 4 * (own_lane >> 5);
   if (!whole) {
     const int64_t at = (((int64_t)number * a.cache.heads + h) * a.splits + piece) * kTileRows + in_tile;
-    if (own_lane < 32) reinterpret_cast<float2*>(a.part)[at] = make_float2(rows.m, l);
+    if (own_lane < 32) reinterpret_cast<float2*>(a.part)[at] = make_float2(m, l);
     float* to = a.part + (int64_t)tiles * a.cache.heads * a.splits * (2 * kTileRows) + at * D + e0;
 #pragma unroll
     for (int j = 0; j < D / 32; ++j)
@@ -266,15 +273,15 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_tile_kerne
       for (int x = 0; x < 4; ++x) {
         f32x4 y;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = rows.o[j][4 * x + e] * rows.s_ref;
+        for (int e = 0; e < 4; ++e) y[e] = rows.o[j][4 * x + e] * s_ref;
         *reinterpret_cast<f32x4*>(to + 64 * (j / 2) + 32 * (x / 2) + 16 * (j & 1) + 8 * (x & 1)) = y;
       }
   } else {
     const int r = t.r0 + in_tile, head = h * a.group + r % a.group;
     const int64_t row = t.row0 + r / a.group;
     if (a.lse != nullptr && own_lane < 32)
-      a.lse[row * a.q_heads + head] = l == 0.0f ? kNone : (rows.m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
-    const float f = l == 0.0f ? 0.0f : rows.s_ref / l;
+      a.lse[row * a.q_heads + head] = l == 0.0f ? kNone : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+    const float f = l == 0.0f ? 0.0f : s_ref / l;
     uint16_t* to = a.y + row * a.ldy + (int64_t)head * D + e0;
 #pragma unroll
     for (int j = 0; j < D / 32; ++j)
