@@ -241,3 +241,22 @@ def test_scores_of_millions(shape):
         want = (VALUES.cuda()[case.v[p, :, slot].long()] * case.vs[p].double()[:, None]).repeat_interleave(group, 0)
         assert torch.equal(y[row:row + n].double(), want.expand(n, -1, -1))
         row += n
+
+
+LONG = [      # dim, page, key heads, group, lengths, new rows, window, stated length
+    (64, 128, 1, 2, [200000, 10], [2, 1], 0, 100), (256, 64, 1, 2, [100000], [3], 0, 100),
+    (128, 64, 1, 8, [60000], [8187], 0, None), (64, 64, 1, 8, [16000], [8187], 0, None), (64, 64, 1, 8, [16000], [8187], 600, None),
+    (256, 64, 8, 8, [2000, 1300, 50, 1999], [60, 40, 50, 50], 0, None), (128, 64, 2, 4, [131072, 77], [1, 1], 0, None),
+    (128, 32, 2, 8, [40000, 5001, 3000, 3065], [7, 7, 1, 7], 3000, None), (64, 32, 2, 2, [40000, 20011], [1, 7], 0, None),
+    (256, 16, 2, 3, [30000, 9000], [1, 1], 0, None),
+]
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("shape", LONG, ids=lambda c: "d%d_h%dx%d_%d_w%d" % (c[0], c[2], c[3], c[4][0], c[6]))
+def test_long_sequences(shape, causal):
+    """Sequences over which random values would average away: every page's weight in y is seen."""
+    dim, page, heads, group, lens, counts, window, stated = shape
+    log("long %s causal %s" % (shape, causal))
+    case = Case(dim, page, heads, lens, seed=dim + lens[0])
+    _run(case, _queries(case, sum(counts), heads * group), counts, causal=causal, window=window, max_len=stated, pages=True)
