@@ -67,9 +67,10 @@ typedef struct nvfp4_kv_cache {
  * its tokens with the new ones, so new row i is token kv_len[b] - n_b + i
  * (rows whose token would be before 0 are dropped by the append, and see
  * nothing).  Token t is in page page_table[b * page_table_stride +
- * t / page_size], slot t % page_size; later entries of the table are not read
- * for their pages.  Sequences may have no rows, no tokens, or share pages that
- * are only read.
+ * t / page_size], slot t % page_size; entries of the table behind its last token,
+ * or wholly in front of the attention's windows, may hold anything, and so may
+ * their pages and scales (scales of the others are finite).  Sequences may have no
+ * rows, no tokens, or share pages that are only read.
  *
  *   page_table   device int32 [n_seqs x max_pages], row stride
  *                page_table_stride >= max_pages entries.

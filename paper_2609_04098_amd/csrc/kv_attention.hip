@@ -82,7 +82,7 @@ kv_attention_rows_kernel(AttentionArgs a) {
 
   const int step = kWaves * kTileTokens;
   int token = (begin & ~(kTileTokens - 1)) + wave * kTileTokens;
-  GroupPages pages = group_pages(a, t.b, h, (int64_t)token + (lane >> 1) * step + (lane & 1) * 16, end);
+  GroupPages pages = group_pages(a, t.b, h, (int64_t)token + (lane >> 1) * step + (lane & 1) * 16, begin, end);
   int in_batch = 0;
   // The tile's scales; then the next batch of pages, if the next tile needs it.
   const auto scales = [&](bool (&there)[2], float (&ks)[2], float (&vs)[2]) __attribute__((always_inline)) {
@@ -93,7 +93,7 @@ kv_attention_rows_kernel(AttentionArgs a) {
       vs[g] = lane_of(pages.v_scale, 2 * in_batch + g);
     }
     if (++in_batch == 32) {
-      pages = group_pages(a, t.b, h, (int64_t)token + step + (lane >> 1) * step + (lane & 1) * 16, end);
+      pages = group_pages(a, t.b, h, (int64_t)token + step + (lane >> 1) * step + (lane & 1) * 16, begin, end);
       in_batch = 0;
       // (Waited for here, or the compiler would, and with them for the tile's values,
       // in front of every tile.)

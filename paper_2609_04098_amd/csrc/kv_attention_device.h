@@ -157,18 +157,20 @@ __device__ __forceinline__ float over_quarters_sum(float x) {
 }
 
 // Page and scales of the groups of 16 tokens that a wave meets next: its lane
-// holds those of the group at `token`, page -1 where that is past the end or
-// its page is not in the cache.
+// holds those of the group at `token`, page -1 where that is past the end or in
+// front of the beginning (a window's first tile may begin in pages that nobody
+// sees, whose scales may be anything) or its page is not in the cache.
 struct GroupPages {
   int page;
   float k_scale, v_scale;
 };
 
-__device__ __forceinline__ GroupPages group_pages(const AttentionArgs& a, int b, int h, int64_t token, int end) {
+__device__ __forceinline__ GroupPages group_pages(const AttentionArgs& a, int b, int h, int64_t token, int begin,
+                                                  int end) {
   GroupPages g;
   g.page = -1;
   g.k_scale = g.v_scale = 0.0f;
-  if (token < end) {
+  if (token < end && token + 16 > begin) {
     const int p = a.batch.table[(int64_t)b * a.batch.table_stride + (token >> a.cache.page_shift)];
     if (p >= 0 && p < a.cache.num_pages) {
       g.page = p;

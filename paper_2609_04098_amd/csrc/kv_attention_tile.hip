@@ -215,7 +215,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_tile_kerne
   // 16 tiles' pages; their key scales times the softmax scale (not 0, so that a
   // masked score, -infinity, stays one).
   const auto look_up = [&](int from) __attribute__((always_inline)) {
-    GroupPages g = group_pages(a, t.b, h, (int64_t)from + 16 * lane, end);
+    GroupPages g = group_pages(a, t.b, h, (int64_t)from + 16 * lane, begin, end);
     g.k_scale = fmaxf(g.k_scale * scale, 1e-37f);
     return g;
   };
