@@ -66,7 +66,7 @@ typedef struct nvfp4_kv_cache {
  * [cu_rows[b], cu_rows[b + 1]) of q, k, v and y, n_b of them; kv_len[b] counts
  * its tokens with the new ones, so new row i is token kv_len[b] - n_b + i
  * (rows whose token would be before 0 are dropped by the append, and see
- * nothing).  Token t is in page page_table[b * page_table_stride +
+ * nothing under a causal mask, without one what the others see).  Token t is in page page_table[b * page_table_stride +
  * t / page_size], slot t % page_size; entries of the table behind its last token,
  * or wholly in front of the attention's windows, may hold anything, and so may
  * their pages and scales (scales of the others are finite).  Sequences may have no

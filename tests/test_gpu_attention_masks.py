@@ -43,3 +43,25 @@ def test_pages_in_front_of_a_window_may_hold_anything(form, causal):
                 dirty.v_scale[hidden[i::3]], dirty.k_scale[hidden[i::3]] = bad, bad
         got = A.attention(q, dirty, batch, causal=causal, window=window, return_lse=True)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), window
+
+
+@pytest.mark.parametrize("causal,window", [(True, 0), (False, 0), (True, 5), (False, 5), (False, 40)])
+@pytest.mark.parametrize("form", [(128, 16, 2, 4, [3, 0, 20], [5, 2, 1]), (64, 32, 1, 3, [50, 7], [70, 9]),
+                                  (128, 16, 32, 8, [30, 60], [66, 70]), (256, 32, 32, 2, [70, 40], [75, 60])], ids=_name)
+def test_more_new_rows_than_tokens(form, causal, window):
+    """Rows whose tokens would be before 0 see nothing under a causal mask, and without one what the formula says."""
+    dim, page, hkv, group, lens, counts = form
+    log("rows before 0 %s %s %d" % (form, causal, window))
+    gen = torch.Generator().manual_seed(dim + window)
+    width = max(1, -(-max(lens) // page))
+    table = torch.randperm(len(lens) * width, generator=gen).view(len(lens), width)
+    cache = _random_cache(gen, len(lens) * width, hkv, page, dim, nan=False)
+    q = (torch.randn(sum(counts), hkv * group, dim, generator=gen) * 0.5).to(torch.bfloat16).cuda()
+    batch = A.Batch(table.int().cuda(), _i32(lens), _i32(_cu(counts)), rows=sum(counts))
+    y, lse = A.attention(q, cache, batch, causal=causal, window=window, return_lse=True)
+    _check(y, lse, cache, q, table, lens, counts, dim ** -0.5, causal, window)
+    if causal:
+        first = [sum(counts[:b]) for b in range(len(counts))]
+        for b, r in enumerate(first):
+            early = slice(r, r + max(0, counts[b] - lens[b]))
+            assert not y[early].any() and torch.isneginf(lse[early]).all()
