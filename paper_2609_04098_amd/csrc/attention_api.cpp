@@ -191,7 +191,7 @@ int nvfp4_kv_attention(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
   a.group = (int)(q_heads / cache->kv_heads);
   a.scale = (float)scale;
   a.causal = causal;
-  a.window = (int)(window < kMaxTokens ? window : kMaxTokens);
+  a.window = (int)window;
   const hipError_t e = nvfp4::launch_kv_attention(a, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? NVFP4_OK : nvfp4::fail_hip(e);
 }

@@ -47,6 +47,10 @@ constexpr float kSmallest = 1.17549435e-38f;
 // is exact.  (Scores that have no fraction left, and -infinity, stay.)
 __device__ __forceinline__ float reference(float top) { return fabsf(top) < 16777216.0f ? rintf(top) - kAbove : top; }
 
+// The first token that token t's row sees of a window of at least 1 (below 0: all).
+// (A t below 0 counts as 0, so that no window below 2^31 takes it out of 32 bits.)
+__device__ __forceinline__ int window_begin(int t, int window) { return max(t, 0) - (window - 1); }
+
 // Packed rows of one tile and the tokens that they see.
 struct Tile {
   int b, row0, rows, r0, n;      // sequence, its first row and rows, first packed row, packed rows of this tile
@@ -71,7 +75,7 @@ __device__ __forceinline__ bool find_tile(const AttentionArgs& a, int number, Ti
   const int lowest = t.first + t.r0 / a.group, highest = t.first + (t.r0 + t.n - 1) / a.group;
   t.end = a.causal ? min(s.len, highest + 1) : s.len;
   // (Not behind the end: a length that makes no sense would put it near 2^31.)
-  t.begin = a.window > 0 ? min(max(0, lowest - a.window + 1), max(0, t.end)) : 0;
+  t.begin = a.window > 0 ? min(max(0, window_begin(lowest, a.window)), max(0, t.end)) : 0;
   return true;
 }
 
@@ -241,7 +245,7 @@ struct RowTiles {
     end = to;
     const int low = t.first + r0 / a.group, high = t.first + (r0 + n - 1) / a.group;
     all1 = a.causal ? min(end, low + 1) : end;
-    all0 = a.window > 0 ? max(begin, high - a.window + 1) : begin;
+    all0 = a.window > 0 ? max(begin, window_begin(high, a.window)) : begin;
     s_ref = kSmallest;
     s_inv = 1.0f / kSmallest;
   }
@@ -290,7 +294,7 @@ struct RowTiles {
 #pragma unroll
       for (int i = 0; i < kTiles; ++i) {
         const int see1 = a.causal ? min(end, at[i] + 1) : end;
-        const int see0 = a.window > 0 ? max(begin, at[i] - a.window + 1) : begin;
+        const int see0 = a.window > 0 ? max(begin, window_begin(at[i], a.window)) : begin;
 #pragma unroll
         for (int g = 0; g < 2; ++g)
 #pragma unroll

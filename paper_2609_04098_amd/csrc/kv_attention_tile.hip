@@ -78,7 +78,7 @@ struct WideRows {
     end = to;
     const int low = t.first + r0 / a.group, high = t.first + (r0 + n - 1) / a.group;
     all1 = a.causal ? min(end, low + 1) : end;
-    all0 = a.window > 0 ? max(begin, high - a.window + 1) : begin;
+    all0 = a.window > 0 ? max(begin, window_begin(high, a.window)) : begin;
     s_ref = kSmallest;
   }
 
@@ -120,7 +120,7 @@ struct WideRows {
       if (!whole) {
         const int at = first + (r0 + min(lane & 31, rows - 1)) / a.group;
         const int see1 = a.causal ? min(end, at + 1) : end;
-        const int see0 = a.window > 0 ? max(begin, at - a.window + 1) : begin;
+        const int see0 = a.window > 0 ? max(begin, window_begin(at, a.window)) : begin;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int j = token + 8 * (r / 4) + 4 * half + r % 4;
@@ -208,7 +208,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_tile_kerne
   // Tokens that one of this wave's rows sees.
   const int low = t.first + r0 / a.group, high = t.first + (r0 + max(n, 1) - 1) / a.group;
   const int mine1 = n <= 0 ? 0 : (a.causal ? min(end, high + 1) : end);
-  const int mine0 = a.window > 0 ? max(begin, low - a.window + 1) : begin;
+  const int mine0 = a.window > 0 ? max(begin, window_begin(low, a.window)) : begin;
 
   const float scale = fabsf(a.scale);
   int token = begin & ~(kStageTokens - 1), in_batch = 0, buffer = 0;

@@ -65,3 +65,21 @@ def test_more_new_rows_than_tokens(form, causal, window):
         for b, r in enumerate(first):
             early = slice(r, r + max(0, counts[b] - lens[b]))
             assert not y[early].any() and torch.isneginf(lse[early]).all()
+
+
+@pytest.mark.parametrize("window", [2 ** 30 + 40, 2 ** 31 - 130, 2 ** 31 - 1])
+@pytest.mark.parametrize("form", [(64, 16, 1, 3, [1], [1, 1, 2]), (128, 16, 32, 8, [1], [66, 70, 5])], ids=_name)
+def test_windows_near_the_largest(form, window):
+    """Windows over 2^30, for rows of any number up to 2^31 - 2 and for rows before token 0."""
+    dim, page, hkv, group, _, counts = form
+    gen = torch.Generator().manual_seed(dim)
+    table = torch.randperm(24, generator=gen).view(3, 8)
+    cache = _random_cache(gen, 24, hkv, page, dim, nan=False)
+    q = (torch.randn(sum(counts), hkv * group, dim, generator=gen) * 0.5).to(torch.bfloat16).cuda()
+    for lens in ([2 ** 31 - 1, 2 ** 30 + 60, 1], [window + 100 if window + 100 < 2 ** 31 else 90, 2 ** 31 - 3, 0]):
+        for causal in (True, False):
+            batch = A.Batch(table.int().cuda(), _i32(lens), _i32(_cu(counts)), rows=sum(counts))
+            y, lse = A.attention(q, cache, batch, causal=causal, window=window, return_lse=True)
+            _check(y, lse, cache, q, table, lens, counts, dim ** -0.5, causal, window)
+            seen = 2 ** 31 - 1 - window < 128 if lens[0] == 2 ** 31 - 1 else True
+            assert bool(y[counts[0] - 1].any()) == seen
