@@ -20,6 +20,11 @@
  * outside [0, rows), slots before 0 and pages outside [0, num_pages) are not
  * read or written; such a page's tokens are dropped by the append and masked
  * in the attention.  Lengths are cut to max_pages * page_size.
+ *
+ * A launch holds fewer than 2^32 work-items.  A step that would take more in one is
+ * refused with NVFP4_EINVAL: with one row for each sequence, an attention from n_seqs
+ * * kv_heads = 2^24 on (q_heads / kv_heads <= 16), an append from n_seqs *
+ * ceil(kv_heads * head_dim / 512) = 2^23 on.
  */
 #ifndef NVFP4_ATTENTION_H
 #define NVFP4_ATTENTION_H

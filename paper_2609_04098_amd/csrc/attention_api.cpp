@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "attention_launch.h"
+#include "attention_plan.h"
 #include "nvfp4_attention.h"
 
 namespace {
@@ -136,11 +137,13 @@ int nvfp4_kv_append(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, co
   if (!valid_rows(k, ldk, cache->kv_heads, cache->head_dim, batch->rows) ||
       !valid_rows(v, ldv, cache->kv_heads, cache->head_dim, batch->rows) || !aligned(k_gamma, 16))
     return NVFP4_EINVAL;
-  const int st = nvfp4::check_device();
-  if (st != NVFP4_OK) return st;
   nvfp4::AppendArgs a;
   a.cache = cache_args(cache);
   a.batch = batch_args(batch, cache->page_size);
+  const nvfp4::AppendPlan p = nvfp4::append_plan(a.cache, a.batch);
+  if (!nvfp4::one_grid(p.workgroups, p.threads)) return NVFP4_EINVAL;
+  const int st = nvfp4::check_device();
+  if (st != NVFP4_OK) return st;
   if (a.batch.seqs == 0 || a.batch.rows == 0 || a.batch.max_tokens == 0) return NVFP4_OK;
   a.x[0] = static_cast<const uint16_t*>(k);
   a.x[1] = static_cast<const uint16_t*>(v);
@@ -157,7 +160,12 @@ int nvfp4_kv_append(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, co
 size_t nvfp4_kv_attention_workspace(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, int64_t q_heads) {
   if (!valid_cache(cache) || !valid_batch(batch, cache->page_size) || !valid_q_heads(q_heads, cache->kv_heads))
     return 0;
-  return nvfp4::kv_attention_workspace_bytes(cache_args(cache), batch_args(batch, cache->page_size), (int)q_heads);
+  const nvfp4::KvCacheArgs c = cache_args(cache);
+  const nvfp4::KvBatchArgs b = batch_args(batch, cache->page_size);
+  if (b.seqs == 0 || b.rows == 0) return 0;
+  const int group = (int)(q_heads / cache->kv_heads);
+  const nvfp4::AttentionPlan p = nvfp4::attention_plan(c, b, group, 0, nvfp4::kAnyRoom);
+  return nvfp4::attention_fits(c, b, group, p) ? nvfp4::part_bytes(c, b, group, p) : 0;
 }
 
 int nvfp4_kv_attention(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const void* q, int64_t ldq,
@@ -171,24 +179,35 @@ int nvfp4_kv_attention(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
   const double scale = (double)softmax_scale * 1.4426950408889634;      // (powers of two)
   if (batch->rows * q_heads >= kI32Lim) return NVFP4_EINVAL;
   if (!isfinite((float)scale) || (causal != 0 && causal != 1) || window < 0 || window >= kI32Lim) return NVFP4_EINVAL;
-  const size_t need = nvfp4_kv_attention_workspace(cache, batch, q_heads);
-  if (need > 0) {
-    if (workspace == nullptr || !aligned(workspace, 16)) return NVFP4_EINVAL;
-    if (workspace_bytes < need) return NVFP4_EWORKSPACE;
-  }
-  const int st = nvfp4::check_device();
-  if (st != NVFP4_OK) return st;
   nvfp4::AttentionArgs a;
   a.cache = cache_args(cache);
   a.batch = batch_args(batch, cache->page_size);
-  if (a.batch.seqs == 0 || a.batch.rows == 0) return NVFP4_OK;
+  a.q_heads = (int)q_heads;
+  a.group = (int)(q_heads / cache->kv_heads);
+  const bool none = a.batch.seqs == 0 || a.batch.rows == 0;
+  nvfp4::AttentionPlan p = {};
+  if (!none) {
+    p = nvfp4::attention_plan(a.cache, a.batch, a.group, 0, nvfp4::kAnyRoom);
+    if (!nvfp4::attention_fits(a.cache, a.batch, a.group, p)) return NVFP4_EINVAL;
+    const size_t need = nvfp4::part_bytes(a.cache, a.batch, a.group, p);
+    if (need > 0) {
+      if (workspace == nullptr || !aligned(workspace, 16)) return NVFP4_EINVAL;
+      if (workspace_bytes < need) return NVFP4_EWORKSPACE;
+    }
+    if (window > 0) p = nvfp4::attention_plan(a.cache, a.batch, a.group, (int)window, p.splits);
+  }
+  const int st = nvfp4::check_device();
+  if (st != NVFP4_OK) return st;
+  if (none) return NVFP4_OK;
+  a.row_tiles = p.tiles;
+  a.waves = p.waves;
+  a.chunk = p.chunk;
+  a.splits = p.splits;
   a.q = static_cast<const uint16_t*>(q);
   a.y = static_cast<uint16_t*>(y);
   a.lse = lse;
   a.ldq = ldq;
   a.ldy = ldy;
-  a.q_heads = (int)q_heads;
-  a.group = (int)(q_heads / cache->kv_heads);
   a.scale = (float)scale;
   a.causal = causal;
   a.window = (int)window;

@@ -65,13 +65,13 @@ struct AttentionArgs {
   int q_heads, group;          // group = q_heads / kv_heads
   float scale;                 // softmax_scale * log2(e)
   int causal, window;
-  int chunk, splits;           // tokens of one piece of a sequence, pieces (launcher)
+  int row_tiles, waves;        // of a workgroup, and
+  int chunk, splits;           // tokens of one piece of a sequence, pieces (attention_plan.h)
   float* part;                 // partial results (launcher)
 };
 
 hipError_t launch_qk_norm_rope(const NormRopeArgs& a, int dim, hipStream_t stream);
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream);
-size_t kv_attention_workspace_bytes(const KvCacheArgs& cache, const KvBatchArgs& batch, int q_heads);
 // The attention of many rows in tiles of 128 packed rows (kv_attention_tile.hip;
 // called by launch_kv_attention, which joins the pieces).
 hipError_t launch_kv_attention_tile(const AttentionArgs& a, int64_t tiles, hipStream_t stream);

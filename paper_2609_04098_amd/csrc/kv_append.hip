@@ -28,6 +28,7 @@
 // where they differ, the same took 123 us.  With the partners of the rotation
 // fetched by lane moves instead of LDS shuffles, 29.6 us.)
 #include "attention_device.h"
+#include "attention_plan.h"
 
 namespace nvfp4 {
 
@@ -561,48 +562,33 @@ __global__ __launch_bounds__(256) void kv_append_tokens_kernel(AppendArgs a) {
 }
 
 template <int D, bool kDynamic>
-static hipError_t launch(const AppendArgs& a, int64_t items, hipStream_t stream) {
-  if (a.batch.cu_rows == nullptr || a.batch.rows < 5 * (int64_t)a.batch.seqs) {
-    const int64_t blocks = 2 * items * ((a.cache.heads * D + 511) / 512);
-    if (blocks >= (int64_t)1 << 31) return hipErrorInvalidValue;
-    kv_append_tokens_kernel<D, kDynamic><<<dim3((unsigned)blocks), 256, 0, stream>>>(a);
-    return hipGetLastError();
-  }
-  // Heads of a workgroup: as many as leave one round of workgroups on 256 compute
-  // units, four of 4096 elements each (pages that are written, about rows / page_size).
+static hipError_t launch(const AppendArgs& a, const AppendPlan& p, hipStream_t stream) {
+  const dim3 grid((unsigned)p.workgroups);
   const int elements = a.cache.page_size * D;
-  const int64_t pages = (a.batch.rows >> a.cache.page_shift) + a.batch.seqs;
-  const int64_t fit = elements <= 4096 ? 1024 : 1024 * 4096 / elements;
-  int64_t each = (pages * a.cache.heads + fit - 1) / fit;
-  if (each > a.cache.heads) each = a.cache.heads;
-  const int64_t parts = (a.cache.heads + each - 1) / each;
-  each = (a.cache.heads + parts - 1) / parts;
-  const int64_t blocks = items * parts;
-  if (blocks >= (int64_t)1 << 31) return hipErrorInvalidValue;
-  const dim3 grid((unsigned)blocks);
-  if (elements <= 2048) {
-    if constexpr (D <= 128) kv_append_pages_kernel<D, 256, 1, kDynamic><<<grid, 256, 0, stream>>>(a, (int)each);
+  if (p.tokens) {
+    kv_append_tokens_kernel<D, kDynamic><<<grid, 256, 0, stream>>>(a);
+  } else if (elements <= 2048) {
+    if constexpr (D <= 128) kv_append_pages_kernel<D, 256, 1, kDynamic><<<grid, 256, 0, stream>>>(a, p.each);
   } else if (elements <= 4096) {
-    kv_append_pages_kernel<D, 256, 2, kDynamic><<<grid, 256, 0, stream>>>(a, (int)each);
+    kv_append_pages_kernel<D, 256, 2, kDynamic><<<grid, 256, 0, stream>>>(a, p.each);
   } else if (elements <= 8192) {
-    kv_append_pages_kernel<D, 512, 2, kDynamic><<<grid, 512, 0, stream>>>(a, (int)each);
+    kv_append_pages_kernel<D, 512, 2, kDynamic><<<grid, 512, 0, stream>>>(a, p.each);
   } else {
-    if constexpr (D >= 128) kv_append_pages_kernel<D, 1024, 2, kDynamic><<<grid, 1024, 0, stream>>>(a, (int)each);
+    if constexpr (D >= 128) kv_append_pages_kernel<D, 1024, 2, kDynamic><<<grid, 1024, 0, stream>>>(a, p.each);
   }
   return hipGetLastError();
 }
 
 template <bool kDynamic>
-static hipError_t launch_mode(const AppendArgs& a, int64_t items, hipStream_t stream) {
-  return a.cache.dim == 64    ? launch<64, kDynamic>(a, items, stream)
-         : a.cache.dim == 128 ? launch<128, kDynamic>(a, items, stream)
-                              : launch<256, kDynamic>(a, items, stream);
+static hipError_t launch_mode(const AppendArgs& a, const AppendPlan& p, hipStream_t stream) {
+  return a.cache.dim == 64    ? launch<64, kDynamic>(a, p, stream)
+         : a.cache.dim == 128 ? launch<128, kDynamic>(a, p, stream)
+                              : launch<256, kDynamic>(a, p, stream);
 }
 
 hipError_t launch_kv_append(const AppendArgs& a, hipStream_t stream) {
-  const int64_t items = a.batch.cu_rows == nullptr ? a.batch.seqs
-                                                   : (a.batch.rows >> a.cache.page_shift) + 2 * (int64_t)a.batch.seqs;
-  return a.dynamic ? launch_mode<true>(a, items, stream) : launch_mode<false>(a, items, stream);
+  const AppendPlan p = append_plan(a.cache, a.batch);
+  return a.dynamic ? launch_mode<true>(a, p, stream) : launch_mode<false>(a, p, stream);
 }
 
 }  // namespace nvfp4
