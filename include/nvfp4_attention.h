@@ -174,8 +174,9 @@ size_t nvfp4_kv_attention_workspace(const nvfp4_kv_cache* cache, const nvfp4_kv_
  * Scores (which have to stay below 2^23 in magnitude), exponentials and sums are
  * binary32, and k is taken exactly.  The product with v is one of binary16
  * factors, summed in binary32: a token's probability is rounded by at most 2^-11
- * of itself or 2^-34 of the largest one that the row has met, whichever is more
- * (exp(-16) of the largest keeps all its 11 bits, exp(-20) is off by 2% at most);
+ * of itself or 2^-34 of the largest one that the row has met (2^-33 with value
+ * scales that are no powers of two), whichever is more: exp(-15) of the largest
+ * keeps its 11 bits, exp(-20) is off by 2% (4%) at most;
  * v is exact, but in pages whose scale is under 2^-22 of the largest value scale
  * among the pages that the row's workgroup looks at, where it is off by 2^-31 of
  * that scale at most.

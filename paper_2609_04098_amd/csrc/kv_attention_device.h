@@ -22,11 +22,11 @@
 // behind an attention sink were lost from Y but not from l (8192 tokens 17 nats
 // below one whose values are zero: Y 41% off; now 0.1%).
 //
-// The page's key scale goes into the scores.  Its value scale, over s_ref (the
-// largest one met so far, less the 2^7 that 448 leaves of binary16's range; Y is
-// multiplied by it at the end), goes into the values' conversion to binary16 (its
-// power of two) and into P (what is left of it, nothing for the powers of two that
-// the append takes).  Values are exact down to a scale of 2^-22 of the largest.
+// The page's key scale goes into the scores.  Its value scale, over the largest one
+// met so far (s_ref, by which Y is multiplied at the end) and times the 2^7 that 448
+// leaves of binary16's range, goes into the values' conversion to binary16 (a power
+// of two) and into P (what is left of it, nothing for the powers of two that the
+// append takes).  Values are exact down to a scale of 2^-22 of the largest.
 #pragma once
 
 #include "attention_device.h"
@@ -37,11 +37,12 @@ constexpr int kTileTokens = 32;
 constexpr float kNone = -__builtin_inff();
 
 // The largest P is 2^kAbove, within half a power of two.  The tile kernel takes
-// 16 of them before it looks for a maximum, so no more than 2^11 would do; with 10,
-// a score may pass the largest by 2^4 (kSlack) or 2^5.5 until it does.
-constexpr float kAbove = 10.0f, kSlack = 4.0f;
-constexpr float kValueRoom = 0.0078125f;      // 2^-7: 448 * 2^7 < 65504
-constexpr float kSmallest = 1.17549435e-38f;
+// 16 of them before it looks for a maximum, so no more than 2^11 would do; with 10, a
+// score may pass the largest by 5.5 until it does, as one in the other kernels (to
+// kHighest: 2^15.9 < 65504).
+constexpr float kAbove = 10.0f, kHighest = 15.9f;
+constexpr float kValueRoom = 128.0f;               // 448 * 2^7 < 65504
+constexpr float kSmallest = 0x1p-119f;             // of s_ref: over kValueRoom, a normal number
 
 // The running m for a largest score: a whole number, so that what it is changed by
 // is exact.  (Scores that have no fraction left, and -infinity, stay.)
@@ -105,11 +106,12 @@ __device__ __forceinline__ int64_t tiles_of(const KvBatchArgs& a, int group, int
                               : (int64_t)a.rows * group / rows + a.seqs;
 }
 
-// s_ref for a largest P of 1, and what Y is multiplied by before: 1, but where s_ref
-// over l might otherwise be no normal number (value scales below 2^-89).
+// At the end: s_ref becomes what Y is multiplied by for a largest P of 1; the result,
+// what Y is multiplied by before that: 1, but where s_ref over l might otherwise be no
+// normal number (value scales below 2^-89).
 __device__ __forceinline__ float last_factor(float& s_ref) {
-  const bool tiny = s_ref < 0x1p-96f;
-  s_ref *= tiny ? 0x1p+30f : 0x1p-10f;
+  const bool tiny = s_ref < 0x1p-89f;
+  s_ref *= tiny ? 0x1p+23f : 0x1p-17f;
   return tiny ? 0x1p-40f : 1.0f;
 }
 
@@ -247,7 +249,7 @@ struct RowTiles {
     all1 = a.causal ? min(end, low + 1) : end;
     all0 = a.window > 0 ? max(begin, window_begin(high, a.window)) : begin;
     s_ref = kSmallest;
-    s_inv = 1.0f / kSmallest;
+    s_inv = kValueRoom / kSmallest;
   }
 
   // At the end: m, l and what Y is multiplied by, for a largest P of 1.
@@ -304,15 +306,14 @@ struct RowTiles {
           }
       }
     }
-    // m follows only where P would pass 2^(kAbove + kSlack): with what is left of a
-    // value scale below 2^15, which binary16 holds.
+    // m follows only where P would pass binary16's range.
     float top[kTiles];
     bool over = false;
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
       top[i] = fmaxf(fmaxf(fmaxf(s[i][0][0], s[i][0][1]), fmaxf(s[i][0][2], s[i][0][3])) * ks[0],
                      fmaxf(fmaxf(s[i][1][0], s[i][1][1]), fmaxf(s[i][1][2], s[i][1][3])) * ks[1]);
-      over |= top[i] - m[i] > kAbove + kSlack;
+      over |= top[i] - m[i] > kHighest;
     }
     if (__any(over)) {
 #pragma unroll
@@ -325,7 +326,7 @@ struct RowTiles {
         m[i] = m_new;
       }
     }
-    const float v_top = fmaxf(vs[0], vs[1]) * kValueRoom;
+    const float v_top = fmaxf(vs[0], vs[1]);
     if (v_top > s_ref) {
       const float f = s_ref / v_top;
 #pragma unroll
@@ -333,7 +334,7 @@ struct RowTiles {
 #pragma unroll
         for (int j = 0; j < kOut; ++j) o[i][j] *= f;
       s_ref = v_top;
-      s_inv = 1.0f / v_top;
+      s_inv = kValueRoom / v_top;
     }
     float w[kTiles][8];
 #pragma unroll
@@ -357,10 +358,12 @@ struct RowTiles {
       power[g] = __uint_as_float(bits & 0x7F800000u);
       rest |= (bits & 0x7FFFFFu) != 0;
     }
-    if (rest) {
+    if (rest) {      // the power of two above the ratio (at most kValueRoom), and 1/2 to 1 of P
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
-        const float f = __uint_as_float((__float_as_uint(vs[g] * s_inv) & 0x7FFFFFu) | 0x3F800000u);
+        const uint32_t part = __float_as_uint(vs[g] * s_inv) & 0x7FFFFFu;
+        const float f = part != 0 ? __uint_as_float(part | 0x3F000000u) : 1.0f;
+        power[g] *= part != 0 ? 2.0f : 1.0f;
 #pragma unroll
         for (int i = 0; i < kTiles; ++i)
 #pragma unroll

@@ -32,6 +32,7 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTileRows = 128;
 constexpr int kStageTokens = 64;
+constexpr int kOneOfRoom = 0x3F800000 + (7 << 23);      // the bits of kValueRoom
 
 // Maximum and sum over lanes lane % 32 and lane % 32 + 32.
 __device__ __forceinline__ float over_halves_max(float x) {
@@ -109,13 +110,13 @@ struct WideRows {
       sum += w;
       p[r / 8][r % 8] = (_Float16)w;
     }
-    float power0 = __uint_as_float(max((int)(v0 - ref) + 0x3F800000, 0));
-    float power1 = __uint_as_float(max((int)(v1 - ref) + 0x3F800000, 0));
+    float power0 = __uint_as_float(max((int)(v0 - ref) + kOneOfRoom, 0));
+    float power1 = __uint_as_float(max((int)(v1 - ref) + kOneOfRoom, 0));
     // Where all rows see all tokens and the value scales are powers of two, at
     // most the largest met, the scores need no maximum: as long as their
     // exponentials' sum fits binary16, so does each.
     // (Before a row's first token m is -infinity, and the sum does not.)
-    const bool plain = whole && max(v0, v1) <= ref + (7u << 23) && ((v0 | v1 | ref) & 0x7FFFFFu) == 0;
+    const bool plain = whole && max(v0, v1) <= ref && ((v0 | v1 | ref) & 0x7FFFFFu) == 0;
     if (!plain || __any(!(sum <= 65504.0f))) {
       if (!whole) {
         const int at = first + (r0 + min(lane & 31, rows - 1)) / a.group;
@@ -134,11 +135,11 @@ struct WideRows {
       const float f = m == m_new ? 1.0f : __builtin_amdgcn_exp2f(m - m_new);      // (0 from nothing)
       l *= f;
       m = m_new;
-      const float s_new = fmaxf(fmaxf(vs0, vs1) * kValueRoom, s_ref), less = f * (s_ref / s_new);
+      const float s_new = fmaxf(fmaxf(vs0, vs1), s_ref), less = f * (s_ref / s_new);
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) o[j] *= less;
       s_ref = s_new;
-      const float s_inv = 1.0f / s_new, base = m == kNone ? 0.0f : m;
+      const float s_inv = kValueRoom / s_new, base = m == kNone ? 0.0f : m;
       const uint32_t r0 = __float_as_uint(vs0 * s_inv), r1 = __float_as_uint(vs1 * s_inv);
       sum = 0.0f;
 #pragma unroll
