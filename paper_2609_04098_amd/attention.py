@@ -10,6 +10,8 @@
 
 q, k and v are bf16 [rows, heads, head_dim] views, as a fused projection's
 output leaves them (heads side by side, any row stride that is a multiple of 8).
+There is no backward pass: a tensor that requires a gradient is refused, unless
+gradients are off (torch.no_grad(), torch.inference_mode()).
 """
 
 import ctypes
@@ -33,11 +35,18 @@ _BF16 = torch.bfloat16
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)      # (the raw query: 0.1 us less)
 
 
+def _no_gradient(name):
+    if torch.is_grad_enabled():
+        raise ValueError(name + " requires a gradient, and none passes through here")
+
+
 def _rows(x, name):
     """(rows, heads, head_dim, row stride) of a bf16 [rows, heads, head_dim]
     tensor whose heads lie side by side (the stride of a single row says nothing)."""
     if x.dtype is not _BF16 or x.dim() != 3:
         raise ValueError(name + " must be a bf16 [rows, heads, head_dim] tensor")
+    if x.requires_grad:
+        _no_gradient(name)
     rows, heads, dim = x.shape
     ld, head, one = x.stride()
     if (one != 1 or (head != dim and heads > 1)) and rows * heads * dim > 0:
@@ -95,6 +104,7 @@ class KVCache:
         for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
             _need(t.dtype == torch.float32 and t.shape == k.shape[:2] and t.stride(0) == k_scale.stride(0)
                   and (t.shape[1] == 1 or t.stride(1) == 1), "%s must be float32 [num_pages, kv_heads]" % name)
+            _need(not t.requires_grad, "%s takes no gradient here" % name)
         _need(k.device == v.device == k_scale.device == v_scale.device, "the cache's buffers are on several devices")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
         self.page_size, self.kv_heads, self.head_dim = page_size, k.shape[1], k.shape[2] // page_size
@@ -169,6 +179,8 @@ def _gamma(gamma, dim, device, name):
     """Address of a bf16 [head_dim] vector, or None."""
     if gamma is None:
         return None
+    if gamma.requires_grad:
+        _no_gradient(name)
     if gamma.dtype is not _BF16 or gamma.dim() != 1 or gamma.numel() != dim or not gamma.is_contiguous():
         raise ValueError(name + " must be bf16 [head_dim]")
     if gamma.get_device() != device:
