@@ -93,7 +93,7 @@ class KVCache:
     """A layer's paged cache over given buffers: k, v uint8 [num_pages,
     kv_heads, page_size * head_dim] in the order that nvfp4_attention.h states
     (any page stride that is a multiple of 16), k_scale, v_scale float32
-    [num_pages, kv_heads] with one row stride."""
+    [num_pages, kv_heads] with one row stride.  (Strides of a single page say nothing.)"""
 
     def __init__(self, k, v, k_scale, v_scale, page_size):
         for name, t in (("k", k), ("v", v)):
@@ -102,7 +102,8 @@ class KVCache:
             _need(t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == t.shape[2]),
                   "the heads of a page of %s must be side by side" % name)
         for name, t in (("k_scale", k_scale), ("v_scale", v_scale)):
-            _need(t.dtype == torch.float32 and t.shape == k.shape[:2] and t.stride(0) == k_scale.stride(0)
+            _need(t.dtype == torch.float32 and t.shape == k.shape[:2]
+                  and (t.stride(0) == k_scale.stride(0) or t.shape[0] == 1)
                   and (t.shape[1] == 1 or t.stride(1) == 1), "%s must be float32 [num_pages, kv_heads]" % name)
             _need(not t.requires_grad, "%s takes no gradient here" % name)
         _need(k.device == v.device == k_scale.device == v_scale.device, "the cache's buffers are on several devices")
@@ -111,6 +112,9 @@ class KVCache:
         self.device, self.index = k.device, k.get_device()
         self.softmax_scale = 1.0 / math.sqrt(self.head_dim)
         self.struct = _a.cache_struct(k, v, k_scale, v_scale, page_size)
+        if k.shape[0] == 1:
+            self.struct.k_page_stride = self.struct.v_page_stride = k.shape[1] * k.shape[2]
+            self.struct.scale_page_stride = k.shape[1]
         self.ref = ctypes.byref(self.struct)
 
     def tokens(self):

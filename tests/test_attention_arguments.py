@@ -29,3 +29,14 @@ def test_tensors_that_require_a_gradient_are_refused():
     # tensors that require none pass with gradients on
     with pytest.raises(ValueError, match="GPU"):
         A.attention(x, c, b)
+
+
+def test_a_single_page_has_any_stride():
+    buf, s = torch.zeros(4 * 16 * 64, dtype=torch.uint8), torch.zeros(8)
+    odd = [torch.as_strided(buf, (1, 2, 16 * 64), (stride, 16 * 64, 1)) for stride in (0, 7)]
+    c = A.KVCache(*odd, torch.as_strided(s, (1, 2), (0, 1)), torch.as_strided(s, (1, 2), (5, 1)), 16)
+    assert (c.struct.k_page_stride, c.struct.v_page_stride, c.struct.scale_page_stride) == (2048, 2048, 2)
+    assert c.struct.num_pages == 1
+    two = torch.as_strided(buf, (2, 1, 16 * 64), (2048, 16 * 64, 1))
+    with pytest.raises(ValueError, match="v_scale"):                # of two pages they do
+        A.KVCache(two, two, torch.zeros(2, 1), torch.as_strided(s, (2, 1), (4, 1)), 16)
