@@ -129,11 +129,13 @@ class KVCache:
 
 def alloc_kv_cache(num_pages, kv_heads, head_dim, page_size, device, scale=None):
     """An empty cache; with ``scale`` every page's scale is set to it (for
-    ``kv_append(..., static=True)``)."""
+    ``kv_append(..., static=True)``): one number, or the keys' and the values'."""
+    both = scale if isinstance(scale, (tuple, list)) else (scale, scale)
+    _need(len(both) == 2, "scale must be a number or the keys' and the values'")
     codes = [torch.empty((num_pages, kv_heads, page_size * head_dim), dtype=torch.uint8, device=device)
              for _ in range(2)]
-    scales = [torch.full((num_pages, kv_heads), 0.0 if scale is None else float(scale), dtype=torch.float32,
-                         device=device) for _ in range(2)]
+    scales = [torch.full((num_pages, kv_heads), 0.0 if s is None else float(s), dtype=torch.float32, device=device)
+              for s in both]
     return KVCache(*codes, *scales, page_size)
 
 

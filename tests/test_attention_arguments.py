@@ -40,3 +40,14 @@ def test_a_single_page_has_any_stride():
     two = torch.as_strided(buf, (2, 1, 16 * 64), (2048, 16 * 64, 1))
     with pytest.raises(ValueError, match="v_scale"):                # of two pages they do
         A.KVCache(two, two, torch.zeros(2, 1), torch.as_strided(s, (2, 1), (4, 1)), 16)
+
+
+def test_calibrated_scales_of_keys_and_of_values():
+    c = A.alloc_kv_cache(3, 2, 64, 16, "cpu", scale=(0.25, 0.5))
+    assert (c.k_scale == 0.25).all() and (c.v_scale == 0.5).all()
+    c = A.alloc_kv_cache(3, 2, 64, 16, "cpu", scale=0.125)
+    assert (c.k_scale == 0.125).all() and (c.v_scale == 0.125).all()
+    c = A.alloc_kv_cache(3, 2, 64, 16, "cpu")
+    assert not c.k_scale.any() and not c.v_scale.any()
+    with pytest.raises(ValueError, match="scale"):
+        A.alloc_kv_cache(3, 2, 64, 16, "cpu", scale=(0.25, 0.5, 1.0))
