@@ -198,6 +198,16 @@ int nvfp4_kv_attention(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
                        int64_t q_heads, void* y, int64_t ldy, float* lse, float softmax_scale, int causal,
                        int64_t window, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Which kernels nvfp4_kv_attention launches for a step (diagnostics: tests and
+ * profiles name the kernel that they mean), from the sizes alone: no device value
+ * is read.  part 0: the attention; part 1: the launch that joins its pieces.
+ * Returns a static string, or NULL where there is no such launch (no rows, a single
+ * piece) or the arguments are invalid (part not 0 or 1) or refused.
+ */
+const char* nvfp4_kv_attention_kernel(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, int64_t q_heads,
+                                      int64_t window, int part);
+
 #ifdef __cplusplus
 }
 #endif

@@ -305,3 +305,9 @@ def attention(q, cache: KVCache, batch: Batch, scale=None, causal=True, window=0
          None if lse is None else lse.data_ptr(), cache.softmax_scale if scale is None else scale, 1 if causal else 0,
          window, None if workspace is None else workspace.data_ptr(), nbytes)
     return (y, lse) if return_lse else y
+
+
+def attention_kernels(q_heads, cache: KVCache, batch: Batch, window=0):
+    """Names of the kernels that attention() launches for a step."""
+    return [name for name in (_a.kv_attention_kernel(cache.ref, batch.ref, q_heads, window, part) for part in (0, 1))
+            if name is not None]

@@ -88,6 +88,25 @@ bool valid_q_heads(int64_t q_heads, int64_t kv_heads) {
   return q_heads >= kv_heads && q_heads <= kMaxHeads && q_heads % kv_heads == 0;
 }
 
+// The kernels of a head size, in the order of kernel_name().
+#define NVFP4_KERNELS(D)                                                                            \
+  {"kv_attention_rows_kernel<" #D ",1,4,false>", "kv_attention_rows_kernel<" #D ",1,4,true>",       \
+   "kv_attention_rows_kernel<" #D ",1,8,false>", "kv_attention_rows_kernel<" #D ",2,4,false>",      \
+   "kv_attention_rows_kernel<" #D ",2,4,true>",  "kv_attention_tile_kernel<" #D ",false>",          \
+   "kv_attention_tile_kernel<" #D ",true>",      "kv_attention_join_kernel<" #D ",1,1>",            \
+   "kv_attention_join_kernel<" #D ",1,4>",       "kv_attention_join_kernel<" #D ",2,1>",            \
+   "kv_attention_join_kernel<" #D ",2,4>",       "kv_attention_join_kernel<" #D ",8,1>",            \
+   "kv_attention_join_kernel<" #D ",8,4>"}
+constexpr const char* kKernels[3][13] = {NVFP4_KERNELS(64), NVFP4_KERNELS(128), NVFP4_KERNELS(256)};
+#undef NVFP4_KERNELS
+
+const char* kernel_name(int dim, const nvfp4::AttentionPlan& p, int part) {
+  const auto& names = kKernels[dim == 64 ? 0 : dim == 128 ? 1 : 2];
+  const int split = p.splits > 1 ? 1 : 0;
+  if (part == 1) return split == 0 ? nullptr : names[7 + (p.tiles == 1 ? 0 : p.tiles == 2 ? 2 : 4) + (p.splits > 8 ? 1 : 0)];
+  return names[p.waves == 8 ? 2 : (p.tiles == 1 ? 0 : p.tiles == 2 ? 3 : 5) + split];
+}
+
 }  // namespace
 
 extern "C" {
@@ -213,6 +232,21 @@ int nvfp4_kv_attention(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
   a.window = (int)window;
   const hipError_t e = nvfp4::launch_kv_attention(a, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? NVFP4_OK : nvfp4::fail_hip(e);
+}
+
+const char* nvfp4_kv_attention_kernel(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, int64_t q_heads,
+                                      int64_t window, int part) {
+  if (!valid_cache(cache) || !valid_batch(batch, cache->page_size) || !valid_q_heads(q_heads, cache->kv_heads))
+    return nullptr;
+  if (window < 0 || window >= kI32Lim || (part != 0 && part != 1) || batch->rows * q_heads >= kI32Lim) return nullptr;
+  const nvfp4::KvCacheArgs c = cache_args(cache);
+  const nvfp4::KvBatchArgs b = batch_args(batch, cache->page_size);
+  if (b.seqs == 0 || b.rows == 0) return nullptr;
+  const int group = (int)(q_heads / cache->kv_heads);
+  nvfp4::AttentionPlan p = nvfp4::attention_plan(c, b, group, 0, nvfp4::kAnyRoom);
+  if (!nvfp4::attention_fits(c, b, group, p)) return nullptr;
+  if (window > 0) p = nvfp4::attention_plan(c, b, group, (int)window, p.splits);
+  return kernel_name(c.dim, p, part);
 }
 
 }  // extern "C"

@@ -29,6 +29,7 @@ SIGNATURES = {
     "nvfp4_kv_append": (_int, [_cache, _batch, _vp, _i64, _vp, _i64, _vp, _f, _vp, _vp, _i64, _int, _int, _vp]),
     "nvfp4_kv_attention_workspace": (_sz, [_cache, _batch, _i64]),
     "nvfp4_kv_attention": (_int, [_cache, _batch, _vp, _i64, _i64, _vp, _i64, _vp, _f, _int, _i64, _vp, _sz, _vp]),
+    "nvfp4_kv_attention_kernel": (ctypes.c_char_p, [_cache, _batch, _i64, _i64, _int]),
 }
 
 _lib = None
@@ -93,3 +94,9 @@ def kv_attention(stream, *args):
     status = (_lib or lib()).nvfp4_kv_attention(*args, _handle(stream))
     if status:
         _c._check(status, "nvfp4_kv_attention")
+
+
+def kv_attention_kernel(cache, batch, q_heads, window=0, part=0):
+    """Name of launch `part` of nvfp4_kv_attention for these sizes, or None."""
+    r = lib().nvfp4_kv_attention_kernel(cache, batch, q_heads, window, part)
+    return None if r is None else r.decode()

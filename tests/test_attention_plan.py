@@ -1,5 +1,6 @@
 """What the host decides about a step of the attention (csrc/attention_plan.h):
-steps that one launch cannot hold are refused before any HIP call.  CPU only."""
+steps that one launch cannot hold are refused before any HIP call, and the GPU tests'
+steps take the kernels that these tests mean.  CPU only."""
 
 import ctypes
 
@@ -7,6 +8,8 @@ import pytest
 
 from paper_2609_04098_amd import nvfp4 as C
 from paper_2609_04098_amd import nvfp4_attention as N
+from tests import test_gpu_attention_forms as forms
+from tests.attention_forms import EVERY, JOIN, ROWS, TILE, name, names
 from tests.test_attention_abi import _append, _attend, _batch, _cache
 
 
@@ -30,3 +33,58 @@ def test_attention_refuses_more_workgroups_than_a_launch_holds(n, heads, group):
 def test_append_refuses_more_workgroups_than_a_launch_holds(n, heads, dim, rows, page):
     c, b = _step(n, heads, dim, rows, page)
     assert _append(c, b, ldk=heads * dim, ldv=heads * dim) == C.NVFP4_EINVAL
+
+
+def _kernels(dim, page, heads, group, lens, rows, window=0, max_len=None, **kw):
+    """The kernels of a step whose tables are as wide as its longest sequence wants."""
+    width = max(1, max(-(-n // page) for n in lens))
+    c = _cache(page_size=page, head_dim=dim, kv_heads=heads, k_page_stride=heads * page * dim,
+               v_page_stride=heads * page * dim, scale_page_stride=heads)
+    b = _batch(n_seqs=len(lens), rows=rows, max_pages=width, page_table_stride=width,
+               max_kv_len=width * page if max_len is None else max_len, **kw)
+    got = [N.kv_attention_kernel(ctypes.byref(c), ctypes.byref(b), heads * group, window, part) for part in (0, 1)]
+    assert (got[1] is None) or N.lib().nvfp4_kv_attention_workspace(ctypes.byref(c), ctypes.byref(b), heads * group) > 0
+    return [k for k in got if k is not None]
+
+
+@pytest.mark.parametrize("step", EVERY, ids=name)
+def test_steps_reach_the_kernels_that_they_name(step):
+    assert _kernels(*step[:5], sum(step[5])) == names(step)
+
+
+def test_every_kernel_has_a_step():
+    got = {k for step in EVERY for k in names(step)}
+    want = {k % d for d in (64, 128, 256) for k in
+            [ROWS + "1,4,false>", ROWS + "1,4,true>", ROWS + "1,8,false>", ROWS + "2,4,false>", ROWS + "2,4,true>",
+             TILE + "false>", TILE + "true>"] + [JOIN + "%d,%d>" % (t, s) for t in (1, 2, 8) for s in (1, 4)]}
+    assert got == want and len(got) == 39
+
+
+@pytest.mark.parametrize("case", forms.TILES, ids=lambda c: "d%d_p%d_h%dx%d" % c[:4])
+def test_the_gpu_tests_of_128_rows_take_128(case):
+    """(Rows: five behind the last sequence.)"""
+    for window in (0, 50, 130, 1):
+        assert _kernels(*case[:5], sum(case[5]) + 5, window)[0].startswith(TILE % case[0])
+
+
+@pytest.mark.parametrize("dim,hkv,group,lens,counts", [
+    (256, 8, 8, [2000, 1300, 50, 1999], [60, 40, 50, 50]), (256, 32, 2, [1500, 700], [65, 65]),
+    (128, 1, 8, [60000], [8187]), (64, 1, 8, [16000], [8187])])
+def test_the_gpu_tests_of_128_rows_in_pieces_take_both(dim, hkv, group, lens, counts):
+    got = _kernels(dim, 64, hkv, group, lens, sum(counts) + 5)
+    assert got[0] == TILE % dim + "true>" and got[1].startswith(JOIN % dim + "8,")
+
+
+def test_the_kernel_query():
+    c, b = _cache(), _batch()
+    f = lambda c=c, b=b, hq=4, window=0, part=0: N.lib().nvfp4_kv_attention_kernel(
+        None if c is None else ctypes.byref(c), None if b is None else ctypes.byref(b), hq, window, part)
+    assert f() == b"kv_attention_rows_kernel<128,1,8,false>" and f(part=1) is None
+    for bad in (dict(c=None), dict(b=None), dict(hq=3), dict(window=-1), dict(window=1 << 31), dict(part=2), dict(part=-1),
+                dict(b=_batch(rows=0)), dict(b=_batch(n_seqs=0)), dict(c=_cache(head_dim=96))):
+        assert f(**bad) is None
+    # the largest steps that one launch holds, and the next ones
+    for n, heads, group, fits in (((1 << 21) - 1, 8, 5, True), (1 << 21, 8, 5, False), (3355443, 5, 1, True),
+                                  ((1 << 20) - 1, 16, 16, True), (1 << 20, 8, 17, True), (1 << 20, 8, 33, False)):
+        c, b = _step(n, heads, 128)
+        assert (f(c, b, heads * group) is not None) == fits

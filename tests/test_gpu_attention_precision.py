@@ -144,10 +144,27 @@ def _queries(case, rows, heads, scale=1.0):
     return (torch.randn(rows, heads, case.dim, generator=case.gen, device="cuda") * scale).to(torch.bfloat16)
 
 
-SINKS = [      # dim, page, key heads, group, lengths, new rows: one row and wave each, 32 rows, 128 rows, whole and in pieces
+SINKS = [      # dim, page, key heads, group, lengths, new rows (every kernel: test_gpu_attention_kernels.py)
     (128, 16, 1, 5, [300], [1]), (64, 32, 2, 4, [9000], [1]), (256, 32, 1, 4, [9000], [2]), (128, 64, 1, 8, [3000], [9]),
     (128, 32, 48, 4, [8200, 8200], [128, 128]), (256, 64, 32, 2, [4100], [260]), (64, 128, 2, 8, [8300], [5400]),
 ]
+
+
+def add_sink(case, q_heads, counts, nats, at):
+    """Queries, and keys changed so that a token at that share of each sequence's older ones, whose values become zero,
+    scores so many nats where all others score about none (with a scale of 1)."""
+    case.k[..., 0] = 0
+    for b, n in enumerate(case.lens):
+        if n == 0:
+            continue
+        p, slot = case.at(b, int((n - counts[b]) * at))
+        case.k[p, :, slot] = 0
+        case.k[p, :, slot, 0] = int(torch.tensor(16.0 * nats).to(torch.float8_e4m3fn).view(torch.uint8))
+        case.v[p, :, slot] = 0
+    case.ks.fill_(2.0 ** -4)
+    q = _queries(case, sum(counts), q_heads, 1 / 64)
+    q[..., 0] = 1.0
+    return q
 
 
 def _name(c):
@@ -162,15 +179,7 @@ def test_tokens_far_below_an_attention_sink(shape, nats):
     log("sink %s %d nats" % (shape, nats))
     for at in (0, 0.7):
         case = Case(dim, page, heads, lens, seed=dim + page + nats)
-        case.k[..., 0] = 0
-        for b, n in enumerate(lens):
-            p, slot = case.at(b, int((n - counts[b]) * at))
-            case.k[p, :, slot] = 0
-            case.k[p, :, slot, 0] = int(torch.tensor(16.0 * nats).to(torch.float8_e4m3fn).view(torch.uint8))
-            case.v[p, :, slot] = 0
-        case.ks.fill_(2.0 ** -4)
-        q = _queries(case, sum(counts), heads * group, 1 / 64)
-        q[..., 0] = 1.0
+        q = add_sink(case, heads * group, counts, nats, at)
         _run(case, q, counts, scale=1.0)
 
 
