@@ -26,13 +26,24 @@ struct AttentionPlan {
 };
 
 // Row tiles: a workgroup takes 16 rows where an average sequence has no more.  It
-// takes 128 where sequences have over 64 and there are enough rows to fill the
-// compute units with such workgroups (heads of 256, whose smaller tiles have a compute
-// unit's registers to themselves: few), more of them for long sequences,
-// where a workgroup that is alone takes long; else 32.  Full tiles times key heads, and
-// the times in tiles of 32 and of 128 rows: heads of 128, 400 of 1500 tokens 74 and 62
-// us, 503 of 447 39 and 22 us, 375 of 3000 104 and 107 us, 192 of 967 29 and 31 us;
-// heads of 256, 81 of 856 40 and 36 us, 31 of 8000 98 and 59 us, 62 of 1000 27 and 31.
+// takes 128 where sequences have over 64 and the full tiles of 128 rows times key
+// heads are enough, by the largest length; else 32.  Largest length, full
+// tiles, and the times in tiles of 32 and of 128 rows (us); the last of each line has
+// ragged lengths:
+//   heads of 64     447 tokens, 260: 18.1 20.0   447, 400: 22.6 19.8   700, 260: 22.6 27.7
+//                   700, 900: 47.4 40.5   3000, 600: 108 121   3000, 1000: 160 150
+//                   16000, 512: 420 409 (one sequence 330 402)   40000, 512: 1028 963
+//                   40000, 800: 1628 1809   40000, 900: 1864 1827   3000, 806: 83 99
+//                   (beyond 10000 tokens neither form is the faster one throughout)
+//   heads of 128    447, 130: 22.1 20.1   447, 260: 31.1 26.9   967, 260: 42.9 46.1
+//                   967, 400: 56.9 46.7   1500, 260: 55.0 68.5   1500, 560: 93.8 83.8
+//                   3000, 260: 91 105   3000, 650: 186 164   8000, 512: 347 391   1500, 346: 51 70
+//   heads of 256    (32 rows have a compute unit to themselves: one round of 256 workgroups up
+//                   to 64)  967, 50: 27.4 37.8   967, 66: 50.5 43.1   2500, 50: 45.9 64.6
+//                   2500, 66: 87 64   4000, 66: 124 87   16000, 30: 159 97   16000, 46: 208 144
+// Of 440 such steps (1 to 8 sequences, half of them ragged) the rule takes the faster
+// form, or one within 5%, in 387, and one within 15% in 423; the worst are (128, 24000
+// tokens, 130 full tiles) 374 us for 271 and (64, 40000, 556, ragged) 1270 for 939.
 // Pieces: the number of them for which an estimate of the time is least, of a
 // step whose sequences all have the largest length and of one that has 0.55 times
 // as many workgroups (lengths of all sizes), together.  (Its figures are those that
@@ -45,7 +56,9 @@ inline AttentionPlan attention_plan(const KvCacheArgs& c, const KvBatchArgs& b, 
   const int64_t seqs = b.seqs > 0 ? b.seqs : 1, rows = ((int64_t)b.rows * group + seqs - 1) / seqs;
   const auto of_rows = [&](int tile) { return (rows + tile - 1) / tile; };
   const double full = (double)b.rows * group * c.heads / 128.0;
-  const double enough = c.dim == 256 ? (b.max_kv_len < 2000 ? 64.0 : 24.0) : (b.max_kv_len < 1600 ? 330.0 : 480.0);
+  const double enough = c.dim == 256   ? (b.max_kv_len < 3500 ? 65.0 : 24.0)
+                        : c.dim == 128 ? (b.max_kv_len < 600 ? 150.0 : b.max_kv_len < 1600 ? 400.0 : 480.0)
+                                       : (b.max_kv_len < 600 ? 330.0 : b.max_kv_len < 10000 ? 850.0 : 500.0);
   p.tiles = rows <= 16 ? 1 : rows > 64 && full >= enough ? 8 : 2;
   const int64_t each_seq = of_rows(16 * p.tiles), work = each_seq * seqs * c.heads;
   // Workgroups of four waves that the estimate counts on a compute unit at a time.
@@ -123,7 +136,17 @@ inline size_t part_bytes(const KvCacheArgs& c, const KvBatchArgs& b, int group, 
   return (size_t)(host_tiles(b, group, 16 * p.tiles) * c.heads * p.splits * 16 * p.tiles) * (c.dim + 2) * sizeof(float);
 }
 
-// The append's form and workgroups.
+// The append's form and workgroups.  Few rows: under 5 for a sequence, of which the
+// host knows no more.  128 sequences of the same n rows, 8 heads of 128, a token at a
+// time and in whole pages (us), pages of 16, 32, 64 and 128:
+//   n = 1    8.1  9.3     8.0  9.1     7.9 12.4     8.1 24.9
+//   n = 4    8.1  9.1     8.1  9.8     8.0 12.1    11.5 15.4
+//   n = 8    8.7 13.2    10.2 10.7    11.1 20.1    11.0 17.9
+//   n = 16  15.9 14.8    16.8 12.0    16.8 15.0    18.9 19.5
+// but a prompt among single tokens, whose pages are a workgroup's of four waves each,
+//   100 x 1 + 500 (5.9 on average)  11.3 11.0   18.5 12.3   33.1 19.5   63.7 38.3
+//   30 x 1 + 100 (4.2)              10.5  8.2   17.9  8.2   32.6  9.1   40.3 15.4
+// so that 5 gives up the former from 5 to 8 rows, and the latter below 5.
 struct AppendPlan {
   bool tokens;             // a token at a time (few rows)
   int each;                // many rows: heads of a workgroup

@@ -15,9 +15,8 @@
 // compute unit: 74 us; with 16 a lane 31.)
 // Few rows (under 5 for a sequence): four waves for each touched page, keys or
 // values, and as many heads as a wave has lanes for (512 / D), a token at a time
-// each; the codes are stored from registers.  96 sequences, 8 heads of 128, of 1, 4
-// and 16 tokens: 6.8, 7.0 and (30 sequences) 9.1 us, in the other form 9.2, 9.5 and
-// 8.2; 100 of one and one of 500: 18.4 and 12.5 (with one wave for a page 54).
+// each; the codes are stored from registers.  (The rule and both sides' times:
+// attention_plan.h.)
 //
 // Keys are computed in binary64: an 8-bit rounding turns the last bit of a
 // binary32 value that is next to a border into a step of 6 to 12 %, and binary64

@@ -26,7 +26,7 @@ EVERY = [
     (64, 32, 16, 8, [300, 0, 220], [200, 0, 180], TILE + "false>", None),
     (128, 32, 16, 8, [300, 0, 220], [200, 0, 180], TILE + "false>", None),
     (256, 32, 8, 8, [100, 90], [70, 75], TILE + "false>", None),
-    (64, 64, 4, 4, [30000], [3900], TILE + "true>", JOIN + "8,1>"),
+    (64, 64, 1, 8, [16000], [8187], TILE + "true>", JOIN + "8,1>"),
     (128, 64, 4, 4, [30000], [3900], TILE + "true>", JOIN + "8,1>"),
     (256, 32, 8, 8, [600, 400], [70, 66], TILE + "true>", JOIN + "8,1>"),
     (64, 64, 2, 64, [87000], [548], TILE + "true>", JOIN + "8,4>"),

@@ -60,19 +60,31 @@ def test_every_kernel_has_a_step():
     assert got == want and len(got) == 39
 
 
-@pytest.mark.parametrize("case", forms.TILES, ids=lambda c: "d%d_p%d_h%dx%d" % c[:4])
+@pytest.mark.parametrize("case", [c for c in forms.TILES if c[0] != 64], ids=lambda c: "d%d_p%d_h%dx%d" % c[:4])
 def test_the_gpu_tests_of_128_rows_take_128(case):
-    """(Rows: five behind the last sequence.)"""
+    """(Rows: five behind the last sequence.  Heads of 64: EVERY's.)"""
     for window in (0, 50, 130, 1):
         assert _kernels(*case[:5], sum(case[5]) + 5, window)[0].startswith(TILE % case[0])
 
 
 @pytest.mark.parametrize("dim,hkv,group,lens,counts", [
-    (256, 8, 8, [2000, 1300, 50, 1999], [60, 40, 50, 50]), (256, 32, 2, [1500, 700], [65, 65]),
-    (128, 1, 8, [60000], [8187]), (64, 1, 8, [16000], [8187])])
+    (256, 8, 8, [2000, 1300, 50, 1999], [60, 40, 50, 50]), (256, 32, 2, [1500, 700], [65, 65]), (128, 1, 8, [60000], [8187]),
+    (64, 1, 8, [16000], [8187])])
 def test_the_gpu_tests_of_128_rows_in_pieces_take_both(dim, hkv, group, lens, counts):
     got = _kernels(dim, 64, hkv, group, lens, sum(counts) + 5)
     assert got[0] == TILE % dim + "true>" and got[1].startswith(JOIN % dim + "8,")
+
+
+@pytest.mark.parametrize("dim,longest,full", [(64, 599, 330), (64, 600, 850), (64, 9999, 850), (64, 1 << 20, 500), (128, 599, 150),
+                                              (128, 600, 400), (128, 1599, 400), (128, 1600, 480), (256, 3499, 65),
+                                              (256, 3500, 24)])
+def test_where_tiles_of_128_rows_begin(dim, longest, full):
+    for heads, group in ((1, 128), (4, 32), (2, 64)):
+        rows = full * 128 // (heads * group)
+        for n, tile in ((rows, TILE), (rows - 1, ROWS)):
+            assert _kernels(dim, 16, heads, group, [longest], n, max_len=longest)[0].startswith(tile % dim)
+    # never for sequences of up to 64 packed rows
+    assert _kernels(dim, 16, 8, 4, [longest] * 1000, 16000, max_len=longest)[0].startswith(ROWS % dim)
 
 
 def test_the_kernel_query():
