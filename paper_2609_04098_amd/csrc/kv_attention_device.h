@@ -36,17 +36,18 @@ namespace nvfp4 {
 constexpr int kTileTokens = 32;
 constexpr float kNone = -__builtin_inff();
 
-// The largest P is 2^kAbove, within half a power of two.  The tile kernel takes
-// 16 of them before it looks for a maximum, so no more than 2^11 would do; with 10, a
-// score may pass the largest by 5.5 until it does, as one in the other kernels (to
-// kHighest: 2^15.9 < 65504).
+// The largest P is 2^kAbove where m was last set.  The tile kernel takes 16 of them
+// before it looks for a maximum, so no more than 2^11 would do; with 10, a score may
+// pass the largest by 6 until it does, and by 5.9 in the other kernels (to kHighest:
+// 2^15.9 < 65504).
 constexpr float kAbove = 10.0f, kHighest = 15.9f;
 constexpr float kValueRoom = 128.0f;               // 448 * 2^7 < 65504
 constexpr float kSmallest = 0x1p-119f;             // of s_ref: over kValueRoom, a normal number
 
-// The running m for a largest score: a whole number, so that what it is changed by
-// is exact.  (Scores that have no fraction left, and -infinity, stay.)
-__device__ __forceinline__ float reference(float top) { return fabsf(top) < 16777216.0f ? rintf(top) - kAbove : top; }
+// The running m for a largest score, whose own P is then 2^kAbove without a rounding
+// (it weighs most; with m a whole number, 9% of y were off by a step of bf16 where
+// it is 7%).  Scores that have no fraction left, and -infinity, stay.
+__device__ __forceinline__ float reference(float top) { return fabsf(top) < 16777216.0f ? top - kAbove : top; }
 
 // The first token that token t's row sees of a window of at least 1 (below 0: all).
 // (A t below 0 counts as 0, so that no window below 2^31 takes it out of 32 bits.)
