@@ -6,10 +6,10 @@
 // loaded by direct loads one tile ahead and read by all four waves.
 //
 // Bound by the instructions that a SIMD issues (one in four cycles, vector or
-// matrix; an exponential takes two turns), 178 vector and 16 matrix instructions
+// matrix; an exponential takes two turns), 168 vector and 16 matrix instructions
 // for 32 rows, 32 tokens and a head of 128: 8192 tokens, 40 heads of 128, causal,
-// take 690 us, 1.0 PFLOP/s, with the vector units busy 73% of the time and the
-// matrix units 47%.  So the products are the largest there are:
+// take 705 us, 0.97 PFLOP/s, with the vector units busy 74% of the time and the
+// matrix units 46%.  So the products are the largest there are:
 //   S^T = K Q^T by v_mfma_f32_32x32x16_bf16, Y^T += V^T P^T by
 //   v_mfma_f32_32x32x16_f16, on keys and values converted on the way.
 // With the products transposed a lane holds the scores of ONE row, for the
@@ -17,10 +17,10 @@
 // product wants just these of it: of 16 tokens, its contraction indexes 8 h + e
 // and 8 h + 4 + e are the tokens 4 h + e and 8 + 4 h + e.  So P never leaves its
 // lane.  (The keys as they are, with Q in two E4M3 parts, by
-// v_mfma_scale_f32_32x32x64_f8f6f4 would take 32 conversions of 180 instructions
+// v_mfma_scale_f32_32x32x64_f8f6f4 would take 32 conversions of 184 instructions
 // off; that instruction drops what is 2^-16 below the largest of 8 products.)
-// (64 tokens a pass, two score tiles in registers and two waves a SIMD: 739 us;
-// keys and values converted once into LDS for the four waves: 857 us.)
+// (At 690 us: 64 tokens a pass, two score tiles in registers and two waves a SIMD, 739;
+// keys and values converted once into LDS for the four waves, 857.)
 //
 // Running maximum, sums and scales: as in kv_attention_device.h.
 #include "kv_attention_device.h"
