@@ -17,8 +17,9 @@
 // kilobyte for each wave.
 //
 // m is kept kAbove below the largest score met, whose P is then about 2^kAbove: so
-// P uses binary16's range up to its end, and a token keeps its 11 bits down to 2^-23
-// of the largest P and is off by 2^-34 of that below.  With a largest P of 1, tokens
+// P uses binary16's range up to its end, and a token keeps its 11 bits down to 2^-24
+// of the largest P and is off by 2^-35 of that below (twice that where P takes a part
+// of a value scale, below).  With a largest P of 1, tokens
 // behind an attention sink were lost from Y but not from l (8192 tokens 17 nats
 // below one whose values are zero: Y 41% off; now 0.1%).
 //
@@ -45,8 +46,8 @@ constexpr float kValueRoom = 128.0f;               // 448 * 2^7 < 65504
 constexpr float kSmallest = 0x1p-119f;             // of s_ref: over kValueRoom, a normal number
 
 // The running m for a largest score, whose own P is then 2^kAbove without a rounding
-// (it weighs most; with m a whole number, 9% of y were off by a step of bf16 where
-// it is 7%).  Scores that have no fraction left, and -infinity, stay.
+// (it weighs most; with m a whole number, 7.5 to 9% of y were one step of bf16 beside
+// the rounded exact value, so 5 to 7%).  Scores that have no fraction left, and -infinity, stay.
 __device__ __forceinline__ float reference(float top) { return fabsf(top) < 16777216.0f ? top - kAbove : top; }
 
 // The first token that token t's row sees of a window of at least 1 (below 0: all).
