@@ -1,0 +1,57 @@
+"""ctypes binding of the paging entry points of libnvfp4.so
+(include/nvfp4_paging.h): argument marshalling only.
+"""
+
+import ctypes
+
+from . import nvfp4 as _c
+from .nvfp4_attention import _f, _handle, _i64, _int, _sz, _vp
+
+
+class RequestsStruct(ctypes.Structure):
+    _fields_ = [("page_table", _vp), ("kv_len", _vp), ("free_pages", _vp), ("free_count", _vp),
+                ("page_table_stride", _i64), ("max_pages", _i64), ("n_seqs", _i64), ("num_pages", _i64),
+                ("page_size", _i64)]
+
+
+_requests = ctypes.POINTER(RequestsStruct)
+
+# name -> (restype, argtypes), in the order of include/nvfp4_paging.h
+SIGNATURES = {
+    "nvfp4_step_tables_workspace": (_sz, [_i64]),
+    "nvfp4_step_tables": (_int, [_requests, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp]),
+}
+
+_lib = None
+
+
+def lib():
+    """The loaded library with the paging entry points declared."""
+    global _lib
+    if _lib is None:
+        l = _c.lib()
+        for name, (res, args) in SIGNATURES.items():
+            fn = getattr(l, name)
+            fn.restype, fn.argtypes = res, args
+        _lib = l
+    return _lib
+
+
+def requests_struct(page_table, kv_len, free_pages, free_count, page_size):
+    """page_table int32 [n_seqs, max_pages]; kv_len int32 [n_seqs]; free_pages
+    int32 [num_pages]; free_count int32 [1]."""
+    return RequestsStruct(page_table.data_ptr(), kv_len.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+                          page_table.stride(0), page_table.shape[1], kv_len.shape[0], free_pages.shape[0], page_size)
+
+
+def step_tables_workspace(n_seqs):
+    return lib().nvfp4_step_tables_workspace(n_seqs)
+
+
+def step_tables(stream, *args):
+    """nvfp4_step_tables: its arguments in order, addresses as integers (or None), the
+    structure by reference, after the stream: a torch stream, a handle or None (the
+    current one)."""
+    status = (_lib or lib()).nvfp4_step_tables(*args, _handle(stream))
+    if status:
+        _c._check(status, "nvfp4_step_tables")

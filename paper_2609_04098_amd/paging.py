@@ -1,0 +1,109 @@
+"""Serving over the paged 8-bit cache of ``attention``, on top of the C ABI
+(include/nvfp4_paging.h): argument checks, buffers and call order only.
+
+    requests = alloc_requests(n_seqs, max_pages, num_pages, page_size, device)   # once: lengths, pages, the pool
+    step = step_tables(requests, new_rows, rows, drop)    # per step: page tables, row offsets, positions, slots
+    attention.kv_append(cache, step.batch, k, v, ...)
+
+Lengths stay on the GPU: nothing here waits for it, and every call may be captured
+into a graph.  There is no backward pass, as in ``attention``.
+"""
+
+import ctypes
+
+import torch
+
+from . import attention as _at
+from . import linear as _l
+from . import nvfp4_paging as _p
+from .attention import _need, _run
+
+_I32 = torch.int32
+
+
+def _vector(t, n, device, name):
+    """Address of an int32 [n] vector on the device, or None."""
+    if t is None:
+        return None
+    if t.dtype is not _I32 or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise ValueError(name + " must be int32, one number for each sequence")
+    if t.get_device() != device:
+        raise ValueError(name + " is on another device")
+    return t.data_ptr()
+
+
+class Requests:
+    """The sequences of a serving loop over given buffers, all on one GPU:
+    page_table int32 [n_seqs, max_pages], kv_len int32 [n_seqs] (tokens held),
+    free_pages int32 [num_pages] of which the first free_count [1] are the free pages'
+    numbers (the last of them the next to be taken)."""
+
+    def __init__(self, page_table, kv_len, free_pages, free_count, page_size):
+        _need(page_size in (16, 32, 64, 128), "page_size must be 16, 32, 64 or 128")
+        _need(page_table.dtype == _I32 and page_table.dim() == 2
+              and (page_table.shape[1] <= 1 or page_table.stride(1) == 1), "page_table must be int32 [n_seqs, max_pages]")
+        _need(kv_len.dtype == _I32 and kv_len.shape == page_table.shape[:1] and kv_len.is_contiguous(),
+              "kv_len must be int32 [n_seqs]")
+        _need(free_pages.dtype == _I32 and free_pages.dim() == 1 and free_pages.shape[0] > 0
+              and free_pages.is_contiguous(), "free_pages must be int32 [num_pages]")
+        _need(free_count.dtype == _I32 and free_count.shape == (1,), "free_count must be int32 [1]")
+        _need(page_table.device == kv_len.device == free_pages.device == free_count.device,
+              "the requests' tensors are on several devices")
+        _need(page_table.shape[0] <= 1 or page_table.stride(0) >= page_table.shape[1],
+              "rows of page_table must not overlap")
+        self.page_table, self.kv_len, self.free_pages, self.free_count = page_table, kv_len, free_pages, free_count
+        self.page_size, self.n_seqs = page_size, kv_len.shape[0]
+        self.device, self.index = kv_len.device, kv_len.get_device()
+        self.struct = _p.requests_struct(page_table, kv_len, free_pages, free_count, page_size)
+        if self.n_seqs <= 1:
+            self.struct.page_table_stride = page_table.shape[1]      # (the stride of a single row says nothing)
+        self.ref = ctypes.byref(self.struct)
+
+
+def alloc_requests(n_seqs, max_pages, num_pages, page_size, device):
+    """Sequences without tokens, all pages free (page 0 is the first to be taken)."""
+    return Requests(torch.zeros((n_seqs, max_pages), dtype=_I32, device=device),
+                    torch.zeros(n_seqs, dtype=_I32, device=device),
+                    torch.arange(num_pages - 1, -1, -1, dtype=_I32, device=device),
+                    torch.full((1,), num_pages, dtype=_I32, device=device), page_size)
+
+
+class Step:
+    """A step's tables: ``batch`` (what kv_append and the attentions take, over the
+    requests' page_table and kv_len), ``positions`` int32 [rows], ``slots`` int64 [rows]
+    (page * page_size + slot).  ``batch.cu_rows`` says which rows each sequence got."""
+
+    def __init__(self, requests, rows, max_len=None):
+        n, device = requests.n_seqs, requests.device
+        self.requests, self.rows, self.max_len = requests, int(rows), max_len
+        cu_rows = torch.empty(n + 1, dtype=_I32, device=device)
+        self.batch = _at.Batch(requests.page_table, requests.kv_len, cu_rows, rows=self.rows, max_len=max_len)
+        self.positions = torch.empty(self.rows, dtype=_I32, device=device)
+        self.slots = torch.empty(self.rows, dtype=torch.int64, device=device)
+        nbytes = _p.step_tables_workspace(n)
+        self._workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self._args = (cu_rows.data_ptr(), self.positions.data_ptr(), self.slots.data_ptr(), self.rows,
+                      self._workspace.data_ptr(), nbytes)
+
+
+def step_tables(requests: Requests, new_rows, rows, drop=None, kept=None, max_len=None, out: Step = None, stream=None):
+    """Takes ``drop`` tokens (int32 [n_seqs], or None) off the sequences' ends and adds
+    ``new_rows`` (int32 [n_seqs]) to them: pages go back to the pool and come from it,
+    page_table, kv_len and the pool change in place.  ``rows``: rows of the step's
+    tensors.  ``kept``: tokens in front of each sequence whose pages never go back (a
+    shared prefix).  From the first sequence for which pages or rows are missing on,
+    none gets rows; one that its row of page_table cannot hold gets none either.
+    ``out``: a Step of an earlier call, whose buffers are written again (always in a
+    captured loop); ``max_len`` as for Batch."""
+    device = requests.index
+    if out is None:
+        with _l._on(stream, requests.device):
+            out = Step(requests, rows, max_len)
+    elif out.requests is not requests or out.rows != rows or out.max_len != max_len:
+        raise ValueError("out is a step of other requests, rows or max_len")
+    n = requests.n_seqs
+    if new_rows is None:
+        raise ValueError("new_rows must be given")
+    _run(device, _p.step_tables, stream, requests.ref, _vector(new_rows, n, device, "new_rows"),
+         _vector(drop, n, device, "drop"), _vector(kept, n, device, "kept"), *out._args)
+    return out
