@@ -1,7 +1,7 @@
 /*
  * nvfp4_paging.h -- C ABI of serving over the paged 8-bit cache of
  * nvfp4_attention.h: the tables of a step made on the GPU from the requests'
- * lengths.
+ * lengths, and the attention of batches whose sequences share prefixes.
  *
  * Conventions are those of nvfp4_attention.h: device pointers owned by the
  * caller, synchronous checks before anything is enqueued, work enqueued on
@@ -87,6 +87,51 @@ size_t nvfp4_step_tables_workspace(int64_t n_seqs);
 int nvfp4_step_tables(const nvfp4_requests* requests, const int32_t* new_rows, const int32_t* drop, const int32_t* kept,
                       int32_t* cu_rows, int32_t* positions, int64_t* slots, int64_t rows, void* workspace,
                       size_t workspace_bytes, void* stream);
+
+/*
+ * Groups of a step's sequences that share a prefix: sequences [cu_seqs[g],
+ * cu_seqs[g + 1]) of the batch begin with the same prefix[g] tokens, in the same pages
+ * (their rows of page_table agree that far).  Sequences in front of cu_seqs[0] or from
+ * cu_seqs[n_groups] on are in no group.
+ *
+ *   cu_seqs      device int32 [n_groups + 1], not decreasing.
+ *   prefix       device int32 [n_groups]: tokens.
+ *   n_groups     0 <= n_groups <= n_seqs.
+ *   max_prefix   the largest prefix, and
+ *   max_own      the largest number of tokens of a sequence behind its prefix, as far as
+ *                the host knows them: work is divided by them (larger ones are computed
+ *                all the same, with less of them side by side).
+ */
+typedef struct nvfp4_shared_prefix {
+  const int32_t* cu_seqs;
+  const int32_t* prefix;
+  int64_t n_groups;
+  int64_t max_prefix;
+  int64_t max_own;
+} nvfp4_shared_prefix;
+
+/* Workspace bytes of nvfp4_kv_attention_shared (partial results); 0: the batch has no
+ * rows, or the arguments are invalid. */
+size_t nvfp4_kv_attention_shared_workspace(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
+                                           const nvfp4_shared_prefix* shared, int64_t q_heads);
+
+/*
+ * nvfp4_kv_attention (without a window) of a batch whose sequences share prefixes: the
+ * same result, with each prefix read once for all sequences of its group.  A sequence
+ * shares where all its rows lie behind the prefix (kv_len[b] - n_b >= prefix[g]); the
+ * prefix is then read through the row of page_table of the group's first sequence that
+ * does.  A sequence that does not, one that is empty for instance, is computed over its
+ * own row of page_table alone.  Accuracy: as stated there, for each of the two parts.
+ *
+ *   workspace, workspace_bytes   at least nvfp4_kv_attention_shared_workspace bytes,
+ *                16-byte aligned.  Its contents on entry do not matter; calls sharing
+ *                one must be ordered.
+ * The others, and the requirements, as for nvfp4_kv_attention.
+ * Errors: NVFP4_EINVAL, NVFP4_EWORKSPACE, NVFP4_EUNSUPPORTED, NVFP4_EHIP.
+ */
+int nvfp4_kv_attention_shared(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_shared_prefix* shared,
+                              const void* q, int64_t ldq, int64_t q_heads, void* y, int64_t ldy, float* lse,
+                              float softmax_scale, int causal, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -56,6 +56,7 @@ struct AppendArgs {
 };
 
 struct AttentionArgs {
+  static constexpr bool kParts = false;      // a piece that is all its rows see writes their results
   KvCacheArgs cache;
   KvBatchArgs batch;
   const uint16_t* q;

@@ -108,6 +108,9 @@ __device__ __forceinline__ int64_t tiles_of(const KvBatchArgs& a, int group, int
                               : (int64_t)a.rows * group / rows + a.seqs;
 }
 
+// Tiles that partial results are kept for.
+__device__ __forceinline__ int64_t part_tiles(const AttentionArgs& a, int rows) { return tiles_of(a.batch, a.group, rows); }
+
 // At the end: s_ref becomes what Y is multiplied by for a largest P of 1; the result,
 // what Y is multiplied by before that: 1, but where s_ref over l might otherwise be no
 // normal number (value scales below 2^-89).

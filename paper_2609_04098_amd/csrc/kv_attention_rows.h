@@ -1,0 +1,174 @@
+// The attention of one workgroup of few rows (kv_attention.hip; with shared prefixes
+// kv_attention_shared.hip, over selected pages kv_attention_selected.hip).  Args says which
+// rows and tokens a workgroup takes and where pages stand: find_tile(), group_pages()
+// and part_tiles() of its type; Args::kParts: all results are partial ones.
+#pragma once
+
+#include "kv_attention_device.h"
+
+namespace nvfp4 {
+
+// Registers: the waves of a SIMD that a kernel of these forms is compiled for.
+constexpr int rows_waves(int dim, int tiles, int waves, bool split) {
+  return waves > 4 ? 2 : dim == 256 && split ? 1 : dim == 256 ? 3 - tiles : 4 - tiles;
+}
+
+// Keys and values of one tile of 32 tokens, as loaded: [group of 16][64
+// elements of the head].
+template <int D>
+struct TileCodes {
+  u32x4 k[2][D / 64], v[2][D / 64];
+};
+
+template <int D>
+__device__ __forceinline__ void load_codes(const AttentionArgs& a, int kind, int h, int token, int page0, int page1,
+                                           int lane, u32x4 (&to)[2][D / 64]) {
+  const int mask = a.cache.page_size - 1;
+  const int64_t head = (int64_t)h * a.cache.page_size * D;
+#pragma unroll
+  for (int g = 0; g < 2; ++g) {
+    const int page = g ? page1 : page0, slot = (token + 16 * g) & mask;
+    const uint8_t* from = a.cache.kv[kind] + (int64_t)max(page, 0) * a.cache.page_stride[kind] + head + slot * D;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) to[g][c] = *reinterpret_cast<const u32x4*>(from + c * 1024 + lane * 16);
+  }
+}
+
+// The next tile's keys are loaded where this one's have been read, and so the values:
+// one tile's registers, and a load's latency to cover either.  (Two tiles' registers,
+// loaded a whole tile ahead: 60 sequences of 2000 tokens, 4 key heads of 64, 17.0 us;
+// so 13.7.  Heads of 256 through a ring of two tiles in LDS: 40 of up to 2500, 3 key
+// heads, 32 us; so 25.)
+// Workgroups of eight waves, and those that take pieces of heads of 256, have a
+// compute unit to themselves, though registers would let in two: those that short
+// sequences leave empty make room for others then, and two long ones do not share a
+// unit (16 sequences of up to 32768, 4 key heads of 256, in four pieces: 105 us, two
+// to a unit 173; 32 of 3000, 8 key heads of 128, eight waves: 38 and 48 us).
+template <int D, int kTiles, int kWaves, bool kSplit, typename Args>
+__device__ __forceinline__ void attention_rows(Args a) {
+  constexpr int kRows = 16 * kTiles, kThreads = kWaves * 64;
+  constexpr int kPart = kWaves > 4 ? 64 : (D > 128 ? 128 : D);            // elements of a row that are joined at a time
+  __shared__ struct {
+    float joined[kWaves][16][kPart + 4];
+    char alone[kWaves > 4 || (D == 256 && kTiles == 1 && kSplit) ? 65536 : 1];      // (so that they have)
+  } lds;
+  __shared__ float2 stats[kWaves][kRows];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, quarter = lane >> 4;
+  int id = blockIdx.x;
+  const int h = id % a.cache.heads;
+  id /= a.cache.heads;
+  const int number = kSplit ? id / a.splits : id;
+  const int piece = kSplit ? piece_of(id % a.splits, number, a.splits) : 0;
+  Tile t;
+  if (!find_tile<kRows>(a, number, t)) return;
+  int begin = t.begin, end = t.end;
+  bool whole = !Args::kParts;    // this piece is all that the rows see
+  if (kSplit) {
+    const int pieces = pieces_of(a, t);
+    if (piece >= pieces) return;
+    whole = whole && pieces == 1;
+    piece_tokens(a, t, piece, begin, end);
+  }
+
+  RowTiles<D, kTiles> rows;
+  rows.start(a, t, h, t.r0, t.n, lane, begin, end);
+  const float scale = fabsf(a.scale);
+
+  const int step = kWaves * kTileTokens;
+  int token = (begin & ~(kTileTokens - 1)) + wave * kTileTokens;
+  GroupPages pages = group_pages(a, t.b, h, (int64_t)token + (lane >> 1) * step + (lane & 1) * 16, begin, end);
+  int in_batch = 0;
+  // The tile's scales; then the next batch of pages, if the next tile needs it.
+  const auto scales = [&](bool (&there)[2], float (&ks)[2], float (&vs)[2]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      there[g] = __builtin_amdgcn_readlane(pages.page, 2 * in_batch + g) >= 0;
+      ks[g] = fmaxf(lane_of(pages.k_scale, 2 * in_batch + g) * scale, 1e-37f);      // (not 0: -infinity stays)
+      vs[g] = lane_of(pages.v_scale, 2 * in_batch + g);
+    }
+    if (++in_batch == 32) {
+      pages = group_pages(a, t.b, h, (int64_t)token + step + (lane >> 1) * step + (lane & 1) * 16, begin, end);
+      in_batch = 0;
+      // (Waited for here, or the compiler would, and with them for the tile's values,
+      // in front of every tile.)
+      __builtin_amdgcn_s_waitcnt(wait_loads(0));
+    }
+  };
+  bool there[2];
+  float ks[2], vs[2];
+  const auto load = [&](int kind, int at, u32x4(&to)[2][D / 64]) __attribute__((always_inline)) {
+    load_codes<D>(a, kind, h, at, __builtin_amdgcn_readlane(pages.page, 2 * in_batch),
+                  __builtin_amdgcn_readlane(pages.page, 2 * in_batch + 1), lane, to);
+  };
+  // (No branch around the loads, where the compiler would wait for whatever may be
+  // outstanding on one of its paths: behind the end they read a page that is there.)
+  TileCodes<D> now;
+  load(0, token, now.k);
+  load(1, token, now.v);
+  while (token < end) {
+    scales(there, ks, vs);
+    rows.pass(
+        a, token, there[0], there[1], ks, vs, lane, [&](int g, int c) { return now.k[g][c]; },
+        [&](int g, int c) { return now.v[g][c]; }, [&]() __attribute__((always_inline)) { load(0, token + step, now.k); },
+        [&]() __attribute__((always_inline)) { load(1, token + step, now.v); });
+    token += step;
+  }
+
+  // The waves' results, joined: Y = sum_w 2^(m_w - m) Y_w.
+  rows.finish();
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    if (quarter == 0) stats[wave][16 * i + col] = make_float2(rows.m[i], rows.l[i]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kTiles; ++i) {
+    float m_all = kNone, l_all = 0.0f;
+    for (int w = 0; w < kWaves; ++w) m_all = fmaxf(m_all, stats[w][16 * i + col].x);
+    const float zero_m = m_all == kNone ? 0.0f : m_all;
+    for (int w = 0; w < kWaves; ++w)
+      l_all += stats[w][16 * i + col].y * __builtin_amdgcn_exp2f(stats[w][16 * i + col].x - zero_m);
+    float mine = __builtin_amdgcn_exp2f(rows.m[i] - zero_m) * rows.s_ref;
+    if (whole) mine *= l_all == 0.0f ? 0.0f : 1.0f / l_all;
+    const int r = t.r0 + 16 * i + col;
+    if (threadIdx.x < 16 && 16 * i + col < t.n) {
+      if (!whole) {
+        float2* to = reinterpret_cast<float2*>(a.part) + (((int64_t)number * a.cache.heads + h) * a.splits + piece) * kRows;
+        to[16 * i + col] = make_float2(m_all, l_all);
+      } else if (a.lse != nullptr) {
+        a.lse[(int64_t)(t.row0 + r / a.group) * a.q_heads + h * a.group + r % a.group] =
+            l_all == 0.0f ? kNone : (m_all + __builtin_amdgcn_logf(l_all)) * 0.69314718055994531f;
+      }
+    }
+#pragma unroll
+    for (int d0 = 0; d0 < D; d0 += kPart) {
+      if (i > 0 || d0 > 0) __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kPart / 16; ++j)
+        *reinterpret_cast<f32x4*>(&lds.joined[wave][col][16 * j + 4 * quarter]) = rows.o[i][d0 / 16 + j] * mine;
+      __syncthreads();
+      // A thread takes four elements of one row.
+      for (int x = threadIdx.x; x < 16 * kPart / 4; x += kThreads) {
+        const int row = 16 * i + x / (kPart / 4), e = (x % (kPart / 4)) * 4;
+        if (row >= t.n) continue;
+        f32x4 y = (f32x4){0, 0, 0, 0};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) y += *reinterpret_cast<const f32x4*>(&lds.joined[w][x / (kPart / 4)][e]);
+        if (!whole) {
+          const int64_t stats_floats = part_tiles(a, kRows) * a.cache.heads * a.splits * (2 * kRows);
+          float* to = a.part + stats_floats +
+                      ((((int64_t)number * a.cache.heads + h) * a.splits + piece) * kRows + row) * D + d0 + e;
+          *reinterpret_cast<f32x4*>(to) = y;
+        } else {
+          const int rr = t.r0 + row;
+          uint16_t* to = a.y + (int64_t)(t.row0 + rr / a.group) * a.ldy + (int64_t)(h * a.group + rr % a.group) * D + d0 + e;
+          *reinterpret_cast<uint2*>(to) = make_uint2(bf16_pair(y[0], y[1]), bf16_pair(y[2], y[3]));
+        }
+      }
+    }
+  }
+}
+
+}  // namespace nvfp4

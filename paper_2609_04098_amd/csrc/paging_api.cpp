@@ -24,6 +24,27 @@ bool valid_requests(const nvfp4_requests* r) {
   return aligned(r->page_table, 4) && aligned(r->kv_len, 4);
 }
 
+bool valid_shared(const nvfp4_shared_prefix* s, const nvfp4_kv_batch* b) {
+  if (s == nullptr || s->n_groups < 0 || s->n_groups > b->n_seqs || s->max_prefix < 0 || s->max_own < 0) return false;
+  if (s->n_groups == 0) return true;
+  return s->cu_seqs != nullptr && s->prefix != nullptr && aligned(s->cu_seqs, 4) && aligned(s->prefix, 4);
+}
+
+SharedArgs shared_args(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_shared_prefix* shared,
+                       int64_t q_heads) {
+  SharedArgs a = {};
+  a.cache = cache_args(cache);
+  a.batch = batch_args(batch, cache->page_size);
+  a.q_heads = (int)q_heads;
+  a.group = (int)(q_heads / cache->kv_heads);
+  a.cu_seqs = shared->cu_seqs;
+  a.prefix = shared->prefix;
+  a.groups = (int)shared->n_groups;
+  a.max_prefix = (int)(shared->max_prefix < a.batch.max_tokens ? shared->max_prefix : a.batch.max_tokens);
+  a.max_own = (int)(shared->max_own < a.batch.max_kv_len ? shared->max_own : a.batch.max_kv_len);
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -62,6 +83,53 @@ int nvfp4_step_tables(const nvfp4_requests* requests, const int32_t* new_rows, c
   a.rows = (int)rows;
   a.plan = static_cast<int32_t*>(workspace);
   const hipError_t e = launch_step_tables(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? NVFP4_OK : fail_hip(e);
+}
+
+size_t nvfp4_kv_attention_shared_workspace(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
+                                           const nvfp4_shared_prefix* shared, int64_t q_heads) {
+  if (!valid_cache(cache) || !valid_batch(batch, cache->page_size) || !valid_shared(shared, batch) ||
+      !valid_q_heads(q_heads, cache->kv_heads))
+    return 0;
+  const SharedArgs a = shared_args(cache, batch, shared, q_heads);
+  if (a.batch.seqs == 0 || a.batch.rows == 0) return 0;
+  const SharedPlan p = shared_plan(a);
+  return shared_fits(a, p) ? p.bytes : 0;
+}
+
+int nvfp4_kv_attention_shared(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_shared_prefix* shared,
+                              const void* q, int64_t ldq, int64_t q_heads, void* y, int64_t ldy, float* lse,
+                              float softmax_scale, int causal, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!valid_cache(cache) || !valid_batch(batch, cache->page_size) || !valid_shared(shared, batch) ||
+      !valid_q_heads(q_heads, cache->kv_heads))
+    return NVFP4_EINVAL;
+  if (!valid_rows(q, ldq, q_heads, cache->head_dim, batch->rows) ||
+      !valid_rows(y, ldy, q_heads, cache->head_dim, batch->rows) || !aligned(lse, 4))
+    return NVFP4_EINVAL;
+  const double scale = (double)softmax_scale * 1.4426950408889634;      // (powers of two)
+  if (batch->rows * q_heads >= kI32Lim || !isfinite((float)scale) || (causal != 0 && causal != 1)) return NVFP4_EINVAL;
+  SharedArgs a = shared_args(cache, batch, shared, q_heads);
+  const bool none = a.batch.seqs == 0 || a.batch.rows == 0;
+  SharedPlan p = {};
+  if (!none) {
+    p = shared_plan(a);
+    if (!shared_fits(a, p)) return NVFP4_EINVAL;
+    if (workspace == nullptr || !aligned(workspace, 16)) return NVFP4_EINVAL;
+    if (workspace_bytes < p.bytes) return NVFP4_EWORKSPACE;
+  }
+  const int st = check_device();
+  if (st != NVFP4_OK) return st;
+  if (none) return NVFP4_OK;
+  a.q = static_cast<const uint16_t*>(q);
+  a.y = static_cast<uint16_t*>(y);
+  a.lse = lse;
+  a.ldq = ldq;
+  a.ldy = ldy;
+  a.scale = (float)scale;
+  a.causal = causal;
+  a.window = 0;
+  a.part = static_cast<float*>(workspace);
+  const hipError_t e = launch_kv_attention_shared(a, p, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? NVFP4_OK : fail_hip(e);
 }
 

@@ -5,7 +5,7 @@
 import ctypes
 
 from . import nvfp4 as _c
-from .nvfp4_attention import _f, _handle, _i64, _int, _sz, _vp
+from .nvfp4_attention import _batch, _cache, _f, _handle, _i64, _int, _sz, _vp
 
 
 class RequestsStruct(ctypes.Structure):
@@ -14,12 +14,19 @@ class RequestsStruct(ctypes.Structure):
                 ("page_size", _i64)]
 
 
-_requests = ctypes.POINTER(RequestsStruct)
+class SharedPrefixStruct(ctypes.Structure):
+    _fields_ = [("cu_seqs", _vp), ("prefix", _vp), ("n_groups", _i64), ("max_prefix", _i64), ("max_own", _i64)]
+
+
+_requests, _shared = ctypes.POINTER(RequestsStruct), ctypes.POINTER(SharedPrefixStruct)
 
 # name -> (restype, argtypes), in the order of include/nvfp4_paging.h
 SIGNATURES = {
     "nvfp4_step_tables_workspace": (_sz, [_i64]),
     "nvfp4_step_tables": (_int, [_requests, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _sz, _vp]),
+    "nvfp4_kv_attention_shared_workspace": (_sz, [_cache, _batch, _shared, _i64]),
+    "nvfp4_kv_attention_shared": (_int, [_cache, _batch, _shared, _vp, _i64, _i64, _vp, _i64, _vp, _f, _int, _vp, _sz,
+                                         _vp]),
 }
 
 _lib = None
@@ -44,6 +51,11 @@ def requests_struct(page_table, kv_len, free_pages, free_count, page_size):
                           page_table.stride(0), page_table.shape[1], kv_len.shape[0], free_pages.shape[0], page_size)
 
 
+def shared_struct(cu_seqs, prefix, max_prefix, max_own):
+    """cu_seqs int32 [n_groups + 1]; prefix int32 [n_groups]."""
+    return SharedPrefixStruct(cu_seqs.data_ptr(), prefix.data_ptr(), prefix.shape[0], max_prefix, max_own)
+
+
 def step_tables_workspace(n_seqs):
     return lib().nvfp4_step_tables_workspace(n_seqs)
 
@@ -55,3 +67,14 @@ def step_tables(stream, *args):
     status = (_lib or lib()).nvfp4_step_tables(*args, _handle(stream))
     if status:
         _c._check(status, "nvfp4_step_tables")
+
+
+def kv_attention_shared_workspace(cache, batch, shared, q_heads):
+    return lib().nvfp4_kv_attention_shared_workspace(cache, batch, shared, q_heads)
+
+
+def kv_attention_shared(stream, *args):
+    """nvfp4_kv_attention_shared, its arguments as above."""
+    status = (_lib or lib()).nvfp4_kv_attention_shared(*args, _handle(stream))
+    if status:
+        _c._check(status, "nvfp4_kv_attention_shared")

@@ -4,6 +4,8 @@
     requests = alloc_requests(n_seqs, max_pages, num_pages, page_size, device)   # once: lengths, pages, the pool
     step = step_tables(requests, new_rows, rows, drop)    # per step: page tables, row offsets, positions, slots
     attention.kv_append(cache, step.batch, k, v, ...)
+    shared = SharedPrefix(cu_seqs, prefix)                # while the groups stay the same
+    y = shared_attention(q, cache, step.batch, shared)    # attention(q, cache, step.batch), prefixes read once
 
 Lengths stay on the GPU: nothing here waits for it, and every call may be captured
 into a graph.  There is no backward pass, as in ``attention``.
@@ -16,7 +18,7 @@ import torch
 from . import attention as _at
 from . import linear as _l
 from . import nvfp4_paging as _p
-from .attention import _need, _run
+from .attention import Batch, KVCache, _like_rows, _need, _rows, _run
 
 _I32 = torch.int32
 
@@ -107,3 +109,81 @@ def step_tables(requests: Requests, new_rows, rows, drop=None, kept=None, max_le
     _run(device, _p.step_tables, stream, requests.ref, _vector(new_rows, n, device, "new_rows"),
          _vector(drop, n, device, "drop"), _vector(kept, n, device, "kept"), *out._args)
     return out
+
+
+class SharedPrefix:
+    """Groups of a batch's sequences that share a prefix, on the GPU: sequences
+    [cu_seqs[g], cu_seqs[g + 1]) begin with the same ``prefix[g]`` tokens in the same
+    pages (int32 [n_groups + 1] and [n_groups]).  ``max_len``, ``max_own``: the longest
+    prefix and the most tokens of a sequence behind it, as far as the host knows (else
+    what the page table can hold): work is divided by them."""
+
+    def __init__(self, cu_seqs, prefix, max_len=None, max_own=None):
+        _need(prefix.dtype == _I32 and prefix.dim() == 1 and prefix.is_contiguous(), "prefix must be int32 [n_groups]")
+        _need(cu_seqs.dtype == _I32 and cu_seqs.shape == (prefix.shape[0] + 1,) and cu_seqs.is_contiguous(),
+              "cu_seqs must be int32 [n_groups + 1]")
+        _need(cu_seqs.device == prefix.device, "the groups' tensors are on several devices")
+        most = (1 << 31) - 1
+        self.cu_seqs, self.prefix, self.index = cu_seqs, prefix, prefix.get_device()
+        self.struct = _p.shared_struct(cu_seqs, prefix, most if max_len is None else int(max_len),
+                                       most if max_own is None else int(max_own))
+        self.ref = ctypes.byref(self.struct)
+        self._workspace = {}
+
+    def workspace_bytes(self, cache, batch, q_heads):
+        b = batch.struct
+        key = (q_heads, cache.kv_heads, cache.head_dim, cache.page_size, b.rows, b.n_seqs, b.max_pages, b.max_kv_len,
+               b.cu_rows is None)
+        if key not in self._workspace:
+            self._workspace[key] = _p.kv_attention_shared_workspace(cache.ref, batch.ref, self.ref, q_heads)
+        return self._workspace[key]
+
+
+def _queries(q, cache, rows, out, stream):
+    """(rows, heads, q's row stride, y, y's row stride) of an attention's queries and output."""
+    n, heads, dim, ldq = _rows(q, "q")
+    if n != rows or dim != cache.head_dim or heads == 0 or heads % cache.kv_heads:
+        raise ValueError("q has the wrong rows, heads or head_dim")
+    if q.get_device() != cache.index:
+        raise ValueError("tensors are on several devices")
+    if out is None:
+        return n, heads, ldq, _like_rows(q, stream), heads * dim
+    rows_y, heads_y, dim_y, ldy = _rows(out, "out")
+    if (rows_y, heads_y, dim_y) != (n, heads, dim) or out.get_device() != cache.index:
+        raise ValueError("out must have q's shape and device")
+    return n, heads, ldq, out, ldy
+
+
+def _room(workspace, nbytes, q, stream):
+    """(workspace, its bytes): the given one, or one of nbytes from the stream that uses it."""
+    if workspace is None:
+        return (_l._scratch(nbytes, q.device, stream), nbytes) if nbytes else (None, 0)
+    if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous, on q's device")
+    return workspace, workspace.numel() * workspace.element_size()
+
+
+def _lse(wanted, rows, heads, q, stream):
+    if not wanted:
+        return None
+    with _l._on(stream, q.device):
+        return torch.empty((rows, heads), dtype=torch.float32, device=q.device)
+
+
+def shared_attention(q, cache: KVCache, batch: Batch, shared: SharedPrefix, scale=None, causal=True, out=None,
+                     return_lse=False, workspace=None, stream=None):
+    """``attention(q, cache, batch)`` of sequences that share prefixes, which are read
+    once for each group.  A sequence whose rows do not all lie behind the prefix is
+    computed from its own pages alone.  Arguments and results as for attention()."""
+    rows, heads, ldq, y, ldy = _queries(q, cache, batch.rows, out, stream)
+    if not cache.index == batch.index == shared.index:
+        raise ValueError("tensors are on several devices")
+    if shared.struct.n_groups > batch.struct.n_seqs:
+        raise ValueError("there are more groups than sequences")
+    lse = _lse(return_lse, rows, heads, q, stream)
+    workspace, nbytes = _room(workspace, 0 if workspace is not None else shared.workspace_bytes(cache, batch, heads), q,
+                              stream)
+    _run(cache.index, _p.kv_attention_shared, stream, cache.ref, batch.ref, shared.ref, q.data_ptr(), ldq, heads,
+         y.data_ptr(), ldy, None if lse is None else lse.data_ptr(), cache.softmax_scale if scale is None else scale,
+         1 if causal else 0, None if workspace is None else workspace.data_ptr(), nbytes)
+    return (y, lse) if return_lse else y

@@ -9,13 +9,14 @@ import re
 import pytest
 import torch
 
+from paper_2609_04098_amd import attention as A
 from paper_2609_04098_amd import nvfp4 as C
 from paper_2609_04098_amd import nvfp4_paging as N
 from paper_2609_04098_amd import paging as P
-from tests.test_attention_abi import FAKE, ROOT
+from tests.test_attention_abi import BAD_BATCHES, BAD_CACHES, FAKE, ROOT, _batch, _cache
 
 HEADER = os.path.join(ROOT, "include", "nvfp4_paging.h")
-STRUCTS = {"nvfp4_requests": N.RequestsStruct}
+STRUCTS = {"nvfp4_requests": N.RequestsStruct, "nvfp4_shared_prefix": N.SharedPrefixStruct}
 
 
 def test_header_matches_the_binding_and_the_library():
@@ -65,6 +66,86 @@ def test_tables_want_their_workspace():
     assert need > 0 and N.lib().nvfp4_step_tables_workspace(-1) == 0 == N.lib().nvfp4_step_tables_workspace(1 << 24)
     assert _tables(wsb=need - 1) == C.NVFP4_EWORKSPACE
     assert N.lib().nvfp4_step_tables(None, FAKE, None, None, FAKE, None, None, 1, FAKE, 1 << 20, None) == C.NVFP4_EINVAL
+
+
+def _groups(**kw):
+    a = dict(cu_seqs=FAKE, prefix=FAKE, n_groups=2, max_prefix=100, max_own=60)
+    a.update(kw)
+    return N.SharedPrefixStruct(**a)
+
+
+def _attend(cache=None, batch=None, groups=None, **kw):
+    a = dict(q=FAKE, ldq=512, hq=4, y=FAKE, ldy=512, lse=None, scale=0.1, causal=1, ws=FAKE, wsb=1 << 30)
+    a.update(kw)
+    c, b, g = (x if x is not None else f() for x, f in ((cache, _cache), (batch, _batch), (groups, _groups)))
+    return N.lib().nvfp4_kv_attention_shared(ctypes.byref(c), ctypes.byref(b), ctypes.byref(g), a["q"], a["ldq"], a["hq"],
+                                             a["y"], a["ldy"], a["lse"], a["scale"], a["causal"], a["ws"], a["wsb"], None)
+
+
+@pytest.mark.parametrize("bad", BAD_CACHES)
+def test_shared_attention_refuses_caches(bad):
+    assert _attend(_cache(**bad)) == C.NVFP4_EINVAL
+
+
+@pytest.mark.parametrize("bad", BAD_BATCHES)
+def test_shared_attention_refuses_batches(bad):
+    assert _attend(batch=_batch(**bad)) == C.NVFP4_EINVAL
+
+
+@pytest.mark.parametrize("bad", [dict(cu_seqs=None), dict(prefix=None), dict(cu_seqs=FAKE + 2), dict(prefix=FAKE + 1),
+                                 dict(n_groups=-1), dict(n_groups=4), dict(max_prefix=-1), dict(max_own=-1)])
+def test_shared_attention_refuses_groups(bad):
+    assert _attend(groups=_groups(**bad)) == C.NVFP4_EINVAL
+
+
+@pytest.mark.parametrize("bad", [
+    dict(q=None), dict(y=None), dict(q=FAKE + 2), dict(y=FAKE + 4), dict(ldq=504), dict(ldy=516), dict(hq=3), dict(hq=0),
+    dict(hq=1026, ldq=1 << 20, ldy=1 << 20), dict(lse=FAKE + 2), dict(scale=float("nan")), dict(scale=3e38), dict(causal=2),
+    dict(ws=None), dict(ws=FAKE + 8)])
+def test_shared_attention_refuses(bad):
+    assert _attend(**bad) == C.NVFP4_EINVAL
+
+
+def test_shared_attention_wants_its_workspace():
+    f, c, b, g = N.lib(), _cache(), _batch(), _groups()
+    need = f.nvfp4_kv_attention_shared_workspace(ctypes.byref(c), ctypes.byref(b), ctypes.byref(g), 4)
+    assert need > 0 and _attend(wsb=need - 1) == C.NVFP4_EWORKSPACE
+    assert f.nvfp4_kv_attention_shared_workspace(ctypes.byref(c), ctypes.byref(b), ctypes.byref(_groups(n_groups=9)), 4) == 0
+    assert f.nvfp4_kv_attention_shared_workspace(ctypes.byref(c), ctypes.byref(b), ctypes.byref(g), 3) == 0
+    for null in range(3):
+        args = [ctypes.byref(c), ctypes.byref(b), ctypes.byref(g)]
+        args[null] = None
+        assert f.nvfp4_kv_attention_shared(*args, FAKE, 512, 4, FAKE, 512, None, 0.1, 1, FAKE, 1 << 30, None) == C.NVFP4_EINVAL
+
+
+@pytest.mark.parametrize("n,heads,group", [(1 << 21, 8, 5), ((1 << 24) - 1, 2, 1), (1 << 20, 8, 33)])
+def test_shared_attention_refuses_more_workgroups_than_a_launch_holds(n, heads, group):
+    c = _cache(kv_heads=heads, page_size=16, k_page_stride=heads * 2048, v_page_stride=heads * 2048, scale_page_stride=heads)
+    b = _batch(n_seqs=n, rows=n, cu_rows=None)
+    assert _attend(c, b, hq=heads * group, ldq=heads * group * 128, ldy=heads * group * 128) == C.NVFP4_EINVAL
+
+
+def test_shared_attention_refuses_wrong_tensors():
+    c = A.alloc_kv_cache(4, 2, 64, 16, "cpu")
+    b = A.Batch(_i32(3, 2), _i32(3))
+    x = torch.zeros(3, 4, 64, dtype=torch.bfloat16)
+    g = P.SharedPrefix(_i32(3), _i32(2))
+    for call in (lambda: P.SharedPrefix(_i32(2), _i32(2)), lambda: P.SharedPrefix(_i32(3).long(), _i32(2)),
+                 lambda: P.SharedPrefix(_i32(3), _i32(2).float()), lambda: P.SharedPrefix(_i32(6)[::2], _i32(2)),
+                 lambda: P.shared_attention(x[:2], c, b, g), lambda: P.shared_attention(x.float(), c, b, g),
+                 lambda: P.shared_attention(x[:, :3], c, b, g), lambda: P.shared_attention(x, c, b, g, out=x[:, :2]),
+                 lambda: P.shared_attention(x, c, b, P.SharedPrefix(_i32(5), _i32(4))),
+                 lambda: P.shared_attention(x.requires_grad_(), c, b, g)):
+        with pytest.raises(ValueError):
+            call()
+    x = x.detach()
+    far = x.to("meta")
+    for call in (lambda: P.SharedPrefix(_i32(3).to("meta"), _i32(2)), lambda: P.shared_attention(far, c, b, g),
+                 lambda: P.shared_attention(x, c, b, g, out=far), lambda: P.shared_attention(x, c, b, g, workspace=far)):
+        with pytest.raises(ValueError, match="device"):
+            call()
+    with pytest.raises(ValueError, match="GPU"):
+        P.shared_attention(x, c, b, g)
 
 
 def _i32(*shape):
