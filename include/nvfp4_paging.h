@@ -1,7 +1,8 @@
 /*
  * nvfp4_paging.h -- C ABI of serving over the paged 8-bit cache of
  * nvfp4_attention.h: the tables of a step made on the GPU from the requests'
- * lengths, and the attention of batches whose sequences share prefixes.
+ * lengths, the attention of batches whose sequences share prefixes, and the attention
+ * over the pages that a cheap score selects for each query.
  *
  * Conventions are those of nvfp4_attention.h: device pointers owned by the
  * caller, synchronous checks before anything is enqueued, work enqueued on
@@ -132,6 +133,91 @@ size_t nvfp4_kv_attention_shared_workspace(const nvfp4_kv_cache* cache, const nv
 int nvfp4_kv_attention_shared(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_shared_prefix* shared,
                               const void* q, int64_t ldq, int64_t q_heads, void* y, int64_t ldy, float* lse,
                               float softmax_scale, int causal, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Bounds of the keys of a cache's pages, in 8 bits: page p and head h hold 2 * head_dim
+ * bytes at codes + p * page_stride + h * 2 * head_dim,
+ *   codes[0][e] = rint(127 hi_e / A),  codes[1][e] = rint(127 lo_e / A)   (to nearest even)
+ *   step[p * step_stride + h] = fl(fl(A * k_scale) / 127)
+ * with hi_e, lo_e the largest and the smallest E4M3 value of element e among the page's
+ * page_size tokens, A the largest |hi_e|, |lo_e| of the head (all 0 if A is), fl binary32.
+ * Requirements: codes 16-byte aligned, int8 [num_pages]; page_stride in bytes, a
+ * multiple of 16, at least 2 * kv_heads * head_dim; step float [num_pages], 4-byte aligned,
+ * step_stride >= kv_heads.
+ */
+typedef struct nvfp4_kv_bounds {
+  void* codes;
+  float* step;
+  int64_t page_stride;
+  int64_t step_stride;
+} nvfp4_kv_bounds;
+
+/*
+ * The bounds of the pages that a step's rows completed: for each sequence the pages that
+ * one of its new rows lies in and that its kv_len[b] tokens fill.  Called behind the append
+ * of every step, it keeps the bounds of all full pages; those of other pages stay as they are.
+ * Errors: NVFP4_EINVAL, NVFP4_EUNSUPPORTED, NVFP4_EHIP.
+ */
+int nvfp4_kv_page_bounds(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_kv_bounds* bounds,
+                         void* stream);
+
+/* Workspace bytes of nvfp4_kv_select_pages; 0: none is used, or the arguments are
+ * invalid. */
+size_t nvfp4_kv_select_pages_workspace(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch);
+
+/*
+ * Chooses up to `count` pages for each row of a step and each key head, of the pages
+ * 0 .. n - 1 of the row's sequence that it sees (n = t / page_size + 1 for the row's token
+ * t; if not causal, t is the sequence's last token): all of them if n <= count; else the
+ * `first` ones, the `recent` last ones and, of those between them, the count - first -
+ * recent with the largest scores, the lowest ones first among equals.  With key head h's
+ * query heads a,
+ *   q_a,e in 8 bits: i_a,e = rint(127 q_a,e / Q_a) (to nearest even),  Q_a = max_e |q_a,e|
+ *   score = fl(max_a fl(fl(Q_a / 127) * sum_e max(i_a,e hi_e, i_a,e lo_e)) * step)
+ * with hi_e, lo_e the page's bounds (codes): but for the 8-bit roundings, the largest
+ * product that a query of the head can have with a key of the page.  (The softmax scale
+ * is taken to be positive.)  The sums are whole numbers, so that the choice is the same
+ * in every run.  A page outside [0, num_pages) is chosen last.
+ *
+ *   index        out, device int32 [rows x kv_heads x count]: the chosen pages' numbers in
+ *                their sequence, ascending; -1 behind them.
+ *   pages        out, the same of the pages themselves (entries of page_table).
+ *   tokens       out, device int32 [rows]: tokens of the chosen pages that the row sees
+ *                (all of them, but t % page_size + 1 of the last); -1 for rows from
+ *                cu_rows[n_seqs] on, whose index and pages are left as they are.
+ *   first, recent   first >= 0, recent >= 1, first + recent <= count.
+ *   workspace, workspace_bytes   at least nvfp4_kv_select_pages_workspace bytes, 16-byte
+ *                aligned (NULL if that is 0).  Its contents on entry do not matter; calls
+ *                sharing one must be ordered.
+ * Requirements: those of the structures; q as for nvfp4_kv_attention; 1 <= count, count *
+ * page_size <= 2^30; a batch that has rows has sequences.
+ * Errors: NVFP4_EINVAL, NVFP4_EWORKSPACE, NVFP4_EUNSUPPORTED, NVFP4_EHIP.
+ */
+int nvfp4_kv_select_pages(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_kv_bounds* bounds,
+                          const void* q, int64_t ldq, int64_t q_heads, int64_t count, int64_t first, int64_t recent, int causal,
+                          int32_t* index, int32_t* pages, int32_t* tokens, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/* Workspace bytes of nvfp4_kv_attention_selected (partial results); 0: none is used, or
+ * the arguments are invalid. */
+size_t nvfp4_kv_attention_selected_workspace(const nvfp4_kv_cache* cache, int64_t rows, int64_t q_heads, int64_t count);
+
+/*
+ * Attention of each row over its chosen pages: of nvfp4_kv_attention's definition, with
+ * the sums over the first tokens[row] tokens of pages[row][h][0 .. count - 1], one page
+ * behind the other.  A row without tokens gets y = 0 and lse = -infinity; one whose
+ * tokens are below 0 is left as it is.  tokens over count * page_size count as that;
+ * tokens of pages outside [0, num_pages) are masked.
+ *   pages, tokens   as nvfp4_kv_select_pages leaves them, or a caller's own choice.
+ *   workspace, workspace_bytes   at least nvfp4_kv_attention_selected_workspace bytes,
+ *                16-byte aligned (NULL if that is 0).  Its contents on entry do not
+ *                matter; calls sharing one must be ordered.
+ * The others, their requirements and the accuracy: as for nvfp4_kv_attention.
+ * Errors: NVFP4_EINVAL, NVFP4_EWORKSPACE, NVFP4_EUNSUPPORTED, NVFP4_EHIP.
+ */
+int nvfp4_kv_attention_selected(const nvfp4_kv_cache* cache, const void* q, int64_t ldq, int64_t q_heads, int64_t rows,
+                                int64_t count, const int32_t* pages, const int32_t* tokens, void* y, int64_t ldy, float* lse,
+                                float softmax_scale, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -56,3 +56,40 @@ class Pool:
                 slots.append(page * self.page + t % self.page if 0 <= page < len(self.stack) else -1)
             self.kv_len[b] += cu[b + 1] - cu[b]
         return np.array(cu), np.array(positions, dtype=np.int64), np.array(slots, dtype=np.int64)
+
+
+def page_bounds(values, scale):
+    """Bounds of one page and head: values [tokens, dim] (of the E4M3 codes), its key
+    scale.  (codes int [2, dim], step)."""
+    hi, lo = values.max(axis=0), values.min(axis=0)
+    top = max(np.abs(hi).max(), np.abs(lo).max())
+    if top == 0:
+        return np.zeros((2, values.shape[1]), dtype=np.int64), np.float32(0)
+    codes = np.rint(np.stack([hi, lo]) * 127 / top).astype(np.int64)      # (float64: exact but for the division)
+    return codes, np.float32(np.float32(top * float(scale)) / np.float32(127))
+
+
+def query_codes(q):
+    """(codes int [heads, dim], units float32 [heads]) of queries [heads, dim]."""
+    top = np.abs(q).max(axis=1, keepdims=True)
+    codes = np.rint(q * 127 / np.where(top > 0, top, 1)).astype(np.int64)
+    return codes, (top[:, 0].astype(np.float32) / np.float32(127))
+
+
+def page_score(codes, units, bounds, step):
+    """Score of a page for a key head's queries: codes int [heads, dim], bounds int [2, dim]."""
+    best = None
+    for i, unit in zip(codes, units):
+        total = int(np.maximum(i * bounds[0], i * bounds[1]).sum())
+        value = np.float32(float(total) * float(unit))
+        best = value if best is None or value > best else best
+    return np.float32(float(best) * float(step))
+
+
+def choose(scores, seen, count, first, recent):
+    """Pages taken of 0 .. seen - 1, ascending; scores[j] of page j (None: not in the cache)."""
+    if seen <= count:
+        return list(range(seen))
+    middle = range(first, seen - recent)
+    best = sorted(middle, key=lambda j: (scores[j] is None, 0 if scores[j] is None else -scores[j], j))
+    return sorted(list(range(first)) + best[:count - first - recent] + list(range(seen - recent, seen)))

@@ -20,7 +20,8 @@ SOURCES = ["api.cpp", "act_quant.hip", "norm_quant.hip", "weight_pack.hip", "gem
            "gemm_lds_super.hip", "gemm_lds_super_f32.hip", "gemm_lds_tall.hip", "gemm_lds_mid.hip", "gemm_lds_low.hip",
            "gemm_splitk.hip", "gemm_rows16.hip", "gemm_reg.hip", "quant_gemm.hip", "attention_api.cpp",
            "qk_norm_rope.hip", "kv_append.hip", "kv_attention.hip", "kv_attention_tile.hip", "paging_api.cpp",
-           "step_tables.hip", "kv_attention_shared.hip"]
+           "step_tables.hip", "kv_attention_shared.hip",
+           "kv_select.hip", "kv_attention_selected.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950",

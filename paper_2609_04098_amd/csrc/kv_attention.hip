@@ -19,91 +19,9 @@ __global__ __launch_bounds__(kWaves * 64, rows_waves(D, kTiles, kWaves, kSplit))
   attention_rows<D, kTiles, kWaves, kSplit>(a);
 }
 
-// Joins the pieces of a sequence.  kShare waves take a packed row, each its
-// share of the pieces, four pieces' loads in flight.
 template <int D, int kTiles, int kShare>
 __global__ __launch_bounds__(256) void kv_attention_join_kernel(AttentionArgs a) {
-  constexpr int kRows = 16 * kTiles, kEach = D / 64, kAhead = 4, kBlockRows = 4 / kShare;
-  __shared__ float sums[kShare > 1 ? 4 : 1][kShare > 1 ? D : 1];
-  __shared__ float totals[4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, share = wave % kShare;
-  const int row = (int)(blockIdx.x % (kRows / kBlockRows)) * kBlockRows + wave / kShare;
-  const int h = (int)(blockIdx.x / (kRows / kBlockRows)) % a.cache.heads;
-  const int number = (int)(blockIdx.x / (kRows / kBlockRows)) / a.cache.heads;
-  Tile t;
-  if (!find_tile<kRows>(a, number, t) || row >= t.n) return;      // (with kShare 4, the whole workgroup)
-  const int pieces = pieces_of(a, t);
-  if (pieces == 1) return;      // its rows are written already
-  const int64_t first = ((int64_t)number * a.cache.heads + h) * a.splits;
-  const float2* stats = reinterpret_cast<const float2*>(a.part) + first * kRows + row;
-  const float* part = a.part + tiles_of(a.batch, a.group, kRows) * a.cache.heads * a.splits * (2 * kRows) +
-                      (first * kRows + row) * D + lane * kEach;
-  float m = kNone, l = 0.0f, y[kEach];
-#pragma unroll
-  for (int i = 0; i < kEach; ++i) y[i] = 0.0f;
-  for (int p = share; p < pieces; p += kShare * kAhead) {
-    float2 st[kAhead];
-    float v[kAhead][kEach];
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const int at = p + u * kShare;
-      st[u] = make_float2(kNone, 0.0f);
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) v[u][i] = 0.0f;
-      if (at < pieces) {
-        st[u] = stats[at * kRows];
-#pragma unroll
-        for (int i = 0; i < kEach; ++i) v[u][i] = part[(int64_t)at * kRows * D + i];
-      }
-    }
-    float top = m;
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) top = fmaxf(top, st[u].x);
-    const float base = top == kNone ? 0.0f : top;
-    const float f = __builtin_amdgcn_exp2f(m - base);
-    m = top;
-    l *= f;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) y[i] *= f;
-#pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      const float g = __builtin_amdgcn_exp2f(st[u].x - base);
-      l = fmaf(st[u].y, g, l);
-#pragma unroll
-      for (int i = 0; i < kEach; ++i) y[i] = fmaf(v[u][i], g, y[i]);
-    }
-  }
-  const int r = t.r0 + row, head = h * a.group + r % a.group;
-  const int64_t token_row = t.row0 + r / a.group;
-  uint16_t* to = a.y + token_row * a.ldy + (int64_t)head * D;
-  if (kShare > 1) {
-    if (lane == 0) totals[wave] = m;
-    __syncthreads();
-    const float top = fmaxf(fmaxf(totals[0], totals[1]), fmaxf(totals[2], totals[3]));
-    const float g = __builtin_amdgcn_exp2f(m - (top == kNone ? 0.0f : top));
-    __syncthreads();
-    if (lane == 0) totals[wave] = l * g;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) sums[kShare > 1 ? wave : 0][kShare > 1 ? lane * kEach + i : 0] = y[i] * g;
-    __syncthreads();
-    m = top;
-    l = (totals[0] + totals[1]) + (totals[2] + totals[3]);
-    if (wave != 0) return;
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int e = kShare > 1 ? lane * kEach + i : 0;
-      y[i] = (sums[0][e] + sums[kShare > 1 ? 1 : 0][e]) + (sums[kShare > 1 ? 2 : 0][e] + sums[kShare > 1 ? 3 : 0][e]);
-    }
-  }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  if (D == 64)
-    to[lane] = __builtin_bit_cast(uint16_t, (__bf16)(y[0] * inv));
-  else
-#pragma unroll
-    for (int i = 0; i + 1 < kEach; i += 2)
-      *reinterpret_cast<uint32_t*>(to + lane * kEach + i) = bf16_pair(y[i] * inv, y[i + 1] * inv);
-  if (a.lse != nullptr && lane == 0)
-    a.lse[token_row * a.q_heads + head] = l == 0.0f ? kNone : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+  attention_join<D, kTiles, kShare>(a);
 }
 
 namespace {

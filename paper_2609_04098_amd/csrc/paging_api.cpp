@@ -45,6 +45,31 @@ SharedArgs shared_args(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
   return a;
 }
 
+bool valid_bounds(const nvfp4_kv_bounds* b, const nvfp4_kv_cache* c) {
+  if (b == nullptr || b->codes == nullptr || b->step == nullptr || !aligned(b->codes, 16) || !aligned(b->step, 4)) return false;
+  return b->page_stride >= 2 * c->kv_heads * c->head_dim && b->page_stride % 16 == 0 && b->step_stride >= c->kv_heads;
+}
+
+PageBoundsArgs bounds_args(const nvfp4_kv_bounds* b) {
+  return {static_cast<int8_t*>(b->codes), b->step, b->page_stride, b->step_stride};
+}
+
+// Pages that a row may take: 1 to 2^30 tokens' in all.
+bool valid_choice(const nvfp4_kv_cache* c, int64_t rows, int64_t count) {
+  return rows >= 0 && rows < kMaxRows && count >= 1 && count <= kMaxTokens / c->page_size;
+}
+
+SelectedArgs selected_args(const nvfp4_kv_cache* cache, int64_t rows, int64_t q_heads, int64_t count) {
+  SelectedArgs a = {};
+  a.cache = cache_args(cache);
+  a.q_heads = (int)q_heads;
+  a.group = (int)(q_heads / cache->kv_heads);
+  a.count = (int)count;
+  a.batch.seqs = a.batch.rows = (int)rows;
+  a.batch.max_tokens = a.batch.max_kv_len = (int)(count * cache->page_size);
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -130,6 +155,114 @@ int nvfp4_kv_attention_shared(const nvfp4_kv_cache* cache, const nvfp4_kv_batch*
   a.window = 0;
   a.part = static_cast<float*>(workspace);
   const hipError_t e = launch_kv_attention_shared(a, p, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? NVFP4_OK : fail_hip(e);
+}
+
+int nvfp4_kv_page_bounds(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_kv_bounds* bounds,
+                         void* stream) {
+  if (!valid_cache(cache) || !valid_batch(batch, cache->page_size) || !valid_bounds(bounds, cache)) return NVFP4_EINVAL;
+  const BoundsArgs a = {cache_args(cache), batch_args(batch, cache->page_size), bounds_args(bounds)};
+  if (!bounds_fit(a)) return NVFP4_EINVAL;
+  const int st = check_device();
+  if (st != NVFP4_OK) return st;
+  if (a.batch.seqs == 0 || a.batch.rows == 0 || a.batch.max_tokens == 0) return NVFP4_OK;
+  const hipError_t e = launch_kv_page_bounds(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? NVFP4_OK : fail_hip(e);
+}
+
+size_t nvfp4_kv_select_pages_workspace(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch) {
+  if (!valid_cache(cache) || !valid_batch(batch, cache->page_size)) return 0;
+  return kv_select_workspace_bytes(batch->rows, cache->kv_heads, batch->max_pages);
+}
+
+int nvfp4_kv_select_pages(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_kv_bounds* bounds,
+                          const void* q, int64_t ldq, int64_t q_heads, int64_t count, int64_t first, int64_t recent, int causal,
+                          int32_t* index, int32_t* pages, int32_t* tokens, void* workspace, size_t workspace_bytes,
+                          void* stream) {
+  if (!valid_cache(cache) || !valid_batch(batch, cache->page_size) || !valid_bounds(bounds, cache) ||
+      !valid_q_heads(q_heads, cache->kv_heads) || !valid_choice(cache, batch->rows, count))
+    return NVFP4_EINVAL;
+  if (first < 0 || recent < 1 || first > count || recent > count - first || (causal != 0 && causal != 1)) return NVFP4_EINVAL;
+  if (!valid_rows(q, ldq, q_heads, cache->head_dim, batch->rows)) return NVFP4_EINVAL;
+  const bool none = batch->rows == 0 || batch->n_seqs == 0;
+  if (batch->rows > 0 && (index == nullptr || pages == nullptr || tokens == nullptr)) return NVFP4_EINVAL;
+  if (!aligned(index, 4) || !aligned(pages, 4) || !aligned(tokens, 4)) return NVFP4_EINVAL;
+  if (batch->rows > 0 && batch->n_seqs == 0) return NVFP4_EINVAL;      // (rows of no sequence)
+  SelectArgs a;
+  a.cache = cache_args(cache);
+  a.batch = batch_args(batch, cache->page_size);
+  a.bounds = bounds_args(bounds);
+  a.q = static_cast<const uint16_t*>(q);
+  a.ldq = ldq;
+  a.group = (int)(q_heads / cache->kv_heads);
+  a.count = (int)count;
+  a.first = (int)first;
+  a.recent = (int)recent;
+  a.causal = causal;
+  a.max_pages = (int)batch->max_pages;
+  a.index = index;
+  a.pages = pages;
+  a.tokens = tokens;
+  if (!none) {
+    if (!select_fits(a)) return NVFP4_EINVAL;
+    const size_t need = kv_select_workspace_bytes(batch->rows, cache->kv_heads, batch->max_pages);
+    if (need > 0 && (workspace == nullptr || !aligned(workspace, 16))) return NVFP4_EINVAL;
+    if (workspace_bytes < need) return NVFP4_EWORKSPACE;
+  }
+  a.scores = static_cast<uint32_t*>(workspace);
+  const int st = check_device();
+  if (st != NVFP4_OK) return st;
+  if (none) return NVFP4_OK;
+  const hipError_t e = launch_kv_select(a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? NVFP4_OK : fail_hip(e);
+}
+
+size_t nvfp4_kv_attention_selected_workspace(const nvfp4_kv_cache* cache, int64_t rows, int64_t q_heads, int64_t count) {
+  if (!valid_cache(cache) || !valid_q_heads(q_heads, cache->kv_heads) || !valid_choice(cache, rows, count) || rows == 0)
+    return 0;
+  const SelectedArgs a = selected_args(cache, rows, q_heads, count);
+  const AttentionPlan p = attention_plan(a.cache, a.batch, a.group, 0, kAnyRoom);
+  return attention_fits(a.cache, a.batch, a.group, p) ? part_bytes(a.cache, a.batch, a.group, p) : 0;
+}
+
+int nvfp4_kv_attention_selected(const nvfp4_kv_cache* cache, const void* q, int64_t ldq, int64_t q_heads, int64_t rows,
+                                int64_t count, const int32_t* pages, const int32_t* tokens, void* y, int64_t ldy, float* lse,
+                                float softmax_scale, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!valid_cache(cache) || !valid_q_heads(q_heads, cache->kv_heads) || !valid_choice(cache, rows, count))
+    return NVFP4_EINVAL;
+  if (!valid_rows(q, ldq, q_heads, cache->head_dim, rows) || !valid_rows(y, ldy, q_heads, cache->head_dim, rows) ||
+      !aligned(lse, 4))
+    return NVFP4_EINVAL;
+  if (rows > 0 && (pages == nullptr || tokens == nullptr || !aligned(pages, 4) || !aligned(tokens, 4))) return NVFP4_EINVAL;
+  const double scale = (double)softmax_scale * 1.4426950408889634;      // (powers of two)
+  if (rows * q_heads >= kI32Lim || !isfinite((float)scale)) return NVFP4_EINVAL;
+  SelectedArgs a = selected_args(cache, rows, q_heads, count);
+  if (rows > 0) {
+    const AttentionPlan p = attention_plan(a.cache, a.batch, a.group, 0, kAnyRoom);
+    if (!attention_fits(a.cache, a.batch, a.group, p)) return NVFP4_EINVAL;
+    const size_t need = part_bytes(a.cache, a.batch, a.group, p);
+    if (need > 0) {
+      if (workspace == nullptr || !aligned(workspace, 16)) return NVFP4_EINVAL;
+      if (workspace_bytes < need) return NVFP4_EWORKSPACE;
+    }
+    a.row_tiles = p.tiles;
+    a.waves = p.waves;
+    a.chunk = p.chunk;
+    a.splits = p.splits;
+  }
+  const int st = check_device();
+  if (st != NVFP4_OK) return st;
+  if (rows == 0) return NVFP4_OK;
+  a.batch.kv_len = tokens;
+  a.pages = pages;
+  a.q = static_cast<const uint16_t*>(q);
+  a.y = static_cast<uint16_t*>(y);
+  a.lse = lse;
+  a.ldq = ldq;
+  a.ldy = ldy;
+  a.scale = (float)scale;
+  a.part = static_cast<float*>(workspace);
+  const hipError_t e = launch_kv_attention_selected(a, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? NVFP4_OK : fail_hip(e);
 }
 

@@ -79,8 +79,46 @@ inline bool shared_fits(const SharedArgs& a, const SharedPlan& p) {
          one_grid(host_tiles(prefix_batch(a), a.group, 16 * p.prefix.tiles) * a.cache.heads * p.prefix.splits, 256);
 }
 
+// Bounds of pages' keys.
+struct PageBoundsArgs {
+  int8_t* codes;               // [page][head][largest, smallest][dim]
+  float* step;
+  int64_t page_stride, step_stride;
+};
+
+struct BoundsArgs {
+  KvCacheArgs cache;
+  KvBatchArgs batch;
+  PageBoundsArgs bounds;
+};
+
+struct SelectArgs {
+  KvCacheArgs cache;
+  KvBatchArgs batch;
+  PageBoundsArgs bounds;
+  const uint16_t* q;
+  int64_t ldq;
+  int group, count, first, recent, causal, max_pages;
+  int32_t* index;              // [row][head][count], and
+  int32_t* pages;              // the pages themselves
+  int32_t* tokens;             // [row]: of the pages taken; -1: a row behind the last sequence
+  uint32_t* scores;            // workspace
+};
+
+// Attention over chosen pages: the batch's sequences are its rows, kv_len their tokens.
+struct SelectedArgs : AttentionArgs {
+  const int32_t* pages;
+  int count;
+};
+
 size_t step_tables_workspace_bytes(int64_t seqs);
 hipError_t launch_step_tables(const TablesArgs& a, hipStream_t stream);
 hipError_t launch_kv_attention_shared(const SharedArgs& a, const SharedPlan& p, hipStream_t stream);      // (a.part: its workspace)
+bool bounds_fit(const BoundsArgs& a);      // (each launch in range)
+hipError_t launch_kv_page_bounds(const BoundsArgs& a, hipStream_t stream);
+size_t kv_select_workspace_bytes(int64_t rows, int64_t heads, int64_t max_pages);
+bool select_fits(const SelectArgs& a);
+hipError_t launch_kv_select(const SelectArgs& a, hipStream_t stream);
+hipError_t launch_kv_attention_selected(const SelectedArgs& a, hipStream_t stream);      // (a.part: its workspace)
 
 }  // namespace nvfp4

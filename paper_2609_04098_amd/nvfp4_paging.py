@@ -18,7 +18,12 @@ class SharedPrefixStruct(ctypes.Structure):
     _fields_ = [("cu_seqs", _vp), ("prefix", _vp), ("n_groups", _i64), ("max_prefix", _i64), ("max_own", _i64)]
 
 
+class BoundsStruct(ctypes.Structure):
+    _fields_ = [("codes", _vp), ("step", _vp), ("page_stride", _i64), ("step_stride", _i64)]
+
+
 _requests, _shared = ctypes.POINTER(RequestsStruct), ctypes.POINTER(SharedPrefixStruct)
+_bounds = ctypes.POINTER(BoundsStruct)
 
 # name -> (restype, argtypes), in the order of include/nvfp4_paging.h
 SIGNATURES = {
@@ -27,6 +32,13 @@ SIGNATURES = {
     "nvfp4_kv_attention_shared_workspace": (_sz, [_cache, _batch, _shared, _i64]),
     "nvfp4_kv_attention_shared": (_int, [_cache, _batch, _shared, _vp, _i64, _i64, _vp, _i64, _vp, _f, _int, _vp, _sz,
                                          _vp]),
+    "nvfp4_kv_page_bounds": (_int, [_cache, _batch, _bounds, _vp]),
+    "nvfp4_kv_select_pages_workspace": (_sz, [_cache, _batch]),
+    "nvfp4_kv_select_pages": (_int, [_cache, _batch, _bounds, _vp, _i64, _i64, _i64, _i64, _i64, _int, _vp, _vp, _vp, _vp,
+                                     _sz, _vp]),
+    "nvfp4_kv_attention_selected_workspace": (_sz, [_cache, _i64, _i64, _i64]),
+    "nvfp4_kv_attention_selected": (_int, [_cache, _vp, _i64, _i64, _i64, _i64, _vp, _vp, _vp, _i64, _vp, _f, _vp, _sz,
+                                           _vp]),
 }
 
 _lib = None
@@ -56,6 +68,11 @@ def shared_struct(cu_seqs, prefix, max_prefix, max_own):
     return SharedPrefixStruct(cu_seqs.data_ptr(), prefix.data_ptr(), prefix.shape[0], max_prefix, max_own)
 
 
+def bounds_struct(codes, step):
+    """codes int8 [num_pages, kv_heads, 2, head_dim]; step float32 [num_pages, kv_heads]."""
+    return BoundsStruct(codes.data_ptr(), step.data_ptr(), codes.stride(0), step.stride(0))
+
+
 def step_tables_workspace(n_seqs):
     return lib().nvfp4_step_tables_workspace(n_seqs)
 
@@ -78,3 +95,32 @@ def kv_attention_shared(stream, *args):
     status = (_lib or lib()).nvfp4_kv_attention_shared(*args, _handle(stream))
     if status:
         _c._check(status, "nvfp4_kv_attention_shared")
+
+
+def kv_page_bounds(stream, *args):
+    """nvfp4_kv_page_bounds, its arguments as above."""
+    status = (_lib or lib()).nvfp4_kv_page_bounds(*args, _handle(stream))
+    if status:
+        _c._check(status, "nvfp4_kv_page_bounds")
+
+
+def kv_select_pages_workspace(cache, batch):
+    return lib().nvfp4_kv_select_pages_workspace(cache, batch)
+
+
+def kv_select_pages(stream, *args):
+    """nvfp4_kv_select_pages, its arguments as above."""
+    status = (_lib or lib()).nvfp4_kv_select_pages(*args, _handle(stream))
+    if status:
+        _c._check(status, "nvfp4_kv_select_pages")
+
+
+def kv_attention_selected_workspace(cache, rows, q_heads, count):
+    return lib().nvfp4_kv_attention_selected_workspace(cache, rows, q_heads, count)
+
+
+def kv_attention_selected(stream, *args):
+    """nvfp4_kv_attention_selected, its arguments as above."""
+    status = (_lib or lib()).nvfp4_kv_attention_selected(*args, _handle(stream))
+    if status:
+        _c._check(status, "nvfp4_kv_attention_selected")

@@ -7,6 +7,11 @@
     shared = SharedPrefix(cu_seqs, prefix)                # while the groups stay the same
     y = shared_attention(q, cache, step.batch, shared)    # attention(q, cache, step.batch), prefixes read once
 
+    bounds = alloc_page_bounds(cache)                     # per layer
+    page_bounds(cache, step.batch, bounds)                # behind each append
+    pages = select_pages(q, cache, step.batch, bounds, count)   # for each row and key head
+    y = selected_attention(q, cache, pages)
+
 Lengths stay on the GPU: nothing here waits for it, and every call may be captured
 into a graph.  There is no backward pass, as in ``attention``.
 """
@@ -186,4 +191,117 @@ def shared_attention(q, cache: KVCache, batch: Batch, shared: SharedPrefix, scal
     _run(cache.index, _p.kv_attention_shared, stream, cache.ref, batch.ref, shared.ref, q.data_ptr(), ldq, heads,
          y.data_ptr(), ldy, None if lse is None else lse.data_ptr(), cache.softmax_scale if scale is None else scale,
          1 if causal else 0, None if workspace is None else workspace.data_ptr(), nbytes)
+    return (y, lse) if return_lse else y
+
+
+class PageBounds:
+    """Bounds of the keys of a cache's full pages over given buffers: codes int8
+    [num_pages, kv_heads, 2, head_dim] (largest, smallest; any page stride that is a
+    multiple of 16), step float32 [num_pages, kv_heads] (nvfp4_paging.h)."""
+
+    def __init__(self, codes, step):
+        _need(codes.dtype == torch.int8 and codes.dim() == 4 and codes.shape[2] == 2 and codes[:1].is_contiguous()
+              and (codes.shape[0] <= 1 or codes.stride(0) >= codes[0].numel()),
+              "codes must be int8 [num_pages, kv_heads, 2, head_dim]")
+        _need(step.dtype == torch.float32 and step.shape == codes.shape[:2] and (step.shape[1] == 1 or step.stride(1) == 1)
+              and (step.shape[0] <= 1 or step.stride(0) >= step.shape[1]), "step must be float32 [num_pages, kv_heads]")
+        _need(not step.requires_grad, "step takes no gradient here")
+        _need(codes.device == step.device, "the bounds' buffers are on several devices")
+        self.codes, self.step, self.index = codes, step, codes.get_device()
+        self.struct = _p.bounds_struct(codes, step)
+        if codes.shape[0] == 1:      # (strides of a single page say nothing)
+            self.struct.page_stride, self.struct.step_stride = codes[0].numel(), codes.shape[1]
+        self.ref = ctypes.byref(self.struct)
+
+
+def alloc_page_bounds(cache: KVCache):
+    """Bounds of an empty cache's pages."""
+    n, h = cache.k_scale.shape
+    return PageBounds(torch.zeros((n, h, 2, cache.head_dim), dtype=torch.int8, device=cache.device),
+                      torch.zeros((n, h), dtype=torch.float32, device=cache.device))
+
+
+def _of_cache(bounds, cache, batch):
+    if bounds.codes.shape[:2] != cache.k_scale.shape or bounds.codes.shape[3] != cache.head_dim:
+        raise ValueError("the bounds are of another cache")
+    if not cache.index == batch.index == bounds.index:
+        raise ValueError("tensors are on several devices")
+
+
+def page_bounds(cache: KVCache, batch: Batch, bounds: PageBounds, stream=None):
+    """The bounds of the pages that a step's appended rows completed."""
+    _of_cache(bounds, cache, batch)
+    _run(cache.index, _p.kv_page_bounds, stream, cache.ref, batch.ref, bounds.ref)
+
+
+class Selection:
+    """The pages chosen for each row and key head: ``index`` int32 [rows, kv_heads, count]
+    (numbers in the row's sequence, ascending, -1 behind them), ``pages`` (the same of the
+    pages themselves) and ``tokens`` int32 [rows] (what the row sees of them; -1: a row
+    behind the last sequence)."""
+
+    def __init__(self, index, pages, tokens):
+        for name, t in (("index", index), ("pages", pages)):
+            _need(t.dtype == _I32 and t.dim() == 3 and t.shape == index.shape and t.is_contiguous(),
+                  name + " must be int32 [rows, kv_heads, count]")
+        _need(tokens.dtype == _I32 and tokens.shape == index.shape[:1] and tokens.is_contiguous(), "tokens must be int32 [rows]")
+        _need(index.device == pages.device == tokens.device, "the selection's tensors are on several devices")
+        self.index, self.pages, self.tokens, self.device_index = index, pages, tokens, index.get_device()
+        self._workspace = {}
+
+    def workspace_bytes(self, cache, q_heads):
+        key = (q_heads, cache.kv_heads, cache.head_dim, cache.page_size)
+        if key not in self._workspace:
+            self._workspace[key] = _p.kv_attention_selected_workspace(cache.ref, self.index.shape[0], q_heads,
+                                                                      self.index.shape[2])
+        return self._workspace[key]
+
+
+def select_pages(q, cache: KVCache, batch: Batch, bounds: PageBounds, count, first=1, recent=1, causal=True,
+                 out: Selection = None, workspace=None, stream=None) -> Selection:
+    """Up to ``count`` pages for each of a step's rows and key heads: the ``first`` ones of
+    its sequence, the ``recent`` ones of those that it sees, and between them those whose
+    keys' bounds allow the largest products with a query of the key head (for a positive
+    softmax scale); all, where there are no more."""
+    rows, heads, dim, ldq = _rows(q, "q")
+    if rows != batch.rows or dim != cache.head_dim or heads == 0 or heads % cache.kv_heads:
+        raise ValueError("q has the wrong rows, heads or head_dim")
+    _of_cache(bounds, cache, batch)
+    if q.get_device() != cache.index:
+        raise ValueError("tensors are on several devices")
+    if count < 1 or first < 0 or recent < 1 or first + recent > count:
+        raise ValueError("first and recent pages must be among the count, with at least one recent page")
+    shape = (rows, cache.kv_heads, int(count))
+    if out is None:
+        with _l._on(stream, q.device):
+            index = torch.empty(shape, dtype=_I32, device=q.device)
+            out = Selection(index, torch.empty_like(index), torch.empty(rows, dtype=_I32, device=q.device))
+    elif out.index.shape != shape:
+        raise ValueError("out must be a selection of these rows, key heads and count")
+    elif out.device_index != cache.index:
+        raise ValueError("out is on another device")
+    workspace, nbytes = _room(workspace, 0 if workspace is not None else
+                              _p.kv_select_pages_workspace(cache.ref, batch.ref), q, stream)
+    _run(cache.index, _p.kv_select_pages, stream, cache.ref, batch.ref, bounds.ref, q.data_ptr(), ldq, heads, count, first,
+         recent, 1 if causal else 0, out.index.data_ptr(), out.pages.data_ptr(), out.tokens.data_ptr(),
+         None if workspace is None else workspace.data_ptr(), nbytes)
+    return out
+
+
+def selected_attention(q, cache: KVCache, selection: Selection, scale=None, out=None, return_lse=False, workspace=None,
+                       stream=None):
+    """Attention of each row over the pages chosen for it.  Returns y (bf16, q's shape),
+    with the log-sum-exp over those tokens if ``return_lse``."""
+    n, kv_heads, count = selection.index.shape
+    rows, heads, ldq, y, ldy = _queries(q, cache, n, out, stream)
+    if kv_heads != cache.kv_heads:
+        raise ValueError("the selection is of other key heads")
+    if selection.device_index != cache.index:
+        raise ValueError("tensors are on several devices")
+    lse = _lse(return_lse, rows, heads, q, stream)
+    workspace, nbytes = _room(workspace, 0 if workspace is not None else selection.workspace_bytes(cache, heads), q, stream)
+    _run(cache.index, _p.kv_attention_selected, stream, cache.ref, q.data_ptr(), ldq, heads, rows, count,
+         selection.pages.data_ptr(), selection.tokens.data_ptr(), y.data_ptr(), ldy,
+         None if lse is None else lse.data_ptr(), cache.softmax_scale if scale is None else scale,
+         None if workspace is None else workspace.data_ptr(), nbytes)
     return (y, lse) if return_lse else y

@@ -2,9 +2,12 @@
 worked examples, and a tally by sets.  CPU only."""
 
 import random
+from fractions import Fraction
 
+import numpy as np
 import pytest
 
+from oracle import attention as OA
 from oracle import paging as OP
 
 
@@ -54,3 +57,47 @@ def test_every_page_is_in_one_place(seed):
             assert got in (0, new[b]) and p.kv_len[b] == base + got
             assert p.table[b][:p.pages(base)] == before[0][b][:p.pages(base)]      # held tokens stay where they are
             assert list(pos[cu[b]:cu[b + 1]]) == list(range(base, base + got))
+
+
+def _brute(q, keys):
+    return max(float(a @ b) for a in q for b in keys)
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_bounds_bound_and_round_as_stated(seed):
+    rng = np.random.default_rng(seed)
+    dim, tokens, heads = 64, 16, 3
+    grid = np.array([v for v in OA.E4M3_VALUES if not np.isnan(v)])
+    values, scale = rng.choice(grid[np.abs(grid) < 20], (tokens, dim)), 2.0 ** -5
+    codes, step = OP.page_bounds(values, scale)
+    top = np.abs(values).max()
+    assert np.abs(codes).max() == 127 and step == np.float32(np.float32(top * scale) / np.float32(127))
+    for e in range(dim):                                   # exact roundings, by rationals
+        for row, v in ((0, values[:, e].max()), (1, values[:, e].min())):
+            assert codes[row, e] == round(Fraction(float(v)) * 127 / Fraction(float(top)))
+    q = rng.standard_normal((heads, dim)).astype(np.float16).astype(np.float64)
+    i, units = OP.query_codes(q)
+    for a in range(heads):
+        most = np.abs(q[a]).max()
+        assert [round(Fraction(float(x)) * 127 / Fraction(float(most))) for x in q[a]] == list(i[a])
+        assert units[a] == np.float32(np.float32(most) / np.float32(127))
+    # The score bounds every product, but for half a step of either factor.
+    score = float(OP.page_score(i, units, codes, step))
+    slack = max(float(units[a]) * np.abs(codes).max() * float(step) * dim / 2 + float(step) / 2 * np.abs(q[a]).sum()
+                for a in range(heads))
+    assert score >= _brute(q, values * scale) - slack
+    # and is the product itself where a page holds one key, written out.
+    one, unit = OP.page_bounds(values[:1].repeat(tokens, 0), scale)
+    assert OP.page_score(i[:1], units[:1], one, unit) == np.float32(
+        float(np.float32(float(i[0] @ one[0]) * float(units[0]))) * float(unit))
+    assert (OP.page_bounds(np.zeros((tokens, dim)), 1.0)[0] == 0).all() and OP.page_bounds(np.zeros((2, 4)), 1.0)[1] == 0
+    assert (OP.query_codes(np.zeros((1, 8)))[0] == 0).all()
+
+
+def test_choice():
+    s = [9.0, 1.0, 5.0, 5.0, 7.0, 5.0, None, 0.0]
+    assert OP.choose(s, 8, 8, 1, 1) == list(range(8)) and OP.choose(s, 3, 4, 1, 1) == [0, 1, 2]
+    assert OP.choose(s, 8, 4, 0, 1) == [0, 2, 4, 7]        # the lowest among equals
+    assert OP.choose(s, 8, 5, 1, 2) == [0, 2, 4, 6, 7]
+    assert OP.choose(s, 8, 3, 2, 1) == [0, 1, 7] and OP.choose(s, 8, 7, 0, 1) == [0, 1, 2, 3, 4, 5, 7]
+    assert OP.choose([-1.0, -3.0, -2.0, 0.0], 4, 3, 0, 1) == [0, 2, 3] and OP.choose(s, 0, 3, 1, 1) == []

@@ -16,7 +16,8 @@ from paper_2609_04098_amd import paging as P
 from tests.test_attention_abi import BAD_BATCHES, BAD_CACHES, FAKE, ROOT, _batch, _cache
 
 HEADER = os.path.join(ROOT, "include", "nvfp4_paging.h")
-STRUCTS = {"nvfp4_requests": N.RequestsStruct, "nvfp4_shared_prefix": N.SharedPrefixStruct}
+STRUCTS = {"nvfp4_requests": N.RequestsStruct, "nvfp4_shared_prefix": N.SharedPrefixStruct,
+           "nvfp4_kv_bounds": N.BoundsStruct}
 
 
 def test_header_matches_the_binding_and_the_library():
@@ -146,6 +147,131 @@ def test_shared_attention_refuses_wrong_tensors():
             call()
     with pytest.raises(ValueError, match="GPU"):
         P.shared_attention(x, c, b, g)
+
+
+def _bounds(**kw):
+    a = dict(codes=FAKE, step=FAKE, page_stride=512, step_stride=2)
+    a.update(kw)
+    return N.BoundsStruct(**a)
+
+
+def _page_bounds(cache=None, batch=None, bounds=None):
+    c, b, g = (x if x is not None else f() for x, f in ((cache, _cache), (batch, _batch), (bounds, _bounds)))
+    return N.lib().nvfp4_kv_page_bounds(ctypes.byref(c), ctypes.byref(b), ctypes.byref(g), None)
+
+
+def _select(cache=None, batch=None, bounds=None, **kw):
+    a = dict(q=FAKE, ldq=512, hq=4, count=4, first=1, recent=1, causal=1, index=FAKE, pages=FAKE, tokens=FAKE, ws=FAKE,
+             wsb=1 << 30)
+    a.update(kw)
+    c, b, g = (x if x is not None else f() for x, f in ((cache, _cache), (batch, _batch), (bounds, _bounds)))
+    return N.lib().nvfp4_kv_select_pages(ctypes.byref(c), ctypes.byref(b), ctypes.byref(g), a["q"], a["ldq"], a["hq"],
+                                         a["count"], a["first"], a["recent"], a["causal"], a["index"], a["pages"],
+                                         a["tokens"], a["ws"], a["wsb"], None)
+
+
+def _selected(cache=None, **kw):
+    a = dict(q=FAKE, ldq=512, hq=4, rows=5, count=4, pages=FAKE, tokens=FAKE, y=FAKE, ldy=512, lse=None, scale=0.1, ws=FAKE,
+             wsb=1 << 30)
+    a.update(kw)
+    c = cache if cache is not None else _cache()
+    return N.lib().nvfp4_kv_attention_selected(ctypes.byref(c), a["q"], a["ldq"], a["hq"], a["rows"], a["count"], a["pages"],
+                                               a["tokens"], a["y"], a["ldy"], a["lse"], a["scale"], a["ws"], a["wsb"], None)
+
+
+@pytest.mark.parametrize("call", [_page_bounds, _select, _selected])
+@pytest.mark.parametrize("bad", BAD_CACHES)
+def test_selection_refuses_caches(call, bad):
+    assert call(cache=_cache(**bad)) == C.NVFP4_EINVAL
+
+
+@pytest.mark.parametrize("call", [_page_bounds, _select])
+@pytest.mark.parametrize("bad", BAD_BATCHES)
+def test_selection_refuses_batches(call, bad):
+    assert call(batch=_batch(**bad)) == C.NVFP4_EINVAL
+
+
+@pytest.mark.parametrize("call", [_page_bounds, _select])
+@pytest.mark.parametrize("bad", [dict(codes=None), dict(step=None), dict(codes=FAKE + 8), dict(step=FAKE + 2),
+                                 dict(page_stride=496), dict(page_stride=520), dict(step_stride=1)])
+def test_selection_refuses_bounds(call, bad):
+    assert call(bounds=_bounds(**bad)) == C.NVFP4_EINVAL
+
+
+@pytest.mark.parametrize("bad", [
+    dict(q=None), dict(q=FAKE + 2), dict(ldq=504), dict(hq=3), dict(hq=0), dict(count=0), dict(count=(1 << 25) + 1),
+    dict(first=-1), dict(recent=0), dict(first=4), dict(first=2, recent=3), dict(recent=5), dict(causal=2),
+    dict(first=(1 << 63) - 1), dict(recent=(1 << 63) - 1), dict(index=None), dict(pages=None), dict(tokens=None),
+    dict(index=FAKE + 2), dict(pages=FAKE + 1), dict(tokens=FAKE + 2), dict(ws=None), dict(ws=FAKE + 8)])
+def test_select_refuses(bad):
+    assert _select(**bad) == C.NVFP4_EINVAL
+
+
+@pytest.mark.parametrize("bad", [
+    dict(q=None), dict(y=None), dict(q=FAKE + 2), dict(y=FAKE + 4), dict(ldq=504), dict(ldy=516), dict(hq=3), dict(hq=0),
+    dict(lse=FAKE + 2), dict(scale=float("inf")), dict(rows=-1), dict(rows=1 << 24), dict(count=0), dict(count=(1 << 25) + 1),
+    dict(pages=None), dict(tokens=None), dict(pages=FAKE + 2), dict(tokens=FAKE + 1),
+    dict(rows=(1 << 24) - 1, hq=130, ldq=1 << 15, ldy=1 << 15)])
+def test_selected_attention_refuses(bad):
+    assert _selected(**bad) == C.NVFP4_EINVAL
+
+
+def test_selection_wants_its_workspaces():
+    f, c, b = N.lib(), _cache(), _batch()
+    need = f.nvfp4_kv_select_pages_workspace(ctypes.byref(c), ctypes.byref(b))
+    assert need > 0 and _select(wsb=need - 1) == C.NVFP4_EWORKSPACE
+    assert f.nvfp4_kv_select_pages_workspace(ctypes.byref(c), ctypes.byref(_batch(rows=-1))) == 0
+    need = f.nvfp4_kv_attention_selected_workspace(ctypes.byref(c), 1, 4, 2000)
+    assert need > 0 and _selected(rows=1, count=2000, wsb=need - 1) == C.NVFP4_EWORKSPACE
+    assert _selected(rows=1, count=2000, ws=None) == C.NVFP4_EINVAL == _selected(rows=1, count=2000, ws=FAKE + 4)
+    assert f.nvfp4_kv_attention_selected_workspace(ctypes.byref(c), 1, 4, 0) == 0
+    assert f.nvfp4_kv_attention_selected_workspace(ctypes.byref(c), 0, 4, 2000) == 0
+    assert f.nvfp4_kv_page_bounds(None, ctypes.byref(b), ctypes.byref(_bounds()), None) == C.NVFP4_EINVAL
+    assert _select(batch=_batch(n_seqs=0)) == C.NVFP4_EINVAL      # rows of no sequence
+
+
+def test_selection_refuses_more_workgroups_than_a_launch_holds():
+    heads = 64
+    c = _cache(kv_heads=heads, page_size=16, k_page_stride=heads * 2048, v_page_stride=heads * 2048, scale_page_stride=heads)
+    b, g = _batch(n_seqs=1 << 21, rows=1 << 21, cu_rows=None), _bounds(page_stride=1 << 16, step_stride=heads)
+    assert _page_bounds(c, b, g) == C.NVFP4_EINVAL
+    assert _select(c, b, g, hq=heads, ldq=heads * 128, wsb=1 << 62) == C.NVFP4_EINVAL
+    assert _selected(c, hq=heads, rows=1 << 21, ldq=heads * 128, ldy=heads * 128) == C.NVFP4_EINVAL
+
+
+def test_selection_refuses_wrong_tensors():
+    c = A.alloc_kv_cache(4, 2, 64, 16, "cpu")
+    b = A.Batch(_i32(3, 2), _i32(3))
+    x = torch.zeros(3, 4, 64, dtype=torch.bfloat16)
+    g = P.alloc_page_bounds(c)
+    sel = P.Selection(_i32(3, 2, 4), _i32(3, 2, 4), _i32(3))
+    other = P.alloc_page_bounds(A.alloc_kv_cache(5, 2, 64, 16, "cpu"))
+    for call in (lambda: P.PageBounds(g.codes.float(), g.step), lambda: P.PageBounds(g.codes[:, :1], g.step),
+                 lambda: P.PageBounds(g.codes.transpose(1, 2), g.step), lambda: P.PageBounds(g.codes, g.step.double()),
+                 lambda: P.PageBounds(g.codes[:1].expand(4, 2, 2, 64), g.step), lambda: P.PageBounds(g.codes, g.step[:1].expand(4, 2)),
+                 lambda: P.page_bounds(c, b, other), lambda: P.select_pages(x, c, b, other, 4),
+                 lambda: P.select_pages(x[:2], c, b, g, 4), lambda: P.select_pages(x.float(), c, b, g, 4),
+                 lambda: P.select_pages(x, c, b, g, 0), lambda: P.select_pages(x, c, b, g, 4, first=4),
+                 lambda: P.select_pages(x, c, b, g, 4, recent=0), lambda: P.select_pages(x, c, b, g, 4, first=-1),
+                 lambda: P.select_pages(x, c, b, g, 5, out=sel), lambda: P.Selection(_i32(3, 2, 4), _i32(3, 2, 3), _i32(3)),
+                 lambda: P.Selection(_i32(3, 2, 4), _i32(3, 2, 4), _i32(2)), lambda: P.Selection(_i32(3, 2, 4).long(), _i32(3, 2, 4), _i32(3)),
+                 lambda: P.selected_attention(x[:2], c, sel), lambda: P.selected_attention(x[:, :3], c, sel),
+                 lambda: P.selected_attention(x, A.alloc_kv_cache(4, 4, 64, 16, "cpu"), sel),
+                 lambda: P.selected_attention(x, c, sel, out=x[:, :2]), lambda: P.selected_attention(x.requires_grad_(), c, sel)):
+        with pytest.raises(ValueError):
+            call()
+    x = x.detach()
+    far, far_sel = x.to("meta"), P.Selection(*[t.to("meta") for t in (sel.index, sel.pages, sel.tokens)])
+    for call in (lambda: P.PageBounds(g.codes, g.step.to("meta")), lambda: P.select_pages(far, c, b, g, 4),
+                 lambda: P.select_pages(x, c, b, g, 4, out=far_sel), lambda: P.selected_attention(x, c, far_sel),
+                 lambda: P.selected_attention(far, c, sel), lambda: P.select_pages(x, c, b, g, 4, workspace=far),
+                 lambda: P.page_bounds(c, b, P.PageBounds(g.codes.to("meta"), g.step.to("meta"))),
+                 lambda: P.Selection(sel.index, sel.pages.to("meta"), sel.tokens)):
+        with pytest.raises(ValueError, match="device"):
+            call()
+    for call in (lambda: P.page_bounds(c, b, g), lambda: P.select_pages(x, c, b, g, 4), lambda: P.selected_attention(x, c, sel)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
 
 
 def _i32(*shape):
