@@ -111,8 +111,8 @@ typedef struct nvfp4_shared_prefix {
   int64_t max_own;
 } nvfp4_shared_prefix;
 
-/* Workspace bytes of nvfp4_kv_attention_shared (partial results); 0: the batch has no
- * rows, or the arguments are invalid. */
+/* Workspace bytes of nvfp4_kv_attention_shared (partial results); 0: none is used, or
+ * the arguments are invalid. */
 size_t nvfp4_kv_attention_shared_workspace(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
                                            const nvfp4_shared_prefix* shared, int64_t q_heads);
 
@@ -124,15 +124,22 @@ size_t nvfp4_kv_attention_shared_workspace(const nvfp4_kv_cache* cache, const nv
  * does.  A sequence that does not, one that is empty for instance, is computed over its
  * own row of page_table alone.  Accuracy: as stated there, for each of the two parts.
  *
+ * Steps for which sharing is taken to be slower by their sizes (short prefixes, many
+ * rows of a sequence) take the kernels of nvfp4_kv_attention.
+ *
  *   workspace, workspace_bytes   at least nvfp4_kv_attention_shared_workspace bytes,
- *                16-byte aligned.  Its contents on entry do not matter; calls sharing
- *                one must be ordered.
+ *                16-byte aligned (NULL if that is 0).  Its contents on entry do not
+ *                matter; calls sharing one must be ordered.
  * The others, and the requirements, as for nvfp4_kv_attention.
  * Errors: NVFP4_EINVAL, NVFP4_EWORKSPACE, NVFP4_EUNSUPPORTED, NVFP4_EHIP.
  */
 int nvfp4_kv_attention_shared(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_shared_prefix* shared,
                               const void* q, int64_t ldq, int64_t q_heads, void* y, int64_t ldy, float* lse,
                               float softmax_scale, int causal, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Which kernels nvfp4_kv_attention_shared launches for a step: as nvfp4_kv_attention_kernel. */
+const char* nvfp4_kv_attention_shared_kernel(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
+                                             const nvfp4_shared_prefix* shared, int64_t q_heads, int part);
 
 /*
  * Bounds of the keys of a cache's pages, in 8 bits: page p and head h hold 2 * head_dim

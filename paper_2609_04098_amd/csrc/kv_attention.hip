@@ -16,7 +16,7 @@ namespace nvfp4 {
 
 template <int D, int kTiles, int kWaves, bool kSplit>
 __global__ __launch_bounds__(kWaves * 64, rows_waves(D, kTiles, kWaves, kSplit)) void kv_attention_rows_kernel(AttentionArgs a) {
-  attention_rows<D, kTiles, kWaves, kSplit>(a);
+  attention_rows_kernel<D, kTiles, kWaves, kSplit>(a);
 }
 
 template <int D, int kTiles, int kShare>

@@ -44,23 +44,26 @@ __device__ __forceinline__ void load_codes(const AttentionArgs& a, int kind, int
 // sequences leave empty make room for others then, and two long ones do not share a
 // unit (16 sequences of up to 32768, 4 key heads of 256, in four pieces: 105 us, two
 // to a unit 173; 32 of 3000, 8 key heads of 128, eight waves: 38 and 48 us).
+template <int D, int kTiles, int kWaves>
+struct RowsLds {
+  static constexpr int kPart = kWaves > 4 ? 64 : (D > 128 ? 128 : D);      // elements of a row that are joined at a time
+  float joined[kWaves][16][kPart + 4];
+  float2 stats[kWaves][16 * kTiles];
+};
+
+// LDS that a kernel asks for and does not use, to have a compute unit to itself.
+constexpr int alone_bytes(int dim, int tiles, int waves, bool split) {
+  return waves > 4 || (dim == 256 && tiles == 1 && split) ? 65536 : 16;
+}
+
+// Key head h, piece `piece` (0, unless kSplit) of the tile with that number.
 template <int D, int kTiles, int kWaves, bool kSplit, typename Args>
-__device__ __forceinline__ void attention_rows(Args a) {
-  constexpr int kRows = 16 * kTiles, kThreads = kWaves * 64;
-  constexpr int kPart = kWaves > 4 ? 64 : (D > 128 ? 128 : D);            // elements of a row that are joined at a time
-  __shared__ struct {
-    float joined[kWaves][16][kPart + 4];
-    char alone[kWaves > 4 || (D == 256 && kTiles == 1 && kSplit) ? 65536 : 1];      // (so that they have)
-  } lds;
-  __shared__ float2 stats[kWaves][kRows];
+__device__ __forceinline__ void attention_rows(Args a, int h, int number, int piece, RowsLds<D, kTiles, kWaves>& lds) {
+  constexpr int kRows = 16 * kTiles, kThreads = kWaves * 64, kPart = RowsLds<D, kTiles, kWaves>::kPart;
+  auto& stats = lds.stats;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quarter = lane >> 4;
-  int id = blockIdx.x;
-  const int h = id % a.cache.heads;
-  id /= a.cache.heads;
-  const int number = kSplit ? id / a.splits : id;
-  const int piece = kSplit ? piece_of(id % a.splits, number, a.splits) : 0;
   Tile t;
   if (!find_tile<kRows>(a, number, t)) return;
   int begin = t.begin, end = t.end;
@@ -169,6 +172,28 @@ __device__ __forceinline__ void attention_rows(Args a) {
       }
     }
   }
+}
+
+// What a workgroup takes: heads side by side, then a tile's pieces.
+template <bool kSplit>
+__device__ __forceinline__ void work_of(const AttentionArgs& a, int& h, int& number, int& piece) {
+  int id = blockIdx.x;
+  h = id % a.cache.heads;
+  id /= a.cache.heads;
+  number = kSplit ? id / a.splits : id;
+  piece = kSplit ? piece_of(id % a.splits, number, a.splits) : 0;
+}
+
+// A whole kernel of it.
+template <int D, int kTiles, int kWaves, bool kSplit, typename Args>
+__device__ __forceinline__ void attention_rows_kernel(Args a) {
+  __shared__ struct {
+    RowsLds<D, kTiles, kWaves> rows;
+    char alone[alone_bytes(D, kTiles, kWaves, kSplit)];
+  } lds;
+  int h, number, piece;
+  work_of<kSplit>(a, h, number, piece);
+  attention_rows<D, kTiles, kWaves, kSplit>(a, h, number, piece, lds.rows);
 }
 
 // Joins the pieces of a sequence.  kShare waves take a packed row, each its

@@ -40,12 +40,12 @@ __device__ __forceinline__ GroupPages group_pages(const SelectedArgs& a, int b, 
 
 template <int D, int kTiles, int kWaves, bool kSplit>
 __global__ __launch_bounds__(kWaves * 64, rows_waves(D, kTiles, kWaves, kSplit)) void kv_selected_rows_kernel(SelectedArgs a) {
-  attention_rows<D, kTiles, kWaves, kSplit>(a);
+  attention_rows_kernel<D, kTiles, kWaves, kSplit>(a);
 }
 
 template <int D>
 __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_selected_tile_kernel(SelectedArgs a, int tiles) {
-  attention_tile<D, true>(a, tiles);
+  attention_tile_kernel<D, true>(a, tiles);
 }
 
 template <int D, int kTiles, int kShare>

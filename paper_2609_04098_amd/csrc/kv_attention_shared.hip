@@ -1,9 +1,9 @@
 // Attention of a batch whose sequences share prefixes, over the paged E4M3 cache
 // (definition: nvfp4_paging.h), for gfx950.
 //
-// Two passes of the attention's kernels and a join: the rows of all of a group's
-// sequences over its prefix, which is read once for all of them, and each sequence's
-// rows over its own tokens.  Both keep (maximum, sum, unscaled y) of every row in
+// Two passes of the attention's kernels, side by side in one launch, and a join: the rows
+// of all of a group's sequences over its prefix, which is read once for all of them, and
+// each sequence's rows over its own tokens.  Both keep (maximum, sum, unscaled y) of every row in
 // 32 bits, and the join takes them together as it does the pieces of one sequence:
 //   m = max m_i,  y = sum_i 2^(m_i - m) y_i / sum_i 2^(m_i - m) l_i.
 #include "attention_plan.h"
@@ -13,58 +13,106 @@
 
 namespace nvfp4 {
 
-template <int D, int kTiles>
-__global__ __launch_bounds__(256, rows_waves(D, kTiles, 4, true)) void kv_attention_prefix_rows_kernel(PrefixArgs a) {
-  attention_rows<D, kTiles, 4, true>(a);
-}
+// The rows of a workgroup in either pass, 16 times kPrefix and kOwn: 8 is the form of
+// 128 rows (kv_attention_wide.h).
+template <int D, int kForm>
+struct PassLds {
+  RowsLds<D, kForm, 4> of;
+};
 
 template <int D>
-__global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_prefix_tile_kernel(PrefixArgs a, int tiles) {
-  attention_tile<D, true>(a, tiles);
+struct PassLds<D, 8> {
+  TileLds<D> of;
+};
+
+constexpr int pass_waves(int dim, int form) { return form == 8 ? (dim == 256 ? 2 : 3) : rows_waves(dim, form, 4, false); }
+constexpr int fewer(int a, int b) { return a < b ? a : b; }
+
+template <int D, int kForm, typename Args>
+__device__ __forceinline__ void pass(const Args& a, int tiles, int h, int number, int piece, void* lds) {
+  auto& of = static_cast<PassLds<D, kForm>*>(lds)->of;
+  if constexpr (kForm == 8)
+    attention_tile<D, true>(a, tiles, h, number, piece, of);
+  else
+    attention_rows<D, kForm, 4, true>(a, h, number, piece, of);
 }
 
-template <int D, int kTiles, int kWaves>
-__global__ __launch_bounds__(kWaves * 64, rows_waves(D, kTiles, kWaves, true)) void kv_attention_own_rows_kernel(OwnArgs a) {
-  attention_rows<D, kTiles, kWaves, true>(a);
+// Both passes in one launch, so that the prefixes' products, which the matrix and vector
+// units bound, run beside the own tokens' loads, which memory bounds.  The prefixes' go
+// first: few long workgroups, spread evenly while the compute units are empty (mixed with
+// the short ones, 3 of 288 came to one unit and none to others: 218 us for 80).
+// Workgroups go to the eight dies in turn: a die takes a run of the prefix's work, in
+// which the tiles of rows that read the same keys follow each other.
+template <int D, int kPrefix, int kOwn>
+__global__ __launch_bounds__(256, fewer(pass_waves(D, kPrefix), pass_waves(D, kOwn))) void kv_attention_shared_kernel(
+    SharedArgs a, PrefixPieces of, SharedWork w) {
+  constexpr size_t kBytes = sizeof(PassLds<D, kPrefix>) > sizeof(PassLds<D, kOwn>) ? sizeof(PassLds<D, kPrefix>)
+                                                                                   : sizeof(PassLds<D, kOwn>);
+  __shared__ __attribute__((aligned(16))) char lds[kBytes];
+  if (blockIdx.x >= 8 * w.prefix_eighth) {
+    const unsigned id = blockIdx.x - 8 * w.prefix_eighth;
+    OwnArgs o;
+    static_cast<SharedArgs&>(o) = a;
+    const unsigned rest = id / a.cache.heads, number = rest / a.splits;
+    pass<D, kOwn>(o, w.own_tiles, (int)(id % a.cache.heads), (int)number, piece_of((int)(rest % a.splits), (int)number, a.splits), lds);
+  } else {
+    const unsigned id = (blockIdx.x & 7) * w.prefix_eighth + (blockIdx.x >> 3);
+    if (id >= w.prefix) return;
+    PrefixArgs p;
+    static_cast<SharedArgs&>(p) = a;
+    p.causal = 0;
+    p.chunk = of.chunk;
+    p.splits = of.splits;
+    p.part = of.part;
+    const unsigned rest = id / w.prefix_tiles;
+    pass<D, kPrefix>(p, w.prefix_tiles, (int)(rest / of.splits), (int)(id % w.prefix_tiles), (int)(rest % of.splits), lds);
+  }
 }
 
+// A wave takes a query head of a row, kAhead pieces' loads in flight: those of its
+// group's prefix, then its own.
 template <int D>
-__global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_own_tile_kernel(OwnArgs a, int tiles) {
-  attention_tile<D, true>(a, tiles);
-}
-
-// A wave takes a packed row, four pieces' loads in flight: those of its group's
-// prefix, then its own.
-template <int D, int kTiles>
 __global__ __launch_bounds__(256) void kv_attention_shared_join_kernel(SharedArgs a, PrefixPieces of) {
-  constexpr int kRows = 16 * kTiles, kEach = D / 64, kAhead = 4;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row = (int)(blockIdx.x % (kRows / 4)) * 4 + wave;
-  const int h = (int)(blockIdx.x / (kRows / 4)) % a.cache.heads;
-  const int number = (int)(blockIdx.x / (kRows / 4)) / a.cache.heads;
+  constexpr int kEach = D / 64, kAhead = 8;
+  const int lane = threadIdx.x & 63;
+  const unsigned item = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int token_row = __builtin_amdgcn_readfirstlane(item / a.q_heads), head = __builtin_amdgcn_readfirstlane(item % a.q_heads);
+  if (token_row >= a.batch.rows) return;
   Tile t;
-  int g, prefix;
-  if (!find_own_tile<kRows>(a, number, t, g, prefix) || row >= t.n) return;
-  const int r = t.r0 + row;                                            // of the sequence
-  const int own = pieces_of(a, t);
-  const int before = prefix > 0 ? min((prefix - 1) / of.chunk, of.splits - 1) + 1 : 0;
+  int g, group_seq, ordinal;
+  const SeqRows s = find_rows(a.batch, token_row, 1, t.b, ordinal, [](int first, int) { return first; });
+  if (ordinal < 0 || ordinal >= s.rows) return;                        // behind the last sequence
+  const int prefix = shared_prefix(a, t.b, s.first, g, group_seq);
+  const int h = head / a.group, r = ordinal * a.group + head % a.group;      // packed row of the sequence
   const float2* stats[2];
   const float* part[2];
-  int stride[2] = {1, kRows};
-  stats[0] = nullptr, part[0] = nullptr;
+  int stride[2];
+  // A row of a tile, of `rows`: its first piece, of `splits` of that many tiles' heads.
+  const auto of_tile = [&](int which, const float* parts, int64_t tile, int64_t tiles, int row, int shift, int splits) {
+    const int64_t first = (((tile * a.cache.heads + h) * splits) << shift) + row;
+    stats[which] = reinterpret_cast<const float2*>(parts) + first;
+    part[which] = parts + 2 * ((tiles * a.cache.heads * splits) << shift) + first * D + lane * kEach;
+    stride[which] = 1 << shift;
+  };
+  const int before = prefix > 0 ? min((prefix - 1) / of.chunk, of.splits - 1) + 1 : 0;
+  stats[0] = nullptr, part[0] = nullptr, stride[0] = 0;
   if (before > 0) {
-    const int row0 = start_row(a.batch, group_start(a, g)), rows = 16 * of.tiles;
-    const int packed = (t.row0 - row0) * a.group + r;
-    const int64_t tile = (int64_t)row0 * a.group / rows + g + packed / rows;
-    const int64_t first = (tile * a.cache.heads + h) * of.splits * rows + packed % rows;
-    const int64_t all = ((int64_t)a.batch.rows * a.group / rows + a.groups) * a.cache.heads * of.splits * rows;
-    stats[0] = reinterpret_cast<const float2*>(of.part) + first;
-    part[0] = of.part + 2 * all + first * D + lane * kEach;
-    stride[0] = rows;
+    const int row0 = start_row(a.batch, group_seq), shift = 4 + __builtin_ctz(of.tiles);
+    const int packed = (s.row - row0) * a.group + r;
+    of_tile(0, of.part, (((int64_t)row0 * a.group) >> shift) + g + (packed >> shift),
+            prefix_tile_numbers((int64_t)a.batch.rows * a.group, 1 << shift, a.groups), packed & ((1 << shift) - 1), shift, of.splits);
   }
-  const int64_t first = ((int64_t)number * a.cache.heads + h) * a.splits * kRows + row;
-  stats[1] = reinterpret_cast<const float2*>(a.part) + first;
-  part[1] = a.part + part_tiles(a, kRows) * a.cache.heads * a.splits * (2 * kRows) + first * D + lane * kEach;
+  int own;
+  {
+    const int shift = 4 + __builtin_ctz(a.row_tiles), rows = 1 << shift, row = r & (rows - 1);
+    const int tile = a.batch.cu_rows == nullptr ? t.b * ((a.group + rows - 1) >> shift) : (int)(((int64_t)s.row * a.group) >> shift) + t.b;
+    of_tile(1, a.part, tile + (r >> shift), tiles_of(a.batch, a.group, rows), row, shift, a.splits);
+    // The tokens of the row's tile, as find_tile() has them.
+    const int last = min(s.rows * a.group, r - row + rows) - 1;
+    t.end = a.causal ? min(s.len, s.first + last / a.group + 1) : s.len;
+    t.begin = min(prefix, max(0, t.end));
+    own = pieces_of(a, t);
+  }
 
   float m = kNone, l = 0.0f, y[kEach];
 #pragma unroll
@@ -102,9 +150,7 @@ __global__ __launch_bounds__(256) void kv_attention_shared_join_kernel(SharedArg
       for (int i = 0; i < kEach; ++i) y[i] = fmaf(v[u][i], w, y[i]);
     }
   }
-  const int head = h * a.group + r % a.group;
-  const int64_t token_row = t.row0 + r / a.group;
-  uint16_t* to = a.y + token_row * a.ldy + (int64_t)head * D;
+  uint16_t* to = a.y + (int64_t)token_row * a.ldy + (int64_t)head * D;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   if (D == 64)
     to[lane] = __builtin_bit_cast(uint16_t, (__bf16)(y[0] * inv));
@@ -113,76 +159,57 @@ __global__ __launch_bounds__(256) void kv_attention_shared_join_kernel(SharedArg
     for (int i = 0; i + 1 < kEach; i += 2)
       *reinterpret_cast<uint32_t*>(to + lane * kEach + i) = bf16_pair(y[i] * inv, y[i + 1] * inv);
   if (a.lse != nullptr && lane == 0)
-    a.lse[token_row * a.q_heads + head] = l == 0.0f ? kNone : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
+    a.lse[(int64_t)token_row * a.q_heads + head] = l == 0.0f ? kNone : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
 
 namespace {
 
-template <int D>
-hipError_t launch_prefix(const PrefixArgs& a, int64_t tiles, hipStream_t stream) {
-  const dim3 grid((unsigned)(tiles * a.cache.heads * a.splits));
-  if (a.row_tiles == 8)
-    kv_attention_prefix_tile_kernel<D><<<grid, 256, 0, stream>>>(a, (int)tiles);
-  else if (a.row_tiles == 2)
-    kv_attention_prefix_rows_kernel<D, 2><<<grid, 256, 0, stream>>>(a);
-  else
-    kv_attention_prefix_rows_kernel<D, 1><<<grid, 256, 0, stream>>>(a);
+template <int D, int kPrefix, int kOwn>
+hipError_t launch_passes(const SharedArgs& a, const PrefixPieces& of, const SharedWork& w, unsigned workgroups, hipStream_t stream) {
+  kv_attention_shared_kernel<D, kPrefix, kOwn><<<dim3(workgroups), 256, 0, stream>>>(a, of, w);
   return hipGetLastError();
 }
 
 template <int D>
-hipError_t launch_own(const OwnArgs& a, int64_t tiles, hipStream_t stream) {
-  const dim3 grid((unsigned)(tiles * a.cache.heads * a.splits));
-  if (a.row_tiles == 8)
-    kv_attention_own_tile_kernel<D><<<grid, 256, 0, stream>>>(a, (int)tiles);
-  else if (a.row_tiles == 2)
-    kv_attention_own_rows_kernel<D, 2, 4><<<grid, 256, 0, stream>>>(a);
-  else if (a.waves == 8)
-    kv_attention_own_rows_kernel<D, 1, 8><<<grid, 512, 0, stream>>>(a);
-  else
-    kv_attention_own_rows_kernel<D, 1, 4><<<grid, 256, 0, stream>>>(a);
-  return hipGetLastError();
-}
-
-template <int D>
-hipError_t launch_join(const SharedArgs& a, const PrefixPieces& of, int64_t tiles, hipStream_t stream) {
-  const dim3 grid((unsigned)(tiles * a.cache.heads * a.row_tiles * 4));
-  if (a.row_tiles == 8)
-    kv_attention_shared_join_kernel<D, 8><<<grid, 256, 0, stream>>>(a, of);
-  else if (a.row_tiles == 2)
-    kv_attention_shared_join_kernel<D, 2><<<grid, 256, 0, stream>>>(a, of);
-  else
-    kv_attention_shared_join_kernel<D, 1><<<grid, 256, 0, stream>>>(a, of);
+hipError_t launch_join(const SharedArgs& a, const PrefixPieces& of, hipStream_t stream) {
+  const int64_t items = (int64_t)a.batch.rows * a.q_heads;
+  kv_attention_shared_join_kernel<D><<<dim3((unsigned)((items + 3) / 4)), 256, 0, stream>>>(a, of);
   return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch(const SharedArgs& a, const SharedPlan& p, hipStream_t stream) {
-  OwnArgs own;
-  static_cast<SharedArgs&>(own) = a;
-  const int64_t tiles = host_tiles(a.batch, a.group, 16 * a.row_tiles);
   const PrefixPieces of = {p.prefix.tiles, p.prefix.chunk, p.prefix.splits, a.part};
-  if (a.groups > 0) {
-    PrefixArgs before;
-    static_cast<SharedArgs&>(before) = a;
-    before.causal = 0;
-    before.row_tiles = p.prefix.tiles;
-    before.waves = 4;
-    before.chunk = p.prefix.chunk;
-    before.splits = p.prefix.splits;
-    const hipError_t e = launch_prefix<D>(before, host_tiles(prefix_batch(a), a.group, 16 * p.prefix.tiles), stream);
-    if (e != hipSuccess) return e;
-  }
+  const SharedWork w = shared_work(a, p);
+  const unsigned workgroups = (unsigned)shared_workgroups(w);
+  SharedArgs own = a;
   own.part = a.part + p.prefix_bytes / sizeof(float);
-  hipError_t e = launch_own<D>(own, tiles, stream);
-  if (e != hipSuccess) return e;
-  return launch_join<D>(own, of, tiles, stream);
+  hipError_t e;
+  const int forms = 10 * p.prefix.tiles + p.own.tiles;
+  if (forms == 11) e = launch_passes<D, 1, 1>(own, of, w, workgroups, stream);
+  else if constexpr (D == 256) {
+    e = forms == 88 ? launch_passes<D, 8, 8>(own, of, w, workgroups, stream) : hipErrorInvalidValue;      // (by the plan, never)
+  } else {
+    e = forms == 21   ? launch_passes<D, 2, 1>(own, of, w, workgroups, stream)
+        : forms == 81 ? launch_passes<D, 8, 1>(own, of, w, workgroups, stream)
+        : forms == 22 ? launch_passes<D, 2, 2>(own, of, w, workgroups, stream)
+        : forms == 82 ? launch_passes<D, 8, 2>(own, of, w, workgroups, stream)
+                      : hipErrorInvalidValue;
+  }
+  return e != hipSuccess ? e : launch_join<D>(own, of, stream);
 }
 
 }  // namespace
 
 hipError_t launch_kv_attention_shared(const SharedArgs& args, const SharedPlan& p, hipStream_t stream) {
   SharedArgs a = args;
+  if (p.apart) {
+    a.row_tiles = p.whole.tiles;
+    a.waves = p.whole.waves;
+    a.chunk = p.whole.chunk;
+    a.splits = p.whole.splits;
+    return launch_kv_attention(a, a.part, p.bytes, stream);
+  }
   a.row_tiles = p.own.tiles;
   a.waves = p.own.waves;
   a.chunk = p.own.chunk;

@@ -29,7 +29,7 @@ namespace nvfp4 {
 
 template <int D, bool kSplit>
 __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void kv_attention_tile_kernel(AttentionArgs a, int tiles) {
-  attention_tile<D, kSplit>(a, tiles);
+  attention_tile_kernel<D, kSplit>(a, tiles);
 }
 
 template <int D>

@@ -160,16 +160,17 @@ struct WideRows {
   }
 };
 
+template <int D>
+struct alignas(16) TileLds {
+  uint8_t stage[2][2][kStageTokens / 16][16 * D];      // [buffer][keys, values]
+};
+
+// Key head h, piece `piece` (0, unless kSplit) of the tile with that number, of `tiles`.
 template <int D, bool kSplit, typename Args>
-__device__ __forceinline__ void attention_tile(Args a, int tiles) {
+__device__ __forceinline__ void attention_tile(Args a, int tiles, int h, int number, int piece, TileLds<D>& lds) {
   constexpr int kGroups = kStageTokens / 16;
-  __shared__ __attribute__((aligned(16))) uint8_t stage[2][2][kGroups][16 * D];      // [buffer][keys, values]
+  auto& stage = lds.stage;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int id = blockIdx.x;
-  const int h = id % a.cache.heads;
-  id /= a.cache.heads;
-  const int number = tiles - 1 - (kSplit ? id / a.splits : id);      // the longest rows first
-  const int piece = kSplit ? piece_of(id % a.splits, number, a.splits) : 0;
   Tile t;
   if (!find_tile<kTileRows>(a, number, t)) return;
   int begin = t.begin, end = t.end;
@@ -271,6 +272,18 @@ __device__ __forceinline__ void attention_tile(Args a, int tiles) {
             make_uint2(bf16_pair(rows.o[j][4 * x] * f, rows.o[j][4 * x + 1] * f),
                        bf16_pair(rows.o[j][4 * x + 2] * f, rows.o[j][4 * x + 3] * f));
   }
+}
+
+// A whole kernel of it: heads side by side, then a tile's pieces, the longest rows first.
+template <int D, bool kSplit, typename Args>
+__device__ __forceinline__ void attention_tile_kernel(Args a, int tiles) {
+  __shared__ TileLds<D> lds;
+  int id = blockIdx.x;
+  const int h = id % a.cache.heads;
+  id /= a.cache.heads;
+  const int number = tiles - 1 - (kSplit ? id / a.splits : id);
+  const int piece = kSplit ? piece_of(id % a.splits, number, a.splits) : 0;
+  attention_tile<D, kSplit>(a, tiles, h, number, piece, lds);
 }
 
 }  // namespace nvfp4

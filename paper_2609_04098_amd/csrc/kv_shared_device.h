@@ -29,10 +29,10 @@ __device__ __forceinline__ int prefix_tokens(const SharedArgs& a, int g) {
   return min(max(a.prefix[g], 0), a.batch.max_tokens);
 }
 
-// The group of sequence b, whose rows begin at token `first`: the prefix that it
-// shares (0: none).  All lanes of a wave call it with the same arguments.
-__device__ __forceinline__ int shared_prefix(const SharedArgs& a, int b, int first, int& g) {
-  g = 0;
+// The group of sequence b, whose rows begin at token `first`, its first sequence, and the
+// prefix that b shares (0: none).  All lanes of a wave call it with the same arguments.
+__device__ __forceinline__ int shared_prefix(const SharedArgs& a, int b, int first, int& g, int& group_seq) {
+  g = group_seq = 0;
   if (a.groups == 0) return 0;
   if (a.groups < 64) {      // all there is to know of them in one load's latency
     const int lane = threadIdx.x & 63;
@@ -41,11 +41,12 @@ __device__ __forceinline__ int shared_prefix(const SharedArgs& a, int b, int fir
     if (hit == 0) return 0;
     g = 63 - __builtin_clzll(hit);
     if (b >= __builtin_amdgcn_readlane(start, g + 1)) return 0;
+    group_seq = __builtin_amdgcn_readlane(start, g);
     const int p = __builtin_amdgcn_readlane(tokens, g);
     return first >= p ? p : 0;
   }
-  const int start = last_at_most(a.groups, b, g, [&](int x) { return group_start(a, x); });
-  if (b < start || b >= group_start(a, g + 1)) return 0;
+  group_seq = last_at_most(a.groups, b, g, [&](int x) { return group_start(a, x); });
+  if (b < group_seq || b >= group_start(a, g + 1)) return 0;
   const int p = prefix_tokens(a, g);
   return first >= p ? p : 0;
 }
@@ -98,22 +99,16 @@ __device__ __forceinline__ bool find_tile(const PrefixArgs& a, int number, Tile&
 }
 
 __device__ __forceinline__ int64_t part_tiles(const PrefixArgs& a, int rows) {
-  return (int64_t)a.batch.rows * a.group / rows + a.groups;
+  return prefix_tile_numbers((int64_t)a.batch.rows * a.group, rows, a.groups);
 }
 
 // A tile of a sequence's rows over its own tokens.
 template <int kRows>
-__device__ __forceinline__ bool find_own_tile(const SharedArgs& a, int number, Tile& t, int& g, int& prefix) {
-  if (!find_tile<kRows>(static_cast<const AttentionArgs&>(a), number, t)) return false;
-  prefix = shared_prefix(a, t.b, t.first, g);
-  t.begin = min(prefix, max(0, t.end));
-  return true;
-}
-
-template <int kRows>
 __device__ __forceinline__ bool find_tile(const OwnArgs& a, int number, Tile& t) {
-  int g, prefix;
-  return find_own_tile<kRows>(a, number, t, g, prefix);
+  if (!find_tile<kRows>(static_cast<const AttentionArgs&>(a), number, t)) return false;
+  int g, group_seq;
+  t.begin = min(shared_prefix(a, t.b, t.first, g, group_seq), max(0, t.end));
+  return true;
 }
 
 }  // namespace nvfp4

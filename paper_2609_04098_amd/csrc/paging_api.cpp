@@ -70,6 +70,15 @@ SelectedArgs selected_args(const nvfp4_kv_cache* cache, int64_t rows, int64_t q_
   return a;
 }
 
+#define NVFP4_SHARED(D)                                                                                         \
+  {"kv_attention_shared_kernel<" #D ",1,1>", "kv_attention_shared_kernel<" #D ",2,1>",                          \
+   "kv_attention_shared_kernel<" #D ",8,1>", "kv_attention_shared_kernel<" #D ",2,2>",                          \
+   "kv_attention_shared_kernel<" #D ",8,2>", "kv_attention_shared_kernel<" #D ",8,8>"}
+constexpr const char* kSharedKernels[3][6] = {NVFP4_SHARED(64), NVFP4_SHARED(128), NVFP4_SHARED(256)};
+#undef NVFP4_SHARED
+constexpr const char* kSharedJoins[3] = {"kv_attention_shared_join_kernel<64>", "kv_attention_shared_join_kernel<128>",
+                                         "kv_attention_shared_join_kernel<256>"};
+
 }  // namespace
 
 extern "C" {
@@ -139,8 +148,10 @@ int nvfp4_kv_attention_shared(const nvfp4_kv_cache* cache, const nvfp4_kv_batch*
   if (!none) {
     p = shared_plan(a);
     if (!shared_fits(a, p)) return NVFP4_EINVAL;
-    if (workspace == nullptr || !aligned(workspace, 16)) return NVFP4_EINVAL;
-    if (workspace_bytes < p.bytes) return NVFP4_EWORKSPACE;
+    if (p.bytes > 0) {
+      if (workspace == nullptr || !aligned(workspace, 16)) return NVFP4_EINVAL;
+      if (workspace_bytes < p.bytes) return NVFP4_EWORKSPACE;
+    }
   }
   const int st = check_device();
   if (st != NVFP4_OK) return st;
@@ -156,6 +167,22 @@ int nvfp4_kv_attention_shared(const nvfp4_kv_cache* cache, const nvfp4_kv_batch*
   a.part = static_cast<float*>(workspace);
   const hipError_t e = launch_kv_attention_shared(a, p, static_cast<hipStream_t>(stream));
   return e == hipSuccess ? NVFP4_OK : fail_hip(e);
+}
+
+const char* nvfp4_kv_attention_shared_kernel(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
+                                             const nvfp4_shared_prefix* shared, int64_t q_heads, int part) {
+  if (!valid_cache(cache) || !valid_batch(batch, cache->page_size) || !valid_shared(shared, batch) ||
+      !valid_q_heads(q_heads, cache->kv_heads) || (part != 0 && part != 1) || batch->rows * q_heads >= kI32Lim)
+    return nullptr;
+  const SharedArgs a = shared_args(cache, batch, shared, q_heads);
+  if (a.batch.seqs == 0 || a.batch.rows == 0) return nullptr;
+  const SharedPlan p = shared_plan(a);
+  if (!shared_fits(a, p)) return nullptr;
+  if (p.apart) return nvfp4_kv_attention_kernel(cache, batch, q_heads, 0, part);
+  const int dim = a.cache.dim == 64 ? 0 : a.cache.dim == 128 ? 1 : 2;
+  if (part == 1) return kSharedJoins[dim];
+  const int forms = 10 * p.prefix.tiles + p.own.tiles;
+  return kSharedKernels[dim][forms == 11 ? 0 : forms == 21 ? 1 : forms == 81 ? 2 : forms == 22 ? 3 : forms == 82 ? 4 : 5];
 }
 
 int nvfp4_kv_page_bounds(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_kv_bounds* bounds,

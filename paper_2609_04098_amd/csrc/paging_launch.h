@@ -35,48 +35,109 @@ struct SharedArgs : AttentionArgs {
 // How the pass over the prefixes left its results.
 struct PrefixPieces {
   int tiles, chunk, splits;
-  const float* part;
+  float* part;
 };
 
-// The two passes' plans (attention_plan.h) and the bytes of their partial results.
+// The workgroups of both passes (kv_attention_shared.hip).
+struct SharedWork {
+  uint32_t own, prefix;        // workgroups
+  uint32_t prefix_eighth;      // of the prefix's for each die
+  int own_tiles, prefix_tiles;
+};
+
+// The two passes' plans and the bytes of their partial results; or that of the attention
+// without sharing (attention_plan.h), if it is taken to be faster.
 struct SharedPlan {
-  AttentionPlan prefix, own;
+  bool apart;
+  AttentionPlan whole, prefix, own;
   size_t prefix_bytes, bytes;
 };
 
-// The groups, as the sequences of a step.
-inline KvBatchArgs prefix_batch(const SharedArgs& a) {
-  KvBatchArgs b = a.batch;
-  b.cu_rows = a.cu_seqs;
-  b.seqs = a.groups;
-  b.max_kv_len = a.max_prefix;
-  return b;
+// Numbers of a group pass's tiles of `rows` packed rows, for n packed rows in all: group g's
+// begin at first row * group / rows + g.
+__host__ __device__ inline int64_t prefix_tile_numbers(int64_t n, int rows, int groups) {
+  return groups == 1 ? (n + rows - 1) / rows : n / rows + groups;
 }
 
-inline size_t all_part_bytes(const KvCacheArgs& c, const KvBatchArgs& b, int group, const AttentionPlan& p) {
-  return (size_t)(host_tiles(b, group, 16 * p.tiles) * c.heads * p.splits * 16 * p.tiles) * (c.dim + 2) * sizeof(float);
+inline int64_t prefix_tiles(const SharedArgs& a, int form) {
+  return prefix_tile_numbers((int64_t)a.batch.rows * a.group, 16 * form, a.groups);
 }
 
+inline size_t all_part_bytes(const KvCacheArgs& c, int64_t tiles, const AttentionPlan& p) {
+  return (size_t)(tiles * c.heads * p.splits * 16 * p.tiles) * (c.dim + 2) * sizeof(float);
+}
+
+// What a step takes, from 18 measured steps (times without and with sharing, in its best
+// form, us; sequences x new rows, prefix, own tokens up to, query / key heads of dim):
+//   4 x 1, 608, 90, 40 / 8 of 128       8.2  9.9     150 x 1, 512, 100, 40 / 8 of 128    21.1 25.8
+//   100 x 1, 1024, 200, 64 / 8 of 64   17.9 21.6     8 x 1, 2048, 300, 32 / 8 of 128     14.0 11.1
+//   60 x 1 (3 groups), 2000, 24 / 4    18.8 17.2     2 x 1, 30000, 500, 40 / 8 of 128    21.9 20.9
+//   16 x 1, 8192, 200, 40 / 8          37.1 17.8     32 x 4, 4096, 500, 32 / 8           43.9 29.7
+//   150 x 1, 4160, 777, 24 / 4 of 256  99.0 49.0     64 x 1, 32768, 1000, 40 / 8          377 76.0
+//   64 x 8 (2 groups), 4000, 64 / 8    94.9  112
+// Pages that sequences share are in the caches after the first one has read them, so what
+// sharing saves is not memory's but the caches' reads; it costs partial results and a join.
+// So it begins at prefixes of 1536 tokens, and not where a sequence's own rows fill 64.
+// Rows of the prefix's workgroups: by the rows of a group,
+//   320 of 128: 85 us with 16, 76 with 32, 79 with 128    512 (4096 tokens): 30.0 29.7 32.9
+//   1024: 126 112 105     2048: 133 128 112     2048 of 64: 97 85 84
+//   900 of 256: 49 (16), 54 (128)     512 of 256 (30000 tokens): 59 (16), 65 (128)
+// Pieces: one workgroup for each compute unit, two where it would take over 6000 tokens
+// (900 rows of 256: 49 us in one of 4160, 56 in two; 320 rows of 128, 32768 tokens: 82 in
+// twelve, 76 in six), three in tiles of 128 rows where it would over 3000 (1024 rows,
+// 16000 tokens: 131 us in four, 92 in twelve, without the join).
 inline SharedPlan shared_plan(const SharedArgs& a) {
   SharedPlan p = {};
-  if (a.groups > 0) {
-    const KvBatchArgs groups = prefix_batch(a);
-    p.prefix = attention_plan(a.cache, groups, a.group, 0, kAnyRoom);
-    p.prefix_bytes = all_part_bytes(a.cache, groups, a.group, p.prefix);
+  const int64_t rows = (int64_t)a.batch.rows * a.group;
+  const int64_t of_seq = (rows + a.batch.seqs - 1) / a.batch.seqs, of_group = a.groups > 0 ? (rows + a.groups - 1) / a.groups : 0;
+  p.apart = a.groups == 0 || a.max_prefix < 1536 || of_seq >= 64;
+  if (p.apart) {
+    p.whole = attention_plan(a.cache, a.batch, a.group, 0, kAnyRoom);
+    p.bytes = part_bytes(a.cache, a.batch, a.group, p.whole);
+    return p;
   }
-  KvBatchArgs own = a.batch;
-  own.max_kv_len = a.max_own;
-  p.own = attention_plan(a.cache, own, a.group, 0, kAnyRoom);
-  p.bytes = p.prefix_bytes + all_part_bytes(a.cache, own, a.group, p.own);
+  const auto pieces = [](int tokens, int64_t work, bool wide, int least) {
+    AttentionPlan q = {};
+    const int resident = wide ? 3 : 2;
+    int64_t n = work < 256 ? 256 / work : 1;
+    if (tokens / n > (wide ? 3000 : 6000)) n = work < 256 * resident ? 256 * resident / work : 1;
+    q.chunk = (int)(((tokens + n - 1) / n + 127) / 128 * 128);
+    if (q.chunk < least) q.chunk = least;
+    q.splits = tokens > 0 ? (tokens + q.chunk - 1) / q.chunk : 1;
+    q.waves = 4;
+    return q;
+  };
+  const int own_form = of_seq <= 16 ? 1 : a.cache.dim == 256 ? 8 : 2;
+  int form = a.cache.dim == 256 || of_group < 256 ? 1 : of_group < 768 ? 2 : 8;
+  if (form < own_form) form = own_form;
+  p.prefix = pieces(a.max_prefix, prefix_tiles(a, form) * a.cache.heads, form == 8, 128);
+  p.prefix.tiles = form;
+  p.prefix_bytes = all_part_bytes(a.cache, prefix_tiles(a, form), p.prefix);
+  const int64_t own_tiles = host_tiles(a.batch, a.group, 16 * own_form);
+  p.own = pieces(a.max_own, own_tiles * a.cache.heads, own_form == 8, 256);
+  p.own.tiles = own_form;
+  p.bytes = p.prefix_bytes + all_part_bytes(a.cache, own_tiles, p.own);
   return p;
 }
 
+inline SharedWork shared_work(const SharedArgs& a, const SharedPlan& p) {
+  SharedWork w = {};
+  w.own_tiles = (int)host_tiles(a.batch, a.group, 16 * p.own.tiles);
+  w.own = (uint32_t)((int64_t)w.own_tiles * a.cache.heads * p.own.splits);
+  w.prefix_tiles = (int)prefix_tiles(a, p.prefix.tiles);
+  w.prefix = (uint32_t)((int64_t)w.prefix_tiles * a.cache.heads * p.prefix.splits);
+  w.prefix_eighth = (w.prefix + 7) / 8;
+  return w;
+}
+
+inline int64_t shared_workgroups(const SharedWork& w) { return (int64_t)w.own + 8 * (int64_t)w.prefix_eighth; }
+
 // Whether every launch of a plan is in range.
 inline bool shared_fits(const SharedArgs& a, const SharedPlan& p) {
+  if (p.apart) return attention_fits(a.cache, a.batch, a.group, p.whole);
   const int64_t own = host_tiles(a.batch, a.group, 16 * p.own.tiles) * a.cache.heads;
-  if (!one_grid(own * p.own.splits, 64 * p.own.waves) || !one_grid(own * p.own.tiles * 4, 256)) return false;
-  return a.groups == 0 ||
-         one_grid(host_tiles(prefix_batch(a), a.group, 16 * p.prefix.tiles) * a.cache.heads * p.prefix.splits, 256);
+  const int64_t prefix = prefix_tiles(a, p.prefix.tiles) * a.cache.heads;
+  return one_grid(((int64_t)a.batch.rows * a.q_heads + 3) / 4, 256) && one_grid(own * p.own.splits + prefix * p.prefix.splits + 16, 256);
 }
 
 // Bounds of pages' keys.

@@ -32,6 +32,7 @@ SIGNATURES = {
     "nvfp4_kv_attention_shared_workspace": (_sz, [_cache, _batch, _shared, _i64]),
     "nvfp4_kv_attention_shared": (_int, [_cache, _batch, _shared, _vp, _i64, _i64, _vp, _i64, _vp, _f, _int, _vp, _sz,
                                          _vp]),
+    "nvfp4_kv_attention_shared_kernel": (ctypes.c_char_p, [_cache, _batch, _shared, _i64, _int]),
     "nvfp4_kv_page_bounds": (_int, [_cache, _batch, _bounds, _vp]),
     "nvfp4_kv_select_pages_workspace": (_sz, [_cache, _batch]),
     "nvfp4_kv_select_pages": (_int, [_cache, _batch, _bounds, _vp, _i64, _i64, _i64, _i64, _i64, _int, _vp, _vp, _vp, _vp,
@@ -95,6 +96,12 @@ def kv_attention_shared(stream, *args):
     status = (_lib or lib()).nvfp4_kv_attention_shared(*args, _handle(stream))
     if status:
         _c._check(status, "nvfp4_kv_attention_shared")
+
+
+def kv_attention_shared_kernel(cache, batch, shared, q_heads, part=0):
+    """Name of launch `part` of nvfp4_kv_attention_shared for these sizes, or None."""
+    r = lib().nvfp4_kv_attention_shared_kernel(cache, batch, shared, q_heads, part)
+    return None if r is None else r.decode()
 
 
 def kv_page_bounds(stream, *args):

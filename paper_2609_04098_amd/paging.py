@@ -194,6 +194,12 @@ def shared_attention(q, cache: KVCache, batch: Batch, shared: SharedPrefix, scal
     return (y, lse) if return_lse else y
 
 
+def shared_attention_kernels(q_heads, cache: KVCache, batch: Batch, shared: SharedPrefix):
+    """Names of the kernels that shared_attention() launches for a step."""
+    return [name for name in (_p.kv_attention_shared_kernel(cache.ref, batch.ref, shared.ref, q_heads, part) for part in (0, 1))
+            if name is not None]
+
+
 class PageBounds:
     """Bounds of the keys of a cache's full pages over given buffers: codes int8
     [num_pages, kv_heads, 2, head_dim] (largest, smallest; any page stride that is a

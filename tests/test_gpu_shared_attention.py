@@ -23,7 +23,7 @@ class Step:
     """Groups [(sequences, prefix)], then `alone` sequences of none; own: tokens of each
     behind its prefix; counts: new rows."""
 
-    def __init__(self, dim, page, heads, group, groups, own, counts, seed, cu=True):
+    def __init__(self, dim, page, heads, group, groups, own, counts, seed, cu=True, least=2048):
         prefix = [p for n, p in groups for _ in range(n)]
         prefix += [0] * (len(own) - len(prefix))
         lens = [p + o for p, o in zip(prefix, own)]
@@ -32,6 +32,9 @@ class Step:
         for g, (n, p) in enumerate(groups):      # (a page that the prefix fills in part is not shared beyond it)
             for b in range(self.first[g] + 1, self.first[g] + n):
                 self.case.table[b, :-(-p // page)] = self.case.table[self.first[g], :-(-p // page)]
+        if self.case.table.shape[1] * page < least:      # a table that could hold a prefix worth sharing
+            more = least // page - self.case.table.shape[1]
+            self.case.table = torch.cat((self.case.table, self.case.table[:, :1].expand(-1, more)), dim=1).contiguous()
         self.counts, self.lens, self.heads = counts, lens, heads * group
         self.groups = groups
         self.q = T._queries(self.case, sum(counts), self.heads)
@@ -51,24 +54,33 @@ class Step:
         return y
 
 
+SHARED = "kv_attention_shared_kernel<%d,%s>"
+
+# dim, page, key heads, group, groups, own tokens, new rows, row offsets or not, the kernel's rows.  (The host is told of
+# prefixes that are worth sharing.)
 STEPS = [
     # one group, single tokens, without row offsets
-    *[(d, p, 2, 3, [(4, 96)], [1, 5, 40, 100], [1] * 4, False) for d, p in ((64, 16), (128, 32), (256, 64))],
-    (128, 128, 1, 1, [(2, 128)], [1, 1], [1, 1], False),
+    *[(d, p, 2, 3, [(4, 96)], [1, 5, 40, 100], [1] * 4, False, "1,1") for d, p in ((64, 16), (128, 32), (256, 64))],
+    (128, 128, 1, 1, [(2, 128)], [1, 1], [1, 1], False, "1,1"),
     # many sequences: 32 and 128 packed rows a tile, pieces of the prefix
-    *[(d, 32, 2, 5, [(40, 2016)], [3 + 7 * i for i in range(40)], [1] * 40, False) for d in (64, 128, 256)],
-    *[(d, 16, 8, 8, [(60, 512)], [30] * 60, [1] * 60, False) for d in (64, 128, 256)],
-    (128, 64, 1, 4, [(5, 9024)], [300, 1, 64, 2, 700], [1] * 5, False),
+    *[(d, 32, 2, 5, [(40, 2016)], [3 + 7 * i for i in range(40)], [1] * 40, False, "1,1") for d in (64, 128, 256)],
+    *[(d, 16, 2, 8, [(50, 512)], [30] * 50, [1] * 50, False, "2,1" if d < 256 else "1,1") for d in (64, 128, 256)],
+    *[(d, 32, 8, 8, [(100, 1504)], [9 + i for i in range(100)], [1] * 100, False, "8,1" if d < 256 else "1,1")
+      for d in (64, 128, 256)],
+    (128, 64, 1, 4, [(5, 9024)], [300, 1, 64, 2, 700], [1] * 5, False, "1,1"),
     # several groups of all kinds, one without a prefix, sequences of none, some without rows
     (64, 16, 2, 3, [(3, 160), (1, 32), (4, 0), (2, 1600)], [9, 20, 1, 5, 8, 3, 1, 2, 70, 4, 33, 500], [2, 1, 1, 3, 1, 0, 1, 2, 5, 4, 7, 9],
-     True),
-    (128, 32, 3, 7, [(2, 64), (0, 96), (3, 640)], [3, 40, 12, 5, 64, 800, 1], [3, 1, 0, 5, 2, 6, 1], True),
-    (256, 16, 1, 16, [(2, 320), (2, 16)], [10, 20, 11, 2], [8, 9, 10, 2], True),
-    # prompts behind a common prefix
-    (128, 32, 4, 4, [(3, 992)], [500, 320, 77], [500, 320, 70], True), (64, 16, 8, 4, [(2, 3008)], [600, 400], [400, 400], True),
-    (256, 32, 8, 8, [(2, 480)], [90, 80], [70, 66], True),
+     True, "1,1"),
+    (128, 32, 3, 7, [(2, 64), (0, 96), (3, 640)], [3, 40, 12, 5, 64, 800, 1], [3, 1, 0, 5, 2, 6, 1], True, "2,2"),
+    (64, 32, 3, 7, [(2, 64), (0, 96), (3, 640)], [3, 40, 12, 5, 64, 800, 1], [3, 1, 0, 5, 2, 6, 1], True, "2,2"),
+    (256, 16, 1, 16, [(2, 320), (2, 16)], [10, 20, 11, 2], [4, 3, 5, 2], True, "8,8"),
+    # drafts of many sequences, several rows each behind a common prefix
+    *[(d, 32, 4, 4, [(30, 992)], [12 + 5 * i for i in range(30)], [8 + i % 3 for i in range(30)], True, "8,2" if d < 256 else "8,8")
+      for d in (64, 128, 256)],
     # a prefix that ends inside a page that the sequences share, and inside a tile
-    (128, 32, 2, 4, [(3, 75)], [1, 1, 1], [1] * 3, False),
+    (128, 32, 2, 4, [(3, 75)], [1, 1, 1], [1] * 3, False, "1,1"),
+    # rows of a sequence that fill tiles of their own: computed apart
+    (128, 32, 4, 4, [(3, 992)], [500, 320, 77], [500, 320, 70], True, None), (256, 32, 8, 8, [(2, 480)], [90, 80], [70, 66], True, None),
 ]
 
 
@@ -79,13 +91,24 @@ def _name(s):
 @pytest.mark.parametrize("step", STEPS, ids=_name)
 def test_shared_attention(step):
     log("shared %s" % _name(step))
-    dim, page, heads, group, groups, own, counts, cu = step
-    s = Step(dim, page, heads, group, groups, own, counts, sum(own) + dim, cu)
-    tight = dict(max_len=max(p for _, p in groups), max_own=max(own))
+    dim, page, heads, group, groups, own, counts, cu, form = step
+    s = Step(dim, page, heads, group, groups, own, counts, sum(own) + dim, cu, least=2048)
+    tight = dict(max_len=max(1536, max(p for _, p in groups)), max_own=max(own))
+    names = P.shared_attention_kernels(s.heads, s.case.cache(), s.batch(max_len=max(s.lens)), s.shared(**tight))
+    if form is not None:
+        assert names == [SHARED % (dim, form), "kv_attention_shared_join_kernel<%d>" % dim]
+    else:
+        assert not any("shared" in n for n in names)
     s.check(hints=tight, max_len=max(s.lens), pages=True)
     s.check(causal=False, hints=tight, max_len=max(s.lens))
     s.check()                                            # nothing known on the host
-    s.check(hints=dict(max_len=1, max_own=1), scale=-0.05)      # too little known
+    s.check(hints=dict(max_len=1536, max_own=1), scale=-0.05)      # too little known
+    s.check(hints=dict(max_len=1, max_own=1))            # so little that nothing is shared
+
+
+def test_every_form_has_a_step():
+    got = {(s[0], s[8]) for s in STEPS if s[8]}
+    assert got == {(d, f) for d in (64, 128) for f in ("1,1", "2,1", "8,1", "2,2", "8,2")} | {(256, "1,1"), (256, "8,8")}
 
 
 @pytest.mark.parametrize("dim", [64, 128, 256])
@@ -96,7 +119,7 @@ def test_more_groups_than_a_wave_has_lanes(dim):
     for cu in (False, True):
         counts = [1] * n if not cu else [i % 3 for i in range(n)]
         s = Step(dim, 16, 1, 2, groups, [1 + counts[i] + i % 20 for i in range(n)], counts, dim, cu)
-        s.check(hints=dict(max_len=48, max_own=25))
+        s.check(hints=dict(max_len=1536, max_own=25))
 
 
 @pytest.mark.parametrize("causal", [True, False])
@@ -161,7 +184,7 @@ def test_runs_are_equal_on_any_stream_and_in_a_graph():
     cache, lens = s.case.cache(), _i32(s.lens)
     batch = A.Batch(s.case.table.int(), lens, max_len=max(s.lens))
     prefix = _i32([1504, 96])
-    shared = P.SharedPrefix(_i32(s.first), prefix, max_len=1504, max_own=300)
+    shared = P.SharedPrefix(_i32(s.first), prefix, max_len=1536, max_own=300)
     want = P.shared_attention(s.q, cache, batch, shared)
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())

@@ -70,15 +70,20 @@ def test_tables_want_their_workspace():
 
 
 def _groups(**kw):
-    a = dict(cu_seqs=FAKE, prefix=FAKE, n_groups=2, max_prefix=100, max_own=60)
+    a = dict(cu_seqs=FAKE, prefix=FAKE, n_groups=2, max_prefix=2000, max_own=60)
     a.update(kw)
     return N.SharedPrefixStruct(**a)
+
+
+def _long(**kw):
+    """A batch whose prefixes may be long enough to be shared."""
+    return _batch(**{**dict(max_pages=100, page_table_stride=100, max_kv_len=3200), **kw})
 
 
 def _attend(cache=None, batch=None, groups=None, **kw):
     a = dict(q=FAKE, ldq=512, hq=4, y=FAKE, ldy=512, lse=None, scale=0.1, causal=1, ws=FAKE, wsb=1 << 30)
     a.update(kw)
-    c, b, g = (x if x is not None else f() for x, f in ((cache, _cache), (batch, _batch), (groups, _groups)))
+    c, b, g = (x if x is not None else f() for x, f in ((cache, _cache), (batch, _long), (groups, _groups)))
     return N.lib().nvfp4_kv_attention_shared(ctypes.byref(c), ctypes.byref(b), ctypes.byref(g), a["q"], a["ldq"], a["hq"],
                                              a["y"], a["ldy"], a["lse"], a["scale"], a["causal"], a["ws"], a["wsb"], None)
 
@@ -108,7 +113,7 @@ def test_shared_attention_refuses(bad):
 
 
 def test_shared_attention_wants_its_workspace():
-    f, c, b, g = N.lib(), _cache(), _batch(), _groups()
+    f, c, b, g = N.lib(), _cache(), _long(), _groups()
     need = f.nvfp4_kv_attention_shared_workspace(ctypes.byref(c), ctypes.byref(b), ctypes.byref(g), 4)
     assert need > 0 and _attend(wsb=need - 1) == C.NVFP4_EWORKSPACE
     assert f.nvfp4_kv_attention_shared_workspace(ctypes.byref(c), ctypes.byref(b), ctypes.byref(_groups(n_groups=9)), 4) == 0
@@ -119,10 +124,30 @@ def test_shared_attention_wants_its_workspace():
         assert f.nvfp4_kv_attention_shared(*args, FAKE, 512, 4, FAKE, 512, None, 0.1, 1, FAKE, 1 << 30, None) == C.NVFP4_EINVAL
 
 
+def _kernels(cache, batch, groups, heads):
+    f = N.lib().nvfp4_kv_attention_shared_kernel
+    return [f(ctypes.byref(cache), ctypes.byref(batch), ctypes.byref(groups), heads, part) for part in (0, 1)]
+
+
+def test_which_steps_share():
+    """By their sizes: prefixes of 1536 tokens, fewer than 64 rows of a sequence."""
+    c = _cache()
+    rows = lambda n, r: _long(n_seqs=n, rows=r)
+    share = lambda k: k[0].startswith(b"kv_attention_shared_kernel<128,") and k[1] == b"kv_attention_shared_join_kernel<128>"
+    assert share(_kernels(c, rows(3, 5), _groups(max_prefix=1536), 4))
+    assert not share(_kernels(c, rows(3, 5), _groups(max_prefix=1535), 4))
+    assert share(_kernels(c, rows(4, 124), _groups(), 4)) and not share(_kernels(c, rows(4, 128), _groups(), 4))
+    assert not share(_kernels(c, rows(4, 4), _groups(n_groups=0), 4))
+    assert not share(_kernels(c, _batch(), _groups(), 4))                    # (256 tokens are all that its table holds)
+    assert _kernels(c, rows(3, 5), _groups(n_groups=5), 4) == _kernels(c, rows(3, 0), _groups(), 4) == [None, None]
+    f = N.lib().nvfp4_kv_attention_shared_kernel
+    assert f(ctypes.byref(c), ctypes.byref(_long()), ctypes.byref(_groups()), 4, 2) is None
+
+
 @pytest.mark.parametrize("n,heads,group", [(1 << 21, 8, 5), ((1 << 24) - 1, 2, 1), (1 << 20, 8, 33)])
 def test_shared_attention_refuses_more_workgroups_than_a_launch_holds(n, heads, group):
     c = _cache(kv_heads=heads, page_size=16, k_page_stride=heads * 2048, v_page_stride=heads * 2048, scale_page_stride=heads)
-    b = _batch(n_seqs=n, rows=n, cu_rows=None)
+    b = _long(n_seqs=n, rows=n, cu_rows=None)
     assert _attend(c, b, hq=heads * group, ldq=heads * group * 128, ldy=heads * group * 128) == C.NVFP4_EINVAL
 
 
