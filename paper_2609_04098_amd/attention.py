@@ -116,6 +116,7 @@ class KVCache:
             self.struct.k_page_stride = self.struct.v_page_stride = k.shape[1] * k.shape[2]
             self.struct.scale_page_stride = k.shape[1]
         self.ref = ctypes.byref(self.struct)
+        self.selected_workspace = {}      # of paging.selected_attention
 
     def tokens(self):
         """(keys, values) as float32 [num_pages, kv_heads, page_size, head_dim]: every

@@ -44,6 +44,62 @@ __device__ __forceinline__ f16x2 over_row(f16x2 v) {
   return fold<0x140, kMax>(v);
 }
 
+// The largest value of a row of 16 lanes.
+__device__ __forceinline__ float row_max(float m) {
+  m = fmaxf(m, __uint_as_float(row_other<0xB1>(__float_as_uint(m))));
+  m = fmaxf(m, __uint_as_float(row_other<0x4E>(__float_as_uint(m))));
+  m = fmaxf(m, __uint_as_float(row_other<0x141>(__float_as_uint(m))));
+  return fmaxf(m, __uint_as_float(row_other<0x140>(__float_as_uint(m))));
+}
+
+// Sums over the lanes up to this one (all lanes active).
+template <int kHow, int kRows>
+__device__ __forceinline__ int from_below(int v) {
+  return __builtin_amdgcn_update_dpp(0, v, kHow, kRows, 0xF, false);
+}
+
+__device__ __forceinline__ int scan_up(int x) {
+  x += from_below<0x111, 0xF>(x);      // one lane below, in a row of 16; two, four, eight
+  x += from_below<0x112, 0xF>(x);
+  x += from_below<0x114, 0xF>(x);
+  x += from_below<0x118, 0xF>(x);
+  x += from_below<0x142, 0xA>(x);      // the last lane of the row below, into rows 1 and 3
+  x += from_below<0x143, 0xC>(x);      // lane 31, into rows 2 and 3
+  return x;
+}
+
+// The sum, the smallest and the largest over a row of 16 lanes.
+__device__ __forceinline__ int row_sum(int v) {
+  v += (int)row_other<0xB1>((uint32_t)v);
+  v += (int)row_other<0x4E>((uint32_t)v);
+  v += (int)row_other<0x141>((uint32_t)v);
+  return v + (int)row_other<0x140>((uint32_t)v);
+}
+
+__device__ __forceinline__ uint32_t row_low(uint32_t v) {
+  v = min(v, row_other<0xB1>(v));
+  v = min(v, row_other<0x4E>(v));
+  v = min(v, row_other<0x141>(v));
+  return min(v, row_other<0x140>(v));
+}
+
+__device__ __forceinline__ uint32_t row_high(uint32_t v) { return ~row_low(~v); }
+
+// The smallest over the four lanes lane % 16 + 16 i.
+__device__ __forceinline__ uint32_t over_quarters_low(uint32_t x) {
+  const auto a = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  const uint32_t y = min(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane16_swap(y, y, false, false);
+  return min(b[0], b[1]);
+}
+
+// What lanes have written to LDS is there for the others of their wave.
+__device__ __forceinline__ void wave_sees_lds() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // A wave takes one head of one full page.  Pages of sequence b that its new rows
 // completed have the numbers from cu_rows[b] / page_size + b on.
 template <int D>
@@ -90,10 +146,7 @@ __global__ __launch_bounds__(256) void kv_page_bounds_kernel(BoundsArgs a, int i
         *reinterpret_cast<f16x2*>(&found[wave][1][64 * c + 16 * (lane >> 4) + 2 * i]) = low;
       }
     }
-  // (One wave's LDS, in the order of its accesses.)
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  wave_sees_lds();
   constexpr int kEach = 2 * D / 64;      // elements of hi, then of lo
   float v[kEach], top = 0.0f;
 #pragma unroll
@@ -139,225 +192,488 @@ __device__ __forceinline__ RowPages row_pages(const SelectArgs& a, int row) {
   return r;
 }
 
-// Whole numbers that order as the scores do (no NaN; -0 is 0).
+// Whole numbers that order as the scores do (no NaN; -0 is 0).  A page that is not in the
+// cache has key 0, which no score has.
 __device__ __forceinline__ uint32_t key_of(float x) {
   const uint32_t b = __float_as_uint(x + 0.0f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-constexpr int kScorePages = 256;         // pages of a workgroup
+constexpr int kColumns = 16;             // query heads of one product
 
+// Query heads in 8 bits: head x's element e at codes[x][e].
 template <int D>
-__global__ __launch_bounds__(256) void kv_page_scores_kernel(SelectArgs a, int chunks) {
-  constexpr int kSteps = D / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
-  int id = blockIdx.x;
-  const int h = id % a.cache.heads;
-  id /= a.cache.heads;
-  const int row = id / chunks, chunk = id % chunks;
-  const RowPages r = row_pages(a, row);
-  if (r.pages <= a.count) return;                                    // (all of them are taken)
-  const int first = a.first, end = r.pages - a.recent;
-  const int from = chunk * kScorePages + wave * 16;
-  if ((int64_t)chunk * kScorePages >= end) return;
-  uint32_t* const scores = a.scores + ((int64_t)row * a.cache.heads + h) * a.max_pages;
-  float best[kScorePages / 64][4];
-#pragma unroll
-  for (int x = 0; x < kScorePages / 64; ++x)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) best[x][e] = -INFINITY;
-  int pages[kScorePages / 64];
-#pragma unroll
-  for (int x = 0; x < kScorePages / 64; ++x) {
-    const int j = from + 64 * x + col;
-    int p = -1;
-    if (j >= first && j < end) p = a.batch.table[(int64_t)r.b * a.batch.table_stride + j];
-    pages[x] = p >= 0 && p < a.cache.num_pages ? p : -1;
+struct QueryCodes {
+  int8_t codes[kColumns][D];
+  float unit[kColumns];
+};
+
+// A lane's elements of a query head.
+template <int D>
+struct QueryLane {
+  static constexpr int kEach = D / 64;
+  uint32_t w[(kEach + 1) / 2];
+
+  __device__ __forceinline__ void load(const SelectArgs& a, int row, int head) {
+    const uint16_t* src = a.q + (int64_t)row * a.ldq + (int64_t)head * D + (threadIdx.x & 63) * kEach;
+    if constexpr (kEach == 1) w[0] = src[0];
+    else if constexpr (kEach == 2) w[0] = *reinterpret_cast<const uint32_t*>(src);
+    else *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(src);
   }
-  for (int a0 = 0; a0 < a.group; a0 += 16) {
-    // Query head h * group + a0 + col in 8 bits; elements 64 s + 16 quarter .. + 15.
-    const uint16_t* src = a.q + (int64_t)row * a.ldq + (int64_t)(h * a.group + min(a0 + col, a.group - 1)) * D + quarter * 16;
-    float v[kSteps][16], top = 0.0f;
+};
+
+// A query head, by a whole wave, into column x.  127 v / top is rounded as the exact
+// quotient is: both have 8 significant bits, so it is a half (then it is representable, and
+// the correction finds it) or further from one than 2^-17 of itself; the quotient is off by
+// 2^-23 at most.  (Elements over 2^e, the top's power of two, keep within range.)
+template <int D>
+__device__ __forceinline__ void query_codes(const QueryLane<D>& lanes, int x, QueryCodes<D>& to) {
+  constexpr int kEach = D / 64;
+  const int lane = threadIdx.x & 63;
+  float v[kEach], top = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) v[i] = i & 1 ? bf16_high(lanes.w[i / 2]) : bf16_low(lanes.w[i / 2]);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) top = fmaxf(top, fabsf(v[i]));
+  top = row_max(top);
+  top = over_quarters_max(top);
+  const int e = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;
+  const float over = top > 0.0f ? __builtin_amdgcn_ldexpf(top, -e) : 1.0f, inv = 1.0f / over;
+  int8_t n[kEach];
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const float y = __builtin_amdgcn_ldexpf(v[i], -e) * 127.0f;      // (exact)
+    float q = y * inv;
+    q = fmaf(fmaf(-q, over, y), inv, q);
+    n[i] = (int8_t)(int)rintf(q);
+  }
+  if constexpr (kEach == 1) to.codes[x][lane] = n[0];
+  else if constexpr (kEach == 2) *reinterpret_cast<char2*>(&to.codes[x][2 * lane]) = make_char2(n[0], n[1]);
+  else *reinterpret_cast<char4*>(&to.codes[x][4 * lane]) = make_char4(n[0], n[1], n[2], n[3]);
+  if (lane == 0) to.unit[x] = top / 127.0f;
+}
+
+// Scores of 16 pages at a time for up to 16 query heads.  Bounds are loaded as they lie,
+// a kilobyte an instruction, and turned in LDS into the product's operands, a page to a lane
+// of 16 (loaded as operands, 16 pages for 16 lanes, 8 times 2048 pages took 25.2 us in one
+// compute unit each; so 18.2).  Pieces of 16 bytes change places by their page's number, so that 16 lanes
+// meet 16 different bank groups.
+template <int D>
+struct Scorer {
+  static constexpr int kSteps = D / 64, kChunks = D / 8, kLoads = D / 32;      // pieces of a page; loads of 16 pages
+  static constexpr int kHalves = D == 256 ? 2 : 1, kPart = kChunks / kHalves;  // what is turned at a time
+  typedef i32x4 Turn[16 * kPart];          // LDS of a wave
+  i32x4 above[kSteps], below[kSteps];      // max(q, 0), min(q, 0): head lane % 16, elements 64 s + 16 (lane / 16) .. + 15
+  float unit;
+
+  // (Columns behind the n heads take the last one.)
+  __device__ __forceinline__ void start(const QueryCodes<D>& q, int n) {
+    const int lane = threadIdx.x & 63, col = min(lane & 15, n - 1), quarter = lane >> 4;
+    unit = q.unit[col];
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
-      const u32x4 w0 = *reinterpret_cast<const u32x4*>(src + 64 * s), w1 = *reinterpret_cast<const u32x4*>(src + 64 * s + 8);
+      const i32x4 w = *reinterpret_cast<const i32x4*>(&q.codes[col][64 * s + 16 * quarter]);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        v[s][2 * i] = bf16_low(w0[i]), v[s][2 * i + 1] = bf16_high(w0[i]);
-        v[s][8 + 2 * i] = bf16_low(w1[i]), v[s][9 + 2 * i] = bf16_high(w1[i]);
+        const uint32_t negative = (((uint32_t)w[i] >> 7) & 0x01010101u) * 255u;
+        below[s][i] = (int)((uint32_t)w[i] & negative);
+        above[s][i] = (int)((uint32_t)w[i] & ~negative);
       }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(v[s][i]));
-    }
-    top = over_quarters_max(top);
-    const float over = top > 0.0f ? top : 1.0f, unit = top / 127.0f;
-    i32x4 above[kSteps], below[kSteps];
-#pragma unroll
-    for (int s = 0; s < kSteps; ++s)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t up = 0, down = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int n = (int)rintf(v[s][4 * i + e] * 127.0f / over);
-          up |= ((uint32_t)max(n, 0) & 255u) << (8 * e);
-          down |= ((uint32_t)min(n, 0) & 255u) << (8 * e);
-        }
-        above[s][i] = (int)up, below[s][i] = (int)down;
-      }
-#pragma unroll
-    for (int x = 0; x < kScorePages / 64; ++x) {
-      const int8_t* at = a.bounds.codes + (int64_t)max(pages[x], 0) * a.bounds.page_stride + (int64_t)h * 2 * D + quarter * 16;
-      i32x4 sum = (i32x4){0, 0, 0, 0};
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const i32x4 hi = *reinterpret_cast<const i32x4*>(at + 64 * s), lo = *reinterpret_cast<const i32x4*>(at + D + 64 * s);
-        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(hi, above[s], sum, 0, 0, 0);
-        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(lo, below[s], sum, 0, 0, 0);
-      }
-      // Pages 4 quarter + e, query head col.
-#pragma unroll
-      for (int e = 0; e < 4; ++e) best[x][e] = fmaxf(best[x][e], (float)sum[e] * unit);
     }
   }
+
+  struct Round {
+    i32x4 raw[kLoads];
+    float step;
+    int page;                              // of lane % 16 (-1: none)
+  };
+
+  static __device__ __forceinline__ int owner(int i) { return (64 / kChunks) * i + (int)(threadIdx.x & 63) / kChunks; }
+  static __device__ __forceinline__ int place(int page, int chunk) {
+    return page * kPart + (chunk ^ (D == 64 ? page >> 1 : page));
+  }
+
+  static __device__ __forceinline__ void load(const SelectArgs& a, int h, int page, Round& to) {
+    const int chunk = (threadIdx.x & 63) % kChunks;
+    to.page = page;
+    to.step = a.bounds.step[(int64_t)max(page, 0) * a.bounds.step_stride + h];
 #pragma unroll
-  for (int x = 0; x < kScorePages / 64; ++x) {
+    for (int i = 0; i < kLoads; ++i) {
+      const int p = max(__shfl(page, owner(i)), 0);
+      to.raw[i] = *reinterpret_cast<const i32x4*>(a.bounds.codes + (int64_t)p * a.bounds.page_stride + (int64_t)h * 2 * D + chunk * 16);
+    }
+  }
+
+  // The key of page 4 quarter + col for the lanes of columns 0 to 3.
+  __device__ __forceinline__ uint32_t key(const Round& p, Turn& turn) const {
+    const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4, chunk = lane % kChunks;
+    i32x4 sum = (i32x4){0, 0, 0, 0};
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      float m = best[x][e];
-      m = fmaxf(m, __uint_as_float(row_other<0xB1>(__float_as_uint(m))));
-      m = fmaxf(m, __uint_as_float(row_other<0x4E>(__float_as_uint(m))));
-      m = fmaxf(m, __uint_as_float(row_other<0x141>(__float_as_uint(m))));
-      best[x][e] = fmaxf(m, __uint_as_float(row_other<0x140>(__float_as_uint(m))));
+    for (int half = 0; half < kHalves; ++half) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        if (kHalves == 1 || chunk / kPart == half) turn[place(owner(i), chunk % kPart)] = p.raw[i];
+      wave_sees_lds();
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        if (kHalves == 1 || half == 0)
+          sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(turn[place(col, 4 * s + quarter)], above[s], sum, 0, 0, 0);
+        if (kHalves == 1 || half == 1)
+          sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(turn[place(col, (kHalves == 1 ? D / 16 : 0) + 4 * s + quarter)], below[s], sum,
+                                                      0, 0, 0);
+      }
+      wave_sees_lds();
     }
-    // Lane col of a quarter writes page 4 quarter + col.
-    const int mine = 4 * quarter + (col & 3), j = from + 64 * x + mine;
-    const float m = (col & 2) ? ((col & 1) ? best[x][3] : best[x][2]) : ((col & 1) ? best[x][1] : best[x][0]);
-    const int page = __shfl(pages[x], mine);
-    if (col < 4 && j >= first && j < end) {
-      const float step = page < 0 ? 0.0f : a.bounds.step[(int64_t)page * a.bounds.step_stride + h];
-      scores[j] = page < 0 ? 0u : key_of(m * step);                   // (a page that is not in the cache: the last choice)
-    }
+    float best[4];      // pages 4 quarter + e
+#pragma unroll
+    for (int e = 0; e < 4; ++e) best[e] = row_max((float)sum[e] * unit);
+    const float m = (col & 2) ? ((col & 1) ? best[3] : best[2]) : ((col & 1) ? best[1] : best[0]);
+    const int mine = 4 * quarter + (col & 3);
+    const float step = __shfl(p.step, mine);
+    return __shfl(p.page, mine) < 0 ? 0u : key_of(m * step);
+  }
+};
+
+// The page of table entry j, -1 where it is not among [first, end) or not in the cache.
+// (No branch around the load, nor a store to memory in a loop that has it: the compiler
+// would wait for all that may be on its way.)
+__device__ __forceinline__ int page_at(const SelectArgs& a, const int32_t* table, int j, int first, int end) {
+  const int p = table[min(max(j, first), end - 1)];
+  return j >= first && j < end && p < a.cache.num_pages ? p : -1;
+}
+
+// The scores of one row and key head's pages j0 + 16 wave .. by rounds of 16 pages a wave
+// up to j1; put(j, key) from the lanes that hold them.
+template <int D, int kWaves, typename Put>
+__device__ __forceinline__ void score_pages(const SelectArgs& a, const QueryCodes<D>& q, int heads, int h, const int32_t* table, int first,
+                                            int end, int j0, int j1, typename Scorer<D>::Turn* turns, Put put) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
+  Scorer<D> scorer;
+  scorer.start(q, heads);
+  int j = j0 + 16 * wave;
+  // Two rounds' bounds ahead (heads of 256: one, none in 16 waves; registers).  A round's pages are
+  // looked up before the bounds of the round in front of it are loaded: loads are waited for in order.
+  constexpr int kAhead = D == 256 ? (kWaves > 4 ? 0 : 1) : 2, kRound = 16 * kWaves;
+  typename Scorer<D>::Round p[kAhead + 1];
+  int pages[kAhead + 1];
+#pragma unroll
+  for (int x = 0; x <= kAhead; ++x) pages[x] = page_at(a, table, j + x * kRound + col, first, end);
+#pragma unroll
+  for (int x = 0; x < kAhead; ++x) Scorer<D>::load(a, h, pages[x], p[x]);
+  int page = pages[kAhead];
+  while (j < j1) {
+    const int behind = page_at(a, table, j + (kAhead + 1) * kRound + col, first, end);
+    Scorer<D>::load(a, h, page, p[kAhead]);
+    page = behind;
+    const uint32_t key = scorer.key(p[0], turns[wave]);
+    const int mine = j + 4 * quarter + (col & 3);
+    if (col < 4 && mine >= first && mine < end) put(mine, key);
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) p[x] = p[x + 1];
+    j += kRound;
   }
 }
 
 // ---------------------------------------------------------------- selection
 
-// One workgroup for each row and key head: the want largest keys of scores[first ..
-// end), the lowest pages first among equals.  The want-th largest key is found 8 bits at
-// a time from the counts of each value of them; then the pages are written in order.
-constexpr int kSelectThreads = 512, kSelectWaves = kSelectThreads / 64;
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr int kBins = 2048, kBinBits = 11;
+constexpr int kHeldKeys = 8192;          // keys of a row and key head in LDS
 
-__global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(SelectArgs a) {
-  __shared__ int counts[256];
-  __shared__ int totals[2][kSelectWaves];
-  __shared__ int found[2];
+struct SelectLds {
+  int counts[2][kBins];
+  int totals[2][kHeldKeys / kSelectThreads][kSelectWaves];      // of every round and wave
+  uint32_t ends[2][kSelectWaves];
+  int sums[kSelectWaves];
+  int found[3];
+};
+
+// What is taken of n keys: those from `cut` on, and the first `ties` of those that are
+// cut - 1 (64 bits, so that there is one behind the largest).
+struct Cut {
+  uint64_t cut;
+  int ties;
+};
+
+// The want largest of key(0) .. key(n - 1) (1 <= want < n).  Their smallest is found in the
+// counts of 2048 equal steps from the smallest to the largest key, then in those of
+// the step that holds it: two or three times for any 32 bits, once for most.
+template <typename Key>
+__device__ __forceinline__ Cut find_cut(SelectLds& lds, int n, int want, Key key) {
+  static_assert(kSelectWaves == 16 && kBins == 2 * kSelectThreads, "a wave for each lane of a row, two steps a thread");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15;
+  const auto clear = [&](int which) {
+    *reinterpret_cast<int2*>(&lds.counts[which][2 * threadIdx.x]) = make_int2(0, 0);
+  };
+  uint32_t lo = ~0u, hi = 0;
+  for (int i = threadIdx.x; i < n; i += kSelectThreads) {
+    const uint32_t k = key(i);
+    lo = min(lo, k), hi = max(hi, k);
+  }
+  clear(0);
+  lo = over_quarters_low(row_low(lo));
+  hi = ~over_quarters_low(row_low(~hi));
+  if (lane == 0) lds.ends[0][wave] = lo, lds.ends[1][wave] = hi;
+  __syncthreads();
+  lo = row_low(lds.ends[0][col]);
+  hi = row_high(lds.ends[1][col]);
+  int left = want;
+  for (int level = 0;; level ^= 1) {
+    const uint32_t range = hi - lo;
+    if (range == 0) return {(uint64_t)lo + 1, left};
+    const int shift = max(0, 32 - __builtin_clz(range) - kBinBits);
+    for (int i = threadIdx.x; i < n; i += kSelectThreads) {
+      const uint32_t k = key(i);
+      if (k >= lo && k <= hi) atomicAdd(&lds.counts[level][(k - lo) >> shift], 1);      // (whole numbers: any order)
+    }
+    clear(level ^ 1);      // (last read before the last level's end)
+    __syncthreads();
+    // The largest step with at least `left` keys at or above it; a thread has two of them.
+    const int top = kBins - 1 - 2 * (int)threadIdx.x;
+    const int first = lds.counts[level][top], second = lds.counts[level][top - 1], up = scan_up(first + second);
+    if (lane == 63) lds.sums[wave] = up;
+    __syncthreads();
+    const int above = row_sum(col < wave ? lds.sums[col] : 0) + up - first - second;
+    if (above < left && above + first + second >= left) {
+      const bool of_first = above + first >= left;
+      lds.found[0] = of_first ? top : top - 1;
+      lds.found[1] = left - above - (of_first ? 0 : first);
+      lds.found[2] = of_first ? first : second;
+    }
+    __syncthreads();
+    const uint32_t from = lo + ((uint32_t)lds.found[0] << shift);
+    left = lds.found[1];
+    if (shift == 0) return {(uint64_t)from + 1, left};
+    if (left == lds.found[2]) return {from, 0};                   // all of the step
+    lo = from;
+    if (hi - lo >= 1u << shift) hi = lo + ((1u << shift) - 1);
+  }
+}
+
+// The positions of the taken ones among all n, in order: put(position, i).
+template <typename Key, typename Put>
+__device__ __forceinline__ void put_taken(SelectLds& lds, int n, const Cut& c, Key key, Put put) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int h = (int)(blockIdx.x % a.cache.heads), row = (int)(blockIdx.x / a.cache.heads);
-  const RowPages r = row_pages(a, row);
+  const unsigned long long below = (1ull << lane) - 1;
+  int taken = 0, equal = 0;      // before these rounds
+  constexpr int kRounds = kHeldKeys / kSelectThreads;
+  for (int i0 = 0; i0 < n; i0 += kHeldKeys) {
+    unsigned long long above_of[kRounds], same_of[kRounds];
+#pragma unroll
+    for (int x = 0; x < kRounds; ++x) {
+      const int i = i0 + x * kSelectThreads + threadIdx.x;
+      const uint32_t k = i < n ? key(i) : 0;
+      above_of[x] = __ballot(i < n && k >= c.cut);
+      same_of[x] = __ballot(i < n && c.ties > 0 && (uint64_t)k + 1 == c.cut);
+      if (lane == 0) lds.totals[0][x][wave] = __popcll(above_of[x]), lds.totals[1][x][wave] = __popcll(same_of[x]);
+    }
+    __syncthreads();
+    if (wave < 2) {      // sums of what is before each round and wave
+      constexpr int kAll = kRounds * kSelectWaves, kEach = kAll / 64;
+      int* const t = &lds.totals[wave][0][0] + kEach * lane;
+      int sum = 0, mine[kEach];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) mine[i] = t[i], sum += mine[i];
+      int before = scan_up(sum) - sum;
+      if (lane == 63) lds.found[wave] = before + sum;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) t[i] = before, before += mine[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < kRounds; ++x) {
+      const bool above = (above_of[x] >> lane) & 1, same = (same_of[x] >> lane) & 1;
+      const int ties = equal + lds.totals[1][x][wave] + __popcll(same_of[x] & below);
+      const int at = taken + lds.totals[0][x][wave] + __popcll(above_of[x] & below) + min(ties, c.ties);
+      if (above || (same && ties < c.ties)) put(at, i0 + x * kSelectThreads + threadIdx.x);
+    }
+    taken += lds.found[0];
+    equal += lds.found[1];
+    __syncthreads();
+  }
+}
+
+// The choice of a row and key head, by its scores.  ready(): where they are not needed (all
+// pages are taken) this is the whole of it.
+struct Chosen {
+  int32_t *index, *pages;
+  const int32_t* table;
+
+  __device__ __forceinline__ void put(int at, int entry) const { put(at, entry, table[entry]); }
+  __device__ __forceinline__ void put(int at, int entry, int page) const {
+    index[at] = entry;
+    pages[at] = page;
+  }
+};
+
+// What does not hang on scores; whether that is all.
+__device__ __forceinline__ bool choose_without(const SelectArgs& a, const RowPages& r, int row, int h, Chosen& to) {
   const int shift = a.cache.page_shift;
   if (h == 0 && threadIdx.x == 0) {
     const int taken = min(r.pages, a.count);
     a.tokens[row] = r.pages <= 0 ? r.pages : ((taken - 1) << shift) + (r.token & ((1 << shift) - 1)) + 1;
   }
-  if (r.pages < 0) return;
-  const int64_t to = ((int64_t)row * a.cache.heads + h) * a.count;
-  const int32_t* const table = a.batch.table + (int64_t)r.b * a.batch.table_stride;
-  const auto put = [&](int at, int entry) {
-    a.index[to + at] = entry;
-    a.pages[to + at] = table[entry];
-  };
+  if (r.pages < 0) return true;
+  const int64_t at = ((int64_t)row * a.cache.heads + h) * a.count;
+  to = {a.index + at, a.pages + at, a.batch.table + (int64_t)r.b * a.batch.table_stride};
   if (r.pages <= a.count) {
     for (int i = threadIdx.x; i < a.count; i += kSelectThreads) {
-      if (i < r.pages) put(i, i);
-      else a.index[to + i] = -1, a.pages[to + i] = -1;
+      if (i < r.pages) to.put(i, i);
+      else to.put(i, -1, -1);
     }
-    return;
+    return true;
   }
-  for (int i = threadIdx.x; i < a.first; i += kSelectThreads) put(i, i);
-  const int first = a.first, end = r.pages - a.recent;
-  for (int i = threadIdx.x; i < a.recent; i += kSelectThreads) put(a.count - a.recent + i, end + i);
-  int want = a.count - a.first - a.recent;
-  if (want == 0) return;
-  const uint32_t* const scores = a.scores + ((int64_t)row * a.cache.heads + h) * a.max_pages;
-  uint32_t prefix = 0;
-  int left = want;                                       // of those with this prefix
-  for (int bit = 24; bit >= 0; bit -= 8) {
-    for (int i = threadIdx.x; i < 256; i += kSelectThreads) counts[i] = 0;
-    __syncthreads();
-    for (int j = first + threadIdx.x; j < end; j += kSelectThreads) {
-      const uint32_t k = scores[j];
-      if (bit == 24 || (k >> (bit + 8)) == prefix) atomicAdd(&counts[(k >> bit) & 255], 1);      // (whole numbers: any order)
-    }
-    __syncthreads();
-    if (wave == 0) {      // the largest value with at least `left` keys at or above it
-      int mine[4], sum = 0;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) sum += mine[i] = counts[255 - 4 * lane - i];
-      int up = sum;
-#pragma unroll
-      for (int d = 1; d < 64; d *= 2) {
-        const int other = __shfl_up(up, d);
-        if (lane >= d) up += other;
-      }
-      int above = up - sum;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (above < left && above + mine[i] >= left) found[0] = 255 - 4 * lane - i, found[1] = left - above;
-        above += mine[i];
-      }
-    }
-    __syncthreads();
-    prefix = (prefix << 8) | (uint32_t)found[0];
-    left = found[1];
-  }
-  // prefix: the want-th largest key; `left` of the pages with it, the lowest, are taken.
-  int taken = 0, equal = 0;                              // before this round of pages
-  for (int j0 = first; j0 < end && taken + min(equal, left) < want; j0 += kSelectThreads) {
-    const int j = j0 + threadIdx.x;
-    const uint32_t k = j < end ? scores[j] : 0;
-    const bool above = j < end && k > prefix, same = j < end && k == prefix;
-    const unsigned long long above_of = __ballot(above), same_of = __ballot(same), below = (1ull << lane) - 1;
-    if (lane == 0) totals[0][wave] = __popcll(above_of), totals[1][wave] = __popcll(same_of);
-    __syncthreads();
-    int before = taken, same_before = equal;
-    for (int w = 0; w < kSelectWaves; ++w) {
-      if (w < wave) before += totals[0][w], same_before += totals[1][w];
-      taken += totals[0][w];
-      equal += totals[1][w];
-    }
-    before += __popcll(above_of & below);
-    same_before += __popcll(same_of & below);
-    if (above || (same && same_before < left)) put(a.first + before + min(same_before, left), j);
-    __syncthreads();
-  }
+  for (int i = threadIdx.x; i < a.first; i += kSelectThreads) to.put(i, i);
+  const int end = r.pages - a.recent;
+  for (int i = threadIdx.x; i < a.recent; i += kSelectThreads) to.put(a.count - a.recent + i, end + i);
+  return a.count == a.first + a.recent;
 }
 
-size_t kv_select_workspace_bytes(int64_t rows, int64_t heads, int64_t max_pages) {
-  return (size_t)(rows * heads * max_pages) * sizeof(uint32_t);
+// One workgroup for each row and key head: scores and choice.
+template <int D>
+__global__ __launch_bounds__(kSelectThreads) void kv_choose_kernel(SelectArgs a) {
+  __shared__ QueryCodes<D> codes;
+  __shared__ SelectLds lds;
+  __shared__ uint32_t keys[kHeldKeys];
+  __shared__ typename Scorer<D>::Turn turns[kSelectWaves];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = (int)(blockIdx.x % a.cache.heads), row = (int)(blockIdx.x / a.cache.heads);
+  QueryLane<D> query;
+  query.load(a, row, h * a.group + min(wave, a.group - 1));
+  const RowPages r = row_pages(a, row);
+  Chosen to;
+  if (choose_without(a, r, row, h, to)) return;
+  const int first = a.first, end = r.pages - a.recent, n = end - first;
+  for (int a0 = 0; a0 < a.group; a0 += kColumns) {
+    const int heads = min(a.group - a0, kColumns);
+    if (a0 > 0) query.load(a, row, h * a.group + a0 + min(wave, heads - 1));
+    if (wave < heads) query_codes<D>(query, wave, codes);
+    __syncthreads();
+    score_pages<D, kSelectWaves>(a, codes, heads, h, to.table, first, end, first & ~15, end, turns, [&](int j, uint32_t key) {
+      keys[j - first] = a0 == 0 ? key : max(keys[j - first], key);
+    });
+    __syncthreads();
+  }
+  const auto key = [&](int i) { return keys[i]; };
+  const Cut c = find_cut(lds, n, a.count - a.first - a.recent, key);
+  put_taken(lds, n, c, key, [&](int at, int i) { to.put(first + at, first + i); });
+}
+
+// The same in two launches, for few rows of long sequences: the scores, a workgroup for
+// `each` pages, and the choice.
+constexpr int kScoreWaves = 4, kScorePages = 1024;
+
+template <int D>
+__global__ __launch_bounds__(64 * kScoreWaves) void kv_page_scores_kernel(SelectArgs a, int chunks, int each) {
+  __shared__ QueryCodes<D> codes;
+  __shared__ uint32_t keys[kScorePages];
+  __shared__ typename Scorer<D>::Turn turns[kScoreWaves];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  int id = blockIdx.x;
+  const int h = id % a.cache.heads;
+  id /= a.cache.heads;
+  const int row = id / chunks, chunk = id % chunks;
+  constexpr int kMine = kColumns / kScoreWaves;
+  QueryLane<D> query[kMine];
+  const auto load = [&](int a0) {
+#pragma unroll
+    for (int x = 0; x < kMine; ++x) query[x].load(a, row, h * a.group + min(a0 + x * kScoreWaves + wave, a.group - 1));
+  };
+  load(0);
+  const RowPages r = row_pages(a, row);
+  if (r.pages <= a.count) return;                                    // (all of them are taken)
+  const int first = a.first, end = r.pages - a.recent;
+  const int j0 = chunk * each, j1 = min(end, j0 + each);
+  if (j0 >= j1) return;
+  const int32_t* const table = a.batch.table + (int64_t)r.b * a.batch.table_stride;
+  for (int a0 = 0; a0 < a.group; a0 += kColumns) {
+    const int heads = min(a.group - a0, kColumns);
+    if (a0 > 0) load(a0);
+#pragma unroll
+    for (int x = 0; x < kMine; ++x)
+      if (x * kScoreWaves + wave < heads) query_codes<D>(query[x], x * kScoreWaves + wave, codes);
+    __syncthreads();
+    score_pages<D, kScoreWaves>(a, codes, heads, h, table, first, end, j0, j1, turns, [&](int j, uint32_t key) {
+      keys[j - j0] = a0 == 0 ? key : max(keys[j - j0], key);
+    });
+    __syncthreads();
+  }
+  uint32_t* const scores = a.scores + ((int64_t)row * a.cache.heads + h) * a.max_pages;
+  for (int j = max(first, j0) + threadIdx.x; j < j1; j += 64 * kScoreWaves) scores[j] = keys[j - j0];
+}
+
+template <bool kHeld>
+__global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(SelectArgs a) {
+  __shared__ SelectLds lds;
+  __shared__ uint32_t keys[kHeld ? kHeldKeys : 1];
+  const int h = (int)(blockIdx.x % a.cache.heads), row = (int)(blockIdx.x / a.cache.heads);
+  const RowPages r = row_pages(a, row);
+  Chosen to;
+  if (choose_without(a, r, row, h, to)) return;
+  const int first = a.first, n = r.pages - a.recent - first;
+  const uint32_t* const scores = a.scores + ((int64_t)row * a.cache.heads + h) * a.max_pages + first;
+  if (kHeld) {
+    for (int i = threadIdx.x; i < n; i += kSelectThreads) keys[i] = scores[i];      // (read by the thread that writes it)
+  }
+  const auto key = [&](int i) { return kHeld ? keys[i] : scores[i]; };
+  const Cut c = find_cut(lds, n, a.count - a.first - a.recent, key);
+  put_taken(lds, n, c, key, [&](int at, int i) { to.put(first + at, first + i); });
+}
+
+namespace {
+
+// Pages of a workgroup that only scores: so that there is one for each compute unit.
+int score_each(const SelectArgs& a) {
+  const int64_t work = (int64_t)a.batch.rows * a.cache.heads * ((a.max_pages + 63) / 64);      // of 64 pages
+  const int64_t n = (work + 2047) / 2048;
+  return (int)(n < 1 ? 1 : n < kScorePages / 64 ? n : kScorePages / 64) * 64;
+}
+
+// One launch or two: one where there is a row and key head for each compute unit, or
+// little for one to do.  In one and in two (us; rows x key heads, largest table):
+//   8, 126   8.0  9.2     26, 627 (heads of 256)   14.8 11.1     32, 1001   13.5 11.5
+//   8, 2049 18.4 11.5     64, 2001 (64)            15.5 14.8     128, 1876  19.5 18.2
+//   256, 2049 24.1 26.5   504, 501                 21.0 22.4     496, 126   16.4 15.5
+bool choose_at_once(const SelectArgs& a) {
+  return a.max_pages <= 256 || (a.max_pages <= kHeldKeys && (int64_t)a.batch.rows * a.cache.heads >= 256);
+}
+
+template <int D>
+hipError_t launch_scores(const SelectArgs& a, hipStream_t stream) {
+  const int each = score_each(a), chunks = (a.max_pages + each - 1) / each;
+  kv_page_scores_kernel<D><<<dim3((unsigned)((int64_t)a.batch.rows * a.cache.heads * chunks)), 64 * kScoreWaves, 0, stream>>>(
+      a, chunks, each);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+size_t kv_select_workspace_bytes(const SelectArgs& a) {
+  return choose_at_once(a) ? 0 : (size_t)((int64_t)a.batch.rows * a.cache.heads * a.max_pages) * sizeof(uint32_t);
 }
 
 bool select_fits(const SelectArgs& a) {
-  const int64_t chunks = (a.batch.max_tokens / a.cache.page_size + kScorePages - 1) / kScorePages;
-  const int64_t each = (int64_t)a.batch.rows * a.cache.heads;
-  return one_grid(each * (chunks > 0 ? chunks : 1), 256) && one_grid(each, kSelectThreads);
+  const int64_t work = (int64_t)a.batch.rows * a.cache.heads;
+  const int each = score_each(a), chunks = (a.max_pages + each - 1) / each;
+  return one_grid(work * (chunks > 0 ? chunks : 1), 64 * kScoreWaves) && one_grid(work, kSelectThreads);
 }
 
 hipError_t launch_kv_select(const SelectArgs& a, hipStream_t stream) {
-  const int chunks = (a.max_pages + kScorePages - 1) / kScorePages;
-  const int64_t each = (int64_t)a.batch.rows * a.cache.heads;
+  const dim3 grid((unsigned)((int64_t)a.batch.rows * a.cache.heads));
+  if (choose_at_once(a)) {
+    if (a.cache.dim == 64) kv_choose_kernel<64><<<grid, kSelectThreads, 0, stream>>>(a);
+    else if (a.cache.dim == 128) kv_choose_kernel<128><<<grid, kSelectThreads, 0, stream>>>(a);
+    else kv_choose_kernel<256><<<grid, kSelectThreads, 0, stream>>>(a);
+    return hipGetLastError();
+  }
   if (a.max_pages > a.count && a.count > a.first + a.recent) {
-    const dim3 grid((unsigned)(each * chunks));
-    if (a.cache.dim == 64)
-      kv_page_scores_kernel<64><<<grid, 256, 0, stream>>>(a, chunks);
-    else if (a.cache.dim == 128)
-      kv_page_scores_kernel<128><<<grid, 256, 0, stream>>>(a, chunks);
-    else
-      kv_page_scores_kernel<256><<<grid, 256, 0, stream>>>(a, chunks);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = a.cache.dim == 64    ? launch_scores<64>(a, stream)
+                         : a.cache.dim == 128 ? launch_scores<128>(a, stream)
+                                              : launch_scores<256>(a, stream);
     if (e != hipSuccess) return e;
   }
-  kv_select_kernel<<<dim3((unsigned)each), kSelectThreads, 0, stream>>>(a);
+  if (a.max_pages <= kHeldKeys) kv_select_kernel<true><<<grid, kSelectThreads, 0, stream>>>(a);
+  else kv_select_kernel<false><<<grid, kSelectThreads, 0, stream>>>(a);
   return hipGetLastError();
 }
 

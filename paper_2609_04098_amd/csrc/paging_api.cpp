@@ -199,7 +199,11 @@ int nvfp4_kv_page_bounds(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batc
 
 size_t nvfp4_kv_select_pages_workspace(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch) {
   if (!valid_cache(cache) || !valid_batch(batch, cache->page_size)) return 0;
-  return kv_select_workspace_bytes(batch->rows, cache->kv_heads, batch->max_pages);
+  SelectArgs a = {};
+  a.cache = cache_args(cache);
+  a.batch = batch_args(batch, cache->page_size);
+  a.max_pages = (int)batch->max_pages;
+  return kv_select_workspace_bytes(a);
 }
 
 int nvfp4_kv_select_pages(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_kv_bounds* bounds,
@@ -232,7 +236,7 @@ int nvfp4_kv_select_pages(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* bat
   a.tokens = tokens;
   if (!none) {
     if (!select_fits(a)) return NVFP4_EINVAL;
-    const size_t need = kv_select_workspace_bytes(batch->rows, cache->kv_heads, batch->max_pages);
+    const size_t need = kv_select_workspace_bytes(a);
     if (need > 0 && (workspace == nullptr || !aligned(workspace, 16))) return NVFP4_EINVAL;
     if (workspace_bytes < need) return NVFP4_EWORKSPACE;
   }

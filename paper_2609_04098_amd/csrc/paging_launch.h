@@ -177,7 +177,7 @@ hipError_t launch_step_tables(const TablesArgs& a, hipStream_t stream);
 hipError_t launch_kv_attention_shared(const SharedArgs& a, const SharedPlan& p, hipStream_t stream);      // (a.part: its workspace)
 bool bounds_fit(const BoundsArgs& a);      // (each launch in range)
 hipError_t launch_kv_page_bounds(const BoundsArgs& a, hipStream_t stream);
-size_t kv_select_workspace_bytes(int64_t rows, int64_t heads, int64_t max_pages);
+size_t kv_select_workspace_bytes(const SelectArgs& a);
 bool select_fits(const SelectArgs& a);
 hipError_t launch_kv_select(const SelectArgs& a, hipStream_t stream);
 hipError_t launch_kv_attention_selected(const SelectedArgs& a, hipStream_t stream);      // (a.part: its workspace)

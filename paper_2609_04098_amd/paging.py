@@ -159,20 +159,20 @@ def _queries(q, cache, rows, out, stream):
     return n, heads, ldq, out, ldy
 
 
-def _room(workspace, nbytes, q, stream):
+def _room(workspace, nbytes, device, index, stream):
     """(workspace, its bytes): the given one, or one of nbytes from the stream that uses it."""
     if workspace is None:
-        return (_l._scratch(nbytes, q.device, stream), nbytes) if nbytes else (None, 0)
-    if workspace.get_device() != q.get_device() or not workspace.is_contiguous():
+        return (_l._scratch(nbytes, device, stream), nbytes) if nbytes else (None, 0)
+    if workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError("workspace must be contiguous, on q's device")
     return workspace, workspace.numel() * workspace.element_size()
 
 
-def _lse(wanted, rows, heads, q, stream):
-    if not wanted:
-        return None
-    with _l._on(stream, q.device):
-        return torch.empty((rows, heads), dtype=torch.float32, device=q.device)
+def _lse(rows, heads, device, stream):
+    if stream is None:
+        return torch.empty((rows, heads), dtype=torch.float32, device=device)
+    with _l._on(stream, device):
+        return torch.empty((rows, heads), dtype=torch.float32, device=device)
 
 
 def shared_attention(q, cache: KVCache, batch: Batch, shared: SharedPrefix, scale=None, causal=True, out=None,
@@ -185,9 +185,9 @@ def shared_attention(q, cache: KVCache, batch: Batch, shared: SharedPrefix, scal
         raise ValueError("tensors are on several devices")
     if shared.struct.n_groups > batch.struct.n_seqs:
         raise ValueError("there are more groups than sequences")
-    lse = _lse(return_lse, rows, heads, q, stream)
-    workspace, nbytes = _room(workspace, 0 if workspace is not None else shared.workspace_bytes(cache, batch, heads), q,
-                              stream)
+    lse = _lse(rows, heads, cache.device, stream) if return_lse else None
+    workspace, nbytes = _room(workspace, 0 if workspace is not None else shared.workspace_bytes(cache, batch, heads),
+                              cache.device, cache.index, stream)
     _run(cache.index, _p.kv_attention_shared, stream, cache.ref, batch.ref, shared.ref, q.data_ptr(), ldq, heads,
          y.data_ptr(), ldy, None if lse is None else lse.data_ptr(), cache.softmax_scale if scale is None else scale,
          1 if causal else 0, None if workspace is None else workspace.data_ptr(), nbytes)
@@ -214,6 +214,7 @@ class PageBounds:
         _need(not step.requires_grad, "step takes no gradient here")
         _need(codes.device == step.device, "the bounds' buffers are on several devices")
         self.codes, self.step, self.index = codes, step, codes.get_device()
+        self.shape = (codes.shape[0], codes.shape[1], codes.shape[3])
         self.struct = _p.bounds_struct(codes, step)
         if codes.shape[0] == 1:      # (strides of a single page say nothing)
             self.struct.page_stride, self.struct.step_stride = codes[0].numel(), codes.shape[1]
@@ -228,7 +229,7 @@ def alloc_page_bounds(cache: KVCache):
 
 
 def _of_cache(bounds, cache, batch):
-    if bounds.codes.shape[:2] != cache.k_scale.shape or bounds.codes.shape[3] != cache.head_dim:
+    if bounds.shape != (cache.struct.num_pages, cache.kv_heads, cache.head_dim):
         raise ValueError("the bounds are of another cache")
     if not cache.index == batch.index == bounds.index:
         raise ValueError("tensors are on several devices")
@@ -253,14 +254,36 @@ class Selection:
         _need(tokens.dtype == _I32 and tokens.shape == index.shape[:1] and tokens.is_contiguous(), "tokens must be int32 [rows]")
         _need(index.device == pages.device == tokens.device, "the selection's tensors are on several devices")
         self.index, self.pages, self.tokens, self.device_index = index, pages, tokens, index.get_device()
-        self._workspace = {}
+        self.shape = tuple(index.shape)
+        self.pointers = (index.data_ptr(), pages.data_ptr(), tokens.data_ptr())
 
-    def workspace_bytes(self, cache, q_heads):
-        key = (q_heads, cache.kv_heads, cache.head_dim, cache.page_size)
-        if key not in self._workspace:
-            self._workspace[key] = _p.kv_attention_selected_workspace(cache.ref, self.index.shape[0], q_heads,
-                                                                      self.index.shape[2])
-        return self._workspace[key]
+    @classmethod
+    def _new(cls, rows, kv_heads, count, more, device, stream):
+        """A new one with ``more`` bytes (a multiple of 16) of workspace, and the address of that."""
+        self = cls.__new__(cls)
+        n, front = rows * kv_heads * count, more // 4
+        if stream is None:
+            data = torch.empty(front + 2 * n + rows, dtype=_I32, device=device)
+        else:
+            with _l._on(stream, device):
+                data = torch.empty(front + 2 * n + rows, dtype=_I32, device=device)
+        self.shape, self.device_index = (rows, kv_heads, count), data.get_device()
+        first = data.data_ptr()
+        at = first + more
+        self.pointers = (at, at + 4 * n, at + 8 * n)
+        self._data, self._front, self._n = data, front, n
+        return self, first
+
+    def __getattr__(self, name):      # (tensors over one allocation, made where they are asked for)
+        if name not in ("index", "pages", "tokens") or "_data" not in self.__dict__:
+            raise AttributeError(name)
+        n, at = self._n, self._front
+        if name == "tokens":
+            t = self._data[at + 2 * n:]
+        else:
+            t = (self._data[at:at + n] if name == "index" else self._data[at + n:at + 2 * n]).view(self.shape)
+        self.__dict__[name] = t
+        return t
 
 
 def select_pages(q, cache: KVCache, batch: Batch, bounds: PageBounds, count, first=1, recent=1, causal=True,
@@ -277,20 +300,25 @@ def select_pages(q, cache: KVCache, batch: Batch, bounds: PageBounds, count, fir
         raise ValueError("tensors are on several devices")
     if count < 1 or first < 0 or recent < 1 or first + recent > count:
         raise ValueError("first and recent pages must be among the count, with at least one recent page")
-    shape = (rows, cache.kv_heads, int(count))
-    if out is None:
-        with _l._on(stream, q.device):
-            index = torch.empty(shape, dtype=_I32, device=q.device)
-            out = Selection(index, torch.empty_like(index), torch.empty(rows, dtype=_I32, device=q.device))
-    elif out.index.shape != shape:
-        raise ValueError("out must be a selection of these rows, key heads and count")
-    elif out.device_index != cache.index:
-        raise ValueError("out is on another device")
-    workspace, nbytes = _room(workspace, 0 if workspace is not None else
-                              _p.kv_select_pages_workspace(cache.ref, batch.ref), q, stream)
+    if out is not None:
+        if out.shape != (rows, cache.kv_heads, count):
+            raise ValueError("out must be a selection of these rows, key heads and count")
+        if out.device_index != cache.index:
+            raise ValueError("out is on another device")
+    nbytes, at = 0, None
+    if workspace is None:
+        key = ("select", cache.kv_heads, cache.head_dim, cache.page_size)
+        nbytes = batch._workspace.get(key)
+        if nbytes is None:
+            nbytes = batch._workspace[key] = (_p.kv_select_pages_workspace(cache.ref, batch.ref) + 15) & ~15
+    if out is None:      # (the scores are this call's own: one allocation for all)
+        out, at = Selection._new(rows, cache.kv_heads, int(count), nbytes, cache.device, stream)
+    if workspace is not None or (nbytes and at is None):
+        workspace, nbytes = _room(workspace, nbytes, cache.device, cache.index, stream)
+        at = workspace.data_ptr()
+    index, pages, tokens = out.pointers
     _run(cache.index, _p.kv_select_pages, stream, cache.ref, batch.ref, bounds.ref, q.data_ptr(), ldq, heads, count, first,
-         recent, 1 if causal else 0, out.index.data_ptr(), out.pages.data_ptr(), out.tokens.data_ptr(),
-         None if workspace is None else workspace.data_ptr(), nbytes)
+         recent, 1 if causal else 0, index, pages, tokens, at, nbytes)
     return out
 
 
@@ -298,16 +326,23 @@ def selected_attention(q, cache: KVCache, selection: Selection, scale=None, out=
                        stream=None):
     """Attention of each row over the pages chosen for it.  Returns y (bf16, q's shape),
     with the log-sum-exp over those tokens if ``return_lse``."""
-    n, kv_heads, count = selection.index.shape
+    n, kv_heads, count = selection.shape
     rows, heads, ldq, y, ldy = _queries(q, cache, n, out, stream)
     if kv_heads != cache.kv_heads:
         raise ValueError("the selection is of other key heads")
     if selection.device_index != cache.index:
         raise ValueError("tensors are on several devices")
-    lse = _lse(return_lse, rows, heads, q, stream)
-    workspace, nbytes = _room(workspace, 0 if workspace is not None else selection.workspace_bytes(cache, heads), q, stream)
-    _run(cache.index, _p.kv_attention_selected, stream, cache.ref, q.data_ptr(), ldq, heads, rows, count,
-         selection.pages.data_ptr(), selection.tokens.data_ptr(), y.data_ptr(), ldy,
-         None if lse is None else lse.data_ptr(), cache.softmax_scale if scale is None else scale,
+    lse = _lse(rows, heads, cache.device, stream) if return_lse else None
+    if workspace is None:
+        key = (rows, count, heads)
+        nbytes = cache.selected_workspace.get(key)
+        if nbytes is None:
+            nbytes = cache.selected_workspace[key] = _p.kv_attention_selected_workspace(cache.ref, rows, heads, count)
+    else:
+        nbytes = 0
+    workspace, nbytes = _room(workspace, nbytes, cache.device, cache.index, stream)
+    _, pages, tokens = selection.pointers
+    _run(cache.index, _p.kv_attention_selected, stream, cache.ref, q.data_ptr(), ldq, heads, rows, count, pages, tokens,
+         y.data_ptr(), ldy, None if lse is None else lse.data_ptr(), cache.softmax_scale if scale is None else scale,
          None if workspace is None else workspace.data_ptr(), nbytes)
     return (y, lse) if return_lse else y

@@ -185,11 +185,16 @@ def _page_bounds(cache=None, batch=None, bounds=None):
     return N.lib().nvfp4_kv_page_bounds(ctypes.byref(c), ctypes.byref(b), ctypes.byref(g), None)
 
 
+def _far(**kw):
+    """A batch of few rows and long sequences, whose scores take a workspace."""
+    return _batch(**{**dict(max_pages=1000, page_table_stride=1000, max_kv_len=32000), **kw})
+
+
 def _select(cache=None, batch=None, bounds=None, **kw):
     a = dict(q=FAKE, ldq=512, hq=4, count=4, first=1, recent=1, causal=1, index=FAKE, pages=FAKE, tokens=FAKE, ws=FAKE,
              wsb=1 << 30)
     a.update(kw)
-    c, b, g = (x if x is not None else f() for x, f in ((cache, _cache), (batch, _batch), (bounds, _bounds)))
+    c, b, g = (x if x is not None else f() for x, f in ((cache, _cache), (batch, _far), (bounds, _bounds)))
     return N.lib().nvfp4_kv_select_pages(ctypes.byref(c), ctypes.byref(b), ctypes.byref(g), a["q"], a["ldq"], a["hq"],
                                          a["count"], a["first"], a["recent"], a["causal"], a["index"], a["pages"],
                                          a["tokens"], a["ws"], a["wsb"], None)
@@ -242,10 +247,11 @@ def test_selected_attention_refuses(bad):
 
 
 def test_selection_wants_its_workspaces():
-    f, c, b = N.lib(), _cache(), _batch()
+    f, c, b = N.lib(), _cache(), _far()
     need = f.nvfp4_kv_select_pages_workspace(ctypes.byref(c), ctypes.byref(b))
     assert need > 0 and _select(wsb=need - 1) == C.NVFP4_EWORKSPACE
     assert f.nvfp4_kv_select_pages_workspace(ctypes.byref(c), ctypes.byref(_batch(rows=-1))) == 0
+    assert f.nvfp4_kv_select_pages_workspace(ctypes.byref(c), ctypes.byref(_batch())) == 0      # (one launch)
     need = f.nvfp4_kv_attention_selected_workspace(ctypes.byref(c), 1, 4, 2000)
     assert need > 0 and _selected(rows=1, count=2000, wsb=need - 1) == C.NVFP4_EWORKSPACE
     assert _selected(rows=1, count=2000, ws=None) == C.NVFP4_EINVAL == _selected(rows=1, count=2000, ws=FAKE + 4)
