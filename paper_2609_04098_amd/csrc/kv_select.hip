@@ -30,18 +30,32 @@ __device__ __forceinline__ uint32_t row_other(uint32_t v) {
 __device__ __forceinline__ f16x2 max2(f16x2 a, f16x2 b) { return __builtin_elementwise_max(a, b); }
 __device__ __forceinline__ f16x2 min2(f16x2 a, f16x2 b) { return __builtin_elementwise_min(a, b); }
 
+template <bool kMax>
+__device__ __forceinline__ f16x2 pick(f16x2 a, f16x2 b) { return kMax ? max2(a, b) : min2(a, b); }
+
 template <int kHow, bool kMax>
 __device__ __forceinline__ f16x2 fold(f16x2 v) {
-  const f16x2 o = __builtin_bit_cast(f16x2, row_other<kHow>(__builtin_bit_cast(uint32_t, v)));
-  return kMax ? max2(v, o) : min2(v, o);
+  return pick<kMax>(v, __builtin_bit_cast(f16x2, row_other<kHow>(__builtin_bit_cast(uint32_t, v))));
 }
 
+// Of 8 pairs of elements in each of 16 lanes the largest (or smallest) over the lanes: a
+// lane ends with pairs 4 (lane % 2) + 2 (lane / 2 % 2) and the one behind it.  (With a
+// neighbour each gives away half of what it has; then lanes that have the same, 4, 8
+// and 12 apart.)
 template <bool kMax>
-__device__ __forceinline__ f16x2 over_row(f16x2 v) {
-  v = fold<0xB1, kMax>(v);
-  v = fold<0x4E, kMax>(v);
-  v = fold<0x141, kMax>(v);
-  return fold<0x140, kMax>(v);
+__device__ __forceinline__ void over_row(const f16x2 (&v)[8], bool odd, bool high, f16x2 (&to)[2]) {
+  f16x2 four[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t send = __builtin_bit_cast(uint32_t, odd ? v[i] : v[i + 4]);
+    four[i] = pick<kMax>(odd ? v[i + 4] : v[i], __builtin_bit_cast(f16x2, row_other<0xB1>(send)));
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t send = __builtin_bit_cast(uint32_t, high ? four[i] : four[i + 2]);
+    to[i] = pick<kMax>(high ? four[i + 2] : four[i], __builtin_bit_cast(f16x2, row_other<0x4E>(send)));
+    to[i] = fold<0x128, kMax>(fold<0x124, kMax>(to[i]));
+  }
 }
 
 // The largest value of a row of 16 lanes.
@@ -104,7 +118,7 @@ __device__ __forceinline__ void wave_sees_lds() {
 // completed have the numbers from cu_rows[b] / page_size + b on.
 template <int D>
 __global__ __launch_bounds__(256) void kv_page_bounds_kernel(BoundsArgs a, int items) {
-  __shared__ _Float16 found[4][2][D];
+  __shared__ __attribute__((aligned(8))) _Float16 found[4][2][D];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t id = (int64_t)blockIdx.x * 4 + wave;
   const int h = (int)(id % a.cache.heads), item = (int)(id / a.cache.heads);
@@ -136,16 +150,21 @@ __global__ __launch_bounds__(256) void kv_page_bounds_kernel(BoundsArgs a, int i
       }
     }
   }
+  const bool odd = lane & 1, high = lane & 2;
 #pragma unroll
-  for (int c = 0; c < D / 64; ++c)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const f16x2 top = over_row<true>(hi[c][i]), low = over_row<false>(lo[c][i]);
-      if ((lane & 15) == 0) {
-        *reinterpret_cast<f16x2*>(&found[wave][0][64 * c + 16 * (lane >> 4) + 2 * i]) = top;
-        *reinterpret_cast<f16x2*>(&found[wave][1][64 * c + 16 * (lane >> 4) + 2 * i]) = low;
-      }
+  for (int c = 0; c < D / 64; ++c) {
+    union {
+      f16x2 pairs[2];
+      uint2 both;
+    } top, low;
+    over_row<true>(hi[c], odd, high, top.pairs);
+    over_row<false>(lo[c], odd, high, low.pairs);
+    if ((lane & 12) == 0) {
+      const int at = 64 * c + 16 * (lane >> 4) + (odd ? 8 : 0) + (high ? 4 : 0);
+      *reinterpret_cast<uint2*>(&found[wave][0][at]) = top.both;
+      *reinterpret_cast<uint2*>(&found[wave][1][at]) = low.both;
     }
+  }
   wave_sees_lds();
   constexpr int kEach = 2 * D / 64;      // elements of hi, then of lo
   float v[kEach], top = 0.0f;
@@ -154,12 +173,16 @@ __global__ __launch_bounds__(256) void kv_page_bounds_kernel(BoundsArgs a, int i
     v[i] = (float)(&found[wave][0][0])[lane * kEach + i];
     top = fmaxf(top, fabsf(v[i]));
   }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-  const float over = top > 0.0f ? top : 1.0f;
+  top = over_quarters_max(row_max(top));
+  const float over = top > 0.0f ? top : 1.0f, inv = 1.0f / over;
   uint32_t packed[(kEach + 3) / 4] = {};
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) packed[i / 4] |= ((uint32_t)(int)rintf(v[i] * 127.0f / over) & 255u) << (8 * (i % 4));
+  for (int i = 0; i < kEach; ++i) {      // (rounded as the exact quotient is: as in query_codes(), with 4 significant bits)
+    const float y = v[i] * 127.0f;
+    float q = y * inv;
+    q = fmaf(fmaf(-q, over, y), inv, q);
+    packed[i / 4] |= ((uint32_t)(int)rintf(q) & 255u) << (8 * (i % 4));
+  }
   int8_t* to = a.bounds.codes + (int64_t)page * a.bounds.page_stride + (int64_t)h * 2 * D + lane * kEach;
   if constexpr (kEach == 2) *reinterpret_cast<uint16_t*>(to) = (uint16_t)packed[0];
   else if constexpr (kEach == 4) *reinterpret_cast<uint32_t*>(to) = packed[0];

@@ -1,12 +1,17 @@
 // A step's page tables, row offsets, positions and slots from the requests'
 // lengths (definition: nvfp4_paging.h), for gfx950.
 //
-// Three sums over the sequences in order: of pages given back, pages taken and
-// rows.  One workgroup computes them (plan); what hangs on them, an entry of the
-// pool, of a table or a row each, is then independent: a thread finds its sequence
-// by bisection of the sums.  Small steps do all of it in that one workgroup, one
-// launch; where there are many rows (prompts) two more launches share it out: pages
-// go back to the pool before any is taken from it.
+// Three sums over the sequences in order: of pages given back, pages taken and rows.
+// What hangs on them, an entry of the pool, of a table or a row each, is then independent.
+// Steps of up to 1024 sequences with up to 8192 rows are one workgroup's: a thread has a
+// sequence; where none has more than a few rows and pages to move (decoding), it moves its
+// own, and a page that comes back and is taken again stays in LDS; else a thread takes an
+// entry and finds its sequence by bisection of the sums.  Where there are more rows
+// (prompts) many workgroups compute the same sums and put pages back, and a second launch
+// takes pages and places rows: pages go back to the pool before any is taken from it.
+//
+// Bound by latency: a launch, then the lengths, the tables' entries and the pool's, each a
+// load's.  500 sequences with up to 5 rows take 3.8 us, one of 1000 tokens 2.7; with bisections and 64-bit sums for all 11.9 and 5.3.
 #include "paging_launch.h"
 
 namespace nvfp4 {
@@ -14,7 +19,6 @@ namespace nvfp4 {
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kHeld = 2048;              // sequences whose sums are held in LDS
 constexpr int kOneLaunchRows = 8192;
 
 // The workspace: a head, then three vectors of seqs + 1.
@@ -109,18 +113,212 @@ __device__ __forceinline__ void place(const TablesArgs& a, const int32_t* cu, co
   a.slots[row] = there ? ((int64_t)page << a.page_shift) + (at & ((1 << a.page_shift) - 1)) : -1;
 }
 
-// The sums, and with kAll the rest of the step; kLds: they stay in LDS.
-template <bool kAll, bool kLds>
+// Sums that stay at 2^32 - 1: in any grouping the same, and exact below.
+__device__ __forceinline__ uint32_t add_sat(uint32_t x, uint32_t y) { return __builtin_elementwise_add_sat(x, y); }
+
+template <int kHow, int kRows>
+__device__ __forceinline__ uint32_t from_below(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kHow, kRows, 0xF, false);
+}
+
+// Over the lanes up to this one (all lanes active).
+__device__ __forceinline__ uint32_t scan_up(uint32_t x) {
+  x = add_sat(x, from_below<0x111, 0xF>(x));      // one lane below, in a row of 16; two, four, eight
+  x = add_sat(x, from_below<0x112, 0xF>(x));
+  x = add_sat(x, from_below<0x114, 0xF>(x));
+  x = add_sat(x, from_below<0x118, 0xF>(x));
+  x = add_sat(x, from_below<0x142, 0xA>(x));      // the last lane of the row below, into rows 1 and 3
+  return add_sat(x, from_below<0x143, 0xC>(x));   // lane 31, into rows 2 and 3
+}
+
+template <int kHow>
+__device__ __forceinline__ uint32_t row_other(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, kHow, 0xF, 0xF, true);
+}
+
+// Over a row of 16 lanes.
+__device__ __forceinline__ uint32_t row_sum(uint32_t v) {
+  v = add_sat(v, row_other<0xB1>(v));
+  v = add_sat(v, row_other<0x4E>(v));
+  v = add_sat(v, row_other<0x141>(v));
+  return add_sat(v, row_other<0x140>(v));
+}
+
+__device__ __forceinline__ uint32_t row_high(uint32_t v) {
+  v = max(v, row_other<0xB1>(v));
+  v = max(v, row_other<0x4E>(v));
+  v = max(v, row_other<0x141>(v));
+  return max(v, row_other<0x140>(v));
+}
+
+// The step's sums for up to 1024 sequences, one of them a thread's: what is before it.
+struct Sums {
+  Request r;
+  bool served;
+  uint32_t given, taken, rows;           // of the sequences before this one
+  int before, backs, pages, all_rows, left;      // the pool, pages given back and taken, rows given, the pool behind
+};
+
+struct SumsLds {
+  uint32_t totals[3][kWaves], ends[2][kWaves], most[kWaves];
+};
+
+// An entry's share of items of a sequence that a thread moves by itself.
+constexpr int kOwnBack = 2, kOwnRows = 8;
+
+__device__ __forceinline__ Sums step_sums(const TablesArgs& a, SumsLds& lds) {
+  static_assert(kWaves == 16, "a wave for each lane of a row");
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, b = threadIdx.x;
+  Sums s;
+  const int count = a.free_count[0];
+  int held = 0, drop = 0, kept = 0, rows = 0;
+  if (b < a.seqs) {
+    held = a.kv_len[b];
+    rows = a.new_rows[b];
+    if (a.drop != nullptr) drop = a.drop[b];
+    if (a.kept != nullptr) kept = a.kept[b];
+  }
+  s.before = min(max(count, 0), a.num_pages);
+  s.r = request(a, b, held, drop, kept, rows);
+  const uint32_t mine[3] = {(uint32_t)s.r.back, (uint32_t)s.r.need, (uint32_t)s.r.rows};
+  uint32_t up[3], own[3], all[3];
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    up[i] = scan_up(mine[i]);
+    if (lane == 63) lds.totals[i][wave] = up[i];
+  }
+  const bool many = s.r.back > kOwnBack || s.r.rows > kOwnRows;
+  if (lane == 0) lds.most[wave] = 0;
+  if (__any(many) && lane == 0) lds.most[wave] = 1;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const uint32_t of_wave = lds.totals[i][col], ahead = row_sum(col < wave ? of_wave : 0u);
+    all[i] = row_sum(of_wave);
+    own[i] = add_sat(ahead, up[i]);      // with this sequence
+  }
+  s.backs = (int)min(all[0], (uint32_t)(a.num_pages - s.before));
+  const uint32_t room = (uint32_t)(s.before + s.backs);
+  // Both sums grow, so those that are served are the first ones.
+  s.served = b < a.seqs && own[1] <= room && own[2] <= (uint32_t)a.rows;
+  const int served = __popcll(__ballot(s.served));
+  const int last = max(served - 1, 0);
+  const uint32_t end_pages = (uint32_t)__builtin_amdgcn_readlane((int)own[1], last), end_rows = (uint32_t)__builtin_amdgcn_readlane((int)own[2], last);
+  if (lane == 0) lds.ends[0][wave] = served ? end_pages : 0u, lds.ends[1][wave] = served ? end_rows : 0u;
+  __syncthreads();
+  s.pages = (int)row_high(lds.ends[0][col]);
+  s.all_rows = (int)row_high(lds.ends[1][col]);
+  s.left = (int)room - s.pages;
+  s.given = own[0] == ~0u ? ~0u : own[0] - mine[0];      // (behind 2^32 - 1 pages nothing is put back)
+  s.taken = s.served ? own[1] - mine[1] : (uint32_t)s.pages;
+  s.rows = s.served ? own[2] - mine[2] : (uint32_t)s.all_rows;
+  return s;
+}
+
+// Offsets and lengths.
+__device__ __forceinline__ void put_lengths(const TablesArgs& a, const Sums& s) {
+  const int b = threadIdx.x;
+  if (b < a.seqs) {
+    a.cu_rows[b] = (int)s.rows;
+    a.kv_len[b] = s.r.base + (s.served ? s.r.rows : 0);
+  }
+  if (b == 0) {
+    a.cu_rows[a.seqs] = s.all_rows;
+    a.free_count[0] = s.left;
+  }
+}
+
+// A whole step of up to 1024 sequences in one workgroup.
+__global__ __launch_bounds__(kThreads) void step_small_kernel(TablesArgs a) {
+  __shared__ SumsLds lds;
+  __shared__ int32_t sums[4][kThreads + 1];      // or, in the first of them, the pages that come back
+  const int b = threadIdx.x, shift = a.page_shift;
+  const Sums s = step_sums(a, lds);
+  const bool many = row_high(lds.most[threadIdx.x & 15]) != 0 || s.backs > kThreads;
+  int32_t* const table = a.table + (int64_t)b * a.table_stride;
+  if (!many) {
+    // Each thread its own sequence's few: at most kOwnBack pages back, one new page, kOwnRows rows.
+    const int have = ceil_shift(s.r.base, shift);
+    int back[kOwnBack], open = -1;
+#pragma unroll
+    for (int i = 0; i < kOwnBack; ++i)
+      if (i < s.r.back) back[i] = table[s.r.back0 + i];
+    if (s.served && s.r.rows > 0 && (s.r.base & ((1 << shift) - 1))) open = table[have - 1];      // the page that is filled on
+    // (a page of the pool that was there before: known now)
+    const int64_t at = (int64_t)s.left + s.taken;
+    const bool takes = s.served && s.r.need > 0;
+    int fresh = takes && at < s.before ? a.free_pages[at] : -1;
+#pragma unroll
+    for (int i = 0; i < kOwnBack; ++i) {
+      const uint32_t to = s.given + i;
+      if (i < s.r.back && to < (uint32_t)s.backs) {
+        sums[0][to] = back[i];
+        a.free_pages[s.before + to] = back[i];
+      }
+    }
+    put_lengths(a, s);
+    __syncthreads();
+    if (takes) {
+      if (at >= s.before) fresh = sums[0][at - s.before];
+      table[have] = fresh;
+    }
+    if (s.served) {
+#pragma unroll
+      for (int i = 0; i < kOwnRows; ++i) {
+        if (i >= s.r.rows) break;
+        const int row = (int)s.rows + i, position = s.r.base + i, page = (position >> shift) >= have ? fresh : open;
+        if (a.positions != nullptr) a.positions[row] = position;
+        if (a.slots != nullptr)
+          a.slots[row] = page >= 0 && page < a.num_pages ? ((int64_t)page << shift) + (position & ((1 << shift) - 1)) : -1;
+      }
+    }
+    return;
+  }
+  if (b < a.seqs) sums[0][b] = (int)min(s.given, 0x7FFFFFFFu), sums[1][b] = (int)s.taken, sums[2][b] = s.r.base, sums[3][b] = (int)s.rows;
+  if (b == 0) sums[0][a.seqs] = 0x7FFFFFFF, sums[1][a.seqs] = s.pages, sums[3][a.seqs] = s.all_rows;
+  put_lengths(a, s);
+  __syncthreads();
+  for (int i = b; i < s.backs; i += kThreads) give_back(a, sums[0], sums[2], i, s.before);
+  __syncthreads();
+  for (int i = b; i < s.all_rows; i += kThreads) place(a, sums[3], sums[1], sums[2], i, s.left);
+  for (int i = b; i < s.pages; i += kThreads) take(a, sums[1], sums[2], i, s.left);
+}
+
+// The first of two launches for up to 1024 sequences with many rows: every workgroup
+// computes the sums for itself and puts its share of the pages back; the first one leaves
+// them, and the lengths, for the second launch (here they are still read).
+__global__ __launch_bounds__(kThreads) void step_begin_kernel(TablesArgs a) {
+  __shared__ SumsLds lds;
+  __shared__ int32_t sums[2][kThreads + 1];
+  const int b = threadIdx.x;
+  const Sums s = step_sums(a, lds);
+  if (b < a.seqs) sums[0][b] = (int)min(s.given, 0x7FFFFFFFu), sums[1][b] = s.r.base;
+  if (b == 0) sums[0][a.seqs] = 0x7FFFFFFF;
+  if (blockIdx.x == 0) {
+    const Plan ws = plan_of(a.plan, a.seqs);
+    if (b < a.seqs) {
+      ws.given[b] = s.r.base + (s.served ? s.r.rows : 0);      // (the lengths to be)
+      ws.taken[b] = (int)s.taken;
+      ws.base[b] = s.r.base;
+      a.cu_rows[b] = (int)s.rows;
+    }
+    if (b == 0) {
+      ws.taken[a.seqs] = s.pages;
+      a.cu_rows[a.seqs] = s.all_rows;
+      *reinterpret_cast<PlanHead*>(a.plan) = {s.backs, s.pages, s.before, s.left, s.all_rows};
+    }
+  }
+  __syncthreads();
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + b; i < s.backs; i += (int64_t)gridDim.x * kThreads)
+    give_back(a, sums[0], sums[1], (int)i, s.before);
+}
+
+// The sums for more sequences.
 __global__ __launch_bounds__(kThreads) void step_plan_kernel(TablesArgs a) {
   __shared__ int64_t totals[3][kWaves];
   __shared__ int ends[2];
-  __shared__ int32_t held_sums[4][kLds ? kHeld + 1 : 1];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const Plan ws = plan_of(a.plan, a.seqs);
-  int32_t* const given = kLds ? held_sums[0] : ws.given;
-  int32_t* const taken = kLds ? held_sums[1] : ws.taken;
-  int32_t* const base = kLds ? held_sums[2] : ws.base;
-  int32_t* const cu = kLds ? held_sums[3] : a.cu_rows;
   const int before = min(max(a.free_count[0], 0), a.num_pages);
   // Pages given back first: what is served hangs on all of them.
   int64_t carry = 0;
@@ -140,7 +338,7 @@ __global__ __launch_bounds__(kThreads) void step_plan_kernel(TablesArgs a) {
       carry += totals[0][w];
     }
     // (Behind the pool's room nothing is put back, so a sum beyond 32 bits may stop there.)
-    if (b < a.seqs) given[b] = (int32_t)min(sum, (int64_t)0x7FFFFFFF);
+    if (b < a.seqs) ws.given[b] = (int32_t)min(sum, (int64_t)0x7FFFFFFF);
     __syncthreads();
   }
   const int backs = (int)min(carry, (int64_t)a.num_pages - before);
@@ -171,34 +369,20 @@ __global__ __launch_bounds__(kThreads) void step_plan_kernel(TablesArgs a) {
     __syncthreads();
     last_pages = ends[0], last_rows = ends[1];
     if (b < a.seqs) {
-      taken[b] = served ? (int)from_pages : last_pages;
-      const int first = served ? (int)from_rows : last_rows;
-      a.cu_rows[b] = first;
-      if (kLds) cu[b] = first;
-      base[b] = r.base;
+      ws.taken[b] = served ? (int)from_pages : last_pages;
+      a.cu_rows[b] = served ? (int)from_rows : last_rows;
+      ws.base[b] = r.base;
       a.kv_len[b] = r.base + (served ? r.rows : 0);
     }
     __syncthreads();
   }
   const int left = room - last_pages;
   if (threadIdx.x == 0) {
-    given[a.seqs] = (int32_t)min(carry, (int64_t)0x7FFFFFFF);
-    taken[a.seqs] = last_pages;
+    ws.given[a.seqs] = (int32_t)min(carry, (int64_t)0x7FFFFFFF);
+    ws.taken[a.seqs] = last_pages;
     a.cu_rows[a.seqs] = last_rows;
-    if (kLds) cu[a.seqs] = last_rows;
     a.free_count[0] = left;
-    if (!kAll) {
-      PlanHead* head = reinterpret_cast<PlanHead*>(a.plan);
-      *head = {backs, last_pages, before, left, last_rows};
-    }
-  }
-  if constexpr (kAll) {
-    __syncthreads();
-    for (int i = threadIdx.x; i < backs; i += kThreads) give_back(a, given, base, i, before);
-    __syncthreads();
-    for (int i = threadIdx.x; i < last_rows; i += kThreads) place(a, cu, taken, base, i, left);
-    __syncthreads();
-    for (int i = threadIdx.x; i < last_pages; i += kThreads) take(a, taken, base, i, left);
+    *reinterpret_cast<PlanHead*>(a.plan) = {backs, last_pages, before, left, last_rows};
   }
 }
 
@@ -209,9 +393,14 @@ __global__ __launch_bounds__(256) void step_give_back_kernel(TablesArgs a) {
     give_back(a, ws.given, ws.base, (int)i, head.before);
 }
 
-__global__ __launch_bounds__(256) void step_fill_kernel(TablesArgs a) {
+// Rows and new pages; lengths: those of step_begin_kernel are still to be put down.
+__global__ __launch_bounds__(256) void step_fill_kernel(TablesArgs a, int lengths) {
   const PlanHead head = *reinterpret_cast<const PlanHead*>(a.plan);
   const Plan ws = plan_of(a.plan, a.seqs);
+  if (lengths && blockIdx.x == 0) {
+    for (int b = threadIdx.x; b < a.seqs; b += 256) a.kv_len[b] = ws.given[b];
+    if (threadIdx.x == 0) a.free_count[0] = head.left;
+  }
   const int64_t all = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
   for (int64_t i = first; i < head.rows; i += all) place(a, a.cu_rows, ws.taken, ws.base, (int)i, head.left);
   // (New entries are those that no row of place() reads: behind the base's pages.)
@@ -223,19 +412,22 @@ __global__ __launch_bounds__(256) void step_fill_kernel(TablesArgs a) {
 size_t step_tables_workspace_bytes(int64_t seqs) { return (size_t)(kHead + 3 * (seqs + 1)) * sizeof(int32_t); }
 
 hipError_t launch_step_tables(const TablesArgs& a, hipStream_t stream) {
-  if (a.rows <= kOneLaunchRows) {
-    if (a.seqs <= kHeld)
-      step_plan_kernel<true, true><<<1, kThreads, 0, stream>>>(a);
-    else
-      step_plan_kernel<true, false><<<1, kThreads, 0, stream>>>(a);
+  hipError_t e;
+  if (a.seqs <= kThreads && a.rows <= kOneLaunchRows) {
+    step_small_kernel<<<1, kThreads, 0, stream>>>(a);
     return hipGetLastError();
   }
-  step_plan_kernel<false, false><<<1, kThreads, 0, stream>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  step_give_back_kernel<<<256, 256, 0, stream>>>(a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  step_fill_kernel<<<512, 256, 0, stream>>>(a);
+  const bool two = a.seqs <= kThreads;
+  if (two) {
+    step_begin_kernel<<<32, kThreads, 0, stream>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  } else {
+    step_plan_kernel<<<1, kThreads, 0, stream>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    step_give_back_kernel<<<256, 256, 0, stream>>>(a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  step_fill_kernel<<<512, 256, 0, stream>>>(a, two ? 1 : 0);
   return hipGetLastError();
 }
 
