@@ -150,7 +150,7 @@ const char* nvfp4_kv_attention_shared_kernel(const nvfp4_kv_cache* cache, const 
  * page_size tokens, A the largest |hi_e|, |lo_e| of the head (all 0 if A is), fl binary32.
  * Requirements: codes 16-byte aligned, int8 [num_pages]; page_stride in bytes, a
  * multiple of 16, at least 2 * kv_heads * head_dim; step float [num_pages], 4-byte aligned,
- * step_stride >= kv_heads.
+ * step_stride >= kv_heads; strides below 2^31.
  */
 typedef struct nvfp4_kv_bounds {
   void* codes;

@@ -66,6 +66,12 @@ __device__ __forceinline__ float row_max(float m) {
   return fmaxf(m, __uint_as_float(row_other<0x140>(__float_as_uint(m))));
 }
 
+// The larger of this and of what another lane sends.
+template <int kHow>
+__device__ __forceinline__ float other_max(float keep, float send) {
+  return fmaxf(keep, __uint_as_float(row_other<kHow>(__float_as_uint(send))));
+}
+
 // Sums over the lanes up to this one (all lanes active).
 template <int kHow, int kRows>
 __device__ __forceinline__ int from_below(int v) {
@@ -318,16 +324,22 @@ struct Scorer {
 
   static __device__ __forceinline__ void load(const SelectArgs& a, int h, int page, Round& to) {
     const int chunk = (threadIdx.x & 63) % kChunks;
+    const uint32_t mine = (uint32_t)max(page, 0);
     to.page = page;
-    to.step = a.bounds.step[(int64_t)max(page, 0) * a.bounds.step_stride + h];
+    to.step = (a.bounds.step + h)[(uint64_t)mine * (uint32_t)a.bounds.step_stride];
+    const int8_t* const at = a.bounds.codes + h * 2 * D + chunk * 16;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int p = max(__shfl(page, owner(i)), 0);
-      to.raw[i] = *reinterpret_cast<const i32x4*>(a.bounds.codes + (int64_t)p * a.bounds.page_stride + (int64_t)h * 2 * D + chunk * 16);
-    }
+    for (int i = 0; i < kLoads; ++i)      // (strides below 2^31: one product each)
+      to.raw[i] = *reinterpret_cast<const i32x4*>(at + (uint64_t)(uint32_t)__shfl((int)mine, owner(i)) * (uint32_t)a.bounds.page_stride);
   }
 
-  // The key of page 4 quarter + col for the lanes of columns 0 to 3.
+  // The page of 16 whose key a lane of columns 0 to 3 gets.
+  static __device__ __forceinline__ int of_lane() {
+    const int lane = threadIdx.x & 63;
+    return 4 * (lane >> 4) + 2 * (lane & 1) + (lane >> 1 & 1);
+  }
+
+  // Its key.
   __device__ __forceinline__ uint32_t key(const Round& p, Turn& turn) const {
     const int lane = threadIdx.x & 63, col = lane & 15, quarter = lane >> 4, chunk = lane % kChunks;
     i32x4 sum = (i32x4){0, 0, 0, 0};
@@ -347,11 +359,17 @@ struct Scorer {
       }
       wave_sees_lds();
     }
-    float best[4];      // pages 4 quarter + e
+    // Pages 4 quarter + e of head col: the largest over the heads, of page 4 quarter + 2
+    // (col % 2) + col / 2 % 2 (a lane gives away half of its pages, twice).
+    const bool odd = col & 1, high = col & 2;
+    float v[4];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) best[e] = row_max((float)sum[e] * unit);
-    const float m = (col & 2) ? ((col & 1) ? best[3] : best[2]) : ((col & 1) ? best[1] : best[0]);
-    const int mine = 4 * quarter + (col & 3);
+    for (int e = 0; e < 4; ++e) v[e] = (float)sum[e] * unit;
+    const float a0 = other_max<0xB1>(odd ? v[2] : v[0], odd ? v[0] : v[2]), a1 = other_max<0xB1>(odd ? v[3] : v[1], odd ? v[1] : v[3]);
+    float m = other_max<0x4E>(high ? a1 : a0, high ? a0 : a1);
+    m = other_max<0x124>(m, m);
+    m = other_max<0x128>(m, m);
+    const int mine = of_lane();
     const float step = __shfl(p.step, mine);
     return __shfl(p.page, mine) < 0 ? 0u : key_of(m * step);
   }
@@ -389,7 +407,7 @@ __device__ __forceinline__ void score_pages(const SelectArgs& a, const QueryCode
     Scorer<D>::load(a, h, page, p[kAhead]);
     page = behind;
     const uint32_t key = scorer.key(p[0], turns[wave]);
-    const int mine = j + 4 * quarter + (col & 3);
+    const int mine = j + Scorer<D>::of_lane();
     if (col < 4 && mine >= first && mine < end) put(mine, key);
 #pragma unroll
     for (int x = 0; x < kAhead; ++x) p[x] = p[x + 1];

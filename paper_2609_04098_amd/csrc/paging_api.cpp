@@ -47,7 +47,8 @@ SharedArgs shared_args(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch,
 
 bool valid_bounds(const nvfp4_kv_bounds* b, const nvfp4_kv_cache* c) {
   if (b == nullptr || b->codes == nullptr || b->step == nullptr || !aligned(b->codes, 16) || !aligned(b->step, 4)) return false;
-  return b->page_stride >= 2 * c->kv_heads * c->head_dim && b->page_stride % 16 == 0 && b->step_stride >= c->kv_heads;
+  return b->page_stride >= 2 * c->kv_heads * c->head_dim && b->page_stride % 16 == 0 && b->page_stride < kI32Lim &&
+         b->step_stride >= c->kv_heads && b->step_stride < kI32Lim;
 }
 
 PageBoundsArgs bounds_args(const nvfp4_kv_bounds* b) {

@@ -223,7 +223,8 @@ def test_selection_refuses_batches(call, bad):
 
 @pytest.mark.parametrize("call", [_page_bounds, _select])
 @pytest.mark.parametrize("bad", [dict(codes=None), dict(step=None), dict(codes=FAKE + 8), dict(step=FAKE + 2),
-                                 dict(page_stride=496), dict(page_stride=520), dict(step_stride=1)])
+                                 dict(page_stride=496), dict(page_stride=520), dict(step_stride=1),
+                                 dict(page_stride=1 << 31), dict(step_stride=1 << 31)])
 def test_selection_refuses_bounds(call, bad):
     assert call(bounds=_bounds(**bad)) == C.NVFP4_EINVAL
 
