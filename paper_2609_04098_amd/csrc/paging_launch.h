@@ -82,10 +82,41 @@ inline size_t all_part_bytes(const KvCacheArgs& c, int64_t tiles, const Attentio
 //   320 of 128: 85 us with 16, 76 with 32, 79 with 128    512 (4096 tokens): 30.0 29.7 32.9
 //   1024: 126 112 105     2048: 133 128 112     2048 of 64: 97 85 84
 //   900 of 256: 49 (16), 54 (128)     512 of 256 (30000 tokens): 59 (16), 65 (128)
-// Pieces: one workgroup for each compute unit, two where it would take over 6000 tokens
-// (900 rows of 256: 49 us in one of 4160, 56 in two; 320 rows of 128, 32768 tokens: 82 in
-// twelve, 76 in six), three in tiles of 128 rows where it would over 3000 (1024 rows,
-// 16000 tokens: 131 us in four, 92 in twelve, without the join).
+// Pieces: the number of them for which an estimate is least, in the time of a token for a
+// workgroup that has its compute unit to itself (3.7 ns for 32 rows of 128): 1400 for its
+// beginning and end; two of them on a unit take 1.5 times as long (1.8 with heads of 256), a
+// few units with two or three, where there is not one for every half, twice; and a piece's partial
+// results, written and read, at 4 TB/s, with a wave's eighth of a load's latency.  (20 users, 64 / 4 heads, a prefix of 30000: 49 us in six
+// pieces, 43 in twelve, 48 in 24; two groups of 20 with 64 / 8 heads, 16000: 69 in two, 43 in
+// six; 900 rows of 256: 49 in one of 4160, 56 in two; 32 x 4: 30 in two, 33 in four.)
+// Tiles of 128 rows: three to a unit (1024 rows, 16000 tokens: 131 us in four, 92 in twelve).
+inline AttentionPlan shared_pieces(int tokens, int64_t work, int64_t packed_rows, int dim, bool wide, int least) {
+  AttentionPlan q = {};
+  const auto chunk_of = [&](int64_t n) {
+    const int c = (int)(((tokens + n - 1) / n + 127) / 128 * 128);
+    return c < least ? least : c;
+  };
+  int64_t best = 1;
+  if (wide) {
+    best = work < 256 ? 256 / work : 1;
+    if (tokens / best > 1000) best = work < 768 ? 768 / work : 1;
+  } else {
+    const double both = dim == 256 ? 1.8 : 1.5, part = 25.0 + (double)packed_rows * (dim + 2) * 8.0 / 4e6 / 3.7e-3;
+    double least_time = 0.0;
+    for (int64_t n = 1; n <= 128 && (n == 1 || tokens / n >= least); ++n) {
+      const int64_t all = work * n;
+      const double each = (double)chunk_of(n);
+      const double time = (all <= 256 ? each + 1400.0 : all < 448 ? 2.0 * each + 1400.0
+                                                                  : (double)((all + 511) / 512) * (both * each + 1400.0)) + n * part;
+      if (n == 1 || time < least_time) least_time = time, best = n;
+    }
+  }
+  q.chunk = chunk_of(best);
+  q.splits = tokens > 0 ? (tokens + q.chunk - 1) / q.chunk : 1;
+  q.waves = 4;
+  return q;
+}
+
 inline SharedPlan shared_plan(const SharedArgs& a) {
   SharedPlan p = {};
   const int64_t rows = (int64_t)a.batch.rows * a.group;
@@ -96,25 +127,15 @@ inline SharedPlan shared_plan(const SharedArgs& a) {
     p.bytes = part_bytes(a.cache, a.batch, a.group, p.whole);
     return p;
   }
-  const auto pieces = [](int tokens, int64_t work, bool wide, int least) {
-    AttentionPlan q = {};
-    const int resident = wide ? 3 : 2;
-    int64_t n = work < 256 ? 256 / work : 1;
-    if (tokens / n > (wide ? 3000 : 6000)) n = work < 256 * resident ? 256 * resident / work : 1;
-    q.chunk = (int)(((tokens + n - 1) / n + 127) / 128 * 128);
-    if (q.chunk < least) q.chunk = least;
-    q.splits = tokens > 0 ? (tokens + q.chunk - 1) / q.chunk : 1;
-    q.waves = 4;
-    return q;
-  };
   const int own_form = of_seq <= 16 ? 1 : a.cache.dim == 256 ? 8 : 2;
   int form = a.cache.dim == 256 || of_group < 256 ? 1 : of_group < 768 ? 2 : 8;
   if (form < own_form) form = own_form;
-  p.prefix = pieces(a.max_prefix, prefix_tiles(a, form) * a.cache.heads, form == 8, 128);
+  const int64_t all_rows = rows * a.cache.heads;
+  p.prefix = shared_pieces(a.max_prefix, prefix_tiles(a, form) * a.cache.heads, all_rows, a.cache.dim, form == 8, 128);
   p.prefix.tiles = form;
   p.prefix_bytes = all_part_bytes(a.cache, prefix_tiles(a, form), p.prefix);
   const int64_t own_tiles = host_tiles(a.batch, a.group, 16 * own_form);
-  p.own = pieces(a.max_own, own_tiles * a.cache.heads, own_form == 8, 256);
+  p.own = shared_pieces(a.max_own, own_tiles * a.cache.heads, all_rows, a.cache.dim, own_form == 8, 256);
   p.own.tiles = own_form;
   p.bytes = p.prefix_bytes + all_part_bytes(a.cache, own_tiles, p.own);
   return p;
