@@ -570,21 +570,6 @@ __device__ __forceinline__ bool choose_without(const SelectArgs& a, const RowPag
   return a.count == a.first + a.recent;
 }
 
-// What a workgroup takes: key head h of an item (a row, a part of a row's pages).  Workgroups go to
-// the eight dies in turn: the heads of an item go to one of them, so that its L2 reads once
-// what they share, the lines of the steps (with the heads on eight dies, for 32 rows of up to 2048 pages 760 thousand lines were read, so 530).
-__device__ __forceinline__ bool work_of(int heads, int items, int& item, int& h) {
-  const unsigned id = blockIdx.x;
-  if (items < 8) {
-    item = (int)(id / heads), h = (int)(id % heads);
-    return true;
-  }
-  item = (int)(id / (8 * heads) * 8 + id % 8), h = (int)(id / 8 % heads);
-  return item < items;
-}
-
-int64_t workgroups(int64_t heads, int64_t items) { return items < 8 ? items * heads : (items + 7) / 8 * 8 * heads; }
-
 // One workgroup for each row and key head: scores and choice.
 template <int D>
 __global__ __launch_bounds__(kSelectThreads) void kv_choose_kernel(SelectArgs a) {
@@ -593,8 +578,7 @@ __global__ __launch_bounds__(kSelectThreads) void kv_choose_kernel(SelectArgs a)
   __shared__ uint32_t keys[kHeldKeys];
   __shared__ typename Scorer<D>::Turn turns[kSelectWaves];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int row, h;
-  if (!work_of(a.cache.heads, a.batch.rows, row, h)) return;
+  const int h = (int)(blockIdx.x % a.cache.heads), row = (int)(blockIdx.x / a.cache.heads);
   QueryLane<D> query;
   query.load(a, row, h * a.group + min(wave, a.group - 1));
   const RowPages r = row_pages(a, row);
@@ -626,9 +610,10 @@ __global__ __launch_bounds__(64 * kScoreWaves) void kv_page_scores_kernel(Select
   __shared__ uint32_t keys[kScorePages];
   __shared__ typename Scorer<D>::Turn turns[kScoreWaves];
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  int item, h;
-  if (!work_of(a.cache.heads, a.batch.rows * chunks, item, h)) return;
-  const int row = item / chunks, chunk = item % chunks;
+  int id = blockIdx.x;
+  const int h = id % a.cache.heads;
+  id /= a.cache.heads;
+  const int row = id / chunks, chunk = id % chunks;
   constexpr int kMine = kColumns / kScoreWaves;
   QueryLane<D> query[kMine];
   const auto load = [&](int a0) {
@@ -662,8 +647,7 @@ template <bool kHeld>
 __global__ __launch_bounds__(kSelectThreads) void kv_select_kernel(SelectArgs a) {
   __shared__ SelectLds lds;
   __shared__ uint32_t keys[kHeld ? kHeldKeys : 1];
-  int row, h;
-  if (!work_of(a.cache.heads, a.batch.rows, row, h)) return;
+  const int h = (int)(blockIdx.x % a.cache.heads), row = (int)(blockIdx.x / a.cache.heads);
   const RowPages r = row_pages(a, row);
   Chosen to;
   if (choose_without(a, r, row, h, to)) return;
@@ -698,7 +682,7 @@ bool choose_at_once(const SelectArgs& a) {
 template <int D>
 hipError_t launch_scores(const SelectArgs& a, hipStream_t stream) {
   const int each = score_each(a), chunks = (a.max_pages + each - 1) / each;
-  kv_page_scores_kernel<D><<<dim3((unsigned)workgroups(a.cache.heads, (int64_t)a.batch.rows * chunks)), 64 * kScoreWaves, 0, stream>>>(
+  kv_page_scores_kernel<D><<<dim3((unsigned)((int64_t)a.batch.rows * a.cache.heads * chunks)), 64 * kScoreWaves, 0, stream>>>(
       a, chunks, each);
   return hipGetLastError();
 }
@@ -710,14 +694,13 @@ size_t kv_select_workspace_bytes(const SelectArgs& a) {
 }
 
 bool select_fits(const SelectArgs& a) {
+  const int64_t work = (int64_t)a.batch.rows * a.cache.heads;
   const int each = score_each(a), chunks = (a.max_pages + each - 1) / each;
-  const int64_t items = (int64_t)a.batch.rows * (chunks > 0 ? chunks : 1);
-  return items < (int64_t)1 << 31 && one_grid(workgroups(a.cache.heads, items), 64 * kScoreWaves) &&
-         one_grid(workgroups(a.cache.heads, a.batch.rows), kSelectThreads);
+  return one_grid(work * (chunks > 0 ? chunks : 1), 64 * kScoreWaves) && one_grid(work, kSelectThreads);
 }
 
 hipError_t launch_kv_select(const SelectArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)workgroups(a.cache.heads, a.batch.rows));
+  const dim3 grid((unsigned)((int64_t)a.batch.rows * a.cache.heads));
   if (choose_at_once(a)) {
     if (a.cache.dim == 64) kv_choose_kernel<64><<<grid, kSelectThreads, 0, stream>>>(a);
     else if (a.cache.dim == 128) kv_choose_kernel<128><<<grid, kSelectThreads, 0, stream>>>(a);
