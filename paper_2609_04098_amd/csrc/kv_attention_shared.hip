@@ -94,10 +94,12 @@ __global__ __launch_bounds__(256) void kv_attention_shared_join_kernel(SharedArg
     part[which] = parts + 2 * ((tiles * a.cache.heads * splits) << shift) + first * D + lane * kEach;
     stride[which] = 1 << shift;
   };
-  const int before = prefix > 0 ? min((prefix - 1) / of.chunk, of.splits - 1) + 1 : 0;
+  const int row0 = prefix > 0 ? start_row(a.batch, group_seq) : 0;
+  // (Offsets that make no sense may put a group's first row behind this one.)
+  const int before = prefix > 0 && row0 <= s.row ? min((prefix - 1) / of.chunk, of.splits - 1) + 1 : 0;
   stats[0] = nullptr, part[0] = nullptr, stride[0] = 0;
   if (before > 0) {
-    const int row0 = start_row(a.batch, group_seq), shift = 4 + __builtin_ctz(of.tiles);
+    const int shift = 4 + __builtin_ctz(of.tiles);
     const int packed = (s.row - row0) * a.group + r;
     of_tile(0, of.part, (((int64_t)row0 * a.group) >> shift) + g + (packed >> shift),
             prefix_tile_numbers((int64_t)a.batch.rows * a.group, 1 << shift, a.groups), packed & ((1 << shift) - 1), shift, of.splits);

@@ -298,6 +298,7 @@ def select_pages(q, cache: KVCache, batch: Batch, bounds: PageBounds, count, fir
     _of_cache(bounds, cache, batch)
     if q.get_device() != cache.index:
         raise ValueError("tensors are on several devices")
+    count, first, recent = int(count), int(first), int(recent)
     if count < 1 or first < 0 or recent < 1 or first + recent > count:
         raise ValueError("first and recent pages must be among the count, with at least one recent page")
     if out is not None:
@@ -312,7 +313,7 @@ def select_pages(q, cache: KVCache, batch: Batch, bounds: PageBounds, count, fir
         if nbytes is None:
             nbytes = batch._workspace[key] = (_p.kv_select_pages_workspace(cache.ref, batch.ref) + 15) & ~15
     if out is None:      # (the scores are this call's own: one allocation for all)
-        out, at = Selection._new(rows, cache.kv_heads, int(count), nbytes, cache.device, stream)
+        out, at = Selection._new(rows, cache.kv_heads, count, nbytes, cache.device, stream)
     if workspace is not None or (nbytes and at is None):
         workspace, nbytes = _room(workspace, nbytes, cache.device, cache.index, stream)
         at = workspace.data_ptr()

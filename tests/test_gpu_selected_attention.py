@@ -183,6 +183,30 @@ def test_ties_zeros_and_pages_outside_the_cache():
             _check_choice(sel, want, cache, table, [1] * 3, count)
 
 
+def test_more_pages_than_lds_holds():
+    """Tables of over 8192 pages: keys in memory, several runs of the selection's rounds."""
+    log("many pages")
+    gen = torch.Generator().manual_seed(9)
+    n_pages, width = 300, 20000
+    cache = G._random_cache(gen, n_pages, 1, 16, 64, nan=False)
+    bounds = _all_bounds(cache)
+    table = torch.randint(0, n_pages, (2, width), generator=gen, dtype=torch.int32)
+    q = G._bf16(gen, 2, 3, 64).cuda()
+    lens = [width * 16 - 5, 16 * 8200]
+    batch = A.Batch(table.cuda(), _i32(lens))
+    # (each page stands in a table many times: its score is looked up)
+    codes, step = bounds.codes.cpu().numpy().astype(np.int64), bounds.step.cpu().numpy()
+    for count in (3, 2000, 8190, 19000):
+        sel = P.select_pages(q, cache, batch, bounds, count)
+        want = []
+        for r, n in enumerate(lens):
+            qi, units = OP.query_codes(q[r].double().cpu().numpy())
+            of = [OP.page_score(qi, units, codes[p, 0], step[p, 0]) for p in range(n_pages)]
+            seen = (n - 1) // 16 + 1
+            want.append((n - 1, [OP.choose([of[p] for p in table[r].tolist()], seen, count, 1, 1)]))
+        _check_choice(sel, want, cache, table, [1, 1], count)
+
+
 def test_lengths_that_make_no_sense():
     log("lengths")
     gen = torch.Generator().manual_seed(2)

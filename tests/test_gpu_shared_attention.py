@@ -157,6 +157,15 @@ def test_prefixes_that_make_no_sense():
                           ([0, 2, 1], [48, 48]), ([2 ** 31 - 1, -2 ** 31], [2 ** 31 - 1])):
         y = P.shared_attention(s.q, cache, batch, P.SharedPrefix(_i32(first), _i32(prefix)))
         assert (y.float() - want).abs().max() <= 2.0 ** -7 * want.abs().max(), (first, prefix)
+    # Offsets and lengths of rows: y is anything, and nothing else is touched.
+    for cu, lens in (([0, 5, 2, 3], [60, 70, 80]), ([3, 1, 0, 0], [60, 70, 80]), ([-7, 1, 2, 900], [60, 70, 80]),
+                     ([0, 1, 2, 3], [2 ** 31 - 1, -2 ** 31, 1 << 29]), ([2 ** 31 - 1, -1, 5, -2 ** 31], [1 << 30] * 3)):
+        around = torch.full((5, 2, 64), 6.0, dtype=torch.bfloat16, device="cuda")
+        odd = A.Batch(s.case.table.int(), _i32(lens), _i32(cu), rows=3)
+        for first in ([0, 3], [1, 3], [0, 1]):
+            P.shared_attention(s.q, cache, odd, P.SharedPrefix(_i32(first), _i32([48])), out=around[1:4])
+            torch.cuda.synchronize()
+            assert (around[0] == 6).all() and (around[4] == 6).all()
     none = P.SharedPrefix(_i32([0]), _i32([]))
     y = P.shared_attention(s.q, cache, batch, none)
     assert (y.float() - want).abs().max() <= 2.0 ** -7 * want.abs().max()
