@@ -11,6 +11,7 @@
 //
 // Bound by the bounds' bytes, 2 D + 4 of a page's page_size * 2 D, where there are many
 // rows; else by launches and the selection's passes over a row's scores.
+#include <type_traits>
 #include "attention_plan.h"
 #include "kv_attention_device.h"
 #include "paging_launch.h"
@@ -375,12 +376,15 @@ struct Scorer {
   }
 };
 
-// The page of table entry j, -1 where it is not among [first, end) or not in the cache.
-// (No branch around the load, nor a store to memory in a loop that has it: the compiler
-// would wait for all that may be on its way.)
-__device__ __forceinline__ int page_at(const SelectArgs& a, const int32_t* table, int j, int first, int end) {
-  const int p = table[min(max(j, first), end - 1)];
-  return j >= first && j < end && p < a.cache.num_pages ? p : -1;
+// Table entry j, of those in [first, end) (another's where it is not), and its page: -1 where it
+// is not among them or not in the cache.  (No branch around the load, nor a store to memory
+// in a loop that has it: the compiler would wait for all that may be on its way.)
+__device__ __forceinline__ int entry_at(const int32_t* table, int j, int first, int end) {
+  return table[min(max(j, first), end - 1)];
+}
+
+__device__ __forceinline__ int page_of(const SelectArgs& a, int entry, int j, int first, int end) {
+  return j >= first && j < end && entry < a.cache.num_pages ? entry : -1;
 }
 
 // The scores of one row and key head's pages j0 + 16 wave .. by rounds of 16 pages a wave
@@ -388,31 +392,36 @@ __device__ __forceinline__ int page_at(const SelectArgs& a, const int32_t* table
 template <int D, int kWaves, typename Put>
 __device__ __forceinline__ void score_pages(const SelectArgs& a, const QueryCodes<D>& q, int heads, int h, const int32_t* table, int first,
                                             int end, int j0, int j1, typename Scorer<D>::Turn* turns, Put put) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quarter = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = threadIdx.x & 15;
   Scorer<D> scorer;
   scorer.start(q, heads);
   int j = j0 + 16 * wave;
-  // Two rounds' bounds ahead (heads of 256: one, none in 16 waves; registers).  A round's pages are
-  // looked up before the bounds of the round in front of it are loaded: loads are waited for in order.
-  constexpr int kAhead = D == 256 ? (kWaves > 4 ? 0 : 1) : 2, kRound = 16 * kWaves;
-  typename Scorer<D>::Round p[kAhead + 1];
-  int pages[kAhead + 1];
+  // Two rounds' bounds ahead (heads of 256: one, none in 16 waves; registers).  A round's entries are
+  // loaded before the bounds of the round in front of it, and looked at a round later: loads are
+  // waited for in order.
+  constexpr int kAhead = D == 256 ? (kWaves > 4 ? 0 : 1) : 2, kRounds = kAhead + 1, kRound = 16 * kWaves;
+  typename Scorer<D>::Round p[kRounds];
+  int entry[kRounds];
 #pragma unroll
-  for (int x = 0; x <= kAhead; ++x) pages[x] = page_at(a, table, j + x * kRound + col, first, end);
+  for (int x = 0; x < kRounds; ++x) entry[x] = entry_at(table, j + x * kRound + col, first, end);
 #pragma unroll
-  for (int x = 0; x < kAhead; ++x) Scorer<D>::load(a, h, pages[x], p[x]);
-  int page = pages[kAhead];
-  while (j < j1) {
-    const int behind = page_at(a, table, j + (kAhead + 1) * kRound + col, first, end);
-    Scorer<D>::load(a, h, page, p[kAhead]);
-    page = behind;
-    const uint32_t key = scorer.key(p[0], turns[wave]);
+  for (int x = 0; x < kAhead; ++x) Scorer<D>::load(a, h, page_of(a, entry[x], j + x * kRound + col, first, end), p[x]);
+  int ahead = entry[kAhead];
+  const auto round = [&](auto at) __attribute__((always_inline)) {
+    constexpr int x = decltype(at)::value;
+    if (j >= j1) return false;
+    const int behind = entry_at(table, j + kRounds * kRound + col, first, end);
+    Scorer<D>::load(a, h, page_of(a, ahead, j + kAhead * kRound + col, first, end), p[(x + kAhead) % kRounds]);
+    const uint32_t key = scorer.key(p[x], turns[wave]);
     const int mine = j + Scorer<D>::of_lane();
     if (col < 4 && mine >= first && mine < end) put(mine, key);
-#pragma unroll
-    for (int x = 0; x < kAhead; ++x) p[x] = p[x + 1];
+    ahead = behind;
     j += kRound;
-  }
+    return true;
+  };
+  // A round by the name of its registers: copied, they would be waited for.
+  while (round(std::integral_constant<int, 0>{}) && (kRounds < 2 || round(std::integral_constant<int, 1 % kRounds>{})) &&
+         (kRounds < 3 || round(std::integral_constant<int, 2 % kRounds>{}))) {}
 }
 
 // ---------------------------------------------------------------- selection
@@ -672,9 +681,9 @@ int score_each(const SelectArgs& a) {
 
 // One launch or two: one where there is a row and key head for each compute unit, or
 // little for one to do.  In one and in two (us; rows x key heads, largest table):
-//   8, 126   8.0  9.2     26, 627 (heads of 256)   14.8 11.1     32, 1001   13.5 11.5
-//   8, 2049 18.4 11.5     64, 2001 (64)            15.5 14.8     128, 1876  19.5 18.2
-//   256, 2049 24.1 26.5   504, 501                 21.0 22.4     496, 126   16.4 15.5
+//   8, 126   7.8  9.2     26, 627 (heads of 256)   14.6 10.8     32, 1001   12.7 11.3
+//   8, 2049 16.9 11.2     64, 2001 (64)            13.8 14.4     128, 1876  18.2 17.5
+//   256, 2049 22.9 25.9   504, 501                 20.2 22.2     496, 126   16.0 15.2
 bool choose_at_once(const SelectArgs& a) {
   return a.max_pages <= 256 || (a.max_pages <= kHeldKeys && (int64_t)a.batch.rows * a.cache.heads >= 256);
 }
