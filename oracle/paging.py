@@ -1,5 +1,5 @@
 """Serving over the paged 8-bit cache: the tables of a step from the requests'
-lengths.
+lengths, and the choice of pages by a score of their keys' bounds.
 
 TEST INFRASTRUCTURE ONLY (see the package docstring).  Plain Python and numpy.
 

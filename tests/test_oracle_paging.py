@@ -101,3 +101,22 @@ def test_choice():
     assert OP.choose(s, 8, 5, 1, 2) == [0, 2, 4, 6, 7]
     assert OP.choose(s, 8, 3, 2, 1) == [0, 1, 7] and OP.choose(s, 8, 7, 0, 1) == [0, 1, 2, 3, 4, 5, 7]
     assert OP.choose([-1.0, -3.0, -2.0, 0.0], 4, 3, 0, 1) == [0, 2, 3] and OP.choose(s, 0, 3, 1, 1) == []
+
+
+def test_a_full_row_and_those_behind_one_that_is_not_served():
+    p = _fresh(1, 2, 4)
+    assert list(p.step([32], [0], [0], 32)[0]) == [0, 32] and p.count == 2      # all that its row of pages holds
+    p = _fresh(3, 4, 3)
+    assert list(p.step([16, 48, 1], [0] * 3, [0] * 3, 100)[0]) == [0, 16, 16, 16]      # the last one would have fitted
+    assert p.kv_len == [16, 0, 0] and p.count == 2
+
+
+def test_bounds_of_negative_keys_and_a_choice_of_few():
+    codes, step = OP.page_bounds(np.array([[-4.0, 1.0], [-2.0, 2.0]]), 0.5)
+    assert codes.tolist() == [[round(-2 * 127 / 4), round(2 * 127 / 4)], [-127, round(127 / 4)]]
+    assert step == np.float32(2) / np.float32(127)
+    # Two query heads: the larger product counts, whichever comes first.
+    i, units = np.array([[127, 0], [0, 127]]), np.array([1.0, 1.0], dtype=np.float32)
+    bounds = np.array([[10, 30], [10, 30]])
+    assert OP.page_score(i, units, bounds, 1.0) == OP.page_score(i[::-1], units, bounds, 1.0) == 30 * 127
+    assert OP.choose([1.0, 2.0], 2, 3, 2, 1) == [0, 1]
