@@ -10,7 +10,7 @@ namespace nvfp4 {
 
 // Registers: the waves of a SIMD that a kernel of these forms is compiled for.
 constexpr int rows_waves(int dim, int tiles, int waves, bool split) {
-  return waves > 4 ? 2 : dim == 256 && split ? 1 : dim == 256 ? 3 - tiles : 4 - tiles;
+  return waves > 4 ? 2 : dim == 256 && split ? 1 : dim == 256 ? 3 - tiles : tiles > 1 ? 2 : 3;
 }
 
 // Keys and values of one tile of 32 tokens, as loaded: [group of 16][64

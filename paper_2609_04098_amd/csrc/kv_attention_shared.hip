@@ -13,8 +13,8 @@
 
 namespace nvfp4 {
 
-// The rows of a workgroup in either pass, 16 times kPrefix and kOwn: 8 is the form of
-// 128 rows (kv_attention_wide.h).
+// The rows of a workgroup in either pass, 16 times kPrefix and kOwn: 8, for heads of 256, is
+// the form of 128 rows (kv_attention_wide.h).
 template <int D, int kForm>
 struct PassLds {
   RowsLds<D, kForm, 4> of;
@@ -25,7 +25,7 @@ struct PassLds<D, 8> {
   TileLds<D> of;
 };
 
-constexpr int pass_waves(int dim, int form) { return form == 8 ? (dim == 256 ? 2 : 3) : rows_waves(dim, form, 4, false); }
+constexpr int pass_waves(int dim, int form) { return form == 8 ? 2 : rows_waves(dim, form, 4, false); }
 constexpr int fewer(int a, int b) { return a < b ? a : b; }
 
 template <int D, int kForm, typename Args>
@@ -69,13 +69,15 @@ __global__ __launch_bounds__(256, fewer(pass_waves(D, kPrefix), pass_waves(D, kO
   }
 }
 
-// A wave takes a query head of a row, kAhead pieces' loads in flight: those of its
-// group's prefix, then its own.
-template <int D>
+// kShare waves take a query head of a row, each its share of the pieces, kAhead of their loads in
+// flight: those of the group's prefix, then its own.
+template <int D, int kShare>
 __global__ __launch_bounds__(256) void kv_attention_shared_join_kernel(SharedArgs a, PrefixPieces of) {
   constexpr int kEach = D / 64, kAhead = 8;
-  const int lane = threadIdx.x & 63;
-  const unsigned item = blockIdx.x * 4 + (threadIdx.x >> 6);
+  __shared__ float sums[kShare > 1 ? 4 : 1][kShare > 1 ? D : 1];
+  __shared__ float2 totals[4];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = wave % kShare;
+  const unsigned item = blockIdx.x * (4 / kShare) + wave / kShare;
   const int token_row = __builtin_amdgcn_readfirstlane(item / a.q_heads), head = __builtin_amdgcn_readfirstlane(item % a.q_heads);
   if (token_row >= a.batch.rows) return;
   Tile t;
@@ -88,27 +90,28 @@ __global__ __launch_bounds__(256) void kv_attention_shared_join_kernel(SharedArg
   const float* part[2];
   int stride[2];
   // A row of a tile, of `rows`: its first piece, of `splits` of that many tiles' heads.
-  const auto of_tile = [&](int which, const float* parts, int64_t tile, int64_t tiles, int row, int shift, int splits) {
-    const int64_t first = (((tile * a.cache.heads + h) * splits) << shift) + row;
+  const auto of_tile = [&](int which, const float* parts, int64_t tile, int64_t tiles, int row, int rows, int splits) {
+    const int64_t first = (tile * a.cache.heads + h) * splits * rows + row;
     stats[which] = reinterpret_cast<const float2*>(parts) + first;
-    part[which] = parts + 2 * ((tiles * a.cache.heads * splits) << shift) + first * D + lane * kEach;
-    stride[which] = 1 << shift;
+    part[which] = parts + 2 * (tiles * a.cache.heads * splits * rows) + first * D + lane * kEach;
+    stride[which] = rows;
   };
   const int row0 = prefix > 0 ? start_row(a.batch, group_seq) : 0;
   // (Offsets that make no sense may put a group's first row behind this one.)
   const int before = prefix > 0 && row0 <= s.row ? min((prefix - 1) / of.chunk, of.splits - 1) + 1 : 0;
   stats[0] = nullptr, part[0] = nullptr, stride[0] = 0;
   if (before > 0) {
-    const int shift = 4 + __builtin_ctz(of.tiles);
-    const int packed = (s.row - row0) * a.group + r;
-    of_tile(0, of.part, (((int64_t)row0 * a.group) >> shift) + g + (packed >> shift),
-            prefix_tile_numbers((int64_t)a.batch.rows * a.group, 1 << shift, a.groups), packed & ((1 << shift) - 1), shift, of.splits);
+    const int rows = 16 * of.tiles, shift = 4 + __builtin_ctz(of.tiles);
+    const auto tiles_in = [&](uint32_t x) { return of.tiles == 3 ? x / 48u : x >> shift; };
+    const uint32_t packed = (uint32_t)(s.row - row0) * a.group + r, tile = tiles_in(packed);
+    of_tile(0, of.part, (int64_t)tiles_in((uint32_t)row0 * a.group) + g + tile,
+            prefix_tile_numbers((int64_t)a.batch.rows * a.group, rows, a.groups), (int)(packed - tile * rows), rows, of.splits);
   }
   int own;
   {
     const int shift = 4 + __builtin_ctz(a.row_tiles), rows = 1 << shift, row = r & (rows - 1);
     const int tile = a.batch.cu_rows == nullptr ? t.b * ((a.group + rows - 1) >> shift) : (int)(((int64_t)s.row * a.group) >> shift) + t.b;
-    of_tile(1, a.part, tile + (r >> shift), tiles_of(a.batch, a.group, rows), row, shift, a.splits);
+    of_tile(1, a.part, tile + (r >> shift), tiles_of(a.batch, a.group, rows), row, rows, a.splits);
     // The tokens of the row's tile, as find_tile() has them.
     const int last = min(s.rows * a.group, r - row + rows) - 1;
     t.end = a.causal ? min(s.len, s.first + last / a.group + 1) : s.len;
@@ -119,7 +122,7 @@ __global__ __launch_bounds__(256) void kv_attention_shared_join_kernel(SharedArg
   float m = kNone, l = 0.0f, y[kEach];
 #pragma unroll
   for (int i = 0; i < kEach; ++i) y[i] = 0.0f;
-  for (int p = 0; p < before + own; p += kAhead) {
+  for (int p = share * kAhead; p < before + own; p += kShare * kAhead) {
     float2 st[kAhead];
     float v[kAhead][kEach];
 #pragma unroll
@@ -152,6 +155,25 @@ __global__ __launch_bounds__(256) void kv_attention_shared_join_kernel(SharedArg
       for (int i = 0; i < kEach; ++i) y[i] = fmaf(v[u][i], w, y[i]);
     }
   }
+  if (kShare > 1) {      // (the workgroup has one row and head: all of its waves are here)
+    if (lane == 0) totals[wave] = make_float2(m, l);
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) sums[kShare > 1 ? wave : 0][kShare > 1 ? lane * kEach + i : 0] = y[i];
+    __syncthreads();
+    if (wave != 0) return;
+    const float top = fmaxf(fmaxf(totals[0].x, totals[1].x), fmaxf(totals[2].x, totals[3].x)), base = top == kNone ? 0.0f : top;
+    m = top;
+    l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) y[i] = 0.0f;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float w = __builtin_amdgcn_exp2f(totals[u].x - base);
+      l = fmaf(totals[u].y, w, l);
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) y[i] = fmaf(sums[kShare > 1 ? u : 0][kShare > 1 ? lane * kEach + i : 0], w, y[i]);
+    }
+  }
   uint16_t* to = a.y + (int64_t)token_row * a.ldy + (int64_t)head * D;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   if (D == 64)
@@ -173,9 +195,12 @@ hipError_t launch_passes(const SharedArgs& a, const PrefixPieces& of, const Shar
 }
 
 template <int D>
-hipError_t launch_join(const SharedArgs& a, const PrefixPieces& of, hipStream_t stream) {
+hipError_t launch_join(const SharedArgs& a, const PrefixPieces& of, int join_share, hipStream_t stream) {
   const int64_t items = (int64_t)a.batch.rows * a.q_heads;
-  kv_attention_shared_join_kernel<D><<<dim3((unsigned)((items + 3) / 4)), 256, 0, stream>>>(a, of);
+  if (join_share == 4)
+    kv_attention_shared_join_kernel<D, 4><<<dim3((unsigned)items), 256, 0, stream>>>(a, of);
+  else
+    kv_attention_shared_join_kernel<D, 1><<<dim3((unsigned)((items + 3) / 4)), 256, 0, stream>>>(a, of);
   return hipGetLastError();
 }
 
@@ -186,19 +211,14 @@ hipError_t launch(const SharedArgs& a, const SharedPlan& p, hipStream_t stream) 
   const unsigned workgroups = (unsigned)shared_workgroups(w);
   SharedArgs own = a;
   own.part = a.part + p.prefix_bytes / sizeof(float);
-  hipError_t e;
-  const int forms = 10 * p.prefix.tiles + p.own.tiles;
-  if (forms == 11) e = launch_passes<D, 1, 1>(own, of, w, workgroups, stream);
-  else if constexpr (D == 256) {
-    e = forms == 88 ? launch_passes<D, 8, 8>(own, of, w, workgroups, stream) : hipErrorInvalidValue;      // (by the plan, never)
-  } else {
-    e = forms == 21   ? launch_passes<D, 2, 1>(own, of, w, workgroups, stream)
-        : forms == 81 ? launch_passes<D, 8, 1>(own, of, w, workgroups, stream)
-        : forms == 22 ? launch_passes<D, 2, 2>(own, of, w, workgroups, stream)
-        : forms == 82 ? launch_passes<D, 8, 2>(own, of, w, workgroups, stream)
-                      : hipErrorInvalidValue;
+  constexpr int kMore = D == 64 ? 2 : D == 128 ? 3 : 8, kMoreOwn = D == 256 ? 8 : 2;
+  hipError_t e = hipErrorInvalidValue;      // (by the plan, never)
+  if (p.own.tiles == kMoreOwn && p.prefix.tiles == kMore) e = launch_passes<D, kMore, kMoreOwn>(own, of, w, workgroups, stream);
+  if (p.own.tiles == 1 && p.prefix.tiles == 1) e = launch_passes<D, 1, 1>(own, of, w, workgroups, stream);
+  if constexpr (D < 256) {
+    if (p.own.tiles == 1 && p.prefix.tiles == kMore) e = launch_passes<D, kMore, 1>(own, of, w, workgroups, stream);
   }
-  return e != hipSuccess ? e : launch_join<D>(own, of, stream);
+  return e != hipSuccess ? e : launch_join<D>(own, of, p.join_share, stream);
 }
 
 }  // namespace

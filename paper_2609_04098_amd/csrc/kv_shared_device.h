@@ -54,7 +54,7 @@ __device__ __forceinline__ int shared_prefix(const SharedArgs& a, int b, int fir
 // The number of the first of group g's tiles of kRows packed rows.
 template <int kRows>
 __device__ __forceinline__ int first_prefix_tile(const SharedArgs& a, int row, int g) {
-  return (int)((int64_t)row * a.group / kRows) + g;
+  return (int)((uint32_t)row * (uint32_t)a.group / kRows) + g;      // (below 2^31 packed rows)
 }
 
 // A tile of a group's rows over its prefix.

@@ -71,14 +71,16 @@ SelectedArgs selected_args(const nvfp4_kv_cache* cache, int64_t rows, int64_t q_
   return a;
 }
 
-#define NVFP4_SHARED(D)                                                                                         \
-  {"kv_attention_shared_kernel<" #D ",1,1>", "kv_attention_shared_kernel<" #D ",2,1>",                          \
-   "kv_attention_shared_kernel<" #D ",8,1>", "kv_attention_shared_kernel<" #D ",2,2>",                          \
-   "kv_attention_shared_kernel<" #D ",8,2>", "kv_attention_shared_kernel<" #D ",8,8>"}
-constexpr const char* kSharedKernels[3][6] = {NVFP4_SHARED(64), NVFP4_SHARED(128), NVFP4_SHARED(256)};
-#undef NVFP4_SHARED
-constexpr const char* kSharedJoins[3] = {"kv_attention_shared_join_kernel<64>", "kv_attention_shared_join_kernel<128>",
-                                         "kv_attention_shared_join_kernel<256>"};
+// (By the rows of a prefix's and of a sequence's own workgroups: 16 both, more of the
+// prefix's, more of both.)
+constexpr const char* kSharedKernels[3][3] = {
+    {"kv_attention_shared_kernel<64,1,1>", "kv_attention_shared_kernel<64,2,1>", "kv_attention_shared_kernel<64,2,2>"},
+    {"kv_attention_shared_kernel<128,1,1>", "kv_attention_shared_kernel<128,3,1>", "kv_attention_shared_kernel<128,3,2>"},
+    {"kv_attention_shared_kernel<256,1,1>", nullptr, "kv_attention_shared_kernel<256,8,8>"}};
+constexpr const char* kSharedJoins[3][2] = {
+    {"kv_attention_shared_join_kernel<64,1>", "kv_attention_shared_join_kernel<64,4>"},
+    {"kv_attention_shared_join_kernel<128,1>", "kv_attention_shared_join_kernel<128,4>"},
+    {"kv_attention_shared_join_kernel<256,1>", "kv_attention_shared_join_kernel<256,4>"}};
 
 }  // namespace
 
@@ -181,9 +183,8 @@ const char* nvfp4_kv_attention_shared_kernel(const nvfp4_kv_cache* cache, const 
   if (!shared_fits(a, p)) return nullptr;
   if (p.apart) return nvfp4_kv_attention_kernel(cache, batch, q_heads, 0, part);
   const int dim = a.cache.dim == 64 ? 0 : a.cache.dim == 128 ? 1 : 2;
-  if (part == 1) return kSharedJoins[dim];
-  const int forms = 10 * p.prefix.tiles + p.own.tiles;
-  return kSharedKernels[dim][forms == 11 ? 0 : forms == 21 ? 1 : forms == 81 ? 2 : forms == 22 ? 3 : forms == 82 ? 4 : 5];
+  if (part == 1) return kSharedJoins[dim][p.join_share == 4 ? 1 : 0];
+  return kSharedKernels[dim][p.prefix.tiles == 1 ? 0 : p.own.tiles == 1 ? 1 : 2];
 }
 
 int nvfp4_kv_page_bounds(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_kv_bounds* bounds,

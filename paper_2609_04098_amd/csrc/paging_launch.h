@@ -51,6 +51,7 @@ struct SharedPlan {
   bool apart;
   AttentionPlan whole, prefix, own;
   size_t prefix_bytes, bytes;
+  int join_share;              // waves that join a row's query head
 };
 
 // Numbers of a group pass's tiles of `rows` packed rows, for n packed rows in all: group g's
@@ -71,46 +72,63 @@ inline size_t all_part_bytes(const KvCacheArgs& c, int64_t tiles, const Attentio
 // form, us; sequences x new rows, prefix, own tokens up to, query / key heads of dim):
 //   4 x 1, 608, 90, 40 / 8 of 128       8.2  9.9     150 x 1, 512, 100, 40 / 8 of 128    21.1 25.8
 //   100 x 1, 1024, 200, 64 / 8 of 64   17.9 21.6     8 x 1, 2048, 300, 32 / 8 of 128     14.0 11.1
-//   60 x 1 (3 groups), 2000, 24 / 4    18.8 17.2     2 x 1, 30000, 500, 40 / 8 of 128    21.9 20.9
+//   60 x 1 (3 groups), 2000, 24 / 4    18.8 17.2     2 x 1, 30000, 500, 40 / 8 of 128    22.6 19.5
 //   16 x 1, 8192, 200, 40 / 8          37.1 17.8     32 x 4, 4096, 500, 32 / 8           43.9 29.7
-//   150 x 1, 4160, 777, 24 / 4 of 256  99.0 49.0     64 x 1, 32768, 1000, 40 / 8          377 76.0
+//   150 x 1, 4160, 777, 24 / 4 of 256  99.0 49.0     64 x 1, 32768, 1000, 40 / 8          377 76.4
 //   64 x 8 (2 groups), 4000, 64 / 8    94.9  112
 // Pages that sequences share are in the caches after the first one has read them, so what
 // sharing saves is not memory's but the caches' reads; it costs partial results and a join.
 // So it begins at prefixes of 1536 tokens, and not where a sequence's own rows fill 64.
-// Rows of the prefix's workgroups: by the rows of a group,
-//   320 of 128: 85 us with 16, 76 with 32, 79 with 128    512 (4096 tokens): 30.0 29.7 32.9
-//   1024: 126 112 105     2048: 133 128 112     2048 of 64: 97 85 84
-//   900 of 256: 49 (16), 54 (128)     512 of 256 (30000 tokens): 59 (16), 65 (128)
-// Pieces: the number of them for which an estimate is least, in the time of a token for a
-// workgroup that has its compute unit to itself (3.7 ns for 32 rows of 128): 1400 for its
-// beginning and end; two of them on a unit take 1.5 times as long (1.8 with heads of 256), a
-// few units with two or three, where there is not one for every half, twice; and a piece's partial
-// results, written and read, at 4 TB/s, with a wave's eighth of a load's latency.  (20 users, 64 / 4 heads, a prefix of 30000: 49 us in six
-// pieces, 43 in twelve, 48 in 24; two groups of 20 with 64 / 8 heads, 16000: 69 in two, 43 in
-// six; 900 rows of 256: 49 in one of 4160, 56 in two; 32 x 4: 30 in two, 33 in four.)
-// Tiles of 128 rows: three to a unit (1024 rows, 16000 tokens: 131 us in four, 92 in twelve).
-inline AttentionPlan shared_pieces(int tokens, int64_t work, int64_t packed_rows, int dim, bool wide, int least) {
+// Rows of a prefix's workgroups, and pieces of either pass: those for which an estimate is
+// least, of what hangs on them.  m workgroups of a compute unit side by side take
+// `alone` + m `each` for a token of their piece and `start` for their beginning and end; those
+// that a unit has no room for come behind them; and partial results are written and read at
+// 2.6 TB/s.  Fitted to 210 measured steps (1 to 4 groups of 36 to 900 rows, prefixes of 2000 to
+// 32000 tokens, 1 to 8 key heads, each in 1 to 48 pieces): what it takes is slower than
+// the fastest by 3% (heads of 64), 4% (128) and 2% (256) on the average, by 8, 10 and 9% in one of ten.
+//   us of the fastest with 16, 32, 48 and 128 rows; groups x rows, prefix, key heads of 128:
+//   1 x 160, 2000, 2    11.8  14.3  16.3        1 x 320, 32768, 8   78.5  77.7  72.4  92.3
+//   4 x 256, 32000, 4    116   112   103   120  1 x 696, 32000, 8    158   140   125   136
+//   2 x 320, 4000, 4    24.9  25.2  25.7  31.1  4 x 510, 8000, 8     183   173   159   141
+//   of 64: 2 x 696, 32000, 4   94.7  80.7  77.1  98.3     2 x 512, 8000, 4   35.2  31.9  32.6  36.7
+// (48 rows of 128 fill the registers that two waves of a SIMD have; of 64 they gain nothing
+// on 32, and 32 of 128 less than 2% on the better of 16 and 48.  128 rows, through LDS, gain 2 to 12%
+// only at a thousand rows and more.  Heads of 256, 900 rows: 49 with 16, 54 with 128, 69 with 32.)
+struct Pace {
+  double alone, each, start;            // us
+  int slots;                            // workgroups that a unit has room for
+};
+
+inline Pace pace_of(int dim, int form) {
+  if (dim == 64) return form == 1 ? Pace{1.3e-3, 1.8e-3, 0.3, 4} : Pace{2.1e-3, 2.5e-3, 0.5, 4};
+  if (dim == 256) return {1.5e-3, 3.5e-3, 0.0, 2};
+  return form == 1 ? Pace{1.8e-3, 1.3e-3, 0.3, 4} : form == 2 ? Pace{2.8e-3, 1.4e-3, 0.6, 2} : Pace{4.0e-3, 1.45e-3, 1.0, 2};
+}
+
+// The pieces of `tokens` for `work` tiles of a form (16 rows times it), at least `least` tokens
+// each, and the estimate.  Tiles of 128 rows: three to a unit.
+inline AttentionPlan shared_pieces(int tokens, int64_t work, int64_t packed_rows, int dim, int form, int least, double* time) {
   AttentionPlan q = {};
-  const auto chunk_of = [&](int64_t n) {
-    const int c = (int)(((tokens + n - 1) / n + 127) / 128 * 128);
+  const auto chunk_of = [&](int n) {
+    const int c = (tokens / n + (tokens % n != 0) + 127) / 128 * 128;
     return c < least ? least : c;
   };
-  int64_t best = 1;
-  if (wide) {
-    best = work < 256 ? 256 / work : 1;
-    if (tokens / best > 1000) best = work < 768 ? 768 / work : 1;
+  int best = 1;
+  if (form == 8) {
+    if (work < 256) best = (int)(256 / work);
+    if (tokens / best > 1000) best = work < 768 ? (int)(768 / work) : 1;
   } else {
-    const double both = dim == 256 ? 1.8 : 1.5, part = 25.0 + (double)packed_rows * (dim + 2) * 8.0 / 4e6 / 3.7e-3;
-    double least_time = 0.0;
-    for (int64_t n = 1; n <= 128 && (n == 1 || tokens / n >= least); ++n) {
-      const int64_t all = work * n;
-      const double each = (double)chunk_of(n);
-      const double time = (all <= 256 ? each + 1400.0 : all < 448 ? 2.0 * each + 1400.0
-                                                                  : (double)((all + 511) / 512) * (both * each + 1400.0)) + n * part;
-      if (n == 1 || time < least_time) least_time = time, best = n;
+    const Pace p = pace_of(dim, form);
+    const double part = (double)packed_rows * (dim + 2) * 8.0 / 2.6e6;
+    for (int n = 1; n <= 128 && (n == 1 || (tokens / n >= least && work * n <= 3072)); ++n) {
+      const double chunk = chunk_of(n);
+      const int64_t m = (work * n + 255) / 256, full = m / p.slots, rest = m % p.slots;
+      const auto side_by_side = [&](int64_t w) { return chunk * (p.alone + w * p.each) + p.start; };
+      const double t = full * side_by_side(p.slots) + (rest > 0 ? side_by_side(rest) : 0.0) + n * part;
+      if (n == 1 || t < *time) *time = t, best = n;
     }
   }
+  q.tiles = form;
   q.chunk = chunk_of(best);
   q.splits = tokens > 0 ? (tokens + q.chunk - 1) / q.chunk : 1;
   q.waves = 4;
@@ -120,24 +138,35 @@ inline AttentionPlan shared_pieces(int tokens, int64_t work, int64_t packed_rows
 inline SharedPlan shared_plan(const SharedArgs& a) {
   SharedPlan p = {};
   const int64_t rows = (int64_t)a.batch.rows * a.group;
-  const int64_t of_seq = (rows + a.batch.seqs - 1) / a.batch.seqs, of_group = a.groups > 0 ? (rows + a.groups - 1) / a.groups : 0;
+  const int64_t of_seq = (rows + a.batch.seqs - 1) / a.batch.seqs;
   p.apart = a.groups == 0 || a.max_prefix < 1536 || of_seq >= 64;
   if (p.apart) {
     p.whole = attention_plan(a.cache, a.batch, a.group, 0, kAnyRoom);
     p.bytes = part_bytes(a.cache, a.batch, a.group, p.whole);
     return p;
   }
-  const int own_form = of_seq <= 16 ? 1 : a.cache.dim == 256 ? 8 : 2;
-  int form = a.cache.dim == 256 || of_group < 256 ? 1 : of_group < 768 ? 2 : 8;
-  if (form < own_form) form = own_form;
-  const int64_t all_rows = rows * a.cache.heads;
-  p.prefix = shared_pieces(a.max_prefix, prefix_tiles(a, form) * a.cache.heads, all_rows, a.cache.dim, form == 8, 128);
-  p.prefix.tiles = form;
-  p.prefix_bytes = all_part_bytes(a.cache, prefix_tiles(a, form), p.prefix);
+  const int dim = a.cache.dim, own_form = of_seq <= 16 ? 1 : dim == 256 ? 8 : 2;
+  const int64_t all_rows = rows * a.cache.heads, of_group = (rows + a.groups - 1) / a.groups;
+  double time = 0.0;
+  const auto prefix = [&](int form, double* t) {      // (as if the groups were of one size)
+    return shared_pieces(a.max_prefix, a.groups * ((of_group + 16 * form - 1) / (16 * form)) * a.cache.heads, all_rows, dim, form, 128, t);
+  };
+  const int more = dim == 64 ? 2 : dim == 128 ? 3 : 8;      // the form of more rows
+  if (own_form > 1) {
+    p.prefix = prefix(more, &time);
+  } else {
+    p.prefix = prefix(1, &time);
+    double other = 0.0;
+    const AttentionPlan q = dim < 256 ? prefix(more, &other) : p.prefix;
+    if (dim < 256 && other < time) p.prefix = q;
+  }
+  p.prefix_bytes = all_part_bytes(a.cache, prefix_tiles(a, p.prefix.tiles), p.prefix);
   const int64_t own_tiles = host_tiles(a.batch, a.group, 16 * own_form);
-  p.own = shared_pieces(a.max_own, own_tiles * a.cache.heads, all_rows, a.cache.dim, own_form == 8, 256);
-  p.own.tiles = own_form;
+  p.own = shared_pieces(a.max_own, own_tiles * a.cache.heads, all_rows, dim, own_form, 256, &time);
   p.bytes = p.prefix_bytes + all_part_bytes(a.cache, own_tiles, p.own);
+  // Few rows of many pieces by four waves (by one and by four, us; rows x query heads, pieces of the prefix:
+  // 16, 128 31.1 19.9;  80, 32 21.6 19.0;  640, 24 34.5 33.5;  720, 5 29.7 35.6;  2048, 6 29.5 32.8).
+  p.join_share = (int64_t)a.batch.rows * a.q_heads <= 1024 && p.prefix.splits + p.own.splits > 8 ? 4 : 1;
   return p;
 }
 

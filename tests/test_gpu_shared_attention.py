@@ -54,31 +54,34 @@ class Step:
         return y
 
 
-SHARED = "kv_attention_shared_kernel<%d,%s>"
+SHARED, JOIN = "kv_attention_shared_kernel<%d,%s>", "kv_attention_shared_join_kernel<%d,%d>"
 
-# dim, page, key heads, group, groups, own tokens, new rows, row offsets or not, the kernel's rows.  (The host is told of
-# prefixes that are worth sharing.)
+# dim, page, key heads, group, groups, own tokens, new rows, row offsets or not, the kernel's rows and the
+# waves that join one.  (The host is told of prefixes that are worth sharing.)
 STEPS = [
     # one group, single tokens, without row offsets
-    *[(d, p, 2, 3, [(4, 96)], [1, 5, 40, 100], [1] * 4, False, "1,1") for d, p in ((64, 16), (128, 32), (256, 64))],
-    (128, 128, 1, 1, [(2, 128)], [1, 1], [1, 1], False, "1,1"),
-    # many sequences: 32 and 128 packed rows a tile, pieces of the prefix
-    *[(d, 32, 2, 5, [(40, 2016)], [3 + 7 * i for i in range(40)], [1] * 40, False, "1,1") for d in (64, 128, 256)],
-    *[(d, 16, 2, 8, [(50, 512)], [30] * 50, [1] * 50, False, "2,1" if d < 256 else "1,1") for d in (64, 128, 256)],
-    *[(d, 32, 8, 8, [(100, 1504)], [9 + i for i in range(100)], [1] * 100, False, "8,1" if d < 256 else "1,1")
+    *[(d, p, 2, 3, [(4, 96)], [1, 5, 40, 100], [1] * 4, False, ("1,1", 4)) for d, p in ((64, 16), (128, 32), (256, 64))],
+    (128, 128, 1, 1, [(2, 128)], [1, 1], [1, 1], False, ("1,1", 4)),
+    # many sequences: 32 and 48 packed rows a tile, pieces of the prefix
+    *[(d, 32, 2, 5, [(40, 2016)], [3 + 7 * i for i in range(40)], [1] * 40, False, ("1,1", 4)) for d in (64, 128, 256)],
+    *[(d, 16, 2, 8, [(50, 512)], [30] * 50, [1] * 50, False, ("1,1", 1)) for d in (64, 128, 256)],
+    *[(d, 32, 8, 8, [(100, 1504)], [9 + i for i in range(100)], [1] * 100, False, ("2,1" if d == 64 else "1,1", 1))
       for d in (64, 128, 256)],
-    (128, 64, 1, 4, [(5, 9024)], [300, 1, 64, 2, 700], [1] * 5, False, "1,1"),
+    (128, 16, 16, 8, [(45, 6000)], [5 + i for i in range(45)], [1] * 45, False, ("3,1", 1)),
+    (128, 16, 16, 16, [(30, 3008), (1, 64), (43, 3200)], [9 + i for i in range(76)], [1] * 76, True, ("3,1", 1)),
+    (128, 64, 1, 4, [(5, 9024)], [300, 1, 64, 2, 700], [1] * 5, False, ("1,1", 4)),
     # several groups of all kinds, one without a prefix, sequences of none, some without rows
     (64, 16, 2, 3, [(3, 160), (1, 32), (4, 0), (2, 1600)], [9, 20, 1, 5, 8, 3, 1, 2, 70, 4, 33, 500], [2, 1, 1, 3, 1, 0, 1, 2, 5, 4, 7, 9],
-     True, "1,1"),
-    (128, 32, 3, 7, [(2, 64), (0, 96), (3, 640)], [3, 40, 12, 5, 64, 800, 1], [3, 1, 0, 5, 2, 6, 1], True, "2,2"),
-    (64, 32, 3, 7, [(2, 64), (0, 96), (3, 640)], [3, 40, 12, 5, 64, 800, 1], [3, 1, 0, 5, 2, 6, 1], True, "2,2"),
-    (256, 16, 1, 16, [(2, 320), (2, 16)], [10, 20, 11, 2], [4, 3, 5, 2], True, "8,8"),
+     True, ("1,1", 1)),
+    (128, 32, 3, 7, [(2, 64), (0, 96), (3, 640)], [3, 40, 12, 5, 64, 800, 1], [3, 1, 0, 5, 2, 6, 1], True, ("3,2", 4)),
+    (64, 32, 3, 7, [(2, 64), (0, 96), (3, 640)], [3, 40, 12, 5, 64, 800, 1], [3, 1, 0, 5, 2, 6, 1], True, ("2,2", 4)),
+    (256, 16, 1, 16, [(2, 320), (2, 16)], [10, 20, 11, 2], [4, 3, 5, 2], True, ("8,8", 4)),
     # drafts of many sequences, several rows each behind a common prefix
-    *[(d, 32, 4, 4, [(30, 992)], [12 + 5 * i for i in range(30)], [8 + i % 3 for i in range(30)], True, "8,2" if d < 256 else "8,8")
+    *[(d, 32, 4, 4, [(30, 992)], [12 + 5 * i for i in range(30)], [8 + i % 3 for i in range(30)], True,
+       ({64: "2,2", 128: "3,2", 256: "8,8"}[d], 1))
       for d in (64, 128, 256)],
     # a prefix that ends inside a page that the sequences share, and inside a tile
-    (128, 32, 2, 4, [(3, 75)], [1, 1, 1], [1] * 3, False, "1,1"),
+    (128, 32, 2, 4, [(3, 75)], [1, 1, 1], [1] * 3, False, ("1,1", 4)),
     # rows of a sequence that fill tiles of their own: computed apart
     (128, 32, 4, 4, [(3, 992)], [500, 320, 77], [500, 320, 70], True, None), (256, 32, 8, 8, [(2, 480)], [90, 80], [70, 66], True, None),
 ]
@@ -96,7 +99,7 @@ def test_shared_attention(step):
     tight = dict(max_len=max(1536, max(p for _, p in groups)), max_own=max(own))
     names = P.shared_attention_kernels(s.heads, s.case.cache(), s.batch(max_len=max(s.lens)), s.shared(**tight))
     if form is not None:
-        assert names == [SHARED % (dim, form), "kv_attention_shared_join_kernel<%d>" % dim]
+        assert names == [SHARED % (dim, form[0]), JOIN % (dim, form[1])]
     else:
         assert not any("shared" in n for n in names)
     s.check(hints=tight, max_len=max(s.lens), pages=True)
@@ -107,8 +110,9 @@ def test_shared_attention(step):
 
 
 def test_every_form_has_a_step():
-    got = {(s[0], s[8]) for s in STEPS if s[8]}
-    assert got == {(d, f) for d in (64, 128) for f in ("1,1", "2,1", "8,1", "2,2", "8,2")} | {(256, "1,1"), (256, "8,8")}
+    got = {(s[0], s[8][0]) for s in STEPS if s[8]}
+    assert {(s[0], s[8][1]) for s in STEPS if s[8]} == {(d, j) for d in (64, 128, 256) for j in (1, 4)}
+    assert got == {(64, "1,1"), (64, "2,1"), (64, "2,2"), (128, "1,1"), (128, "3,1"), (128, "3,2"), (256, "1,1"), (256, "8,8")}
 
 
 @pytest.mark.parametrize("dim", [64, 128, 256])
