@@ -6,6 +6,12 @@
 // each sequence's rows over its own tokens.  Both keep (maximum, sum, unscaled y) of every row in
 // 32 bits, and the join takes them together as it does the pieces of one sequence:
 //   m = max m_i,  y = sum_i 2^(m_i - m) y_i / sum_i 2^(m_i - m) l_i.
+//
+// Bound by the conversions and exponentials beside the products, and by what waits between
+// them with two waves a SIMD: 64 rows of 40 / 8 heads of 128 behind 32768 tokens take 76.6 us
+// (0.56 PFLOP/s; vector units busy 54%, matrix units 25%; 16 rows a workgroup 78.5, 32 77.7, as the
+// codes of 32 tokens are converted for more of them at once), the join 7.5, a launch and four
+// loads' latencies.  150 rows of 24 / 4 heads of 256 behind 4160: 46.8 (40%, 16%) and 7.1.
 #include "attention_plan.h"
 #include "kv_attention_rows.h"
 #include "kv_attention_wide.h"

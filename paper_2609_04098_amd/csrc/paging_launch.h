@@ -85,7 +85,7 @@ inline size_t all_part_bytes(const KvCacheArgs& c, int64_t tiles, const Attentio
 // that a unit has no room for come behind them; and partial results are written and read at
 // 2.6 TB/s.  Fitted to 210 measured steps (1 to 4 groups of 36 to 900 rows, prefixes of 2000 to
 // 32000 tokens, 1 to 8 key heads, each in 1 to 48 pieces): what it takes is slower than
-// the fastest by 3% (heads of 64), 4% (128) and 2% (256) on the average, by 8, 10 and 9% in one of ten.
+// the fastest of them by 3% (heads of 64), 4% (128) and 2% (256) on the average, timed anew by 6, 7 and 5%.
 //   us of the fastest with 16, 32, 48 and 128 rows; groups x rows, prefix, key heads of 128:
 //   1 x 160, 2000, 2    11.8  14.3  16.3        1 x 320, 32768, 8   78.5  77.7  72.4  92.3
 //   4 x 256, 32000, 4    116   112   103   120  1 x 696, 32000, 8    158   140   125   136
