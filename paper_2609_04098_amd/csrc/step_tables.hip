@@ -393,18 +393,34 @@ __global__ __launch_bounds__(256) void step_give_back_kernel(TablesArgs a) {
     give_back(a, ws.given, ws.base, (int)i, head.before);
 }
 
-// Rows and new pages; lengths: those of step_begin_kernel are still to be put down.
-__global__ __launch_bounds__(256) void step_fill_kernel(TablesArgs a, int lengths) {
+// Rows and new pages.  Behind step_begin_kernel (up to 1024 sequences) the sums are searched in LDS,
+// and its lengths are still to be put down.
+template <bool kFew>
+__global__ __launch_bounds__(256) void step_fill_kernel(TablesArgs a) {
+  __shared__ int32_t sums[3][kFew ? kThreads + 1 : 1];
   const PlanHead head = *reinterpret_cast<const PlanHead*>(a.plan);
   const Plan ws = plan_of(a.plan, a.seqs);
-  if (lengths && blockIdx.x == 0) {
-    for (int b = threadIdx.x; b < a.seqs; b += 256) a.kv_len[b] = ws.given[b];
-    if (threadIdx.x == 0) a.free_count[0] = head.left;
-  }
   const int64_t all = (int64_t)gridDim.x * 256, first = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  for (int64_t i = first; i < head.rows; i += all) place(a, a.cu_rows, ws.taken, ws.base, (int)i, head.left);
-  // (New entries are those that no row of place() reads: behind the base's pages.)
-  for (int64_t i = first; i < head.taken; i += all) take(a, ws.taken, ws.base, (int)i, head.left);
+  const auto fill = [&](const int32_t* cu, const int32_t* taken, const int32_t* base) {
+    for (int64_t i = first; i < head.rows; i += all) place(a, cu, taken, base, (int)i, head.left);
+    // (New entries are those that no row of place() reads: behind the base's pages.)
+    for (int64_t i = first; i < head.taken; i += all) take(a, taken, base, (int)i, head.left);
+  };
+  if constexpr (kFew) {
+    for (int b = threadIdx.x; b <= a.seqs; b += 256) {
+      sums[0][b] = a.cu_rows[b];
+      sums[1][b] = ws.taken[b];
+      if (b < a.seqs) sums[2][b] = ws.base[b];
+    }
+    if (blockIdx.x == 0) {
+      for (int b = threadIdx.x; b < a.seqs; b += 256) a.kv_len[b] = ws.given[b];
+      if (threadIdx.x == 0) a.free_count[0] = head.left;
+    }
+    __syncthreads();
+    fill(sums[0], sums[1], sums[2]);
+  } else {
+    fill(a.cu_rows, ws.taken, ws.base);
+  }
 }
 
 }  // namespace
@@ -427,7 +443,8 @@ hipError_t launch_step_tables(const TablesArgs& a, hipStream_t stream) {
     step_give_back_kernel<<<256, 256, 0, stream>>>(a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  step_fill_kernel<<<512, 256, 0, stream>>>(a, two ? 1 : 0);
+  if (two) step_fill_kernel<true><<<512, 256, 0, stream>>>(a);
+  else step_fill_kernel<false><<<512, 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 
