@@ -120,7 +120,7 @@ inline AttentionPlan shared_pieces(int tokens, int64_t work, int64_t packed_rows
   } else {
     const Pace p = pace_of(dim, form);
     const double part = (double)packed_rows * (dim + 2) * 8.0 / 2.6e6;
-    for (int n = 1; n <= 128 && (n == 1 || (tokens / n >= least && work * n <= 3072)); ++n) {
+    for (int n = 1; n <= 128 && (n == 1 || (tokens / n >= least && work * n <= 12 * 256)); ++n) {
       const double chunk = chunk_of(n);
       const int64_t m = (work * n + 255) / 256, full = m / p.slots, rest = m % p.slots;
       const auto side_by_side = [&](int64_t w) { return chunk * (p.alone + w * p.each) + p.start; };
