@@ -11,8 +11,8 @@
 //
 // Bound by the bounds' bytes, 2 D + 4 of a page's page_size * 2 D, where there are many
 // rows; else by launches and the selection's passes over a row's scores.  32 rows of up to 32768
-// tokens, 8 key heads of 128, pages of 16: 23 us for 61 MB, the selection 8 of it, during which
-// a compute unit's only workgroup loads nothing; one row of 131072, pages of 64: 4.9 and 7.4.
+// tokens, 8 key heads of 128, pages of 16: 23 us for 61 MB, the selection (7.4 where it is a launch
+// of its own) among them, during which a compute unit's only workgroup loads nothing; one row of 131072, pages of 64: 4.9 and 7.4.
 // The bounds of two prompts of up to 16000 tokens, 8 heads of 128, pages of 32: 10.4 us for 28 MB,
 // a launch and three loads' latencies in front of them.
 #include <type_traits>
