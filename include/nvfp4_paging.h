@@ -184,7 +184,9 @@ size_t nvfp4_kv_select_pages_workspace(const nvfp4_kv_cache* cache, const nvfp4_
  * with hi_e, lo_e the page's bounds (codes): but for the 8-bit roundings, the largest
  * product that a query of the head can have with a key of the page.  (The softmax scale
  * is taken to be positive.)  The sums are whole numbers, so that the choice is the same
- * in every run.  A page outside [0, num_pages) is chosen last.
+ * in every run.  A query head that has an infinity or a NaN among its elements is left out
+ * of the maximum; a score that is no number (of a page for which no head is left, too)
+ * counts as -infinity.  A page outside [0, num_pages) is chosen last.
  *
  *   index        out, device int32 [rows x kv_heads x count]: the chosen pages' numbers in
  *                their sequence, ascending; -1 behind them.

@@ -70,24 +70,30 @@ def page_bounds(values, scale):
 
 
 def query_codes(q):
-    """(codes int [heads, dim], units float32 [heads]) of queries [heads, dim]."""
+    """(codes int [heads, dim], units float32 [heads]) of queries [heads, dim]; the unit of a
+    head that is not finite is NaN."""
+    whole = np.isfinite(q).all(axis=1)
+    q = np.where(whole[:, None], q, 0.0)
     top = np.abs(q).max(axis=1, keepdims=True)
     codes = np.rint(q * 127 / np.where(top > 0, top, 1)).astype(np.int64)
-    return codes, (top[:, 0].astype(np.float32) / np.float32(127))
+    return codes, np.where(whole, top[:, 0].astype(np.float32) / np.float32(127), np.float32(np.nan))
 
 
 def page_score(codes, units, bounds, step):
-    """Score of a page for a key head's queries: codes int [heads, dim], bounds int [2, dim]."""
-    best = None
+    """Score of a page for a key head's queries: codes int [heads, dim], bounds int [2, dim].
+    (No comparison with NaN holds: heads that are not finite are passed over.)"""
+    best = -np.inf
     for i, unit in zip(codes, units):
         total = int(np.maximum(i * bounds[0], i * bounds[1]).sum())
         value = np.float32(float(total) * float(unit))
-        best = value if best is None or value > best else best
+        best = value if value > best else best
     return np.float32(float(best) * float(step))
 
 
 def choose(scores, seen, count, first, recent):
-    """Pages taken of 0 .. seen - 1, ascending; scores[j] of page j (None: not in the cache)."""
+    """Pages taken of 0 .. seen - 1, ascending; scores[j] of page j (None: not in the cache; NaN
+    counts as -infinity)."""
+    scores = [s if s is None or s == s else -np.inf for s in scores]
     if seen <= count:
         return list(range(seen))
     middle = range(first, seen - recent)

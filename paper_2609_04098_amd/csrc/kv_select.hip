@@ -226,10 +226,10 @@ __device__ __forceinline__ RowPages row_pages(const SelectArgs& a, int row) {
   return r;
 }
 
-// Whole numbers that order as the scores do (no NaN; -0 is 0).  A page that is not in the
-// cache has key 0, which no score has.
+// Whole numbers that order as the scores do (-0 is 0, NaN is -infinity).  A page that is
+// not in the cache has key 0, which no score has.
 __device__ __forceinline__ uint32_t key_of(float x) {
-  const uint32_t b = __float_as_uint(x + 0.0f);
+  const uint32_t b = __float_as_uint(x == x ? x + 0.0f : -INFINITY);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
@@ -260,6 +260,8 @@ struct QueryLane {
 // quotient is: both have 8 significant bits, so it is a half (then it is representable, and
 // the correction finds it) or further from one than 2^-17 of itself; the quotient is off by
 // 2^-23 at most.  (Elements over 2^e, the top's power of two, keep within range.)
+// A head that is not finite has a unit of NaN: so have its products, and a maximum passes
+// them over.
 template <int D>
 __device__ __forceinline__ void query_codes(const QueryLane<D>& lanes, int x, QueryCodes<D>& to) {
   constexpr int kEach = D / 64;
@@ -267,8 +269,15 @@ __device__ __forceinline__ void query_codes(const QueryLane<D>& lanes, int x, Qu
   float v[kEach], top = 0.0f;
 #pragma unroll
   for (int i = 0; i < kEach; ++i) v[i] = i & 1 ? bf16_high(lanes.w[i / 2]) : bf16_low(lanes.w[i / 2]);
+  bool finite = true;
 #pragma unroll
-  for (int i = 0; i < kEach; ++i) top = fmaxf(top, fabsf(v[i]));
+  for (int i = 0; i < kEach; ++i) finite = finite && fabsf(v[i]) < INFINITY;
+  finite = __all(finite);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    v[i] = finite ? v[i] : 0.0f;
+    top = fmaxf(top, fabsf(v[i]));
+  }
   top = row_max(top);
   top = over_quarters_max(top);
   const int e = top > 0.0f ? __builtin_amdgcn_frexp_expf(top) : 0;
@@ -284,7 +293,7 @@ __device__ __forceinline__ void query_codes(const QueryLane<D>& lanes, int x, Qu
   if constexpr (kEach == 1) to.codes[x][lane] = n[0];
   else if constexpr (kEach == 2) *reinterpret_cast<char2*>(&to.codes[x][2 * lane]) = make_char2(n[0], n[1]);
   else *reinterpret_cast<char4*>(&to.codes[x][4 * lane]) = make_char4(n[0], n[1], n[2], n[3]);
-  if (lane == 0) to.unit[x] = top / 127.0f;
+  if (lane == 0) to.unit[x] = finite ? top / 127.0f : NAN;
 }
 
 // Scores of 16 pages at a time for up to 16 query heads.  Bounds are loaded as they lie,

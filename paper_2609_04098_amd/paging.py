@@ -291,7 +291,8 @@ def select_pages(q, cache: KVCache, batch: Batch, bounds: PageBounds, count, fir
     """Up to ``count`` pages for each of a step's rows and key heads: the ``first`` ones of
     its sequence, the ``recent`` ones of those that it sees, and between them those whose
     keys' bounds allow the largest products with a query of the key head (for a positive
-    softmax scale); all, where there are no more."""
+    softmax scale; one with an infinity or a NaN among its elements has no say); all, where
+    there are no more."""
     rows, heads, dim, ldq = _rows(q, "q")
     if rows != batch.rows or dim != cache.head_dim or heads == 0 or heads % cache.kv_heads:
         raise ValueError("q has the wrong rows, heads or head_dim")

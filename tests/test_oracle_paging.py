@@ -120,3 +120,21 @@ def test_bounds_of_negative_keys_and_a_choice_of_few():
     bounds = np.array([[10, 30], [10, 30]])
     assert OP.page_score(i, units, bounds, 1.0) == OP.page_score(i[::-1], units, bounds, 1.0) == 30 * 127
     assert OP.choose([1.0, 2.0], 2, 3, 2, 1) == [0, 1]
+
+
+def test_queries_that_are_not_finite_have_no_say():
+    rng = np.random.default_rng(5)
+    q = rng.standard_normal((4, 8))
+    bounds = np.array([[9, 4, 3, 8, 1, 7, 2, 5], [-3, -9, -1, 0, -4, 1, -2, -8]])
+    i, units = OP.query_codes(q)
+    for bad in (np.nan, np.inf, -np.inf):
+        some = q.copy()
+        some[0, 3] = some[2, 0] = bad
+        codes, unit = OP.query_codes(some)
+        assert np.isnan(unit[[0, 2]]).all() and (unit[[1, 3]] == units[[1, 3]]).all() and (codes[[1, 3]] == i[[1, 3]]).all()
+        assert OP.page_score(codes, unit, bounds, 0.5) == OP.page_score(i[[1, 3]], units[[1, 3]], bounds, 0.5)
+        assert np.isneginf(OP.page_score(codes[[0, 2]], unit[[0, 2]], bounds, 0.5))
+    # NaN counts as -infinity: behind every number, in front of pages that are not there.
+    s = [np.nan, -9.0, None, -np.inf, np.nan, 4.0, 0.0]
+    assert OP.choose(s, 7, 3, 0, 1) == [1, 5, 6] and OP.choose(s, 7, 5, 0, 1) == [0, 1, 3, 5, 6]
+    assert OP.choose(s, 7, 6, 0, 1) == [0, 1, 3, 4, 5, 6]

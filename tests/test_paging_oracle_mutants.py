@@ -49,6 +49,11 @@ MUTANTS = [
     ("highest_among_equals", "else -scores[j], j))", "else -scores[j], -j))"),
     ("outside_first", "(scores[j] is None, 0 if", "(scores[j] is not None, 0 if"),
     ("first_dropped", "middle = range(first, seen - recent)", "middle = range(0, seen - recent)"),
+    ("finite_ignored", "whole = np.isfinite(q).all(axis=1)", "whole = np.ones(len(q), dtype=bool)"),
+    ("one_finite_is_enough", "np.isfinite(q).all(axis=1)", "np.isfinite(q).any(axis=1)"),
+    ("infinity_left_in", "np.isfinite(q)", "~np.isnan(q)"),
+    ("nan_is_largest", "else -np.inf for s in scores", "else np.inf for s in scores"),
+    ("nan_is_not_there", "else -np.inf for s in scores", "else None for s in scores"),
     ("recent_dropped", "list(range(seen - recent, seen))", "list(range(seen - 1, seen))"),
 ]
 
