@@ -147,7 +147,8 @@ const char* nvfp4_kv_attention_shared_kernel(const nvfp4_kv_cache* cache, const 
  *   codes[0][e] = rint(127 hi_e / A),  codes[1][e] = rint(127 lo_e / A)   (to nearest even)
  *   step[p * step_stride + h] = fl(fl(A * k_scale) / 127)
  * with hi_e, lo_e the largest and the smallest E4M3 value of element e among the page's
- * page_size tokens, A the largest |hi_e|, |lo_e| of the head (all 0 if A is), fl binary32.
+ * page_size tokens (NaN codes left out; 0 where there are no others), A the largest |hi_e|,
+ * |lo_e| of the head (all 0 if A is), fl binary32.
  * Requirements: codes 16-byte aligned, int8 [num_pages]; page_stride in bytes, a
  * multiple of 16, at least 2 * kv_heads * head_dim; step float [num_pages], 4-byte aligned,
  * step_stride >= kv_heads; strides below 2^31.

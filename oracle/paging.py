@@ -60,8 +60,8 @@ class Pool:
 
 def page_bounds(values, scale):
     """Bounds of one page and head: values [tokens, dim] (of the E4M3 codes), its key
-    scale.  (codes int [2, dim], step)."""
-    hi, lo = values.max(axis=0), values.min(axis=0)
+    scale.  (codes int [2, dim], step).  NaN is left out, and 0 where there is nothing else."""
+    hi, lo = np.nan_to_num(np.fmax.reduce(values)), np.nan_to_num(np.fmin.reduce(values))
     top = max(np.abs(hi).max(), np.abs(lo).max())
     if top == 0:
         return np.zeros((2, values.shape[1]), dtype=np.int64), np.float32(0)

@@ -182,6 +182,7 @@ __global__ __launch_bounds__(256) void kv_page_bounds_kernel(BoundsArgs a, int i
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     v[i] = (float)(&found[wave][0][0])[lane * kEach + i];
+    if (fabsf(v[i]) == INFINITY) v[i] = 0.0f;      // (E4M3 has none: only NaN, which a maximum passes over)
     top = fmaxf(top, fabsf(v[i]));
   }
   top = over_quarters_max(row_max(top));

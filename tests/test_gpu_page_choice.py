@@ -1,10 +1,12 @@
-"""GPU tests of the choice of pages where queries are not finite.  Everything is equal to
+"""GPU tests of the pages' bounds and of the choice of pages where keys or queries are not
+finite.  Everything is equal to
 the oracle's, as in test_gpu_selected_attention.py, whose helpers these are."""
 
 import numpy as np
 import pytest
 import torch
 
+from oracle import attention as OA
 from paper_2609_04098_amd import attention as A
 from paper_2609_04098_amd import paging as P
 from tests import test_gpu_attention as G
@@ -45,3 +47,33 @@ def test_queries_that_are_not_finite(dim, heads, group, width):
         S._check_choice(sel, want, cache, table, [1] * rows, count)
         again = P.select_pages(q, cache, batch, bounds, count, first)
         assert torch.equal(sel.index, again.index) and torch.equal(sel.pages, again.pages)
+
+
+@pytest.mark.parametrize("dim,page,heads", [(64, 16, 2), (128, 32, 1), (128, 128, 3), (256, 16, 2), (256, 64, 1)])
+def test_bounds_of_keys_that_are_not_numbers(dim, page, heads):
+    """NaN of both codes: among an element's tokens, all of an element, all of a page."""
+    log("NaN keys %s" % ((dim, page, heads),))
+    gen = torch.Generator().manual_seed(dim + page)
+    n_pages = 8
+    cache = G._random_cache(gen, n_pages, heads, page, dim, nan=True)
+    places = torch.from_numpy(OA.byte_places(page, dim, False))
+    nat = cache.k.cpu()[:, :, places]                             # [page, head, token, element]
+    nat[1, :, :, dim // 2] = 0x7F
+    nat[2, :, :, 0], nat[2, :, ::2, dim - 1], nat[2, :, 1::2, dim - 1] = 0xFF, 0x7F, 0xFF
+    nat[3, 0] = 0x7F
+    nat[4, heads - 1, :, 1:] = 0xFF                               # one element is left
+    nat[5, :, 1:] = 0x7F                                          # one token is left
+    k = torch.empty_like(cache.k.cpu())
+    k[:, :, places] = nat
+    cache.k.copy_(k)
+    table, lens = torch.randperm(n_pages, generator=gen).view(2, 4).int(), [4 * page, 4 * page]
+    bounds = P.PageBounds(torch.full((n_pages, heads, 2, dim), -77, dtype=torch.int8, device="cuda"),
+                          torch.full((n_pages, heads), -7.0, device="cuda"))
+    P.page_bounds(cache, A.Batch(table.cuda(), S._i32(lens), S._i32([0, lens[0], 2 * lens[0]]), rows=2 * lens[0]), bounds)
+    want = S._want_bounds(cache, table, lens, lens, np.zeros((n_pages, heads, 2, dim), dtype=np.int64),
+                          np.zeros((n_pages, heads), dtype=np.float32))
+    assert np.array_equal(bounds.codes.cpu().numpy(), want[0]) and np.array_equal(bounds.step.cpu().numpy(), want[1])
+    assert not bounds.codes[3, 0].any() and bounds.step[3, 0] == 0
+    q = G._bf16(gen, 2, heads * 2, dim).cuda()
+    sel = P.select_pages(q, cache, A.Batch(table.cuda(), S._i32(lens)), bounds, 3)
+    S._check_choice(sel, S._want_choice(q, cache, bounds, table, lens, [1, 1], 3, 1, 1, True), cache, table, [1, 1], 3)

@@ -138,3 +138,13 @@ def test_queries_that_are_not_finite_have_no_say():
     s = [np.nan, -9.0, None, -np.inf, np.nan, 4.0, 0.0]
     assert OP.choose(s, 7, 3, 0, 1) == [1, 5, 6] and OP.choose(s, 7, 5, 0, 1) == [0, 1, 3, 5, 6]
     assert OP.choose(s, 7, 6, 0, 1) == [0, 1, 3, 4, 5, 6]
+
+
+def test_bounds_of_keys_that_are_not_numbers():
+    nan = np.nan
+    values = np.array([[nan, 2.0, nan, -1.0], [3.0, nan, nan, -4.0], [-1.0, nan, nan, nan]])
+    codes, step = OP.page_bounds(values, 0.5)
+    assert codes.tolist() == [[round(3 * 127 / 4), round(2 * 127 / 4), 0, round(-127 / 4)],
+                              [round(-127 / 4), round(2 * 127 / 4), 0, -127]] and step == np.float32(2) / np.float32(127)
+    codes, step = OP.page_bounds(values[:, 2:3], 0.5)
+    assert not codes.any() and step == 0

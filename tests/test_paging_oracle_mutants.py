@@ -49,6 +49,9 @@ MUTANTS = [
     ("highest_among_equals", "else -scores[j], j))", "else -scores[j], -j))"),
     ("outside_first", "(scores[j] is None, 0 if", "(scores[j] is not None, 0 if"),
     ("first_dropped", "middle = range(first, seen - recent)", "middle = range(0, seen - recent)"),
+    ("largest_with_nan", "np.fmax.reduce(values)", "np.maximum.reduce(values)"),
+    ("smallest_with_nan", "np.fmin.reduce(values)", "np.minimum.reduce(values)"),
+    ("nothing_stays_nan", "np.nan_to_num(np.fmax.reduce(values))", "np.fmax.reduce(values)"),
     ("finite_ignored", "whole = np.isfinite(q).all(axis=1)", "whole = np.ones(len(q), dtype=bool)"),
     ("one_finite_is_enough", "np.isfinite(q).all(axis=1)", "np.isfinite(q).any(axis=1)"),
     ("infinity_left_in", "np.isfinite(q)", "~np.isnan(q)"),
