@@ -9,7 +9,8 @@
  * ``stream``, no host synchronization, no allocation, safe from several host
  * threads.  Values in device memory are not checked on the host; the kernels
  * bound every access by the sizes given here.  Every function may be captured
- * into a graph.
+ * into a graph.  Sizes for which a launch would have 2^32 work-items or more are
+ * refused (NVFP4_EINVAL).
  */
 #ifndef NVFP4_PAGING_H
 #define NVFP4_PAGING_H
@@ -200,7 +201,8 @@ size_t nvfp4_kv_select_pages_workspace(const nvfp4_kv_cache* cache, const nvfp4_
  *                aligned (NULL if that is 0).  Its contents on entry do not matter; calls
  *                sharing one must be ordered.
  * Requirements: those of the structures; q as for nvfp4_kv_attention; 1 <= count, count *
- * page_size <= 2^30; a batch that has rows has sequences.
+ * page_size <= 2^30; a batch that has rows has sequences; rows * kv_heads < 2^22, and with
+ * max_pages over 8192 and over count rows * kv_heads * ceil(max_pages / 1024) < 2^24.
  * Errors: NVFP4_EINVAL, NVFP4_EWORKSPACE, NVFP4_EUNSUPPORTED, NVFP4_EHIP.
  */
 int nvfp4_kv_select_pages(const nvfp4_kv_cache* cache, const nvfp4_kv_batch* batch, const nvfp4_kv_bounds* bounds,

@@ -702,6 +702,11 @@ bool choose_at_once(const SelectArgs& a) {
   return a.max_pages <= 256 || (a.max_pages <= kHeldKeys && (int64_t)a.batch.rows * a.cache.heads >= 256);
 }
 
+// Whether a launch of its own scores pages: not where all are taken.
+bool scores_apart(const SelectArgs& a) {
+  return !choose_at_once(a) && a.max_pages > a.count && a.count > a.first + a.recent;
+}
+
 template <int D>
 hipError_t launch_scores(const SelectArgs& a, hipStream_t stream) {
   const int each = score_each(a), chunks = (a.max_pages + each - 1) / each;
@@ -718,8 +723,9 @@ size_t kv_select_workspace_bytes(const SelectArgs& a) {
 
 bool select_fits(const SelectArgs& a) {
   const int64_t work = (int64_t)a.batch.rows * a.cache.heads;
-  const int each = score_each(a), chunks = (a.max_pages + each - 1) / each;
-  return one_grid(work * (chunks > 0 ? chunks : 1), 64 * kScoreWaves) && one_grid(work, kSelectThreads);
+  if (!one_grid(work, kSelectThreads)) return false;
+  const int each = score_each(a);
+  return !scores_apart(a) || one_grid(work * ((a.max_pages + each - 1) / each), 64 * kScoreWaves);
 }
 
 hipError_t launch_kv_select(const SelectArgs& a, hipStream_t stream) {
@@ -730,7 +736,7 @@ hipError_t launch_kv_select(const SelectArgs& a, hipStream_t stream) {
     else kv_choose_kernel<256><<<grid, kSelectThreads, 0, stream>>>(a);
     return hipGetLastError();
   }
-  if (a.max_pages > a.count && a.count > a.first + a.recent) {
+  if (scores_apart(a)) {
     const hipError_t e = a.cache.dim == 64    ? launch_scores<64>(a, stream)
                          : a.cache.dim == 128 ? launch_scores<128>(a, stream)
                                               : launch_scores<256>(a, stream);

@@ -344,3 +344,18 @@ def test_step_tables_refuses_wrong_tensors():
         P.step_tables(r, new.to("meta"), 5)
     with pytest.raises(ValueError, match="GPU"):      # CPU tensors are refused, not computed
         P.step_tables(r, new, 5)
+
+
+@pytest.mark.skipif(torch.cuda.device_count() > 0, reason="valid arguments, but no memory behind them")
+@pytest.mark.parametrize("rows,pages", [((1 << 16) - 1, 8192), ((1 << 15) + 1, 8192), ((1 << 16) - 1, 2048)])
+def test_selection_in_one_launch_is_bounded_by_it_alone(rows, pages):
+    """Rows x key heads below 2^22 whose scores need no launch of their own are only stopped
+    by the missing device."""
+    heads = 64
+    c = _cache(kv_heads=heads, page_size=16, k_page_stride=heads * 2048, v_page_stride=heads * 2048, scale_page_stride=heads)
+    b = _batch(n_seqs=rows, rows=rows, cu_rows=None, max_pages=pages, page_table_stride=pages, max_kv_len=16 * pages)
+    g = _bounds(page_stride=1 << 16, step_stride=heads)
+    status = _select(c, b, g, hq=heads, ldq=heads * 128, wsb=1 << 62)
+    assert status in (C.NVFP4_EUNSUPPORTED, C.NVFP4_EHIP)
+    more = _batch(n_seqs=1 << 16, rows=1 << 16, cu_rows=None, max_pages=pages, page_table_stride=pages, max_kv_len=16 * pages)
+    assert _select(c, more, g, hq=heads, ldq=heads * 128, wsb=1 << 62) == C.NVFP4_EINVAL
