@@ -241,6 +241,11 @@ def page_bounds(cache: KVCache, batch: Batch, bounds: PageBounds, stream=None):
     _run(cache.index, _p.kv_page_bounds, stream, cache.ref, batch.ref, bounds.ref)
 
 
+# Bytes of scores that a choice may keep for as long as it lives.  (An allocation of their
+# own takes the host another microsecond.)
+_FEW_SCORES = 1 << 20
+
+
 class Selection:
     """The pages chosen for each row and key head: ``index`` int32 [rows, kv_heads, count]
     (numbers in the row's sequence, ascending, -1 behind them), ``pages`` (the same of the
@@ -307,15 +312,16 @@ def select_pages(q, cache: KVCache, batch: Batch, bounds: PageBounds, count, fir
             raise ValueError("out must be a selection of these rows, key heads and count")
         if out.device_index != cache.index:
             raise ValueError("out is on another device")
-    nbytes, at = 0, None
+    nbytes, at, more = 0, None, 0
     if workspace is None:
         key = ("select", cache.kv_heads, cache.head_dim, cache.page_size)
         nbytes = batch._workspace.get(key)
         if nbytes is None:
             nbytes = batch._workspace[key] = (_p.kv_select_pages_workspace(cache.ref, batch.ref) + 15) & ~15
-    if out is None:      # (the scores are this call's own: one allocation for all)
-        out, at = Selection._new(rows, cache.kv_heads, count, nbytes, cache.device, stream)
-    if workspace is not None or (nbytes and at is None):
+    if out is None:      # (the scores are this call's own; few are left in the choice's allocation)
+        more = nbytes if nbytes <= _FEW_SCORES else 0
+        out, at = Selection._new(rows, cache.kv_heads, count, more, cache.device, stream)
+    if workspace is not None or nbytes > more:
         workspace, nbytes = _room(workspace, nbytes, cache.device, cache.index, stream)
         at = workspace.data_ptr()
     index, pages, tokens = out.pointers

@@ -77,3 +77,29 @@ def test_bounds_of_keys_that_are_not_numbers(dim, page, heads):
     q = G._bf16(gen, 2, heads * 2, dim).cuda()
     sel = P.select_pages(q, cache, A.Batch(table.cuda(), S._i32(lens)), bounds, 3)
     S._check_choice(sel, S._want_choice(q, cache, bounds, table, lens, [1, 1], 3, 1, 1, True), cache, table, [1, 1], 3)
+
+
+@pytest.mark.parametrize("rows,heads,width", [(5, 2, 3000), (20, 3, 9000)])
+def test_a_choice_keeps_few_scores(rows, heads, width):
+    """Of tables over 256 pages: what a call scores is gone with it, but for a megabyte at
+    most, on any stream."""
+    log("memory of a choice %s" % ((rows, heads, width),))
+    gen = torch.Generator().manual_seed(4)
+    n_pages, count = 50, 6
+    cache = G._random_cache(gen, n_pages, heads, 16, 64, nan=False)
+    bounds = S._all_bounds(cache)
+    batch = A.Batch(torch.randint(0, n_pages, (rows, width), generator=gen, dtype=torch.int32).cuda(),
+                    S._i32([16 * width - 7 * r for r in range(rows)]))
+    q = G._bf16(gen, rows, heads * 3, 64).cuda()
+    scores = 4 * rows * heads * width
+    assert P._p.kv_select_pages_workspace(cache.ref, batch.ref) == scores
+    want = P.select_pages(q, cache, batch, bounds, count)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    others = [P.select_pages(q, cache, batch, bounds, count, stream=side) for _ in range(3)]
+    torch.cuda.current_stream().wait_stream(side)
+    others += [P.select_pages(q, cache, batch, bounds, count, workspace=torch.empty(scores, dtype=torch.uint8, device="cuda")),
+               P.select_pages(q, cache, batch, bounds, count, out=P.Selection(want.index.clone(), want.pages.clone(), want.tokens + 1))]
+    for sel in [want] + others:
+        assert sel.index.untyped_storage().nbytes() <= 4 * (2 * rows * heads * count + rows) + (1 << 20)
+        assert torch.equal(sel.index, want.index) and torch.equal(sel.pages, want.pages) and torch.equal(sel.tokens, want.tokens)
