@@ -242,7 +242,7 @@ def page_bounds(cache: KVCache, batch: Batch, bounds: PageBounds, stream=None):
 
 
 # Bytes of scores that a choice may keep for as long as it lives.  (An allocation of their
-# own takes the host another microsecond.)
+# own takes the host 1.3 us.)
 _FEW_SCORES = 1 << 20
 
 
