@@ -125,8 +125,10 @@ size_t nvfp4_kv_attention_shared_workspace(const nvfp4_kv_cache* cache, const nv
  * does.  A sequence that does not, one that is empty for instance, is computed over its
  * own row of page_table alone.  Accuracy: as stated there, for each of the two parts.
  *
- * Steps for which sharing is taken to be slower by their sizes (short prefixes, many
- * rows of a sequence) take the kernels of nvfp4_kv_attention.
+ * Steps for which sharing is taken to be slower by their sizes take the kernels of
+ * nvfp4_kv_attention, for all of their sequences: those whose max_prefix is below 1536, and
+ * those with 64 packed rows (new rows times q_heads / kv_heads) and more for each sequence
+ * on the average, be they one prompt's among single tokens.
  *
  *   workspace, workspace_bytes   at least nvfp4_kv_attention_shared_workspace bytes,
  *                16-byte aligned (NULL if that is 0).  Its contents on entry do not

@@ -78,7 +78,10 @@ inline size_t all_part_bytes(const KvCacheArgs& c, int64_t tiles, const Attentio
 //   64 x 8 (2 groups), 4000, 64 / 8    94.9  112
 // Pages that sequences share are in the caches after the first one has read them, so what
 // sharing saves is not memory's but the caches' reads; it costs partial results and a join.
-// So it begins at prefixes of 1536 tokens, and not where a sequence's own rows fill 64.
+// So it begins at prefixes of 1536 tokens, and not where an average sequence's own rows fill 64.
+// (The average is all that the host has, and a bad one for a prompt among single tokens: 64 x 1 behind 32768,
+// 40 / 8 heads of 128, take 80 us alone, 110 beside a prompt of 256 rows, 289 of 512, and 513 of 1024, where
+// nothing is shared any more; without sharing 378, 513, 394, 513.)
 // Rows of a prefix's workgroups, and pieces of either pass: those for which an estimate is
 // least, of what hangs on them.  m workgroups of a compute unit side by side take
 // `alone` + m `each` for a token of their piece and `start` for their beginning and end; those

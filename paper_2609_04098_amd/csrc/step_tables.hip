@@ -12,6 +12,9 @@
 //
 // Bound by latency: a launch, then the lengths, the tables' entries and the pool's, each a
 // load's.  500 sequences with up to 5 rows take 3.8 us, one of 1000 tokens 2.7; with bisections and 64-bit sums for all 11.9 and 5.3.
+// Over 1024 sequences one workgroup computes the sums of 1024 at a time: 1500 take 19.2 us and 20000 201, and the
+// launches behind it 4.6 + 6.7 and 6.8 + 10.1.  Where many pages come back with few rows, one workgroup moves them:
+// 223632 of 150 ended requests 190 us.
 #include "paging_launch.h"
 
 namespace nvfp4 {

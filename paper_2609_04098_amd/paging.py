@@ -179,7 +179,9 @@ def shared_attention(q, cache: KVCache, batch: Batch, shared: SharedPrefix, scal
                      return_lse=False, workspace=None, stream=None):
     """``attention(q, cache, batch)`` of sequences that share prefixes, which are read
     once for each group.  A sequence whose rows do not all lie behind the prefix is
-    computed from its own pages alone.  Arguments and results as for attention()."""
+    computed from its own pages alone.  Steps with prefixes below 1536 tokens, or with 64
+    and more rows of a key head's query heads for an average sequence, take attention()'s
+    kernels.  Arguments and results as for attention()."""
     rows, heads, ldq, y, ldy = _queries(q, cache, batch.rows, out, stream)
     if not cache.index == batch.index == shared.index:
         raise ValueError("tensors are on several devices")
